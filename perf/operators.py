@@ -15,7 +15,8 @@ Keys of a case: ``op`` (delta / delta_step / logprob / adamw) and
   (random initial state instead of none), ``fused`` (q, k and v are slices of
   one projection's rows);
 - delta_step: ``slots`` states in the pool, ``B`` of them advanced;
-- logprob: ``mode`` (train / score), ``dtype``, ``N`` rows, ``V`` columns,
+- logprob: ``mode`` (train / policy, which has its gradient in a call of its
+  own, / score), ``dtype``, ``N`` rows, ``V`` columns,
   ``top`` alternatives, ``masked`` columns at the lowest value of the type
   or minus infinity;
 - adamw: ``tensors`` of ``lo`` .. ``hi`` elements, ``bits`` of the states,
@@ -91,7 +92,7 @@ def _log_int(rng, lo, hi, step=1):
 
 
 def draw(rng):
-    kind = rng.choice(["delta", "delta", "infer", "step", "score", "loss", "adamw", "adamw"])
+    kind = rng.choice(["delta", "delta", "infer", "step", "score", "train", "policy", "adamw"])
     dtype = rng.choice(["f32", "bf16"])
     for _ in range(10000):
         if kind in ("delta", "infer", "step"):
@@ -118,9 +119,8 @@ def draw(rng):
             fits = sum(_sizes(c)) <= 230 << 20
         else:
             N, V = _log_int(rng, 1, 8192), _log_int(rng, 1000, 200000)
-            top = rng.choice([1, 4, 8, 16]) if kind == "score" else 0
-            c = _logprob("", "score" if kind == "score" else "train", dtype, N, V, top,
-                         rng.choice([0, rng.randint(1, V // 4)]))
+            top = rng.choice([1, 4, 8, 16]) if kind != "train" else 0
+            c = _logprob("", kind, dtype, N, V, top, rng.choice([0, rng.randint(1, V // 4)]))
             fits = N * V * (2 if dtype == "bf16" else 4) <= (1 << 30) // (2 if top else 1)
         if fits:
             del c["name"]
@@ -220,10 +220,13 @@ def _logprob_inputs(c, seed):
         t[1::7] = -1                         # tokens outside the loss
         x[3] = -math.inf                     # a row in which nothing is allowed
     d = dict(logits=x, targets=t)
-    if c["mode"] == "train":
+    if c["mode"] != "score":
         scale = 1.0 / N
         d["dlogp"] = -scale * (0.5 + torch.rand(N, device=DEV, generator=g))
         d["dentropy"] = -0.01 * scale * torch.rand(N, device=DEV, generator=g)
+        d["dtop"] = None
+    if c["mode"] == "policy" and c["top"]:   # the alternatives drawn towards a teacher's
+        d["dtop"] = scale * torch.randn(N, c["top"], device=DEV, generator=g)
     return d
 
 
@@ -292,7 +295,7 @@ def prepare(case, seed):
         s["logp"], s["entropy"], s["lse"] = new(N), new(N), new(N)
         s["top_ids"] = new(N, top, t=torch.int32) if top else None
         s["top_logp"] = new(N, top) if top else None
-        if c["mode"] == "train":
+        if c["mode"] != "score":
             s["dlogits"] = torch.empty_like(s["logits"])
     if own:
         _plan(c, s)
@@ -305,7 +308,7 @@ def _plan(c, s):
         tokens = ("q", "k", "v") + (("dq", "dk", "dv") if c["mode"] == "train" else ())
         ld = {n + "_ld": s[n].stride(1) for n in tokens}
         s["plan"] = ll.DeltaPlan(c["T"], c["B"], c["Hk"], c["Hv"], c["Dk"], c["Dv"],
-                                 dtype=c["dtype"], **ld)
+                                 dtype=c["dtype"], inference=c["mode"] == "infer", **ld)
     elif c["op"] == "logprob":
         s["plan"] = ll.LogprobPlan(c["N"], c["V"], dtype=c["dtype"], top_k=c["top"])
     elif c["op"] == "adamw":
@@ -332,8 +335,8 @@ def _run_own(c, s):
     from paper_1805_01772_amd import lstmloop as ll
     if c["op"] == "delta":
         train = c["mode"] == "train"
-        ins = (s["q"], s["k"], s["v"], s["g"], s["beta"], s["seq_len"], s["S0"])
-        s["plan"].fwd(*ins, s["y"], s["ST"], save_for_backward=train)
+        ins = (s["q"], s["k"], s["v"], s["g"], s["beta"], s["seq_len"])
+        s["plan"].fwd(*ins, s["S0"], s["y"], s["ST"], save_for_backward=train)
         res = dict(y=s["y"], ST=s["ST"])
         if train:
             s["plan"].bwd(*ins, s["dy"], s["dST"], s["dq"], s["dk"], s["dv"], s["dg"], s["dbeta"],
@@ -345,14 +348,19 @@ def _run_own(c, s):
                            slots=s["slots"])
         return dict(y=s["y"], S=s["S"])
     if c["op"] == "logprob":
-        s["plan"].fwd(s["logits"], s["targets"], s["logp"], s["entropy"], s["lse"], s["top_ids"],
-                      s["top_logp"])
         res = dict(logp=s["logp"], entropy=s["entropy"], lse=s["lse"])
+        if c["mode"] == "train":             # the loss's weights are known beforehand
+            s["plan"].fwd_bwd(s["logits"], s["targets"], s["dlogp"], s["dentropy"], s["logp"],
+                              s["entropy"], s["lse"], s["dlogits"])
+        else:
+            s["plan"].fwd(s["logits"], s["targets"], s["logp"], s["entropy"], s["lse"],
+                          s["top_ids"], s["top_logp"])
+        if c["mode"] == "policy":            # the gradient comes after, from values of its own
+            s["plan"].bwd(s["logits"], s["targets"], s["lse"], s["entropy"], s["top_ids"],
+                          s["dlogp"], s["dentropy"], s["dtop"], s["dlogits"])
         if c["top"]:
             res.update(top_ids=s["top_ids"], top_logp=s["top_logp"])
-        if c["mode"] == "train":
-            s["plan"].bwd(s["logits"], s["targets"], s["lse"], s["entropy"], None, s["dlogp"],
-                          s["dentropy"], None, s["dlogits"])
+        if c["mode"] != "score":
             res["dlogits"] = s["dlogits"]
         return res
     s["plan"].step(s["grads"], grad_scale=s["grad_scale"], **s["hyper"])
@@ -485,10 +493,13 @@ def _plain_logprob(c, s):
         top = x.gather(1, ids)
         res["top_ids"] = ids.to(torch.int32)
         res["top_logp"] = torch.where(top == -math.inf, -math.inf, top - lse)
-    if c["mode"] == "train":
+    if c["mode"] != "score":
         dl = torch.where(t < 0, 0.0, s["dlogp"])[:, None]
-        d = -p * (dl + s["dentropy"][:, None] * (lp + ent[:, None]))
+        every = dl + s["dtop"].sum(1, keepdim=True) if s["dtop"] is not None else dl
+        d = -p * (every + s["dentropy"][:, None] * (lp + ent[:, None]))
         d.scatter_add_(1, t.clamp(min=0)[:, None], dl)
+        if s["dtop"] is not None:
+            d.scatter_add_(1, ids, s["dtop"])
         res["dlogits"] = torch.where(none, 0.0, d).to(_op_type(c))
     return res
 
@@ -508,7 +519,7 @@ def _quant(x, power, top, rnd):
     down at random so that the mean is x; a positive v never becomes 0."""
     a = x.abs()
     scale = a.amax(1, keepdim=True)
-    w = torch.where(scale > 0, a / scale, 0.0)
+    w = torch.where(scale >= 2.0 ** -126, a * (1.0 / scale), 0.0)
     if power == 2:
         y = (w.sqrt() * top).floor().clamp(max=top - 1)
         lo, hi = y * y, (y + 1) * (y + 1)
@@ -577,11 +588,11 @@ def work(case):
     es = 2 if c["dtype"] == "bf16" else 4
     if c["op"] == "logprob":
         n = c["N"] * c["V"]
-        train = c["mode"] == "train"
         # in training the gradient needs each row's sum first, but a row may
         # stay on the chip between: read once, written once
-        return {"bytes": n * es * (2 if train else 1) + c["N"] * (4 * 6 + 8 * c["top"]),
-                "flops": (12.0 if train else 5.0) * n}
+        passes = {"score": 1, "train": 2, "policy": 3}[c["mode"]]
+        return {"bytes": n * es * passes + c["N"] * (4 * 6 + 8 * c["top"]),
+                "flops": (5.0 if passes == 1 else 12.0) * n}
     Hk, Hv, Dk, Dv = c["Hk"], c["Hv"], c["Dk"], c["Dv"]
     tok = 2 * Hk * Dk * es + 2 * Hv * Dv * es + 8 * Hv
     if c["op"] == "delta_step":
@@ -704,13 +715,18 @@ def _exact_logprob(c, seed):
         has = t >= 0
         row = torch.arange(len(t), device=DEV)
         one["logp"] = torch.where(has, lp[row, t.clamp(min=0)], 0.0)
-        if c["top"]:
-            one["top_logp"] = lp.topk(c["top"], dim=1).values
-        if c["mode"] == "train":
+        if c["top"]:                         # stable: equal ones by index
+            order = lp.sort(dim=1, descending=True, stable=True).indices[:, :c["top"]]
+            one["top_logp"] = lp.gather(1, order)
+        if c["mode"] != "score":
             dl = torch.where(has, d["dlogp"][i:i + 256].double(), 0.0)
             de = d["dentropy"][i:i + 256].double()
             w = -(plp + p * one["entropy"][:, None]) * de[:, None] - p * dl[:, None]
             w[row, t.clamp(min=0)] += dl
+            if d["dtop"] is not None:
+                dt = d["dtop"][i:i + 256].double()
+                w = w - p * dt.sum(1, keepdim=True)
+                w.scatter_add_(1, order, dt)
             one["dlogits"] = torch.where(dead[:, None], 0.0, w).to(
                 torch.float32 if c["dtype"] == "bf16" else torch.float64)
         outs.append(one)
