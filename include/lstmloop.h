@@ -400,6 +400,244 @@ ll_status ll_measure_mfma_peak(int32_t device, int32_t dtype, int32_t shape, dou
  * values or n < 0 give LL_EINVAL. */
 ll_status ll_eval_activations(int32_t device, const float* in, float* out, int64_t n, int32_t fn);
 
+/* ===========================================================================
+ * Operators of sequence models beside the loops: a recurrence whose state is
+ * a matrix (the gated delta rule), the log probabilities a model is trained
+ * and scored by, and the AdamW step that applies the gradients.  They follow
+ * the conventions above (device pointers, 16-byte aligned unless an argument
+ * says otherwise; asynchronous on `stream`; a plan serves one stream at a
+ * time and its calls do not overlap; checkable errors come back at once and
+ * enqueue nothing, data-dependent ones set bits of a device error word).  They
+ * need no co-resident work-groups and allocate only when a plan is created, so
+ * they may run beside the loops and be captured into graphs.
+ */
+
+/* More device error word bits. */
+#define LL_DEVERR_SLOT 4     /* a state slot >= n_slots                       */
+#define LL_DEVERR_TARGET 8   /* a target < -1 or >= V                         */
+
+/*
+ * The gated delta rule, a loop with a state S [Dk, Dv] per row and value head:
+ *     S'  = e^{g_t} S_{t-1}                      (decay)
+ *     u_t = beta_t (v_t - S'^T k_t)              (what the key's place lacks)
+ *     S_t = S' + k_t u_t^T,   y_t = scale S_t^T q_t
+ * Rows keep their state at t >= seq_len[b] and output y = 0 there.  Value head
+ * h reads key head h / (Hv / Hk).
+ *   T_max, B, Hk, Hv, Dk, Dv >= 1; Hv a multiple of Hk; Dk <= 128, Dv <= 512,
+ *     both multiples of 8 (else LL_EUNSUPPORTED); dtype an ll_dtype, the type
+ *     of q, k, v, y and their gradients (g, beta, states and their gradients
+ *     are float).  Inside, sums, states and everything between two products
+ *     are held in float, products keep float's 24 bits.
+ *   inference  nonzero: the plan holds no buffers for the gradient
+ *     (save_for_backward then gives LL_EINVAL).
+ *   q_ld .. dv_ld  elements from one token (t, b) to the next; heads are
+ *     contiguous within a token.  0: heads * head size.  So q, k and v (dq, dk
+ *     and dv) may be slices of the rows of one projection; a token's stride is
+ *     a multiple of 16 bytes.
+ *   scale  0 means 1 / sqrt(Dk).
+ */
+typedef struct {
+  int32_t T_max, B, Hk, Hv, Dk, Dv;
+  int32_t dtype;
+  int32_t inference;
+  int64_t q_ld, k_ld, v_ld, dq_ld, dk_ld, dv_ld;
+  float scale;
+  int32_t reserved;   /* must be 0 */
+} ll_delta_desc;
+
+typedef struct ll_delta_plan ll_delta_plan;
+
+ll_status ll_delta_plan_create(const ll_delta_desc* desc, int device, ll_delta_plan** out);
+/* Waits for the device's work.  NULL is accepted. */
+ll_status ll_delta_plan_destroy(ll_delta_plan* plan);
+/* Bytes of device memory that the plan holds. */
+ll_status ll_delta_plan_bytes(const ll_delta_plan* plan, int64_t* device_bytes);
+
+/*
+ * Forward loop.
+ *   q, k     [T_max,B,Hk,Dk], v [T_max,B,Hv,Dv] dtype, tokens q_ld, k_ld, v_ld
+ *            apart.  Entries at t >= seq_len[b] may hold anything (NaN).
+ *   g, beta  [T_max,B,Hv] float.  g is the logarithm of the decay (minus
+ *            infinity forgets the state).
+ *   seq_len  [B] int32 in [0, T_max], or NULL: every row has T_max tokens.  A
+ *            length outside counts as 0 and sets LL_DEVERR_SEQ_LEN.
+ *   S0       [B,Hv,Dk,Dv] float, or NULL for zeros.
+ *   y        [T_max,B,Hv,Dv] dtype.
+ *   ST       [B,Hv,Dk,Dv] float, the state after the last token, or NULL; may
+ *            be S0 itself.
+ *   save_for_backward  nonzero: the plan keeps what delta_loop_bwd needs, and
+ *            the pointers q, k, v, g, beta, seq_len, whose contents must stay
+ *            as they are until the gradient has been enqueued.
+ */
+ll_status delta_loop_fwd(ll_delta_plan* plan, void* stream, const void* q, const void* k,
+                         const void* v, const float* g, const float* beta,
+                         const int32_t* seq_len, const float* S0, void* y, float* ST,
+                         int32_t save_for_backward);
+
+/*
+ * Gradient loop of the last saved forward (LL_ESTATE if there is none;
+ * LL_EINVAL, with the saved forward kept, if q .. seq_len are not its
+ * pointers).  Consumes the saved forward.
+ *   dy       [T_max,B,Hv,Dv] dtype; entries at t >= seq_len[b] are not used.
+ *   dST      [B,Hv,Dk,Dv] float, or NULL (zero).
+ *   dq, dk   [T_max,B,Hk,Dk], dv [T_max,B,Hv,Dv] dtype, dg, dbeta [T_max,B,Hv]
+ *            float: overwritten, 0 at t >= seq_len[b].  dq and dk are summed
+ *            over the value heads that share a key head.
+ *   dS0      [B,Hv,Dk,Dv] float, or NULL.
+ */
+ll_status delta_loop_bwd(ll_delta_plan* plan, void* stream, const void* q, const void* k,
+                         const void* v, const float* g, const float* beta,
+                         const int32_t* seq_len, const void* dy, const float* dST, void* dq,
+                         void* dk, void* dv, float* dg, float* dbeta, float* dS0);
+
+/* Wait for the device's work, then read and clear the plan's error word. */
+ll_status ll_delta_status_sync(ll_delta_plan* plan, int32_t* device_error);
+
+/*
+ * One token for B rows, states updated in place, no plan (serving).
+ *   desc     as above with T_max = 1; inference and dq_ld .. dv_ld are ignored.
+ *   q, k     [B,Hk,Dk], v [B,Hv,Dv] dtype (rows q_ld, k_ld, v_ld apart),
+ *            g, beta [B,Hv] float, y [B,Hv,Dv] dtype.
+ *   S        [n_slots,Hv,Dk,Dv] float.
+ *   slots    [B] int32: the state of each row (rows with a state of their own
+ *            each: two rows of one slot race), -1: no sequence in this place,
+ *            y = 0 there.  A slot < -1 or >= n_slots does the same and sets
+ *            LL_DEVERR_SLOT.  NULL: row b has state b (n_slots >= B).
+ *   device_error  device int32 whose bits are set (never cleared) by the
+ *            call, or NULL.
+ */
+ll_status delta_loop_step(const ll_delta_desc* desc, void* stream, const void* q, const void* k,
+                          const void* v, const float* g, const float* beta, float* S,
+                          const int32_t* slots, int32_t n_slots, void* y,
+                          int32_t* device_error);
+
+/*
+ * Log probabilities of given tokens under softmax(logits), with the entropy
+ * and the most likely alternatives, and their gradient.
+ *   N rows at most, V columns >= 1; dtype the logits' type; top_k in [0, 32],
+ *   at most V; ld: elements from row to row (0: V; any ld >= V, rows need the
+ *   alignment of an element only).
+ */
+typedef struct {
+  int32_t N, V;
+  int32_t dtype;
+  int32_t top_k;
+  int64_t ld;
+  int32_t reserved[2];   /* must be 0 */
+} ll_logprob_desc;
+
+#define LL_LOGPROB_TOP_MAX 32
+
+typedef struct ll_logprob_plan ll_logprob_plan;
+
+ll_status ll_logprob_plan_create(const ll_logprob_desc* desc, int device, ll_logprob_plan** out);
+ll_status ll_logprob_plan_destroy(ll_logprob_plan* plan);
+
+/*
+ *   rows     rows of this call, 0 .. N.
+ *   logits   [rows,V] dtype, ld apart.  Minus infinity: a token that is not
+ *            allowed (probability 0).  In a row where nothing is allowed lse,
+ *            logp and top_logp are minus infinity, the entropy and the
+ *            gradient are 0.  A row that holds NaN or plus infinity gives NaN.
+ *   targets  [rows] int32, or NULL; -1: no target (logp = 0, and no gradient
+ *            through it).  Others outside [0, V) count as -1 and set
+ *            LL_DEVERR_TARGET.
+ *   logp     [rows] float: log probability of the target; with targets only.
+ *   entropy  [rows] float, -sum p log p, or NULL.
+ *   lse      [rows] float, log sum exp of the row's logits.
+ *   top_ids, top_logp  [rows,top_k] int32 and float: the top_k most likely
+ *            tokens, most likely first, equal logits by index.  Required when
+ *            top_k > 0.  (In a row that holds NaN the ids are in range, and no
+ *            more than that.)
+ */
+ll_status ll_logprob_fwd(ll_logprob_plan* plan, void* stream, int32_t rows, const void* logits,
+                         const int32_t* targets, float* logp, float* entropy, float* lse,
+                         int32_t* top_ids, float* top_logp);
+
+/*
+ * dlogits [rows,V] dtype (ld apart, may be logits itself) of
+ *     sum_i dlogp_i logp_i + dentropy_i entropy_i + sum_j dtop_ij top_logp_ij
+ * from the forward's lse, entropy and top_ids.  dlogp, dentropy, dtop may be
+ * NULL (zero).  entropy is read only with dentropy, top_ids only with dtop.
+ */
+ll_status ll_logprob_bwd(ll_logprob_plan* plan, void* stream, int32_t rows, const void* logits,
+                         const int32_t* targets, const float* lse, const float* entropy,
+                         const int32_t* top_ids, const float* dlogp, const float* dentropy,
+                         const float* dtop, void* dlogits);
+
+/* Both in one call, where dlogp and dentropy (NULL: zero) are known beforehand
+ * (a weighted mean as the loss): the row stays on the chip between, so the
+ * logits are read once.  dlogits may be logits. */
+ll_status ll_logprob_fwd_bwd(ll_logprob_plan* plan, void* stream, int32_t rows,
+                             const void* logits, const int32_t* targets, const float* dlogp,
+                             const float* dentropy, float* logp, float* entropy, float* lse,
+                             void* dlogits);
+
+ll_status ll_logprob_status_sync(ll_logprob_plan* plan, int32_t* device_error);
+
+/*
+ * AdamW over many tensors in one call:
+ *     g = grad * grad_scale
+ *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *     p = (1 - lr weight_decay) p
+ *         - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * p is float; `copy`, if given, gets bfloat16(p) (an operand of the loops).
+ * state_bits 32: m and v are float [n].  state_bits 8: m is int8 and v uint8
+ * [n], in rows of LL_ADAMW_ROW elements of the tensor with a float scale each
+ * (m_scale, v_scale [ceil(n / LL_ADAMW_ROW)], the row's largest magnitude):
+ *     m = sign(c) (c / 127)^2 scale,   v = (c / 255)^4 scale
+ * The step reads the stored values and uses the new ones before rounding; the
+ * codes are rounded up or down at random, so that their mean is the value (a
+ * slow average would stand still otherwise), from a hash of the element's
+ * place, the tensor's number and `seed`; a positive v never becomes 0.  Zeroed
+ * codes and scales are the state before the first step.
+ */
+#define LL_ADAMW_ROW 256
+
+typedef struct {
+  float* p;
+  void* copy;        /* bfloat16 [n], or NULL */
+  void* m;
+  void* v;
+  float* m_scale;    /* state_bits 8 only */
+  float* v_scale;
+  int64_t n;         /* elements, >= 0 */
+  float weight_decay;
+  int32_t reserved;  /* must be 0 */
+} ll_adamw_tensor;
+
+typedef struct {
+  int32_t n_tensors;    /* 1 .. 65536 */
+  int32_t state_bits;   /* 32 or 8 */
+  int32_t grad_dtype;   /* an ll_dtype */
+  int32_t reserved;     /* must be 0 */
+} ll_adamw_desc;
+
+typedef struct {
+  double lr, beta1, beta2, eps;   /* lr >= 0, 0 <= beta < 1, eps > 0 */
+  int64_t step;                   /* 1 at the first step */
+  uint32_t seed;                  /* of the random rounding (state_bits 8) */
+  int32_t reserved;               /* must be 0 */
+} ll_adamw_hyper;
+
+typedef struct ll_adamw_plan ll_adamw_plan;
+
+/* The plan keeps the pointers of the tensors and their states, which stay the
+ * caller's and must not overlap. */
+ll_status ll_adamw_plan_create(const ll_adamw_desc* desc, const ll_adamw_tensor* tensors,
+                               int device, ll_adamw_plan** out);
+ll_status ll_adamw_plan_destroy(ll_adamw_plan* plan);
+
+/*
+ *   grads    host array of n_tensors device pointers (grad_dtype [n] each);
+ *            NULL entries: that tensor and its state stay as they are.
+ *   grad_scale  device float that multiplies every gradient (a clip factor, a
+ *            loss scale's inverse), or NULL for 1.  If it is not finite the
+ *            call changes nothing.
+ */
+ll_status ll_adamw_step(ll_adamw_plan* plan, void* stream, const void* const* grads,
+                        const ll_adamw_hyper* hyper, const float* grad_scale);
+
 /* Library version string. */
 const char* ll_version(void);
 

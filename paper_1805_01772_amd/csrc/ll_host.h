@@ -1,0 +1,54 @@
+// Host-side helpers shared by the entry points (errors, device selection).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "lstmloop.h"
+
+namespace ll {
+
+// Sets the calling thread's message (ll_last_error) and returns s.
+ll_status fail(ll_status s, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+
+// hipMalloc with the library's errors; zero bytes allocate a little.
+ll_status dalloc(void** out, size_t bytes, const char* what);
+
+// LL_EINVAL unless `device` is one of the machine's.
+ll_status check_device(int device);
+
+// Waits for the device, then reads the error word at `word` into *out (may be
+// NULL) and clears it.
+ll_status read_error_word(int* word, int32_t* out);
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+class DeviceGuard {
+ public:
+  explicit DeviceGuard(int dev) {
+    if (hipGetDevice(&prev_) != hipSuccess) prev_ = -1;
+    if (prev_ != dev) (void)hipSetDevice(dev);
+  }
+  ~DeviceGuard() {
+    int cur = -1;
+    if (prev_ >= 0 && hipGetDevice(&cur) == hipSuccess && cur != prev_) (void)hipSetDevice(prev_);
+  }
+
+ private:
+  int prev_ = -1;
+};
+
+}  // namespace ll
+
+#define LL_HIP(call)                                                              \
+  do {                                                                            \
+    hipError_t e_ = (call);                                                       \
+    if (e_ != hipSuccess)                                                         \
+      return ll::fail(LL_EHIP, "%s failed: %s", #call, hipGetErrorString(e_));    \
+  } while (0)
+
+#define LL_STATUS(call)         \
+  do {                          \
+    ll_status st_ = (call);     \
+    if (st_ != LL_OK) return st_; \
+  } while (0)

@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "lstmloop.h"
+#include "ll_host.h"
 #include "ll_kernels.h"
 
 using ll::bf16_t;
@@ -21,6 +22,10 @@ using ll::bf16_t;
 namespace {
 
 thread_local std::string g_last_error;
+
+}  // namespace
+
+namespace ll {
 
 ll_status fail(ll_status s, const char* fmt, ...) {
   char buf[512];
@@ -32,35 +37,46 @@ ll_status fail(ll_status s, const char* fmt, ...) {
   return s;
 }
 
-#define LL_HIP(call)                                                              \
-  do {                                                                            \
-    hipError_t e_ = (call);                                                       \
-    if (e_ != hipSuccess)                                                         \
-      return fail(LL_EHIP, "%s failed: %s", #call, hipGetErrorString(e_));        \
-  } while (0)
+ll_status dalloc(void** out, size_t bytes, const char* what) {
+  *out = nullptr;
+  if (bytes == 0) bytes = 16;
+  hipError_t e = hipMalloc(out, bytes);
+  if (e != hipSuccess) {
+    *out = nullptr;
+    (void)hipGetLastError();
+    return fail(LL_ENOMEM, "device allocation of %zu bytes for %s failed: %s", bytes, what,
+                hipGetErrorString(e));
+  }
+  return LL_OK;
+}
 
-#define LL_STATUS(call)         \
-  do {                          \
-    ll_status st_ = (call);     \
-    if (st_ != LL_OK) return st_; \
-  } while (0)
+ll_status read_error_word(int* word, int32_t* out) {
+  LL_HIP(hipDeviceSynchronize());
+  int32_t e = 0;
+  const int32_t zero = 0;
+  LL_HIP(hipMemcpy(&e, word, sizeof e, hipMemcpyDeviceToHost));
+  LL_HIP(hipMemcpy(word, &zero, sizeof zero, hipMemcpyHostToDevice));
+  if (out) *out = e;
+  return LL_OK;
+}
+
+ll_status check_device(int device) {
+  int ndev = 0;
+  LL_HIP(hipGetDeviceCount(&ndev));
+  if (device < 0 || device >= ndev)
+    return fail(LL_EINVAL, "device %d out of range (%d devices)", device, ndev);
+  return LL_OK;
+}
+
+}  // namespace ll
+
+namespace {
+
+using ll::dalloc;
+using ll::DeviceGuard;
+using ll::fail;
 
 enum PlanState { ST_EMPTY = 0, ST_FWD_DONE = 1 };
-
-class DeviceGuard {
- public:
-  explicit DeviceGuard(int dev) {
-    if (hipGetDevice(&prev_) != hipSuccess) prev_ = -1;
-    if (prev_ != dev) hipSetDevice(dev);
-  }
-  ~DeviceGuard() {
-    int cur = -1;
-    if (prev_ >= 0 && hipGetDevice(&cur) == hipSuccess && cur != prev_) hipSetDevice(prev_);
-  }
-
- private:
-  int prev_ = -1;
-};
 
 long round_up(long v, long m) { return (v + m - 1) / m * m; }
 
@@ -402,19 +418,6 @@ void free_plan_memory(ll_plan* p) {
   if (p->ev_join) (void)hipEventDestroy(p->ev_join);
   if (p->ev_done) (void)hipEventDestroy(p->ev_done);
   if (p->gstream) (void)hipStreamDestroy(p->gstream);
-}
-
-ll_status dalloc(void** out, size_t bytes, const char* what) {
-  *out = nullptr;
-  if (bytes == 0) bytes = 16;
-  hipError_t e = hipMalloc(out, bytes);
-  if (e != hipSuccess) {
-    *out = nullptr;
-    (void)hipGetLastError();
-    return fail(LL_ENOMEM, "device allocation of %zu bytes for %s failed: %s", bytes, what,
-                hipGetErrorString(e));
-  }
-  return LL_OK;
 }
 
 // Choose the loop work split: hidden units per work-group HJ in {16, 8, 4},

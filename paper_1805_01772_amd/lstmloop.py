@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(_PKG, "liblstmloop.so")
 
 LL_OK, LL_EINVAL, LL_ENOMEM, LL_EHIP, LL_ESTATE, LL_EUNSUPPORTED = range(6)
 LL_F32, LL_BF16 = 0, 1
-LL_DEVERR_SEQ_LEN, LL_DEVERR_BARRIER = 1, 2
+LL_DEVERR_SEQ_LEN, LL_DEVERR_BARRIER, LL_DEVERR_SLOT, LL_DEVERR_TARGET = 1, 2, 4, 8
 LL_LOOPS_GRID, LL_LOOPS_XCD, LL_LOOPS_CHIP = 0, 1, 2
 LL_CELL_LSTM, LL_CELL_RNN, LL_CELL_GRU, LL_CELL_LSTM_SKIP, LL_CELL_LSTM_ACT = 0, 1, 2, 3, 4
 LL_ACT_EPS = 0.01
@@ -30,7 +30,12 @@ EXPORTED = ("ll_plan_create", "ll_plan_destroy", "ll_plan_stack_bytes",
             "ll_plan_geometry", "lstm_loop_fwd", "lstm_loop_bwd",
             "ll_status_sync", "ll_last_error", "ll_version",
             "ll_plan_set_timing", "ll_plan_set_timing_stages", "ll_plan_read_timing",
-            "ll_measure_mfma_peak", "ll_eval_activations", "lstm_loop_fwd_noalloc")
+            "ll_measure_mfma_peak", "ll_eval_activations", "lstm_loop_fwd_noalloc",
+            "ll_delta_plan_create", "ll_delta_plan_destroy", "ll_delta_plan_bytes",
+            "delta_loop_fwd", "delta_loop_bwd", "delta_loop_step", "ll_delta_status_sync",
+            "ll_logprob_plan_create", "ll_logprob_plan_destroy", "ll_logprob_fwd",
+            "ll_logprob_bwd", "ll_logprob_fwd_bwd", "ll_logprob_status_sync",
+            "ll_adamw_plan_create", "ll_adamw_plan_destroy", "ll_adamw_step")
 STAGES = ("prep", "input_proj", "fwd_loop", "bwd_loop", "bwd_operands", "dw", "dx", "loop_setup",
           "recompute")
 
@@ -45,6 +50,39 @@ class ll_desc(ctypes.Structure):
                 ("ponder_max", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class ll_delta_desc(ctypes.Structure):
+    _fields_ = [("T_max", ctypes.c_int32), ("B", ctypes.c_int32), ("Hk", ctypes.c_int32),
+                ("Hv", ctypes.c_int32), ("Dk", ctypes.c_int32), ("Dv", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("inference", ctypes.c_int32),
+                ("q_ld", ctypes.c_int64), ("k_ld", ctypes.c_int64), ("v_ld", ctypes.c_int64),
+                ("dq_ld", ctypes.c_int64), ("dk_ld", ctypes.c_int64), ("dv_ld", ctypes.c_int64),
+                ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class ll_logprob_desc(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("top_k", ctypes.c_int32), ("ld", ctypes.c_int64),
+                ("reserved", ctypes.c_int32 * 2)]
+
+
+class ll_adamw_tensor(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("weight_decay", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class ll_adamw_desc(ctypes.Structure):
+    _fields_ = [("n_tensors", ctypes.c_int32), ("state_bits", ctypes.c_int32),
+                ("grad_dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class ll_adamw_hyper(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint32),
+                ("reserved", ctypes.c_int32)]
+
+
 class LoopError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {msg}")
@@ -54,7 +92,7 @@ class LoopError(RuntimeError):
 _lib = None
 # Plans still open: closed by an exit hook that runs while the HIP runtime is
 # alive (its own teardown happens later, in the C library's exit handlers).
-_live_plans: "weakref.WeakSet[Plan]" = weakref.WeakSet()
+_live_plans: "weakref.WeakSet" = weakref.WeakSet()
 
 
 def _close_live_plans() -> None:
@@ -102,12 +140,35 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.ll_eval_activations.argtypes = [ctypes.c_int32, vp, vp, i64, i32]
     lib.lstm_loop_fwd_noalloc.argtypes = [ctypes.POINTER(ll_desc), vp, vp, vp, ctypes.POINTER(vp),
                                           ctypes.POINTER(vp), vp, vp, vp, vp, vp, vp, vp]
+    pvp = ctypes.POINTER(vp)
+    lib.ll_delta_plan_create.argtypes = [ctypes.POINTER(ll_delta_desc), ctypes.c_int, pvp]
+    lib.ll_delta_plan_destroy.argtypes = [vp]
+    lib.ll_delta_plan_bytes.argtypes = [vp, ctypes.POINTER(i64)]
+    lib.delta_loop_fwd.argtypes = [vp] * 11 + [i32]
+    lib.delta_loop_bwd.argtypes = [vp] * 16
+    lib.delta_loop_step.argtypes = [ctypes.POINTER(ll_delta_desc)] + [vp] * 8 + [i32, vp, vp]
+    lib.ll_delta_status_sync.argtypes = [vp, ctypes.POINTER(i32)]
+    lib.ll_logprob_plan_create.argtypes = [ctypes.POINTER(ll_logprob_desc), ctypes.c_int, pvp]
+    lib.ll_logprob_plan_destroy.argtypes = [vp]
+    lib.ll_logprob_fwd.argtypes = [vp, vp, i32] + [vp] * 7
+    lib.ll_logprob_bwd.argtypes = [vp, vp, i32] + [vp] * 9
+    lib.ll_logprob_fwd_bwd.argtypes = [vp, vp, i32] + [vp] * 8
+    lib.ll_logprob_status_sync.argtypes = [vp, ctypes.POINTER(i32)]
+    lib.ll_adamw_plan_create.argtypes = [ctypes.POINTER(ll_adamw_desc),
+                                         ctypes.POINTER(ll_adamw_tensor), ctypes.c_int, pvp]
+    lib.ll_adamw_plan_destroy.argtypes = [vp]
+    lib.ll_adamw_step.argtypes = [vp, vp, pvp, ctypes.POINTER(ll_adamw_hyper), vp]
     lib.ll_last_error.restype = ctypes.c_char_p
     lib.ll_version.restype = ctypes.c_char_p
     for name in ("ll_plan_create", "ll_plan_destroy", "ll_plan_stack_bytes", "ll_plan_geometry",
                  "lstm_loop_fwd", "lstm_loop_bwd", "ll_status_sync", "ll_plan_set_timing",
                  "ll_plan_set_timing_stages", "ll_plan_read_timing", "ll_measure_mfma_peak",
-                 "ll_eval_activations", "lstm_loop_fwd_noalloc"):
+                 "ll_eval_activations", "lstm_loop_fwd_noalloc", "ll_delta_plan_create",
+                 "ll_delta_plan_destroy", "ll_delta_plan_bytes", "delta_loop_fwd",
+                 "delta_loop_bwd", "delta_loop_step", "ll_delta_status_sync",
+                 "ll_logprob_plan_create", "ll_logprob_plan_destroy", "ll_logprob_fwd",
+                 "ll_logprob_bwd", "ll_logprob_fwd_bwd", "ll_logprob_status_sync",
+                 "ll_adamw_plan_create", "ll_adamw_plan_destroy", "ll_adamw_step"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -309,3 +370,307 @@ def ll_status_sync(plan: Plan) -> int:
 
 def ll_plan_stack_bytes(plan: Plan):
     return plan.stack_bytes()
+
+
+# --------------------------------------------------------------------------
+# the operators beside the loops
+# --------------------------------------------------------------------------
+def _op_name(dtype) -> str:
+    name = str(dtype)
+    return {"torch.bfloat16": "bf16", "torch.float32": "f32"}.get(name, name)
+
+
+def _want(t, name: str, shape, dtype: str, optional: bool = False):
+    """The tensor's address; shape and type are what the call says."""
+    if t is None and optional:
+        return None
+    if tuple(t.shape) != tuple(shape) or str(t.dtype) != "torch." + dtype:
+        raise ValueError(f"{name}: {tuple(shape)} {dtype} is wanted, got {tuple(t.shape)} {t.dtype}")
+    return _ptr(t)
+
+
+def _tokens(t, name: str, shape, ld: int, dtype: str):
+    """Address of a token array whose tokens are ld elements apart."""
+    if tuple(t.shape) != tuple(shape) or str(t.dtype) != "torch." + dtype:
+        raise ValueError(f"{name}: {tuple(shape)} {dtype} is wanted, got {tuple(t.shape)} {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError("tensors passed to the library must live on the GPU")
+    want = [ld, shape[-1], 1] if len(shape) == 3 else [shape[1] * ld, ld, shape[-1], 1]
+    if any(s != w and n > 1 for s, w, n in zip(t.stride(), want, shape)):
+        raise ValueError(f"{name}: strides {tuple(t.stride())}, {tuple(want)} are wanted "
+                         f"(tokens {ld} elements apart)")
+    return t.data_ptr()
+
+
+_TORCH = {"f32": "float32", "bf16": "bfloat16"}
+
+
+class _OpPlan:
+    """Owner of an operator's plan handle."""
+
+    _destroy = ""
+
+    def _create(self, make, desc, *args):
+        lib = load_library()
+        h = ctypes.c_void_p()
+        _check(getattr(lib, make)(ctypes.byref(desc), *args, ctypes.byref(h)))
+        self._lib, self._h = lib, h
+        _live_plans.add(self)
+
+    def close(self) -> None:
+        if getattr(self, "_h", None) is not None and self._h.value:
+            getattr(self._lib, self._destroy)(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def _status(self, fn) -> int:
+        e = ctypes.c_int32()
+        _check(getattr(self._lib, fn)(self._h, ctypes.byref(e)))
+        return e.value
+
+
+def make_delta_desc(T_max: int, B: int, Hk: int, Hv: int, Dk: int, Dv: int, dtype: str = "f32",
+                    inference: bool = False, q_ld: int = 0, k_ld: int = 0, v_ld: int = 0,
+                    dq_ld: int = 0, dk_ld: int = 0, dv_ld: int = 0,
+                    scale: float = 0.0) -> ll_delta_desc:
+    return ll_delta_desc(T_max, B, Hk, Hv, Dk, Dv,
+                         LL_BF16 if dtype == "bf16" else LL_F32 if dtype == "f32" else int(dtype),
+                         1 if inference else 0, q_ld, k_ld, v_ld, dq_ld, dk_ld, dv_ld, scale, 0)
+
+
+class DeltaPlan(_OpPlan):
+    """The gated delta rule over [T_max, B] tokens (ll_delta_plan)."""
+
+    _destroy = "ll_delta_plan_destroy"
+
+    def __init__(self, T_max: int, B: int, Hk: int, Hv: int, Dk: int, Dv: int, dtype: str = "f32",
+                 inference: bool = False, q_ld: int = 0, k_ld: int = 0, v_ld: int = 0,
+                 dq_ld: int = 0, dk_ld: int = 0, dv_ld: int = 0, scale: float = 0.0,
+                 device: int = 0):
+        self.desc = d = make_delta_desc(T_max, B, Hk, Hv, Dk, Dv, dtype, inference, q_ld, k_ld,
+                                        v_ld, dq_ld, dk_ld, dv_ld, scale)
+        self.dtype = dtype
+        self._create("ll_delta_plan_create", d, device)
+        qk, v = Hk * Dk, Hv * Dv
+        self._ld = dict(q=q_ld or qk, k=k_ld or qk, v=v_ld or v, dq=dq_ld or qk, dk=dk_ld or qk,
+                        dv=dv_ld or v)
+        self._qk, self._v = (T_max, B, Hk, Dk), (T_max, B, Hv, Dv)
+        self._gate, self._state = (T_max, B, Hv), (B, Hv, Dk, Dv)
+
+    def _inputs(self, q, k, v, g, beta, seq_len):
+        t = _TORCH[self.dtype]
+        return (_tokens(q, "q", self._qk, self._ld["q"], t),
+                _tokens(k, "k", self._qk, self._ld["k"], t),
+                _tokens(v, "v", self._v, self._ld["v"], t),
+                _want(g, "g", self._gate, "float32"), _want(beta, "beta", self._gate, "float32"),
+                _want(seq_len, "seq_len", self._qk[1:2], "int32", optional=True))
+
+    def fwd(self, q, k, v, g, beta, seq_len, S0, y, ST, save_for_backward: bool = True,
+            stream=None) -> None:
+        """delta_loop_fwd (asynchronous on `stream`, default: torch's current)."""
+        _check(self._lib.delta_loop_fwd(
+            self._h, _stream(stream), *self._inputs(q, k, v, g, beta, seq_len),
+            _want(S0, "S0", self._state, "float32", optional=True),
+            _want(y, "y", self._v, _TORCH[self.dtype]),
+            _want(ST, "ST", self._state, "float32", optional=True), 1 if save_for_backward else 0))
+
+    def bwd(self, q, k, v, g, beta, seq_len, dy, dST, dq, dk, dv, dg, dbeta, dS0=None,
+            stream=None) -> None:
+        """delta_loop_bwd (asynchronous on `stream`); q .. seq_len are the
+        tensors the saved forward was given."""
+        t = _TORCH[self.dtype]
+        _check(self._lib.delta_loop_bwd(
+            self._h, _stream(stream), *self._inputs(q, k, v, g, beta, seq_len),
+            _want(dy, "dy", self._v, t), _want(dST, "dST", self._state, "float32", optional=True),
+            _tokens(dq, "dq", self._qk, self._ld["dq"], t),
+            _tokens(dk, "dk", self._qk, self._ld["dk"], t),
+            _tokens(dv, "dv", self._v, self._ld["dv"], t),
+            _want(dg, "dg", self._gate, "float32"), _want(dbeta, "dbeta", self._gate, "float32"),
+            _want(dS0, "dS0", self._state, "float32", optional=True)))
+
+    def bytes(self) -> int:
+        """ll_delta_plan_bytes: device memory that the plan holds."""
+        n = ctypes.c_int64()
+        _check(self._lib.ll_delta_plan_bytes(self._h, ctypes.byref(n)))
+        return n.value
+
+    def status_sync(self) -> int:
+        """ll_delta_status_sync: wait, then return (and clear) the device error word."""
+        return self._status("ll_delta_status_sync")
+
+
+def delta_loop_fwd(plan: DeltaPlan, *args, **kw):
+    return plan.fwd(*args, **kw)
+
+
+def delta_loop_bwd(plan: DeltaPlan, *args, **kw):
+    return plan.bwd(*args, **kw)
+
+
+def delta_loop_step(q, k, v, g, beta, S, y, slots=None, scale: float = 0.0, device_error=None,
+                    stream=None) -> None:
+    """delta_loop_step: one token for the B rows of q [B, Hk, Dk], k, v [B, Hv, Dv]
+    (rows may be slices of a projection's), states S [n_slots, Hv, Dk, Dv]
+    updated in place (asynchronous on `stream`)."""
+    (B, Hk, Dk), (Hv, Dv) = q.shape, v.shape[1:]
+    dtype = _op_name(q.dtype)
+    if dtype not in _TORCH:
+        raise ValueError(f"q: float32 or bfloat16 is wanted, got {q.dtype}")
+    t = _TORCH[dtype]
+    ld = [a.stride(0) if B > 1 else a.shape[1] * a.shape[2] for a in (q, k, v)]
+    desc = make_delta_desc(1, B, Hk, Hv, Dk, Dv, dtype, True, *ld, scale=scale)
+    _check(load_library().delta_loop_step(
+        ctypes.byref(desc), _stream(stream), _tokens(q, "q", (B, Hk, Dk), ld[0], t),
+        _tokens(k, "k", (B, Hk, Dk), ld[1], t), _tokens(v, "v", (B, Hv, Dv), ld[2], t),
+        _want(g, "g", (B, Hv), "float32"), _want(beta, "beta", (B, Hv), "float32"),
+        _want(S, "S", (S.shape[0], Hv, Dk, Dv), "float32"),
+        _want(slots, "slots", (B,), "int32", optional=True), S.shape[0],
+        _want(y, "y", (B, Hv, Dv), t), _want(device_error, "device_error", (1,), "int32", optional=True)))
+
+
+class LogprobPlan(_OpPlan):
+    """Log probabilities of given tokens, entropy, alternatives (ll_logprob_plan)
+    of up to N rows of V logits, rows ld elements apart (0: V)."""
+
+    _destroy = "ll_logprob_plan_destroy"
+
+    def __init__(self, N: int, V: int, dtype: str = "f32", top_k: int = 0, ld: int = 0,
+                 device: int = 0):
+        d = ll_logprob_desc(N, V, LL_BF16 if dtype == "bf16" else LL_F32, top_k, ld)
+        if dtype not in _TORCH:
+            raise ValueError(f"dtype {dtype!r} is neither 'f32' nor 'bf16'")
+        self.desc, self.dtype, self.top_k, self.V = d, dtype, top_k, V
+        self.ld = ld or V
+        self._create("ll_logprob_plan_create", d, device)
+
+    def _rows(self, x, name: str, n: int):
+        if (tuple(x.shape) != (n, self.V) or str(x.dtype) != "torch." + _TORCH[self.dtype]
+                or (self.V > 1 and x.stride(1) != 1) or (n > 1 and x.stride(0) != self.ld)):
+            raise ValueError(f"{name}: [rows, {self.V}] {_TORCH[self.dtype]} with rows {self.ld} apart "
+                             f"is wanted, got {tuple(x.shape)} {x.dtype} strides {tuple(x.stride())}")
+        if not x.is_cuda:
+            raise ValueError("tensors passed to the library must live on the GPU")
+        return x.data_ptr()
+
+    def fwd(self, logits, targets, logp, entropy=None, lse=None, top_ids=None, top_logp=None,
+            stream=None) -> None:
+        """ll_logprob_fwd (asynchronous on `stream`)."""
+        n = logits.shape[0]
+        _check(self._lib.ll_logprob_fwd(
+            self._h, _stream(stream), n, self._rows(logits, "logits", n),
+            _want(targets, "targets", (n,), "int32", optional=True),
+            _want(logp, "logp", (n,), "float32", optional=True),
+            _want(entropy, "entropy", (n,), "float32", optional=True),
+            _want(lse, "lse", (n,), "float32", optional=True),
+            _want(top_ids, "top_ids", (n, self.top_k), "int32", optional=True),
+            _want(top_logp, "top_logp", (n, self.top_k), "float32", optional=True)))
+
+    def bwd(self, logits, targets, lse, entropy, top_ids, dlogp, dentropy, dtop, dlogits,
+            stream=None) -> None:
+        """ll_logprob_bwd (asynchronous on `stream`); dlogits may be logits."""
+        n = logits.shape[0]
+        _check(self._lib.ll_logprob_bwd(
+            self._h, _stream(stream), n, self._rows(logits, "logits", n),
+            _want(targets, "targets", (n,), "int32", optional=True),
+            _want(lse, "lse", (n,), "float32"),
+            _want(entropy, "entropy", (n,), "float32", optional=True),
+            _want(top_ids, "top_ids", (n, self.top_k), "int32", optional=True),
+            _want(dlogp, "dlogp", (n,), "float32", optional=True),
+            _want(dentropy, "dentropy", (n,), "float32", optional=True),
+            _want(dtop, "dtop", (n, self.top_k), "float32", optional=True),
+            self._rows(dlogits, "dlogits", n)))
+
+    def fwd_bwd(self, logits, targets, dlogp, dentropy, logp, entropy, lse, dlogits,
+                stream=None) -> None:
+        """ll_logprob_fwd_bwd (asynchronous on `stream`); dlogits may be logits."""
+        n = logits.shape[0]
+        _check(self._lib.ll_logprob_fwd_bwd(
+            self._h, _stream(stream), n, self._rows(logits, "logits", n),
+            _want(targets, "targets", (n,), "int32", optional=True),
+            _want(dlogp, "dlogp", (n,), "float32", optional=True),
+            _want(dentropy, "dentropy", (n,), "float32", optional=True),
+            _want(logp, "logp", (n,), "float32", optional=True),
+            _want(entropy, "entropy", (n,), "float32", optional=True),
+            _want(lse, "lse", (n,), "float32", optional=True),
+            self._rows(dlogits, "dlogits", n)))
+
+    def status_sync(self) -> int:
+        """ll_logprob_status_sync: wait, then return (and clear) the device error word."""
+        return self._status("ll_logprob_status_sync")
+
+
+ADAMW_ROW = 256   # LL_ADAMW_ROW
+
+
+class AdamWPlan(_OpPlan):
+    """AdamW over many tensors (ll_adamw_plan).  params: float32 tensors; m and
+    v: float32, or int8 and uint8 with m_scale and v_scale (ceil(n / ADAMW_ROW)
+    floats a tensor); copies: bfloat16 tensors or None, a list or None;
+    weight_decay: one number or one a tensor.  The plan keeps the tensors."""
+
+    _destroy = "ll_adamw_plan_destroy"
+
+    def __init__(self, params: Sequence, m: Sequence, v: Sequence, m_scale=None, v_scale=None,
+                 copies=None, weight_decay=0.0, grad_dtype: str = "f32", device: int = 0):
+        n = len(params)
+        q8 = m_scale is not None
+        if grad_dtype not in _TORCH:
+            raise ValueError(f"grad_dtype {grad_dtype!r} is neither 'f32' nor 'bf16'")
+        if q8 != (v_scale is not None):
+            raise ValueError("m_scale and v_scale go together")
+        wd = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * n
+        if n == 0:
+            raise ValueError("no tensors")
+        lists = [m, v, wd] + [x for x in (m_scale, v_scale, copies) if x is not None]
+        if any(len(x) != n for x in lists):
+            raise ValueError(f"{n} params, but lists of {[len(x) for x in lists]} for them")
+        recs = (ll_adamw_tensor * n)()
+        mt, vt = ("int8", "uint8") if q8 else ("float32", "float32")
+        for i, p in enumerate(params):
+            shape, rows = tuple(p.shape), (-(-p.numel() // ADAMW_ROW),)
+            recs[i] = ll_adamw_tensor(
+                _want(p, f"params[{i}]", shape, "float32"),
+                _want(copies[i] if copies is not None else None, f"copies[{i}]", shape, "bfloat16",
+                      optional=True),
+                _want(m[i], f"m[{i}]", shape, mt), _want(v[i], f"v[{i}]", shape, vt),
+                _want(m_scale[i], f"m_scale[{i}]", rows, "float32") if q8 else None,
+                _want(v_scale[i], f"v_scale[{i}]", rows, "float32") if q8 else None,
+                p.numel(), wd[i], 0)
+        self._keep = (list(params), list(m), list(v), m_scale, v_scale, copies)
+        import torch
+        self._grad_type = getattr(torch, _TORCH[grad_dtype])
+        self._sizes = [p.numel() for p in params]
+        self._ptrs = (ctypes.c_void_p * n)()
+        desc = ll_adamw_desc(n, 8 if q8 else 32, LL_BF16 if grad_dtype == "bf16" else LL_F32, 0)
+        self._create("ll_adamw_plan_create", desc, recs, device)
+
+    def step(self, grads: Sequence, lr: float, beta1: float = 0.9, beta2: float = 0.999,
+             eps: float = 1e-8, step: int = 1, seed: int = 0, grad_scale=None, stream=None) -> None:
+        """ll_adamw_step (asynchronous on `stream`): grads has a tensor, or None,
+        for each parameter; grad_scale a float32 tensor of one value, or None."""
+        if len(grads) != len(self._sizes):
+            raise ValueError(f"{len(self._sizes)} tensors, but {len(grads)} gradients")
+        ptrs, dtype = self._ptrs, self._grad_type
+        for i, (g, n) in enumerate(zip(grads, self._sizes)):
+            if g is None:
+                ptrs[i] = None
+                continue
+            if g.numel() != n or g.dtype is not dtype or not g.is_cuda or not g.is_contiguous():
+                raise ValueError(f"grads[{i}]: {n} contiguous elements of {dtype} on the GPU are "
+                                 f"wanted, got {tuple(g.shape)} {g.dtype}")
+            ptrs[i] = g.data_ptr()
+        hyper = ll_adamw_hyper(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFF, 0)
+        _check(self._lib.ll_adamw_step(
+            self._h, _stream(stream), self._ptrs, ctypes.byref(hyper),
+            _want(grad_scale, "grad_scale", (1,), "float32", optional=True)))
