@@ -9,7 +9,15 @@ constexpr int kDeltaChunk = 64;      // tokens per chunk
 constexpr int kDeltaMaxDk = 128;
 constexpr int kDeltaMaxDv = 512;
 
-// Chunk n of (row b, value head h) is item (b * Hv + h) * nch + n.
+// Head size of the keys in 32-element steps of a matrix instruction, rounded
+// up to a power of two (1, 2, 4).
+inline int delta_ksteps(int Dk) { return Dk <= 32 ? 1 : Dk <= 64 ? 2 : 4; }
+// Pieces of bfloat16 that hold an operand of the call's type.
+inline int delta_pieces(bool bf16) { return bf16 ? 1 : 3; }
+
+// Chunk n of (row b, value head h) is item (b * Hv + h) * nch + n; of key head
+// hk item (b * Hk + hk) * nch + n.  Matrices in pieces are row-major, one
+// piece after the other.
 struct DeltaArgs {
   int T, B, Hk, Hv, Dk, Dv, nch;
   float scale;
@@ -20,10 +28,13 @@ struct DeltaArgs {
   void *y, *dq, *dk, *dv;
   float *ST, *dg, *dbeta, *dS0;
   int* err;
-  // per item: T = (I + A)^-1 and P [64][64], decays of its tokens
-  float *tm, *pm;
+  // made by prep, per item: T = (I + A)^-1 and P with their transposes,
+  // [3][64][64] each; decays of the tokens
+  bf16_t *tp, *pp, *ttp, *ptp;
   double* G;                         // [64] sums of g from the chunk's start
   float4* tok;                       // [64] e^G, e^{G_end - G}, beta, -
+  // per item of a key head: K^T and Q^T [pieces][32 * ksteps][64]
+  bf16_t *ktp, *qtp;
   // per item, kept for the gradient
   float *st, *u;                     // entering state [Dk][Dv], U [64][Dv]
   float *dst, *dr;                   // gradient of the leaving state, of R
@@ -34,7 +45,7 @@ __device__ __forceinline__ int delta_len(const DeltaArgs& a, int b) {
   return L < 0 || L > a.T ? 0 : L;
 }
 
-template <typename T> hipError_t delta_launch_fwd(const DeltaArgs& a, bool save, hipStream_t s);
-template <typename T> hipError_t delta_launch_bwd(const DeltaArgs& a, hipStream_t s);
+template <typename T> hipError_t delta_launch_fwd(const DeltaArgs& a, bool save, int cus, hipStream_t s);
+template <typename T> hipError_t delta_launch_bwd(const DeltaArgs& a, int cus, hipStream_t s);
 
 }  // namespace ll

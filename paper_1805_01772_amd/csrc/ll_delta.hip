@@ -12,7 +12,7 @@ using ll::fail;
 
 struct ll_delta_plan {
   ll_delta_desc d;
-  int device = 0;
+  int device = 0, cus = 0;
   DeltaArgs a{};                       // sizes and the plan's buffers
   int64_t bytes = 0;
   bool saved = false;
@@ -161,7 +161,7 @@ DeltaArgs sizes(const ll_delta_desc& d) {
 }
 
 void release(ll_delta_plan* p) {
-  void* all[] = {p->a.tm, p->a.pm, p->a.G, p->a.tok, p->a.st, p->a.u, p->a.dst, p->a.dr, p->a.err};
+  void* all[] = {p->a.tp, p->a.pp, p->a.ttp, p->a.ptp, p->a.ktp, p->a.qtp, p->a.G, p->a.tok, p->a.st, p->a.u, p->a.dst, p->a.dr, p->a.err};
   for (void* m : all)
     if (m) (void)hipFree(m);
 }
@@ -191,12 +191,24 @@ ll_status ll_delta_plan_create(const ll_delta_desc* desc, int device, ll_delta_p
   p->device = device;
   p->a = sizes(*desc);
   const size_t items = (size_t)desc->B * desc->Hv * p->a.nch, C = ll::kDeltaChunk;
-  const size_t sq = sizeof(float) * items * C * C, st = sizeof(float) * items * desc->Dk * desc->Dv,
+  const size_t sq = sizeof(bf16_t) * 3 * items * C * C, st = sizeof(float) * items * desc->Dk * desc->Dv,
                rows = sizeof(float) * items * C * desc->Dv;
+  const size_t tr = sizeof(bf16_t) * ll::delta_pieces(desc->dtype == LL_BF16) * 32 * ll::delta_ksteps(desc->Dk) *
+                    C * desc->B * desc->Hk * p->a.nch;
+  hipDeviceProp_t prop;
+  if (hipGetDeviceProperties(&prop, device) != hipSuccess) {
+    delete p;
+    return fail(LL_EHIP, "hipGetDeviceProperties failed");
+  }
+  p->cus = prop.multiProcessorCount;
   struct { void** at; size_t bytes; const char* what; bool grad; } bufs[] = {
-      {(void**)&p->a.tm, sq, "the chunks' T", false},
-      {(void**)&p->a.pm, sq, "the chunks' P", false},
-      {(void**)&p->a.G, sizeof(double) * items * C, "the sums of g", false},
+      {(void**)&p->a.tp, sq, "the chunks' T", false},
+      {(void**)&p->a.pp, sq, "the chunks' P", false},
+      {(void**)&p->a.ktp, tr, "the chunks' K^T", false},
+      {(void**)&p->a.ttp, sq, "the chunks' T^T", true},
+      {(void**)&p->a.ptp, sq, "the chunks' P^T", true},
+      {(void**)&p->a.qtp, tr, "the chunks' Q^T", true},
+      {(void**)&p->a.G, sizeof(double) * items * C, "the sums of g", true},
       {(void**)&p->a.tok, sizeof(float4) * items * C, "the tokens' decays", false},
       {(void**)&p->a.err, sizeof(int), "the error word", false},
       {(void**)&p->a.st, st, "the chunks' states", true},
@@ -252,8 +264,8 @@ ll_status delta_loop_fwd(ll_delta_plan* p, void* stream, const void* q, const vo
   a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta; a.seq_len = seq_len; a.S0 = S0; a.y = y; a.ST = ST;
   p->saved = false;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  LL_HIP(p->d.dtype == LL_BF16 ? ll::delta_launch_fwd<bf16_t>(a, save_for_backward != 0, s)
-                               : ll::delta_launch_fwd<float>(a, save_for_backward != 0, s));
+  LL_HIP(p->d.dtype == LL_BF16 ? ll::delta_launch_fwd<bf16_t>(a, save_for_backward != 0, p->cus, s)
+                               : ll::delta_launch_fwd<float>(a, save_for_backward != 0, p->cus, s));
   if (save_for_backward) {
     p->saved = true;
     p->a.q = q; p->a.k = k; p->a.v = v; p->a.g = g; p->a.beta = beta; p->a.seq_len = seq_len;
@@ -279,7 +291,8 @@ ll_status delta_loop_bwd(ll_delta_plan* p, void* stream, const void* q, const vo
   a.dy = dy; a.dST = dST; a.dq = dq; a.dk = dk; a.dv = dv; a.dg = dg; a.dbeta = dbeta; a.dS0 = dS0;
   p->saved = false;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  LL_HIP(p->d.dtype == LL_BF16 ? ll::delta_launch_bwd<bf16_t>(a, s) : ll::delta_launch_bwd<float>(a, s));
+  LL_HIP(p->d.dtype == LL_BF16 ? ll::delta_launch_bwd<bf16_t>(a, p->cus, s)
+                               : ll::delta_launch_bwd<float>(a, p->cus, s));
   return LL_OK;
 }
 

@@ -5,10 +5,10 @@
 //   P_ij = scale e^{G_i - G_j} q_i.k_j   (j <= i)
 // the recurrence of the chunk's tokens is
 //   R = V - diag(e^G) K S0,   U = T diag(beta) R
-//   Y = scale diag(e^G) Q S0 + P U,   S' = e^{G_end} S0 + (diag(e^{G_end - G}) K)^T U
+//   Y = scale diag(e^G) Q S0 + P U,   S' = e^{G_end} S0 + K^T diag(e^{G_end - G}) U
 // and its gradient, from dY and dS',
 //   dU = P^T dY + diag(e^{G_end - G}) K dS',   Z = T^T dU,   dV = dR = beta Z
-//   dS0 = scale (diag(e^G) Q)^T dY + e^{G_end} dS' - (diag(e^G) K)^T dR
+//   dS0 = Q^T (scale diag(e^G) dY) + e^{G_end} dS' - K^T (diag(e^G) dR)
 //   F = scale tril(e^{G_i - G_j} dY_i.U_j),  H = -stril(e^{G_i - G_j} dR_i.U_j)
 //   dQ = scale diag(e^G) dY S0^T + F K
 //   dK = F^T Q + diag(e^{G_end - G}) U dS'^T - diag(e^G) dR S0^T + (H + H^T) K
@@ -16,9 +16,17 @@
 //   dg_t = sum_{i >= t} (dq_i.q_i - dv_i.v_i) + <dS', S'>   (i within the chunk)
 // beta counts as at least 2^-40 in magnitude, so that U_i / beta_i exists.
 //
-// Kernels: prep (T, P of every chunk at once), state_fwd (S, U, Y from chunk to
-// chunk, 32 columns of the state per work-group), state_bwd (dS, dR backwards,
-// the same split), grads (dQ, dK, dbeta, dg of every chunk at once).
+// Kernels: prep (T, P and the transposes of every chunk at once), state_fwd (S,
+// U, Y from chunk to chunk), state_bwd (dS, dR backwards), grads (dQ, dK, dbeta,
+// dg of every chunk at once).  The columns of the state do not meet in the two
+// loops, so each work-group has 16 or 32 of them (cols_of).
+//
+// Arithmetic.  The bfloat16 matrix instructions run at sixteen times the rate of
+// the float32 ones, so a float operand is taken as the sum of three bfloat16
+// pieces (24 bits, exactly), a bfloat16 one is its own piece, and a product of
+// pieces i and j is taken while i + j <= 2: what is dropped is below 2^-24 of the
+// term.  Results that leave the call as bfloat16 and feed nothing else take two
+// pieces (2^-16 against the rounding's 2^-9).  Sums are float32.
 #include "ll_delta.h"
 #include "ll_kernels.h"
 
@@ -27,508 +35,1237 @@ namespace ll {
 namespace {
 
 constexpr int CT = kDeltaChunk;
-constexpr int NT = 32;               // columns of the state per work-group
-constexpr int SC = CT + 4, SN = NT + 4;   // LDS row pitches
+constexpr int SC = CT + 4;           // row pitch of float [64][64] in LDS
+constexpr int RC = CT + 8;           // of bfloat16 [..][64]: 16 rows hit all banks
+constexpr int SQ = CT * CT;
+
+typedef bf16x8_t frag;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
 
 __device__ __forceinline__ f32x4 zero_acc() { return f32x4{0.f, 0.f, 0.f, 0.f}; }
+__device__ __forceinline__ f32x4 mfma(frag a, frag b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ frag as_frag(uint4 u) { return __builtin_bit_cast(frag, u); }
 
-// acc[n] += A[16 rows of the wave][K] B[K][16 n ..]: element (i, k) of A at
-// A[i * ar + k * ak], (k, c) of B at B[k * bk + c * bc].
-template <int N>
-__device__ __forceinline__ void mm(const float* A, int ar, int ak, const float* B, int bk, int bc, int K,
-                                   f32x4* acc) {
-  const int l = threadIdx.x & 63, lo = l & 15, hi = l >> 4;
-  for (int k = hi; k < K; k += 4) {
-    const float a = A[lo * ar + k * ak];
+// acc += A B for operands in NA and NB pieces, smallest products first.
+template <int NA, int NB, int LIM>
+__device__ __forceinline__ void mma(const frag* a, const frag* b, f32x4& acc) {
 #pragma unroll
-    for (int n = 0; n < N; ++n)
-      acc[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, B[k * bk + (16 * n + lo) * bc], acc[n], 0, 0, 0);
+  for (int s = LIM; s >= 0; --s)
+#pragma unroll
+    for (int i = 0; i < NA; ++i) {
+      const int j = s - i;
+      if (j >= 0 && j < NB) acc = mfma(a[i], b[j], acc);
+    }
+}
+
+// Two floats to two bfloat16 (round to nearest even).
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  const f32x2 v = {x, y};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
+}
+
+// x, y = sum of N bfloat16 pairs.
+template <int N>
+__device__ __forceinline__ void split2(float x, float y, uint32_t* p) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    p[i] = pack2(x, y);
+    if (i + 1 < N) {
+      x -= __uint_as_float(p[i] << 16);
+      y -= __uint_as_float(p[i] & 0xffff0000u);
+    }
   }
 }
 
-// rows [64][D] of a token array into LDS (pitch p, D padded to Dp by zeros),
-// zeros past the row's end
-template <typename T>
-__device__ void load_rows(float* dst, int p, const void* src, long ld, long head_off, int c0, int D, int Dp,
-                          int t0, int len, int b, int B) {
-  for (int i = threadIdx.x; i < CT * Dp; i += 256) {
-    const int r = i / Dp, c = i % Dp;
-    const int t = t0 + r;
-    float v = 0.f;
-    if (t < len && c < D)
-      v = Op<T>::to_f32(static_cast<const T*>(src)[((long)t * B + b) * ld + head_off + c0 + c]);
-    dst[r * p + c] = v;
+// Four floats to N pieces of four bfloat16, stored at dst + i * stride (elements).
+template <int N>
+__device__ __forceinline__ void split4_store(f32x4 x, bf16_t* dst, int stride) {
+  uint32_t a[N], b[N];
+  split2<N>(x[0], x[1], a);
+  split2<N>(x[2], x[3], b);
+#pragma unroll
+  for (int i = 0; i < N; ++i) *reinterpret_cast<uint2*>(dst + i * stride) = make_uint2(a[i], b[i]);
+}
+
+// Eight floats to N pieces.
+template <int N>
+__device__ __forceinline__ void split8(const float* x, uint4* p) {
+  uint32_t w[4][N];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) split2<N>(x[2 * e], x[2 * e + 1], w[e]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) p[i] = make_uint4(w[0][i], w[1][i], w[2][i], w[3][i]);
+}
+
+// Raw eight elements of an operand, and their pieces.
+template <typename T> struct Raw8;
+template <> struct Raw8<bf16_t> {
+  uint4 u;
+  __device__ __forceinline__ void zero() { u = zero4(); }
+  __device__ __forceinline__ void load(const bf16_t* p) { u = ld16(p); }
+  __device__ __forceinline__ void pieces(uint4* f) const { f[0] = u; }
+};
+template <> struct Raw8<float> {
+  uint4 u, v;
+  __device__ __forceinline__ void zero() { u = v = zero4(); }
+  __device__ __forceinline__ void load(const float* p) {
+    u = ld16(p);
+    v = ld16(p + 4);
   }
-}
+  __device__ __forceinline__ void pieces(uint4* f) const {
+    const float x[8] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w),
+                        __uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)};
+    split8<3>(x, f);
+  }
+};
 
-__device__ void load_square(float* dst, const float* src) {
-  for (int i = threadIdx.x; i < CT * CT; i += 256) dst[(i / CT) * SC + i % CT] = src[i];
-}
+template <typename T> struct Pieces { static constexpr int n = 3; };
+template <> struct Pieces<bf16_t> { static constexpr int n = 1; };
 
-__device__ __forceinline__ int pad16(int d) { return (d + 15) & ~15; }
+__device__ __forceinline__ frag lds_frag(const bf16_t* p) { return as_frag(ld16(p)); }
+
+// LDS written by other lanes of the same wave is read next.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 
 }  // namespace
 
-template <typename T>
+// ---------------------------------------------------------------------------
+// prep: one work-group per item.  k k^T and q k^T on the matrix cores, the
+// inverse of I + A by blocks of 16 (each diagonal block by substitution, the
+// blocks below by float32 products: T_rc = -T_rr sum_k A_rk T_kc, a wave per
+// block column), then everything the loops read in the order in which a lane
+// reads it, 16 bytes at a time.
+// ---------------------------------------------------------------------------
+template <typename T, int KS, bool SAVE>
 __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
-  extern __shared__ float lds[];
+  constexpr int NP = Pieces<T>::n, DP = 32 * KS, KP = DP + 8, PP = NP == 1 ? 2 : 3;
+  constexpr int kOps = 2 * NP * CT * KP * 2, kMats = 2 * CT * SC * 4;
+  __shared__ __align__(16) unsigned char raw[kOps > kMats ? kOps : kMats];
+  __shared__ __align__(16) float tm[CT * SC];
+  __shared__ double G[CT];
+  __shared__ float be[CT];
   const int n = blockIdx.x % a.nch, bh = blockIdx.x / a.nch;
-  const int b = bh / a.Hv, h = bh % a.Hv, hk = h / (a.Hv / a.Hk);
+  const int b = bh / a.Hv, h = bh % a.Hv, grp = a.Hv / a.Hk, hk = h / grp;
   const int len = delta_len(a, b), t0 = n * CT;
-  if (n == 0 && h == 0 && threadIdx.x == 0 && a.seq_len && (a.seq_len[b] < 0 || a.seq_len[b] > a.T))
+  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, lo = l & 15, hi = l >> 4;
+  if (n == 0 && h == 0 && tid == 0 && a.seq_len && (a.seq_len[b] < 0 || a.seq_len[b] > a.T))
     atomicOr(a.err, LL_DEVERR_SEQ_LEN_BIT);
   if (t0 >= len) return;
-  const int Dp = pad16(a.Dk), p = Dp + 4;
-  float* ks = lds;
-  float* qs = ks + CT * p;
-  float* am = qs + CT * p;
-  float* tm = am + CT * SC;
-  double* G = reinterpret_cast<double*>(tm + CT * SC);
-  float* be = reinterpret_cast<float*>(G + CT);
-  load_rows<T>(ks, p, a.k, a.k_ld, (long)hk * a.Dk, 0, a.Dk, Dp, t0, len, b, a.B);
-  load_rows<T>(qs, p, a.q, a.q_ld, (long)hk * a.Dk, 0, a.Dk, Dp, t0, len, b, a.B);
-  const long item = blockIdx.x;
-  if (threadIdx.x < CT) {
-    const int i = threadIdx.x, t = t0 + i;
+  const long item = blockIdx.x, kitem = ((long)b * a.Hk + hk) * a.nch + n;
+  bf16_t* kp = reinterpret_cast<bf16_t*>(raw);           // [NP][64][KP]
+  bf16_t* qp = kp + NP * CT * KP;
+  for (int i = tid; i < CT * DP / 8; i += 256) {
+    const int r = i / (DP / 8), c = (i % (DP / 8)) * 8, t = t0 + r;
+    Raw8<T> x, y;
+    if (t < len && c < a.Dk) {
+      const long tok = (long)t * a.B + b;
+      x.load(static_cast<const T*>(a.k) + tok * a.k_ld + (long)hk * a.Dk + c);
+      y.load(static_cast<const T*>(a.q) + tok * a.q_ld + (long)hk * a.Dk + c);
+    } else {
+      x.zero();
+      y.zero();
+    }
+    uint4 p[NP];
+    x.pieces(p);
+#pragma unroll
+    for (int e = 0; e < NP; ++e) *reinterpret_cast<uint4*>(kp + (e * CT + r) * KP + c) = p[e];
+    y.pieces(p);
+#pragma unroll
+    for (int e = 0; e < NP; ++e) *reinterpret_cast<uint4*>(qp + (e * CT + r) * KP + c) = p[e];
+  }
+  if (tid < CT) {
+    const int t = t0 + tid;
     float g = 0.f, bt = 0.f;
     if (t < len) {
       const long at = ((long)t * a.B + b) * a.Hv + h;
       g = a.g[at];
       bt = a.beta[at];
-      if (g < -200.f) g = -200.f;          // e^g is 0 all the same
+      if (g < -200.f) g = -200.f;          // e^g is 0 all the same, and sums stay finite
     }
     if (fabsf(bt) < 0x1p-40f) bt = copysignf(0x1p-40f, bt);
-    be[i] = bt;
-    double s = g;
+    be[tid] = bt;
+    double s = g;                          // differences of the sums keep float's bits
     for (int d = 1; d < 64; d <<= 1) {
       const double o = __shfl_up(s, d, 64);
-      if (i >= d) s += o;
+      if (tid >= d) s += o;
     }
-    G[i] = s;
+    G[tid] = s;
     const double end = __shfl(s, 63, 64);
-    a.G[item * CT + i] = s;
-    a.tok[item * CT + i] = make_float4(expf((float)s), expf((float)(end - s)), bt, 0.f);
+    if (SAVE) a.G[item * CT + tid] = s;
+    a.tok[item * CT + tid] = make_float4(expf((float)s), expf((float)(end - s)), bt, 0.f);
   }
   __syncthreads();
-  const int w = threadIdx.x >> 6, l = threadIdx.x & 63, lo = l & 15, hi = l >> 4;
   f32x4 kk[4], qk[4];
-  for (int i = 0; i < 4; ++i) kk[i] = qk[i] = zero_acc();
-  mm<4>(ks + 16 * w * p, p, 1, ks, 1, p, Dp, kk);
-  mm<4>(qs + 16 * w * p, p, 1, ks, 1, p, Dp, qk);
+#pragma unroll
+  for (int m = 0; m < 4; ++m) kk[m] = qk[m] = zero_acc();
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    frag ka[NP], qa[NP];
+#pragma unroll
+    for (int e = 0; e < NP; ++e) {
+      ka[e] = lds_frag(kp + (e * CT + 16 * w + lo) * KP + 32 * s + 8 * hi);
+      qa[e] = lds_frag(qp + (e * CT + 16 * w + lo) * KP + 32 * s + 8 * hi);
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+      if (m <= w) {
+        frag kb[NP];
+#pragma unroll
+        for (int e = 0; e < NP; ++e) kb[e] = lds_frag(kp + (e * CT + 16 * m + lo) * KP + 32 * s + 8 * hi);
+        mma<NP, NP, 2>(ka, kb, kk[m]);
+        mma<NP, NP, 2>(qa, kb, qk[m]);
+      }
+  }
+  // K^T (and Q^T): once per key head
+  if (h == hk * grp)
+    for (int i = tid; i < NP * DP * 8; i += 256) {
+      const int c = i % DP, j = (i / DP) % 8 * 8, e = i / (DP * 8);
+      uint32_t x[4], y[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const bf16_t* k0 = kp + (e * CT + j + 2 * m) * KP + c;
+        x[m] = (uint32_t)k0[0] | (uint32_t)k0[KP] << 16;
+        if (SAVE) {
+          const bf16_t* q0 = qp + (e * CT + j + 2 * m) * KP + c;
+          y[m] = (uint32_t)q0[0] | (uint32_t)q0[KP] << 16;
+        }
+      }
+      const long at = ((kitem * NP + e) * DP + c) * CT + j;
+      *reinterpret_cast<uint4*>(a.ktp + at) = make_uint4(x[0], x[1], x[2], x[3]);
+      if (SAVE) *reinterpret_cast<uint4*>(a.qtp + at) = make_uint4(y[0], y[1], y[2], y[3]);
+    }
+  __syncthreads();
+  float* am = reinterpret_cast<float*>(raw);
+  float* pm = am + CT * SC;
+#pragma unroll
   for (int m = 0; m < 4; ++m)
+#pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int i = 16 * w + 4 * hi + r, j = 16 * m + lo;
       const float d = j <= i ? expf((float)(G[i] - G[j])) : 0.f;
       am[i * SC + j] = j < i ? be[i] * d * kk[m][r] : 0.f;
-      a.pm[item * CT * CT + i * CT + j] = j <= i ? a.scale * d * qk[m][r] : 0.f;
+      pm[i * SC + j] = j <= i ? a.scale * d * qk[m][r] : 0.f;
     }
   __syncthreads();
-  if (threadIdx.x < CT) {
-    const int c = threadIdx.x;
-    for (int i = 0; i < CT; ++i) {
-      float x = i == c ? 1.f : 0.f;
-      for (int j = c; j < i; ++j) x -= am[i * SC + j] * tm[j * SC + c];
-      tm[i * SC + c] = x;
+  {
+    // diagonal block w: column lo by substitution, in registers
+    const float* A = am + 16 * w * SC + 16 * w;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float s = i == lo ? 1.f : 0.f;
+#pragma unroll
+      for (int j = 0; j < i; ++j) s -= A[i * SC + j] * x[j];
+      x[i] = s;
     }
+    if (hi == 0) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) tm[(16 * w + i) * SC + 16 * w + lo] = x[i];
+    }
+    // above the diagonal: zero
+    for (int m = 0; m < w; ++m)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) tm[(16 * m + 4 * hi + r) * SC + 16 * w + lo] = 0.f;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < CT * CT; i += 256) a.tm[item * CT * CT + i] = tm[(i / CT) * SC + i % CT];
+  for (int r = w + 1; r < 4; ++r) {
+    f32x4 x = zero_acc(), z = zero_acc();
+    for (int k = w; k < r; ++k)
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        x = __builtin_amdgcn_mfma_f32_16x16x4f32(am[(16 * r + lo) * SC + 16 * k + 4 * s + hi],
+                                                 tm[(16 * k + 4 * s + hi) * SC + 16 * w + lo], x, 0, 0, 0);
+    float* blk = tm + 16 * r * SC + 16 * w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) blk[(4 * hi + e) * SC + lo] = -x[e];
+    wave_lds_fence();
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      z = __builtin_amdgcn_mfma_f32_16x16x4f32(tm[(16 * r + lo) * SC + 16 * r + 4 * s + hi],
+                                               blk[(4 * s + hi) * SC + lo], z, 0, 0, 0);
+    wave_lds_fence();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) blk[(4 * hi + e) * SC + lo] = z[e];
+    wave_lds_fence();
+  }
+  __syncthreads();
+  for (int i = tid; i < CT * 8; i += 256) {
+    const int r = i / 8, j = i % 8 * 8;
+    float x[8];
+    uint4 p[3];
+    const long at = (long)r * CT + j;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = tm[r * SC + j + e];
+    split8<3>(x, p);
+#pragma unroll
+    for (int e = 0; e < 3; ++e) *reinterpret_cast<uint4*>(a.tp + (item * 3 + e) * SQ + at) = p[e];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = pm[r * SC + j + e];
+    split8<PP>(x, p);
+#pragma unroll
+    for (int e = 0; e < PP; ++e) *reinterpret_cast<uint4*>(a.pp + (item * 3 + e) * SQ + at) = p[e];
+  }
+  if (SAVE)
+    for (int i = tid; i < CT * 8; i += 256) {
+      const int r = i % CT, j = i / CT * 8;              // row r of the transpose: column r
+      float x[8];
+      uint4 p[3];
+      const long at = (long)r * CT + j;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = tm[(j + e) * SC + r];
+      split8<3>(x, p);
+#pragma unroll
+      for (int e = 0; e < 3; ++e) *reinterpret_cast<uint4*>(a.ttp + (item * 3 + e) * SQ + at) = p[e];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = pm[(j + e) * SC + r];
+      split8<3>(x, p);
+#pragma unroll
+      for (int e = 0; e < 3; ++e) *reinterpret_cast<uint4*>(a.ptp + (item * 3 + e) * SQ + at) = p[e];
+    }
 }
 
-template <typename T, bool SAVE>
-__global__ __launch_bounds__(256) void delta_state_fwd_kernel(DeltaArgs a) {
-  extern __shared__ float lds[];
-  const int ntile = (a.Dv + NT - 1) / NT;
-  const int ct = blockIdx.x % ntile, bh = blockIdx.x / ntile;
-  const int b = bh / a.Hv, h = bh % a.Hv, hk = h / (a.Hv / a.Hk);
-  const int len = delta_len(a, b), live = (len + CT - 1) / CT;
-  const int Dp = pad16(a.Dk), p = Dp + 4, c0 = ct * NT;
-  float* ks = lds;
-  float* qs = ks + CT * p;
-  float* S = qs + CT * p;              // [Dp][NT]
-  float* tm = S + Dp * SN;
-  float* pm = tm + CT * SC;
-  float* R = pm + CT * SC;             // [64][NT]
-  float* U = R + CT * SN;
-  float4* tok = reinterpret_cast<float4*>(U + CT * SN);
-  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, lo = l & 15, hi = l >> 4;
-  const long head = (long)bh * a.Dk * a.Dv;
-  for (int i = tid; i < Dp * NT; i += 256) {
-    const int d = i / NT, c = i % NT;
-    S[d * SN + c] = a.S0 && d < a.Dk && c0 + c < a.Dv ? a.S0[head + (long)d * a.Dv + c0 + c] : 0.f;
+namespace {
+
+// Barrier of the work-group that orders LDS only: loads and stores of global
+// memory stay in flight across it.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// One row and head's walk by a wave of the two loops: its place, and the
+// addresses that move from chunk to chunk.
+struct Walk {
+  int b, h, hk, len, live, c0, w, lo, hi, arow, crow;
+  long head, item0, kitem0;
+  __device__ Walk(const DeltaArgs& a, int NT) {
+    const int ntile = (a.Dv + NT - 1) / NT;
+    const int bh = blockIdx.x / ntile;
+    c0 = (int)(blockIdx.x % ntile) * NT;
+    b = bh / a.Hv;
+    h = bh % a.Hv;
+    hk = h / (a.Hv / a.Hk);
+    len = delta_len(a, b);
+    live = (len + CT - 1) / CT;
+    head = (long)bh * a.Dk * a.Dv;
+    item0 = (long)bh * a.nch;
+    kitem0 = ((long)b * a.Hk + hk) * a.nch;
+    const int l = threadIdx.x & 63;
+    w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6) & 3);
+    lo = l & 15;
+    hi = l >> 4;
+    arow = 16 * w + lo;                // row of an A operand
+    crow = 16 * w + 4 * hi;            // first of the four rows of a result
   }
-  for (int n = 0; n < live; ++n) {
-    const long item = (long)bh * a.nch + n;
-    const int t0 = n * CT;
-    __syncthreads();
-    load_rows<T>(ks, p, a.k, a.k_ld, (long)hk * a.Dk, 0, a.Dk, Dp, t0, len, b, a.B);
-    load_rows<T>(qs, p, a.q, a.q_ld, (long)hk * a.Dk, 0, a.Dk, Dp, t0, len, b, a.B);
-    load_rows<T>(R, SN, a.v, a.v_ld, (long)h * a.Dv, c0, min(NT, a.Dv - c0), NT, t0, len, b, a.B);
-    load_square(tm, a.tm + item * CT * CT);
-    load_square(pm, a.pm + item * CT * CT);
-    if (tid < CT) tok[tid] = a.tok[item * CT + tid];
-    if (SAVE)
-      for (int i = tid; i < a.Dk * NT; i += 256) {
-        const int d = i / NT, c = i % NT;
-        if (c0 + c < a.Dv) a.st[item * a.Dk * a.Dv + (long)d * a.Dv + c0 + c] = S[d * SN + c];
-      }
-    __syncthreads();
-    f32x4 acc[2] = {zero_acc(), zero_acc()};
-    mm<2>(ks + 16 * w * p, p, 1, S, SN, 1, Dp, acc);
+};
+
+// Rows 16 w .. of K or Q of a chunk, 32 elements a step.
+template <typename T, int KS>
+__device__ __forceinline__ void load_rows16(Raw8<T>* x, const T* p, bool in, int Dk, int hi) {
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
-      for (int r = 0; r < 4; ++r) {
-        const int i = 16 * w + 4 * hi + r, c = 16 * m + lo;
-        R[i * SN + c] = tok[i].z * (R[i * SN + c] - tok[i].x * acc[m][r]);
-      }
-    __syncthreads();
-    f32x4 u[2] = {zero_acc(), zero_acc()};
-    mm<2>(tm + 16 * w * SC, SC, 1, R, SN, 1, CT, u);
+  for (int s = 0; s < KS; ++s) {
+    if (in && 32 * s + 8 * hi < Dk) x[s].load(p + 32 * s);
+    else x[s].zero();
+  }
+}
+
+// Rows 16 w .. of a [64][64] in N pieces; p: the wave's row, its lane's chunk.
+template <int N>
+__device__ __forceinline__ void load_square16(uint4 (*x)[2], const bf16_t* p) {
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
-      for (int r = 0; r < 4; ++r) {
-        const int i = 16 * w + 4 * hi + r, c = 16 * m + lo;
-        U[i * SN + c] = u[m][r];
-        if (SAVE && c0 + c < a.Dv) a.u[(item * CT + i) * a.Dv + c0 + c] = u[m][r];
-      }
-    __syncthreads();
-    f32x4 y0[2] = {zero_acc(), zero_acc()}, y1[2] = {zero_acc(), zero_acc()};
-    mm<2>(qs + 16 * w * p, p, 1, S, SN, 1, Dp, y0);
-    mm<2>(pm + 16 * w * SC, SC, 1, U, SN, 1, CT, y1);
+  for (int e = 0; e < N; ++e)
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
-      for (int r = 0; r < 4; ++r) {
-        const int i = 16 * w + 4 * hi + r, c = 16 * m + lo, t = t0 + i;
-        if (t < a.T && c0 + c < a.Dv)
-          static_cast<T*>(a.y)[(((long)t * a.B + b) * a.Hv + h) * a.Dv + c0 + c] =
-              Op<T>::from_f32(t < len ? a.scale * tok[i].x * y0[m][r] + y1[m][r] : 0.f);
-      }
-    __syncthreads();
-    for (int i = tid; i < CT * NT; i += 256) U[(i / NT) * SN + i % NT] *= tok[i / NT].y;
-    __syncthreads();
-    const float end = tok[CT - 1].x;
-    for (int mt = w; mt < Dp / 16; mt += 4) {
-      f32x4 s[2] = {zero_acc(), zero_acc()};
-      mm<2>(ks + 16 * mt, 1, p, U, SN, 1, CT, s);
-  #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int s = 0; s < 2; ++s) x[e][s] = ld16(p + e * SQ + 32 * s);
+}
+
+// MT tiles of 16 rows of K^T or Q^T.
+template <int NP, int MT, int DP>
+__device__ __forceinline__ void load_transposed(uint4 (*x)[MT][2], const bf16_t* p, bool in) {
+#pragma unroll
+  for (int e = 0; e < NP; ++e)
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) x[e][m][s] = in ? ld16(p + (e * DP + 16 * m) * CT + 32 * s) : zero4();
+}
+
+// B operand: NN pieces of column `col` at k, from LDS [piece][NT][pitch].
+template <int NN>
+__device__ __forceinline__ void load_b(frag* f, const bf16_t* p, int stride) {
+#pragma unroll
+  for (int e = 0; e < NN; ++e) f[e] = lds_frag(p + e * stride);
+}
+
+template <int MT, int NL>
+struct State {
+  f32x4 x[MT][NL];
+  // (d, c) of [Dk][Dv] floats at p; zeros without one and past its end
+  __device__ __forceinline__ void load(const Walk& k, const DeltaArgs& a, const float* p) {
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int q = 0; q < NL; ++q)
+#pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float& x = S[(16 * mt + 4 * hi + r) * SN + 16 * m + lo];
-          x = end * x + s[m][r];
+          const int d = 16 * (k.w * MT + m) + 4 * k.hi + r, c = k.c0 + 16 * q + k.lo;
+          x[m][q][r] = p && d < a.Dk && c < a.Dv ? p[(unsigned)(d * a.Dv + c)] : 0.f;
         }
-    }
   }
-  __syncthreads();
-  if (a.ST)
-    for (int i = tid; i < a.Dk * NT; i += 256) {
-      const int d = i / NT, c = i % NT;
-      if (c0 + c < a.Dv) a.ST[head + (long)d * a.Dv + c0 + c] = S[d * SN + c];
-    }
-  for (int t = live * CT + tid / NT; t < a.T; t += 256 / NT)
-    if (c0 + tid % NT < a.Dv)
-      static_cast<T*>(a.y)[(((long)t * a.B + b) * a.Hv + h) * a.Dv + c0 + tid % NT] = Op<T>::from_f32(0.f);
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void delta_state_bwd_kernel(DeltaArgs a) {
-  extern __shared__ float lds[];
-  const int ntile = (a.Dv + NT - 1) / NT;
-  const int ct = blockIdx.x % ntile, bh = blockIdx.x / ntile;
-  const int b = bh / a.Hv, h = bh % a.Hv, hk = h / (a.Hv / a.Hk);
-  const int len = delta_len(a, b), live = (len + CT - 1) / CT;
-  const int Dp = pad16(a.Dk), p = Dp + 4, c0 = ct * NT;
-  float* ks = lds;
-  float* qs = ks + CT * p;
-  float* S = qs + CT * p;              // dS [Dp][NT]
-  float* tm = S + Dp * SN;
-  float* pm = tm + CT * SC;
-  float* dY = pm + CT * SC;            // [64][NT]
-  float* U = dY + CT * SN;             // dU, then dR
-  float4* tok = reinterpret_cast<float4*>(U + CT * SN);
-  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, lo = l & 15, hi = l >> 4;
-  const long head = (long)bh * a.Dk * a.Dv;
-  for (int i = tid; i < Dp * NT; i += 256) {
-    const int d = i / NT, c = i % NT;
-    S[d * SN + c] = a.dST && d < a.Dk && c0 + c < a.Dv ? a.dST[head + (long)d * a.Dv + c0 + c] : 0.f;
-  }
-  for (int n = live - 1; n >= 0; --n) {
-    const long item = (long)bh * a.nch + n;
-    const int t0 = n * CT;
-    __syncthreads();
-    load_rows<T>(ks, p, a.k, a.k_ld, (long)hk * a.Dk, 0, a.Dk, Dp, t0, len, b, a.B);
-    load_rows<T>(qs, p, a.q, a.q_ld, (long)hk * a.Dk, 0, a.Dk, Dp, t0, len, b, a.B);
-    load_rows<T>(dY, SN, a.dy, (long)a.Hv * a.Dv, (long)h * a.Dv, c0, min(NT, a.Dv - c0), NT, t0, len, b, a.B);
-    load_square(tm, a.tm + item * CT * CT);
-    load_square(pm, a.pm + item * CT * CT);
-    if (tid < CT) tok[tid] = a.tok[item * CT + tid];
-    for (int i = tid; i < a.Dk * NT; i += 256) {
-      const int d = i / NT, c = i % NT;
-      if (c0 + c < a.Dv) a.dst[item * a.Dk * a.Dv + (long)d * a.Dv + c0 + c] = S[d * SN + c];
-    }
-    __syncthreads();
-    f32x4 u0[2] = {zero_acc(), zero_acc()}, u1[2] = {zero_acc(), zero_acc()};
-    mm<2>(pm + 16 * w, 1, SC, dY, SN, 1, CT, u0);
-    mm<2>(ks + 16 * w * p, p, 1, S, SN, 1, Dp, u1);
+  __device__ __forceinline__ void store(const Walk& k, const DeltaArgs& a, float* p) {
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
-      for (int r = 0; r < 4; ++r) {
-        const int i = 16 * w + 4 * hi + r;
-        U[i * SN + 16 * m + lo] = u0[m][r] + tok[i].y * u1[m][r];
-      }
-    __syncthreads();
-    f32x4 z[2] = {zero_acc(), zero_acc()};
-    mm<2>(tm + 16 * w, 1, SC, U, SN, 1, CT, z);
-    __syncthreads();
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
-      for (int r = 0; r < 4; ++r) {
-        const int i = 16 * w + 4 * hi + r, c = 16 * m + lo, t = t0 + i;
-        const float dr = tok[i].z * z[m][r];
-        U[i * SN + c] = tok[i].x * dr;
-        if (c0 + c < a.Dv) {
-          a.dr[(item * CT + i) * a.Dv + c0 + c] = dr;
-          if (t < a.T)
-            static_cast<T*>(a.dv)[((long)t * a.B + b) * a.dv_ld + (long)h * a.Dv + c0 + c] =
-                Op<T>::from_f32(t < len ? dr : 0.f);
-        }
-        dY[i * SN + c] *= a.scale * tok[i].x;
-      }
-    __syncthreads();
-    const float end = tok[CT - 1].x;
-    for (int mt = w; mt < Dp / 16; mt += 4) {
-      f32x4 s0[2] = {zero_acc(), zero_acc()}, s1[2] = {zero_acc(), zero_acc()};
-      mm<2>(qs + 16 * mt, 1, p, dY, SN, 1, CT, s0);
-      mm<2>(ks + 16 * mt, 1, p, U, SN, 1, CT, s1);
-  #pragma unroll
-    for (int m = 0; m < 2; ++m)
+      for (int q = 0; q < NL; ++q)
+#pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float& x = S[(16 * mt + 4 * hi + r) * SN + 16 * m + lo];
-          x = end * x + s0[m][r] - s1[m][r];
+          const int d = 16 * (k.w * MT + m) + 4 * k.hi + r, c = k.c0 + 16 * q + k.lo;
+          if (d < a.Dk && c < a.Dv) p[(unsigned)(d * a.Dv + c)] = x[m][q][r];
         }
-    }
   }
-  __syncthreads();
-  if (a.dS0)
-    for (int i = tid; i < a.Dk * NT; i += 256) {
-      const int d = i / NT, c = i % NT;
-      if (c0 + c < a.Dv) a.dS0[head + (long)d * a.Dv + c0 + c] = S[d * SN + c];
-    }
-  for (int t = live * CT + tid / NT; t < a.T; t += 256 / NT)
-    if (c0 + tid % NT < a.Dv)
-      static_cast<T*>(a.dv)[((long)t * a.B + b) * a.dv_ld + (long)h * a.Dv + c0 + tid % NT] = Op<T>::from_f32(0.f);
+  // in pieces, column-major, for the products that read it
+  __device__ __forceinline__ void publish(const Walk& k, bf16_t* Sp, int KP) {
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int q = 0; q < NL; ++q)
+        split4_store<3>(x[m][q], Sp + (16 * q + k.lo) * KP + 16 * (k.w * MT + m) + 4 * k.hi, 16 * NL * KP);
+  }
+};
+
+template <typename T, int NT>
+__device__ void zero_rest(T* out, long tok_ld, const DeltaArgs& a, const Walk& k) {
+  const int tid = threadIdx.x, c = k.c0 + tid % NT;
+  if (c < a.Dv)
+    for (int t = k.live * CT + tid / NT; t < a.T; t += 512 / NT)
+      out[((long)t * a.B + k.b) * tok_ld + (long)k.h * a.Dv + c] = Op<T>::from_f32(0.f);
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void delta_grads_kernel(DeltaArgs a) {
-  extern __shared__ float lds[];
+}  // namespace
+
+// ---------------------------------------------------------------------------
+// state_fwd: the loop over a row's chunks for 16 NL columns of one head's state.
+// Waves 0-3 carry the recurrence: K S, T R, K^T U, each wave 16 of the 64 tokens
+// (and a quarter of the state's rows, which stay in its accumulators in float32);
+// what the next product needs of the other waves goes through LDS in pieces.
+// Waves 4-7 make Y beside them from the same pieces.  Three barriers a chunk.
+// The operands that do not depend on the state are loaded a chunk ahead.
+// ---------------------------------------------------------------------------
+template <typename T, int KS, int NL, bool SAVE>
+__global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
+  constexpr int NP = Pieces<T>::n, PP = NP == 1 ? 2 : 3, DP = 32 * KS, KP = DP + 8, NT = 16 * NL;
+  constexpr int MT = KS == 4 ? 2 : 1;                  // 16-row tiles of the state per wave
+  // K^T a chunk ahead too, where the registers hold it
+  constexpr bool AHEAD = NP == 1;
+  __shared__ __align__(16) bf16_t Sp[3 * NT * KP];     // state, column-major pieces
+  __shared__ __align__(16) bf16_t Rp[3 * NT * RC], Up[3 * NT * RC], Uy[PP * NT * RC];
+  __shared__ float s_end;
+  const Walk k(a, NT);
+  const int lo = k.lo, hi = k.hi;
+  T* const y0 = static_cast<T*>(a.y);
+  if (threadIdx.x < 256) {
+    const bool own = k.w * MT * 16 < DP;               // this wave holds rows of the state
+    State<MT, NL> S;
+    S.load(k, a, a.S0 && own ? a.S0 + k.head : nullptr);
+    if (own) S.publish(k, Sp, KP);
+    const T* kp = static_cast<const T*>(a.k) + ((long)k.arow * a.B + k.b) * a.k_ld + (long)k.hk * a.Dk + 8 * hi;
+    const T* vp = static_cast<const T*>(a.v) + ((long)k.crow * a.B + k.b) * a.v_ld + (long)k.h * a.Dv + k.c0 + lo;
+    const bf16_t* tp = a.tp + k.item0 * 3 * SQ + k.arow * CT + 8 * hi;
+    const bf16_t* ktp = a.ktp + (k.kitem0 * NP * DP + 16 * k.w * MT + lo) * CT + 8 * hi;
+    const float4* tkp = a.tok + k.item0 * CT + k.crow;
+    const long kstep = (long)CT * a.B * a.k_ld, vstep = (long)CT * a.B * a.v_ld, vrow = (long)a.B * a.v_ld;
+    Raw8<T> rows[KS];
+    uint4 sq[3][2], kt[NP][MT][2];
+    float4 tok[4];
+    T vraw[4][NL];
+    auto fetch = [&](int n) {
+      load_rows16<T, KS>(rows, kp, n * CT + k.arow < k.len, a.Dk, hi);
+      load_square16<3>(sq, tp);
+      if (AHEAD) load_transposed<NP, MT, DP>(kt, ktp, own);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        tok[r] = tkp[r];
+#pragma unroll
+        for (int q = 0; q < NL; ++q)
+          vraw[r][q] = n * CT + k.crow + r < k.len && k.c0 + 16 * q + lo < a.Dv ? vp[r * vrow + 16 * q] : (T)0;
+      }
+      kp += kstep;
+      vp += vstep;
+      tp += 3 * SQ;
+      tkp += CT;
+      if (AHEAD) ktp += (long)NP * DP * CT;
+    };
+    if (k.live > 0) fetch(0);
+    lds_barrier();
+    for (int n = 0; n < k.live; ++n) {
+      const long item = k.item0 + n;
+      frag ra[KS][NP];
+      uint4 ta[3][2], ka[NP][MT][2];
+      float4 tk[4];
+      float v[4][NL];
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        uint4 p[NP];
+        rows[s].pieces(p);
+#pragma unroll
+        for (int e = 0; e < NP; ++e) ra[s][e] = as_frag(p[e]);
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+#pragma unroll
+        for (int e = 0; e < 3; ++e) ta[e][s] = sq[e][s];
+        if (AHEAD)
+#pragma unroll
+          for (int e = 0; e < NP; ++e)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) ka[e][m][s] = kt[e][m][s];
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        tk[r] = tok[r];
+#pragma unroll
+        for (int q = 0; q < NL; ++q) v[r][q] = Op<T>::to_f32(vraw[r][q]);
+      }
+      if (k.w == 3 && hi == 3 && lo == 0) s_end = tk[3].x;
+      if (!AHEAD) {
+        load_transposed<NP, MT, DP>(ka, ktp, own);
+        ktp += (long)NP * DP * CT;
+      }
+      if (n + 1 < k.live) fetch(n + 1);
+      f32x4 ks[NL];
+#pragma unroll
+      for (int q = 0; q < NL; ++q) ks[q] = zero_acc();
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int q = 0; q < NL; ++q) {
+          frag sb[3];
+          load_b<3>(sb, Sp + (16 * q + lo) * KP + 32 * s + 8 * hi, NT * KP);
+          mma<NP, 3, 2>(ra[s], sb, ks[q]);
+        }
+#pragma unroll
+      for (int q = 0; q < NL; ++q) {
+        f32x4 rr;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) rr[r] = tk[r].z * (v[r][q] - tk[r].x * ks[q][r]);
+        split4_store<3>(rr, Rp + (16 * q + lo) * RC + k.crow, NT * RC);
+      }
+      if (SAVE && own) S.store(k, a, a.st + item * a.Dk * a.Dv);
+      lds_barrier();
+#pragma unroll
+      for (int q = 0; q < NL; ++q) {
+        f32x4 u = zero_acc(), us;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          frag rb[3], tf[3];
+          load_b<3>(rb, Rp + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
+#pragma unroll
+          for (int e = 0; e < 3; ++e) tf[e] = as_frag(ta[e][s]);
+          mma<3, 3, 2>(tf, rb, u);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) us[r] = tk[r].y * u[r];
+        split4_store<3>(us, Up + (16 * q + lo) * RC + k.crow, NT * RC);
+        split4_store<PP>(u, Uy + (16 * q + lo) * RC + k.crow, NT * RC);
+        if (SAVE && k.c0 + 16 * q + lo < a.Dv) {
+          float* up = a.u + (item * CT + 16 * k.w) * a.Dv + k.c0 + 16 * q;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) up[(unsigned)((4 * hi + r) * a.Dv + lo)] = u[r];
+        }
+      }
+      lds_barrier();
+      if (own) {
+        const float e_end = s_end;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int q = 0; q < NL; ++q) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S.x[m][q][r] *= e_end;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              frag ub[3], kf[NP];
+              load_b<3>(ub, Up + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
+#pragma unroll
+              for (int e = 0; e < NP; ++e) kf[e] = as_frag(ka[e][m][s]);
+              mma<NP, 3, 2>(kf, ub, S.x[m][q]);
+            }
+          }
+        S.publish(k, Sp, KP);
+      }
+      lds_barrier();
+    }
+    if (own && a.ST) S.store(k, a, a.ST + k.head);
+  } else {
+    const T* qp = static_cast<const T*>(a.q) + ((long)k.arow * a.B + k.b) * a.q_ld + (long)k.hk * a.Dk + 8 * hi;
+    const bf16_t* pp = a.pp + k.item0 * 3 * SQ + k.arow * CT + 8 * hi;
+    const float4* tkp = a.tok + k.item0 * CT + k.crow;
+    T* yp = y0 + (((long)k.crow * a.B + k.b) * a.Hv + k.h) * a.Dv + k.c0 + lo;
+    const long qstep = (long)CT * a.B * a.q_ld, yrow = (long)a.B * a.Hv * a.Dv;
+    Raw8<T> rows[KS];
+    uint4 sq[3][2];
+    float tok[4];
+    auto fetch = [&](int n) {
+      load_rows16<T, KS>(rows, qp, n * CT + k.arow < k.len, a.Dk, hi);
+      load_square16<PP>(sq, pp);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) tok[r] = tkp[r].x;
+      qp += qstep;
+      pp += 3 * SQ;
+      tkp += CT;
+    };
+    if (k.live > 0) fetch(0);
+    lds_barrier();
+    for (int n = 0; n < k.live; ++n) {
+      uint4 pa[PP][2];
+      float tk[4];
+      f32x4 y[NL];
+#pragma unroll
+      for (int q = 0; q < NL; ++q) y[q] = zero_acc();
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        frag ra[NP];
+        uint4 p[NP];
+        rows[s].pieces(p);
+#pragma unroll
+        for (int e = 0; e < NP; ++e) ra[e] = as_frag(p[e]);
+#pragma unroll
+        for (int q = 0; q < NL; ++q) {
+          frag sb[PP];
+          load_b<PP>(sb, Sp + (16 * q + lo) * KP + 32 * s + 8 * hi, NT * KP);
+          mma<NP, PP, PP - 1>(ra, sb, y[q]);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < PP; ++e)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) pa[e][s] = sq[e][s];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) tk[r] = a.scale * tok[r];
+      if (n + 1 < k.live) fetch(n + 1);
+      lds_barrier();
+      lds_barrier();
+#pragma unroll
+      for (int q = 0; q < NL; ++q) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[q][r] *= tk[r];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          frag ub[PP], pf[PP];
+          load_b<PP>(ub, Uy + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
+#pragma unroll
+          for (int e = 0; e < PP; ++e) pf[e] = as_frag(pa[e][s]);
+          mma<PP, PP, PP - 1>(pf, ub, y[q]);
+        }
+        if (k.c0 + 16 * q + lo < a.Dv) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int t = n * CT + k.crow + r;
+            if (t < a.T) yp[r * yrow + 16 * q] = Op<T>::from_f32(t < k.len ? y[q][r] : 0.f);
+          }
+        }
+      }
+      yp += CT * yrow;
+      lds_barrier();
+    }
+  }
+  zero_rest<T, NT>(y0, (long)a.Hv * a.Dv, a, k);
+}
+
+// ---------------------------------------------------------------------------
+// state_bwd: the gradient loop, the same split.  Waves 0-3 carry dS: K dS, T^T dU,
+// K^T dR.  Waves 4-7 make what does not depend on it, P^T dY and Q^T (scale e^G
+// dY), one chunk ahead, each for the chain wave of its rows (through LDS, in the
+// accumulators' order).
+// ---------------------------------------------------------------------------
+template <typename T, int KS, int NL>
+__global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
+  constexpr int NP = Pieces<T>::n, DP = 32 * KS, KP = DP + 8, NT = 16 * NL;
+  constexpr int MT = KS == 4 ? 2 : 1;
+  constexpr bool AHEAD = NP == 1;
+  __shared__ __align__(16) bf16_t Sp[3 * NT * KP];
+  __shared__ __align__(16) bf16_t Rp[3 * NT * RC], Up[3 * NT * RC];
+  __shared__ __align__(16) bf16_t Yp[NP * NT * RC], Ys[3 * NT * RC];   // dY, scale e^G dY of the next chunk
+  __shared__ f32x4 mail[2][4][(MT + 1) * NL][64];
+  __shared__ float s_end;
+  const Walk k(a, NT);
+  const int lo = k.lo, hi = k.hi, l = threadIdx.x & 63;
+  const bool rows_here = k.w * MT * 16 < DP;
+  const long last = k.live - 1;                          // the loop runs from here down
+  T* const dv0 = static_cast<T*>(a.dv);
+  if (threadIdx.x < 256) {
+    State<MT, NL> S;
+    S.load(k, a, a.dST && rows_here ? a.dST + k.head : nullptr);
+    if (rows_here) S.publish(k, Sp, KP);
+    const T* kp = static_cast<const T*>(a.k) + ((last * CT + k.arow) * a.B + k.b) * a.k_ld + (long)k.hk * a.Dk + 8 * hi;
+    const bf16_t* tp = a.ttp + (k.item0 + last) * 3 * SQ + k.arow * CT + 8 * hi;
+    const bf16_t* ktp = a.ktp + ((k.kitem0 + last) * NP * DP + 16 * k.w * MT + lo) * CT + 8 * hi;
+    const float4* tkp = a.tok + (k.item0 + last) * CT + k.crow;
+    T* vp = dv0 + ((last * CT + k.crow) * a.B + k.b) * a.dv_ld + (long)k.h * a.Dv + k.c0 + lo;
+    const long kstep = (long)CT * a.B * a.k_ld, vrow = (long)a.B * a.dv_ld;
+    Raw8<T> rows[KS];
+    uint4 sq[3][2], kt[NP][MT][2];
+    float4 tok[4];
+    auto fetch = [&](int n) {
+      load_rows16<T, KS>(rows, kp, n * CT + k.arow < k.len, a.Dk, hi);
+      load_square16<3>(sq, tp);
+      if (AHEAD) load_transposed<NP, MT, DP>(kt, ktp, rows_here);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) tok[r] = tkp[r];
+      kp -= kstep;
+      tp -= 3 * SQ;
+      tkp -= CT;
+      if (AHEAD) ktp -= (long)NP * DP * CT;
+    };
+    if (k.live > 0) fetch(k.live - 1);
+    lds_barrier();
+    lds_barrier();
+    for (int n = k.live - 1; n >= 0; --n) {
+      const long item = k.item0 + n;
+      const int slot = n & 1;
+      frag ra[KS][NP];
+      uint4 ta[3][2], ka[NP][MT][2];
+      float4 tk[4];
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        uint4 p[NP];
+        rows[s].pieces(p);
+#pragma unroll
+        for (int e = 0; e < NP; ++e) ra[s][e] = as_frag(p[e]);
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+#pragma unroll
+        for (int e = 0; e < 3; ++e) ta[e][s] = sq[e][s];
+        if (AHEAD)
+#pragma unroll
+          for (int e = 0; e < NP; ++e)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) ka[e][m][s] = kt[e][m][s];
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) tk[r] = tok[r];
+      if (k.w == 3 && hi == 3 && lo == 0) s_end = tk[3].x;   // e^{G_end}
+      if (!AHEAD) {
+        load_transposed<NP, MT, DP>(ka, ktp, rows_here);
+        ktp -= (long)NP * DP * CT;
+      }
+      if (n > 0) fetch(n - 1);
+      f32x4 du[NL];
+#pragma unroll
+      for (int q = 0; q < NL; ++q) du[q] = zero_acc();
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int q = 0; q < NL; ++q) {
+          frag sb[3];
+          load_b<3>(sb, Sp + (16 * q + lo) * KP + 32 * s + 8 * hi, NT * KP);
+          mma<NP, 3, 2>(ra[s], sb, du[q]);
+        }
+#pragma unroll
+      for (int q = 0; q < NL; ++q) {
+        const f32x4 x = mail[slot][k.w][q][l];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) du[q][r] = x[r] + tk[r].y * du[q][r];
+        split4_store<3>(du[q], Rp + (16 * q + lo) * RC + k.crow, NT * RC);
+      }
+      if (rows_here) S.store(k, a, a.dst + item * a.Dk * a.Dv);
+      lds_barrier();
+#pragma unroll
+      for (int q = 0; q < NL; ++q) {
+        f32x4 z = zero_acc(), zs;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          frag rb[3], tf[3];
+          load_b<3>(rb, Rp + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
+#pragma unroll
+          for (int e = 0; e < 3; ++e) tf[e] = as_frag(ta[e][s]);
+          mma<3, 3, 2>(tf, rb, z);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          z[r] *= tk[r].z;                               // dR
+          zs[r] = -tk[r].x * z[r];
+        }
+        split4_store<3>(zs, Up + (16 * q + lo) * RC + k.crow, NT * RC);
+        if (k.c0 + 16 * q + lo < a.Dv) {
+          float* rp = a.dr + (item * CT + 16 * k.w) * a.Dv + k.c0 + 16 * q;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int t = n * CT + k.crow + r;
+            rp[(unsigned)((4 * hi + r) * a.Dv + lo)] = z[r];
+            if (t < a.T) vp[r * vrow + 16 * q] = Op<T>::from_f32(t < k.len ? z[r] : 0.f);
+          }
+        }
+      }
+      vp -= CT * vrow;
+      lds_barrier();
+      if (rows_here) {
+        const float e_end = s_end;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int q = 0; q < NL; ++q) {
+            const f32x4 x = mail[slot][k.w][NL + m * NL + q][l];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S.x[m][q][r] = e_end * S.x[m][q][r] + x[r];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              frag ub[3], kf[NP];
+              load_b<3>(ub, Up + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
+#pragma unroll
+              for (int e = 0; e < NP; ++e) kf[e] = as_frag(ka[e][m][s]);
+              mma<NP, 3, 2>(kf, ub, S.x[m][q]);
+            }
+          }
+        S.publish(k, Sp, KP);
+      }
+      lds_barrier();
+    }
+    if (rows_here && a.dS0) S.store(k, a, a.dS0 + k.head);
+  } else {
+    const bf16_t* tp = a.ptp + (k.item0 + last) * 3 * SQ + k.arow * CT + 8 * hi;
+    const bf16_t* qtp = a.qtp + ((k.kitem0 + last) * NP * DP + 16 * k.w * MT + lo) * CT + 8 * hi;
+    const float4* tkp = a.tok + (k.item0 + last) * CT + k.crow;
+    const T* yp = static_cast<const T*>(a.dy) + (((last * CT + k.crow) * a.B + k.b) * a.Hv + k.h) * a.Dv + k.c0 + lo;
+    const long yrow = (long)a.B * a.Hv * a.Dv;
+    uint4 sq[3][2], qt[NP][MT][2];
+    float tok[4];
+    T yraw[4][NL];
+    auto fetch = [&](int n) {
+      load_square16<3>(sq, tp);
+      load_transposed<NP, MT, DP>(qt, qtp, rows_here);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        tok[r] = tkp[r].x;
+#pragma unroll
+        for (int q = 0; q < NL; ++q)
+          yraw[r][q] = n * CT + k.crow + r < k.len && k.c0 + 16 * q + lo < a.Dv ? yp[r * yrow + 16 * q] : (T)0;
+      }
+      tp -= 3 * SQ;
+      qtp -= (long)NP * DP * CT;
+      tkp -= CT;
+      yp -= CT * yrow;
+    };
+    // dY of the fetched chunk into LDS ..
+    auto lay_dy = [&]() {
+#pragma unroll
+      for (int q = 0; q < NL; ++q) {
+        f32x4 y, ys;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          y[r] = Op<T>::to_f32(yraw[r][q]);
+          ys[r] = a.scale * tok[r] * y[r];
+        }
+        split4_store<NP>(y, Yp + (16 * q + lo) * RC + k.crow, NT * RC);
+        split4_store<3>(ys, Ys + (16 * q + lo) * RC + k.crow, NT * RC);
+      }
+    };
+    // .. and the two products into the mailbox
+    auto products = [&](int slot) {
+#pragma unroll
+      for (int q = 0; q < NL; ++q) {
+        f32x4 x = zero_acc();
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          frag yb[NP], pa[3];
+          load_b<NP>(yb, Yp + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
+#pragma unroll
+          for (int e = 0; e < 3; ++e) pa[e] = as_frag(sq[e][s]);
+          mma<3, NP, 2>(pa, yb, x);
+        }
+        mail[slot][k.w][q][l] = x;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          f32x4 z = zero_acc();
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            frag yb[3], qa[NP];
+            load_b<3>(yb, Ys + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
+#pragma unroll
+            for (int e = 0; e < NP; ++e) qa[e] = as_frag(qt[e][m][s]);
+            mma<NP, 3, 2>(qa, yb, z);
+          }
+          mail[slot][k.w][NL + m * NL + q][l] = z;
+        }
+      }
+    };
+    if (k.live > 0) {
+      fetch(k.live - 1);
+      lay_dy();
+    }
+    lds_barrier();
+    if (k.live > 0) products((k.live - 1) & 1);
+    if (k.live > 1) fetch(k.live - 2);
+    lds_barrier();
+    for (int n = k.live - 1; n >= 0; --n) {
+      if (n > 0) lay_dy();                               // of chunk n - 1
+      lds_barrier();
+      if (n > 0) products((n - 1) & 1);
+      lds_barrier();
+      if (n > 1) fetch(n - 2);
+      lds_barrier();
+    }
+  }
+  zero_rest<T, NT>(dv0, a.dv_ld, a, k);
+}
+
+// ---------------------------------------------------------------------------
+// grads: one work-group of eight waves per item of a key head; wave = 16 of the
+// 64 tokens x half of the columns.  The value columns are walked 32 at a time:
+// dY, U, dR and the two states go through LDS in pieces, F, H and the three
+// products with the states stay in accumulators.  The value heads of a key head
+// follow one another, so dQ and dK are summed in a fixed order.
+// ---------------------------------------------------------------------------
+template <typename T, int KS>
+__global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
+  constexpr int NP = Pieces<T>::n, XP = NP == 1 ? 2 : 3;   // pieces where the result is only dK
+  constexpr int DP = 32 * KS, NC = 32, CP = NC + 8, NDT = DP / 16, ND = NDT / 2 > 0 ? NDT / 2 : 1;
+  constexpr int kWalk = (NP * CT + 3 * CT + XP * CT + 6 * DP) * CP, kSq = (3 + XP + XP) * CT * RC;
+  __shared__ __align__(16) bf16_t pool[kWalk > kSq ? kWalk : kSq];
+  __shared__ float4 tok[CT];
+  __shared__ double G[CT];
+  __shared__ float dG[2][CT], part[8], sub[CT], sbeta[CT];
+  bf16_t* Yp = pool;                   // [NP][64][CP] dY
+  bf16_t* Up = Yp + NP * CT * CP;      // [3][64][CP]
+  bf16_t* Rp = Up + 3 * CT * CP;       // [XP][64][CP] dR
+  bf16_t* Sp = Rp + XP * CT * CP;      // [3][DP][CP]
+  bf16_t* Dp = Sp + 3 * DP * CP;       // [3][DP][CP] dS
+  bf16_t* Fp = pool;                   // [3][64][RC] F, rows i          (after the walk)
+  bf16_t* Ft = Fp + 3 * CT * RC;       // [XP][64][RC] F^T
+  bf16_t* Hp = Ft + XP * CT * RC;      // [XP][64][RC] H + H^T
   const int n = blockIdx.x % a.nch, bk = blockIdx.x / a.nch;
   const int b = bk / a.Hk, hk = bk % a.Hk, grp = a.Hv / a.Hk;
   const int len = delta_len(a, b), t0 = n * CT;
-  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, lo = l & 15, hi = l >> 4;
+  const int tid = threadIdx.x, wave = tid >> 6, w = wave & 3, half = wave >> 2, l = tid & 63, lo = l & 15, hi = l >> 4;
+  const int arow = 16 * w + lo, crow = 16 * w + 4 * hi;
   T* dq = static_cast<T*>(a.dq);
   T* dk = static_cast<T*>(a.dk);
   if (t0 >= len) {
-    for (int r = tid >> 6; r < CT && t0 + r < a.T; r += 4) {
-      const long tok = (long)(t0 + r) * a.B + b;
+    for (int r = wave; r < CT && t0 + r < a.T; r += 8) {
+      const long at = (long)(t0 + r) * a.B + b;
       for (int c = l; c < a.Dk; c += 64) {
-        dq[tok * a.dq_ld + (long)hk * a.Dk + c] = Op<T>::from_f32(0.f);
-        dk[tok * a.dk_ld + (long)hk * a.Dk + c] = Op<T>::from_f32(0.f);
+        dq[at * a.dq_ld + (long)hk * a.Dk + c] = Op<T>::from_f32(0.f);
+        dk[at * a.dk_ld + (long)hk * a.Dk + c] = Op<T>::from_f32(0.f);
       }
       for (int c = l; c < grp; c += 64) {
-        a.dg[tok * a.Hv + hk * grp + c] = 0.f;
-        a.dbeta[tok * a.Hv + hk * grp + c] = 0.f;
+        a.dg[at * a.Hv + hk * grp + c] = 0.f;
+        a.dbeta[at * a.Hv + hk * grp + c] = 0.f;
       }
     }
     return;
   }
-  const int Dp = pad16(a.Dk), p = Dp + 4;
-  float* ks = lds;
-  float* qs = ks + CT * p;
-  float* S = qs + CT * p;              // [Dp][NT]; F after the column loop
-  float* dS = S + kDeltaMaxDk * SN;    // [Dp][NT]; H after it
-  float* dY = dS + kDeltaMaxDk * SN;
-  float* U = dY + CT * SN;
-  float* dR = U + CT * SN;
-  float4* tok = reinterpret_cast<float4*>(dR + CT * SN);
-  double* G = reinterpret_cast<double*>(tok + CT);
-  float* dG = reinterpret_cast<float*>(G + CT);
-  float* part = dG + CT;               // [4]
-  load_rows<T>(ks, p, a.k, a.k_ld, (long)hk * a.Dk, 0, a.Dk, Dp, t0, len, b, a.B);
-  load_rows<T>(qs, p, a.q, a.q_ld, (long)hk * a.Dk, 0, a.Dk, Dp, t0, len, b, a.B);
-  f32x4 tq[8], tk[8];
+  const bool dcols = half * ND < NDT;  // (one 16-column tile: the second half has none)
+  f32x4 tq[ND], tkk[ND];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) tq[i] = tk[i] = zero_acc();
+  for (int i = 0; i < ND; ++i) tq[i] = tkk[i] = zero_acc();
+  const long kitem = bk * (long)a.nch + n;
   for (int hh = 0; hh < grp; ++hh) {
     const int h = hk * grp + hh;
-    const long bh = (long)b * a.Hv + h, item = bh * a.nch + n;
-    f32x4 aq[8], ku[8], kr[8], F[4], H[4];
-  #pragma unroll
-  for (int i = 0; i < 8; ++i) aq[i] = ku[i] = kr[i] = zero_acc();
-    for (int i = 0; i < 4; ++i) F[i] = H[i] = zero_acc();
+    const long item = ((long)b * a.Hv + h) * a.nch + n;
+    f32x4 aq[ND], ku[ND], kr[ND], F[2], H[2];
+#pragma unroll
+    for (int i = 0; i < ND; ++i) aq[i] = ku[i] = kr[i] = zero_acc();
+    F[0] = F[1] = H[0] = H[1] = zero_acc();
     float ss = 0.f, ub = 0.f, vr = 0.f;
-    const int row = tid >> 2, q4 = (tid & 3) * 8;
-    for (int c0 = 0; c0 < a.Dv; c0 += NT) {
-      __syncthreads();
-      const int nc = min(NT, a.Dv - c0);
-      load_rows<T>(dY, SN, a.dy, (long)a.Hv * a.Dv, (long)h * a.Dv, c0, nc, NT, t0, len, b, a.B);
-      for (int i = tid; i < CT * NT; i += 256) {
-        const int r = i / NT, c = i % NT;
-        const long at = (item * CT + r) * a.Dv + c0 + c;
-        U[r * SN + c] = c < nc ? a.u[at] : 0.f;
-        dR[r * SN + c] = c < nc ? a.dr[at] : 0.f;
-      }
-      for (int i = tid; i < Dp * NT; i += 256) {
-        const int d = i / NT, c = i % NT;
-        const long at = item * a.Dk * a.Dv + (long)d * a.Dv + c0 + c;
-        const bool in = d < a.Dk && c < nc;
-        const float s = in ? a.st[at] : 0.f, ds = in ? a.dst[at] : 0.f;
-        S[d * SN + c] = s;
-        dS[d * SN + c] = ds;
-        ss += s * ds;
-      }
-      if (c0 == 0 && tid < CT) {
-        tok[tid] = a.tok[item * CT + tid];
-        G[tid] = a.G[item * CT + tid];
-      }
-      __syncthreads();
-      for (int e = 0; e < 8; ++e) {
-        const int c = q4 + e;
-        const float r = dR[row * SN + c];
-        ub += r * U[row * SN + c];
-        if (t0 + row < len && c < nc)
-          vr += r * Op<T>::to_f32(static_cast<const T*>(a.v)[((long)(t0 + row) * a.B + b) * a.v_ld +
-                                                             (long)h * a.Dv + c0 + c]);
-      }
-      mm<4>(dY + 16 * w * SN, SN, 1, U, 1, SN, NT, F);
-      mm<4>(dR + 16 * w * SN, SN, 1, U, 1, SN, NT, H);
-    #pragma unroll
-  for (int i = 0; i < 8; ++i)
-        if (16 * i < Dp) {
-          mm<1>(dY + 16 * w * SN, SN, 1, S + 16 * i * SN, 1, SN, NT, aq + i);
-          mm<1>(U + 16 * w * SN, SN, 1, dS + 16 * i * SN, 1, SN, NT, ku + i);
-          mm<1>(dR + 16 * w * SN, SN, 1, S + 16 * i * SN, 1, SN, NT, kr + i);
+    const int row = tid >> 3, rc = (tid & 7) * 4;        // four of a row's 32 columns
+    __syncthreads();
+    if (tid < CT) {
+      tok[tid] = a.tok[item * CT + tid];
+      G[tid] = a.G[item * CT + tid];
+    }
+    for (int c0 = 0; c0 < a.Dv; c0 += NC) {
+      if (c0) __syncthreads();
+      {
+        const int t = t0 + row, c = c0 + rc;
+        const bool in = c < a.Dv;
+        f32x4 u = zero_acc(), r = zero_acc(), y = zero_acc(), v = zero_acc();
+        if (in) {
+          u = *reinterpret_cast<const f32x4*>(a.u + (item * CT + row) * a.Dv + c);
+          r = *reinterpret_cast<const f32x4*>(a.dr + (item * CT + row) * a.Dv + c);
+          if (t < len) {
+            const T* yp = static_cast<const T*>(a.dy) + (((long)t * a.B + b) * a.Hv + h) * a.Dv + c;
+            const T* vp = static_cast<const T*>(a.v) + ((long)t * a.B + b) * a.v_ld + (long)h * a.Dv + c;
+            struct alignas(4 * sizeof(T)) Four { T x[4]; };
+            const Four fy = *reinterpret_cast<const Four*>(yp), fv = *reinterpret_cast<const Four*>(vp);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              y[e] = Op<T>::to_f32(fy.x[e]);
+              v[e] = Op<T>::to_f32(fv.x[e]);
+            }
+          }
         }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          ub += r[e] * u[e];
+          vr += r[e] * v[e];
+        }
+        split4_store<NP>(y, Yp + row * CP + rc, CT * CP);
+        split4_store<3>(u, Up + row * CP + rc, CT * CP);
+        split4_store<XP>(r, Rp + row * CP + rc, CT * CP);
+        for (int i = tid; i < DP * 8; i += 512) {
+          const int d = i >> 3, cc = (i & 7) * 4;
+          f32x4 s = zero_acc(), ds = zero_acc();
+          if (d < a.Dk && c0 + cc < a.Dv) {
+            s = *reinterpret_cast<const f32x4*>(a.st + (item * a.Dk + d) * a.Dv + c0 + cc);
+            ds = *reinterpret_cast<const f32x4*>(a.dst + (item * a.Dk + d) * a.Dv + c0 + cc);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) ss += s[e] * ds[e];
+          split4_store<3>(s, Sp + d * CP + cc, DP * CP);
+          split4_store<3>(ds, Dp + d * CP + cc, DP * CP);
+        }
+      }
+      __syncthreads();
+      frag ya[NP], ua[3], ra[XP];
+#pragma unroll
+      for (int e = 0; e < NP; ++e) ya[e] = lds_frag(Yp + (e * CT + arow) * CP + 8 * hi);
+#pragma unroll
+      for (int e = 0; e < 3; ++e) ua[e] = lds_frag(Up + (e * CT + arow) * CP + 8 * hi);
+#pragma unroll
+      for (int e = 0; e < XP; ++e) ra[e] = lds_frag(Rp + (e * CT + arow) * CP + 8 * hi);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const int j = 2 * half + m;
+        if (j <= w) {
+          frag un[3];
+#pragma unroll
+          for (int e = 0; e < 3; ++e) un[e] = lds_frag(Up + (e * CT + 16 * j + lo) * CP + 8 * hi);
+          mma<NP, 3, 2>(ya, un, F[m]);
+          mma<XP, XP, XP - 1>(ra, un, H[m]);
+        }
+      }
+      if (dcols) {
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+          const int d = 16 * (half * ND + i) + lo;
+          frag sb[3], db[3];
+#pragma unroll
+          for (int e = 0; e < 3; ++e) {
+            sb[e] = lds_frag(Sp + (e * DP + d) * CP + 8 * hi);
+            db[e] = lds_frag(Dp + (e * DP + d) * CP + 8 * hi);
+          }
+          mma<NP, 3, 2>(ya, sb, aq[i]);
+          mma<3, 3, 2>(ua, db, ku[i]);
+          mma<XP, XP, XP - 1>(ra, sb, kr[i]);
+        }
+      }
     }
     __syncthreads();
-    float* Fm = S;
-    float* Hm = dS;
-    for (int m = 0; m < 4; ++m)
+    // F, F^T and H + H^T in pieces (F_ij of tile (w, j), j <= w; zero above)
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const int j = 16 * (2 * half + m) + lo;
+      f32x4 f, hh4;
+#pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int i = 16 * w + 4 * hi + r, j = 16 * m + lo;
+        const int i = crow + r;
         const float d = j <= i ? expf((float)(G[i] - G[j])) : 0.f;
-        Fm[i * SC + j] = a.scale * d * F[m][r];
-        Hm[i * SC + j] = j < i ? -d * H[m][r] : 0.f;
+        f[r] = j <= i ? a.scale * d * F[m][r] : 0.f;
+        hh4[r] = j < i ? -d * H[m][r] : 0.f;
       }
-    // <dS', S'> without the part of U
-    const float end = tok[CT - 1].x;
-    ss *= end;
+      // rows i .. i + 3 of column j: consecutive in the transpose
+      split4_store<XP>(f, Ft + j * RC + crow, CT * RC);
+      uint32_t p0[3], p1[3];
+      split2<3>(f[0], f[1], p0);
+      split2<3>(f[2], f[3], p1);
+#pragma unroll
+      for (int e = 0; e < 3; ++e) {
+        bf16_t* x = Fp + (e * CT + crow) * RC + j;
+        x[0] = (bf16_t)p0[e];
+        x[RC] = (bf16_t)(p0[e] >> 16);
+        x[2 * RC] = (bf16_t)p1[e];
+        x[3 * RC] = (bf16_t)(p1[e] >> 16);
+      }
+      // H below the diagonal, its mirror above (the diagonal is 0): tile (w, j)
+      // with j < w writes both, a diagonal tile its lower entries and mirrors
+      if (2 * half + m < w) split4_store<XP>(hh4, Hp + j * RC + crow, CT * RC);
+      if (2 * half + m <= w) {
+        split2<XP>(hh4[0], hh4[1], p0);
+        split2<XP>(hh4[2], hh4[3], p1);
+#pragma unroll
+        for (int e = 0; e < XP; ++e) {
+          const bf16_t q[4] = {(bf16_t)p0[e], (bf16_t)(p0[e] >> 16), (bf16_t)p1[e], (bf16_t)(p1[e] >> 16)};
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int i = crow + r;
+            if (j <= i) {
+              Hp[(e * CT + i) * RC + j] = q[r];
+              if (2 * half + m == w) Hp[(e * CT + j) * RC + i] = q[r];
+            }
+          }
+        }
+      }
+    }
+    ss *= tok[CT - 1].x;
     float dots[4] = {0.f, 0.f, 0.f, 0.f};
-  #pragma unroll
-  for (int i = 0; i < 8; ++i)
-      if (16 * i < Dp)
-        for (int r = 0; r < 4; ++r) {
-          const int j = 16 * w + 4 * hi + r;
-          ku[i][r] *= tok[j].y;
-          ss += ku[i][r] * ks[j * p + 16 * i + lo];
-          aq[i][r] *= a.scale * tok[j].x;
-          kr[i][r] *= tok[j].x;
-        }
-    for (int d = 1; d < 64; d <<= 1) ss += __shfl_xor(ss, d, 64);
-    if (l == 0) part[w] = ss;
-    __syncthreads();
-  #pragma unroll
-  for (int i = 0; i < 8; ++i)
-      if (16 * i < Dp) {
-        mm<1>(Fm + 16 * w * SC, SC, 1, ks + 16 * i, p, 1, CT, aq + i);
-        f32x4 x = zero_acc();
-        mm<1>(Fm + 16 * w, 1, SC, qs + 16 * i, p, 1, CT, &x);
-        mm<1>(Hm + 16 * w * SC, SC, 1, ks + 16 * i, p, 1, CT, &x);
-        mm<1>(Hm + 16 * w, 1, SC, ks + 16 * i, p, 1, CT, &x);
-        for (int r = 0; r < 4; ++r) {
-          const int j = 16 * w + 4 * hi + r;
-          dots[r] += aq[i][r] * qs[j * p + 16 * i + lo];
-          tq[i][r] += aq[i][r];
-          tk[i][r] += x[r] + ku[i][r] - kr[i][r];
-        }
+    // K and Q at the result's places (row, column), for the dots
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int c = 16 * (half * ND + i) + lo, t = t0 + crow + r;
+        ku[i][r] *= tok[crow + r].y;
+        aq[i][r] *= a.scale * tok[crow + r].x;
+        kr[i][r] *= tok[crow + r].x;
+        if (dcols && t < len && c < a.Dk)
+          ss += ku[i][r] * Op<T>::to_f32(static_cast<const T*>(a.k)[((long)t * a.B + b) * a.k_ld + (long)hk * a.Dk + c]);
       }
-    for (int d = 1; d < 4; d <<= 1) {
+    for (int d = 1; d < 64; d <<= 1) ss += __shfl_xor(ss, d, 64);
+    if (l == 0) part[wave] = ss;
+    for (int d = 1; d < 8; d <<= 1) {
       ub += __shfl_xor(ub, d, 64);
       vr += __shfl_xor(vr, d, 64);
     }
-    for (int r = 0; r < 4; ++r) {
-      for (int d = 1; d < 16; d <<= 1) dots[r] += __shfl_xor(dots[r], d, 64);
-      if (lo == 0) dG[16 * w + 4 * hi + r] = dots[r];
+    if ((tid & 7) == 0) {
+      sub[row] = vr;
+      sbeta[row] = ub;
     }
     __syncthreads();
-    if ((tid & 3) == 0) {
-      dG[row] -= vr;
-      const float bt = tok[row].z;
-      if (t0 + row < a.T)
-        a.dbeta[((long)(t0 + row) * a.B + b) * a.Hv + h] = t0 + row < len ? ub / (bt * bt) : 0.f;
+    if (dcols) {
+#pragma unroll
+      for (int i = 0; i < ND; ++i) {
+        const int d = 16 * (half * ND + i) + lo;
+        f32x4 x = zero_acc();
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          frag kb[NP], qb[NP], fa[3], ta[XP], ha[XP];
+#pragma unroll
+          for (int e = 0; e < NP; ++e) {
+            const long at = ((kitem * NP + e) * DP + d) * CT + 32 * s + 8 * hi;
+            kb[e] = as_frag(ld16(a.ktp + at));
+            qb[e] = as_frag(ld16(a.qtp + at));
+          }
+#pragma unroll
+          for (int e = 0; e < 3; ++e) fa[e] = lds_frag(Fp + (e * CT + arow) * RC + 32 * s + 8 * hi);
+#pragma unroll
+          for (int e = 0; e < XP; ++e) {
+            ta[e] = lds_frag(Ft + (e * CT + arow) * RC + 32 * s + 8 * hi);
+            ha[e] = lds_frag(Hp + (e * CT + arow) * RC + 32 * s + 8 * hi);
+          }
+          mma<3, NP, 2>(fa, kb, aq[i]);
+          mma<XP, NP, XP - 1>(ta, qb, x);
+          mma<XP, NP, XP - 1>(ha, kb, x);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int t = t0 + crow + r;
+          if (t < len && d < a.Dk)
+            dots[r] += aq[i][r] * Op<T>::to_f32(static_cast<const T*>(a.q)[((long)t * a.B + b) * a.q_ld + (long)hk * a.Dk + d]);
+          tq[i][r] += aq[i][r];
+          tkk[i][r] += x[r] + ku[i][r] - kr[i][r];
+        }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      for (int d = 1; d < 16; d <<= 1) dots[r] += __shfl_xor(dots[r], d, 64);
+      if (lo == 0) dG[half][crow + r] = dots[r];
     }
     __syncthreads();
     if (tid < CT) {
-      float s = dG[CT - 1 - tid];        // sums from the chunk's end
+      const float bt = tok[tid].z;
+      if (t0 + tid < a.T)
+        a.dbeta[((long)(t0 + tid) * a.B + b) * a.Hv + h] = t0 + tid < len ? sbeta[tid] / (bt * bt) : 0.f;
+      const int at = CT - 1 - tid;
+      float s = dG[0][at] + dG[1][at] - sub[at];         // sums from the chunk's end
       for (int d = 1; d < 64; d <<= 1) {
         const float o = __shfl_up(s, d, 64);
         if (tid >= d) s += o;
       }
-      const int t = t0 + CT - 1 - tid;
-      if (t < a.T)
-        a.dg[((long)t * a.B + b) * a.Hv + h] = t < len ? s + ((part[0] + part[1]) + (part[2] + part[3])) : 0.f;
+      float all = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) all += part[i];
+      if (t0 + at < a.T) a.dg[((long)(t0 + at) * a.B + b) * a.Hv + h] = t0 + at < len ? s + all : 0.f;
     }
   }
+  if (!dcols) return;
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int i = 0; i < ND; ++i)
+#pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int t = t0 + 16 * w + 4 * hi + r, c = 16 * i + lo;
+      const int t = t0 + crow + r, c = 16 * (half * ND + i) + lo;
       if (t < a.T && c < a.Dk) {
         const long at = (long)t * a.B + b;
         dq[at * a.dq_ld + (long)hk * a.Dk + c] = Op<T>::from_f32(t < len ? tq[i][r] : 0.f);
-        dk[at * a.dk_ld + (long)hk * a.Dk + c] = Op<T>::from_f32(t < len ? tk[i][r] : 0.f);
+        dk[at * a.dk_ld + (long)hk * a.Dk + c] = Op<T>::from_f32(t < len ? tkk[i][r] : 0.f);
       }
     }
 }
 
 namespace {
 
-template <typename K>
-hipError_t launch(K kernel, long grid, size_t lds, const DeltaArgs& a, hipStream_t s) {
-  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                     hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+// Columns of the state per work-group, in 16s: 32 where that still gives every
+// compute unit a work-group (16 read the chunk's operands twice as often).
+int cols_of(const DeltaArgs& a, int cus) {
+  return a.Dv > 16 && (long)a.B * a.Hv * ((a.Dv + 31) / 32) >= cus ? 2 : 1;
+}
+
+template <typename T, int KS, int NL>
+void launch_state(const DeltaArgs& a, bool save, bool bwd, hipStream_t s) {
+  const dim3 grid((unsigned)((long)a.B * a.Hv * ((a.Dv + 16 * NL - 1) / (16 * NL))));
+  if (bwd) delta_state_bwd_kernel<T, KS, NL><<<grid, dim3(512), 0, s>>>(a);
+  else if (save) delta_state_fwd_kernel<T, KS, NL, true><<<grid, dim3(512), 0, s>>>(a);
+  else delta_state_fwd_kernel<T, KS, NL, false><<<grid, dim3(512), 0, s>>>(a);
+}
+
+template <typename T, int KS>
+void launch_cols(const DeltaArgs& a, bool save, bool bwd, int cus, hipStream_t s) {
+  switch (cols_of(a, cus)) {
+    case 1: launch_state<T, KS, 1>(a, save, bwd, s); break;
+    default: launch_state<T, KS, 2>(a, save, bwd, s); break;
+  }
+}
+
+template <typename T, int KS>
+hipError_t launch_fwd(const DeltaArgs& a, bool save, int cus, hipStream_t s) {
+  const dim3 items((unsigned)((long)a.B * a.Hv * a.nch));
+  if (save) delta_prep_kernel<T, KS, true><<<items, dim3(256), 0, s>>>(a);
+  else delta_prep_kernel<T, KS, false><<<items, dim3(256), 0, s>>>(a);
+  hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  kernel<<<dim3((unsigned)grid), dim3(256), lds, s>>>(a);
+  launch_cols<T, KS>(a, save, false, cus, s);
+  return hipGetLastError();
+}
+
+template <typename T, int KS>
+hipError_t launch_bwd(const DeltaArgs& a, int cus, hipStream_t s) {
+  launch_cols<T, KS>(a, true, true, cus, s);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  delta_grads_kernel<T, KS><<<dim3((unsigned)((long)a.B * a.Hk * a.nch)), dim3(512), 0, s>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 template <typename T>
-hipError_t delta_launch_fwd(const DeltaArgs& a, bool save, hipStream_t s) {
-  const int Dp = (a.Dk + 15) & ~15, p = Dp + 4;
-  const long bh = (long)a.B * a.Hv, ntile = (a.Dv + NT - 1) / NT;
-  hipError_t e = launch(delta_prep_kernel<T>, bh * a.nch,
-                        sizeof(float) * (2 * CT * p + 2 * CT * SC + 3 * CT), a, s);
-  if (e != hipSuccess) return e;
-  const size_t lds = sizeof(float) * (2 * CT * p + Dp * SN + 2 * CT * SC + 2 * CT * SN + 4 * CT);
-  return save ? launch(delta_state_fwd_kernel<T, true>, bh * ntile, lds, a, s)
-              : launch(delta_state_fwd_kernel<T, false>, bh * ntile, lds, a, s);
+hipError_t delta_launch_fwd(const DeltaArgs& a, bool save, int cus, hipStream_t s) {
+  switch (delta_ksteps(a.Dk)) {
+    case 1: return launch_fwd<T, 1>(a, save, cus, s);
+    case 2: return launch_fwd<T, 2>(a, save, cus, s);
+    default: return launch_fwd<T, 4>(a, save, cus, s);
+  }
 }
 
 template <typename T>
-hipError_t delta_launch_bwd(const DeltaArgs& a, hipStream_t s) {
-  const int Dp = (a.Dk + 15) & ~15, p = Dp + 4;
-  const long bh = (long)a.B * a.Hv, ntile = (a.Dv + NT - 1) / NT;
-  hipError_t e = launch(delta_state_bwd_kernel<T>, bh * ntile,
-                        sizeof(float) * (2 * CT * p + Dp * SN + 2 * CT * SC + 2 * CT * SN + 4 * CT), a, s);
-  if (e != hipSuccess) return e;
-  return launch(delta_grads_kernel<T>, (long)a.B * a.Hk * a.nch,
-                sizeof(float) * (2 * CT * p + 2 * kDeltaMaxDk * SN + 3 * CT * SN + 4 * CT + 3 * CT + 4), a, s);
+hipError_t delta_launch_bwd(const DeltaArgs& a, int cus, hipStream_t s) {
+  switch (delta_ksteps(a.Dk)) {
+    case 1: return launch_bwd<T, 1>(a, cus, s);
+    case 2: return launch_bwd<T, 2>(a, cus, s);
+    default: return launch_bwd<T, 4>(a, cus, s);
+  }
 }
 
-template hipError_t delta_launch_fwd<float>(const DeltaArgs&, bool, hipStream_t);
-template hipError_t delta_launch_fwd<bf16_t>(const DeltaArgs&, bool, hipStream_t);
-template hipError_t delta_launch_bwd<float>(const DeltaArgs&, hipStream_t);
-template hipError_t delta_launch_bwd<bf16_t>(const DeltaArgs&, hipStream_t);
+template hipError_t delta_launch_fwd<float>(const DeltaArgs&, bool, int, hipStream_t);
+template hipError_t delta_launch_fwd<bf16_t>(const DeltaArgs&, bool, int, hipStream_t);
+template hipError_t delta_launch_bwd<float>(const DeltaArgs&, int, hipStream_t);
+template hipError_t delta_launch_bwd<bf16_t>(const DeltaArgs&, int, hipStream_t);
 
 }  // namespace ll
