@@ -33,8 +33,9 @@ struct DeltaArgs {
   bf16_t *tp, *pp, *ttp, *ptp;
   double* G;                         // [64] sums of g from the chunk's start
   float4* tok;                       // [64] e^G, e^{G_end - G}, beta, -
-  // per item of a key head: K^T and Q^T [pieces][32 * ksteps][64]
-  bf16_t *ktp, *qtp;
+  // per item of a key head, zeros past the row's end and Dk: K and Q
+  // [pieces][64][32 * ksteps], K^T and Q^T [pieces][32 * ksteps][64]
+  bf16_t *kp, *qp, *ktp, *qtp;
   // per item, kept for the gradient
   float *st, *u;                     // entering state [Dk][Dv], U [64][Dv]
   float *dst, *dr;                   // gradient of the leaving state, of R

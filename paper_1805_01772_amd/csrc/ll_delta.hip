@@ -1,5 +1,6 @@
 // The gated delta rule's entry points: plan, argument checks, the launch
 // sequence of the chunked forward and gradient, and the one-token step.
+#include <algorithm>
 #include <cmath>
 #include <new>
 
@@ -138,6 +139,10 @@ ll_status validate(const ll_delta_desc* d, bool step) {
     if (ld[i] && (ld[i] < need[i] || ld[i] * es % 16 || ld[i] > (int64_t)1 << 31))
       return fail(LL_EINVAL, "%s = %lld must be 0, or at least %lld, at most 2^31 and a multiple of 16 bytes",
                   names[i], (long long)ld[i], (long long)need[i]);
+  const int64_t widest = std::max({d->v_ld, step ? 0 : d->dv_ld, v});
+  if (!step && widest * d->B * es > (int64_t)1 << 27)
+    return fail(LL_EUNSUPPORTED, "a time step of v, y or dv spans %lld bytes (at most 2^27)",
+                (long long)(widest * d->B * es));
   const int64_t nch = (d->T_max + ll::kDeltaChunk - 1) / ll::kDeltaChunk;
   if ((int64_t)d->B * d->Hv > 1 << 24 || (int64_t)d->B * d->Hv * nch > 1 << 26)
     return fail(LL_EUNSUPPORTED, "B * Hv = %lld (at most 2^24) with T_max = %d: more than 2^26 chunks",
@@ -161,7 +166,7 @@ DeltaArgs sizes(const ll_delta_desc& d) {
 }
 
 void release(ll_delta_plan* p) {
-  void* all[] = {p->a.tp, p->a.pp, p->a.ttp, p->a.ptp, p->a.ktp, p->a.qtp, p->a.G, p->a.tok, p->a.st, p->a.u, p->a.dst, p->a.dr, p->a.err};
+  void* all[] = {p->a.tp, p->a.pp, p->a.ttp, p->a.ptp, p->a.kp, p->a.qp, p->a.ktp, p->a.qtp, p->a.G, p->a.tok, p->a.st, p->a.u, p->a.dst, p->a.dr, p->a.err};
   for (void* m : all)
     if (m) (void)hipFree(m);
 }
@@ -204,6 +209,8 @@ ll_status ll_delta_plan_create(const ll_delta_desc* desc, int device, ll_delta_p
   struct { void** at; size_t bytes; const char* what; bool grad; } bufs[] = {
       {(void**)&p->a.tp, sq, "the chunks' T", false},
       {(void**)&p->a.pp, sq, "the chunks' P", false},
+      {(void**)&p->a.kp, tr, "the chunks' K", false},
+      {(void**)&p->a.qp, tr, "the chunks' Q", false},
       {(void**)&p->a.ktp, tr, "the chunks' K^T", false},
       {(void**)&p->a.ttp, sq, "the chunks' T^T", true},
       {(void**)&p->a.ptp, sq, "the chunks' P^T", true},

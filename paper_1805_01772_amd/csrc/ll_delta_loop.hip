@@ -28,6 +28,7 @@
 // term.  Results that leave the call as bfloat16 and feed nothing else take two
 // pieces (2^-16 against the rounding's 2^-9).  Sums are float32.
 #include "ll_delta.h"
+#include "ll_exchange.h"
 #include "ll_kernels.h"
 
 namespace ll {
@@ -158,6 +159,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
     atomicOr(a.err, LL_DEVERR_SEQ_LEN_BIT);
   if (t0 >= len) return;
   const long item = blockIdx.x, kitem = ((long)b * a.Hk + hk) * a.nch + n;
+  const bool first = h == hk * grp;                      // what the key head's value heads share is written once
   bf16_t* kp = reinterpret_cast<bf16_t*>(raw);           // [NP][64][KP]
   bf16_t* qp = kp + NP * CT * KP;
   for (int i = tid; i < CT * DP / 8; i += 256) {
@@ -171,13 +173,19 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
       x.zero();
       y.zero();
     }
-    uint4 p[NP];
+    uint4 p[NP], q[NP];
     x.pieces(p);
+    y.pieces(q);
 #pragma unroll
-    for (int e = 0; e < NP; ++e) *reinterpret_cast<uint4*>(kp + (e * CT + r) * KP + c) = p[e];
-    y.pieces(p);
-#pragma unroll
-    for (int e = 0; e < NP; ++e) *reinterpret_cast<uint4*>(qp + (e * CT + r) * KP + c) = p[e];
+    for (int e = 0; e < NP; ++e) {
+      *reinterpret_cast<uint4*>(kp + (e * CT + r) * KP + c) = p[e];
+      *reinterpret_cast<uint4*>(qp + (e * CT + r) * KP + c) = q[e];
+      if (first) {
+        const long at = ((kitem * NP + e) * CT + r) * DP + c;
+        *reinterpret_cast<uint4*>(a.kp + at) = p[e];
+        *reinterpret_cast<uint4*>(a.qp + at) = q[e];
+      }
+    }
   }
   if (tid < CT) {
     const int t = t0 + tid;
@@ -222,8 +230,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
         mma<NP, NP, 2>(qa, kb, qk[m]);
       }
   }
-  // K^T (and Q^T): once per key head
-  if (h == hk * grp)
+  if (first)
     for (int i = tid; i < NP * DP * 8; i += 256) {
       const int c = i % DP, j = (i / DP) % 8 * 8, e = i / (DP * 8);
       uint32_t x[4], y[4];
@@ -340,23 +347,58 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// One row and head's walk by a wave of the two loops: its place, and the
-// addresses that move from chunk to chunk.
+// The loops' loads and stores go through buffer descriptors made for each
+// chunk: what lies past a row's end, past Dk or past Dv is out of the buffer's
+// range (read as 0, not written), so there is no branch around any of them
+// and the wait for one counts exactly what was issued after it.  A lane that
+// has no place at all gets an offset past every range; rows span at most 2^27
+// bytes (validated), so 16 of them stay below it.
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+constexpr unsigned kNowhere = 0x80000000u;
+
+// `rows` rows of `cols` elements, `ld` apart (none: an empty range).
+template <typename T>
+__device__ __forceinline__ rsrc_t rows_rsrc(const T* base, int rows, long ld, int cols) {
+  return make_rsrc(base, rows > 0 ? (unsigned)(((rows - 1) * ld + cols) * (long)sizeof(T)) : 0u);
+}
+__device__ __forceinline__ uint4 bload16(rsrc_t r, unsigned off) {
+  return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+}
+template <typename T> __device__ __forceinline__ T bload(rsrc_t r, unsigned off);
+template <> __device__ __forceinline__ float bload<float>(rsrc_t r, unsigned off) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0));
+}
+template <> __device__ __forceinline__ bf16_t bload<bf16_t>(rsrc_t r, unsigned off) {
+  return __builtin_bit_cast(bf16_t, __builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0));
+}
+__device__ __forceinline__ void bstore(rsrc_t r, unsigned off, float v) {
+  __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), r, off, 0, 0);
+}
+__device__ __forceinline__ void bstore(rsrc_t r, unsigned off, bf16_t v) {
+  __builtin_amdgcn_raw_buffer_store_b16(v, r, off, 0, 0);
+}
+
+// One row and head's walk by a wave of the two loops.
 struct Walk {
-  int b, h, hk, len, live, c0, w, lo, hi, arow, crow;
+  int b, h, len, live, c0, nc, w, lo, hi, arow, crow;
   long head, item0, kitem0;
+  bool none;                           // no head for this work-group
   __device__ Walk(const DeltaArgs& a, int NT) {
-    const int ntile = (a.Dv + NT - 1) / NT;
-    const int bh = blockIdx.x / ntile;
-    c0 = (int)(blockIdx.x % ntile) * NT;
+    // work-groups go to the XCDs in turn: a head's columns to one of them, whose
+    // L2 then reads the head's operands once
+    const int ntile = (a.Dv + NT - 1) / NT, at = (int)(blockIdx.x >> 3);
+    const int bh = (int)(blockIdx.x & 7) + 8 * (at / ntile);
+    none = bh >= a.B * a.Hv;
+    if (none) return;
+    c0 = at % ntile * NT;
+    nc = min(NT, a.Dv - c0);
     b = bh / a.Hv;
     h = bh % a.Hv;
-    hk = h / (a.Hv / a.Hk);
     len = delta_len(a, b);
     live = (len + CT - 1) / CT;
     head = (long)bh * a.Dk * a.Dv;
     item0 = (long)bh * a.nch;
-    kitem0 = ((long)b * a.Hk + hk) * a.nch;
+    kitem0 = ((long)b * a.Hk + h / (a.Hv / a.Hk)) * a.nch;
     const int l = threadIdx.x & 63;
     w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6) & 3);
     lo = l & 15;
@@ -364,73 +406,85 @@ struct Walk {
     arow = 16 * w + lo;                // row of an A operand
     crow = 16 * w + 4 * hi;            // first of the four rows of a result
   }
+  // Byte offset of the lane's first row and column 16 q + lo in rows ld apart,
+  // from the wave's first row.
+  template <typename T>
+  __device__ __forceinline__ unsigned place(int q, long ld) const {
+    return 16 * q + lo < nc ? (unsigned)((4 * hi * ld + 16 * q + lo) * (long)sizeof(T)) : kNowhere;
+  }
 };
 
-// Rows 16 w .. of K or Q of a chunk, 32 elements a step.
-template <typename T, int KS>
-__device__ __forceinline__ void load_rows16(Raw8<T>* x, const T* p, bool in, int Dk, int hi) {
+// Rows 16 w .. of K or Q of a chunk: piece, 32 elements a step.
+template <int NP, int KS>
+__device__ __forceinline__ void load_rows16(uint4 (*x)[KS], const bf16_t* base, const Walk& k) {
+  constexpr unsigned DP = 32 * KS;
+  const rsrc_t r = make_rsrc(base, NP * CT * DP * 2);
 #pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    if (in && 32 * s + 8 * hi < Dk) x[s].load(p + 32 * s);
-    else x[s].zero();
-  }
+  for (int e = 0; e < NP; ++e)
+#pragma unroll
+    for (int s = 0; s < KS; ++s) x[e][s] = bload16(r, (k.arow * DP + 8 * k.hi) * 2 + e * CT * DP * 2 + 64 * s);
 }
 
-// Rows 16 w .. of a [64][64] in N pieces; p: the wave's row, its lane's chunk.
+// Rows 16 w .. of a [64][64] in N pieces.
 template <int N>
-__device__ __forceinline__ void load_square16(uint4 (*x)[2], const bf16_t* p) {
+__device__ __forceinline__ void load_square16(uint4 (*x)[2], const bf16_t* base, const Walk& k) {
+  const rsrc_t r = make_rsrc(base, 3 * SQ * 2);
 #pragma unroll
   for (int e = 0; e < N; ++e)
 #pragma unroll
-    for (int s = 0; s < 2; ++s) x[e][s] = ld16(p + e * SQ + 32 * s);
+    for (int s = 0; s < 2; ++s) x[e][s] = bload16(r, (k.arow * CT + 8 * k.hi) * 2 + e * SQ * 2 + 64 * s);
 }
 
-// MT tiles of 16 rows of K^T or Q^T.
+// The wave's MT tiles of 16 rows of K^T or Q^T (rows past the last read 0).
 template <int NP, int MT, int DP>
-__device__ __forceinline__ void load_transposed(uint4 (*x)[MT][2], const bf16_t* p, bool in) {
+__device__ __forceinline__ void load_transposed(uint4 (*x)[MT][2], const bf16_t* base, const Walk& k, bool own) {
+  const rsrc_t r = make_rsrc(base, own ? NP * DP * CT * 2 : 0);
 #pragma unroll
   for (int e = 0; e < NP; ++e)
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) x[e][m][s] = in ? ld16(p + (e * DP + 16 * m) * CT + 32 * s) : zero4();
+      for (int s = 0; s < 2; ++s)
+        x[e][m][s] = bload16(r, ((16 * k.w * MT + k.lo) * CT + 8 * k.hi) * 2 + (e * DP + 16 * m) * CT * 2 + 64 * s);
 }
 
-// B operand: NN pieces of column `col` at k, from LDS [piece][NT][pitch].
+// B operand: NN pieces of a column, from LDS [piece][NT][pitch].
 template <int NN>
 __device__ __forceinline__ void load_b(frag* f, const bf16_t* p, int stride) {
 #pragma unroll
   for (int e = 0; e < NN; ++e) f[e] = lds_frag(p + e * stride);
 }
 
+// The wave's rows of the state: tiles of 16 from 16 w MT on.
 template <int MT, int NL>
 struct State {
   f32x4 x[MT][NL];
-  // (d, c) of [Dk][Dv] floats at p; zeros without one and past its end
-  __device__ __forceinline__ void load(const Walk& k, const DeltaArgs& a, const float* p) {
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int q = 0; q < NL; ++q)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int d = 16 * (k.w * MT + m) + 4 * k.hi + r, c = k.c0 + 16 * q + k.lo;
-          x[m][q][r] = p && d < a.Dk && c < a.Dv ? p[(unsigned)(d * a.Dv + c)] : 0.f;
-        }
+  __device__ __forceinline__ rsrc_t range(const Walk& k, const DeltaArgs& a, const float* p) const {
+    const int d0 = 16 * k.w * MT;
+    return rows_rsrc(p + (long)d0 * a.Dv + k.c0, min(16 * MT, a.Dk - d0), a.Dv, k.nc);
   }
-  __device__ __forceinline__ void store(const Walk& k, const DeltaArgs& a, float* p) {
+  // from [Dk][Dv] floats at p; zeros without one
+  __device__ __forceinline__ void load(const Walk& k, const DeltaArgs& a, const float* p) {
+    const rsrc_t rs = range(k, a, p);
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int q = 0; q < NL; ++q)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int d = 16 * (k.w * MT + m) + 4 * k.hi + r, c = k.c0 + 16 * q + k.lo;
-          if (d < a.Dk && c < a.Dv) p[(unsigned)(d * a.Dv + c)] = x[m][q][r];
-        }
+        for (int r = 0; r < 4; ++r)
+          x[m][q][r] = p ? bload<float>(rs, k.place<float>(q, a.Dv) + (16 * m + r) * a.Dv * 4) : 0.f;
+  }
+  __device__ __forceinline__ void store(const Walk& k, const DeltaArgs& a, float* p) const {
+    const rsrc_t rs = range(k, a, p);
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int q = 0; q < NL; ++q)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) bstore(rs, k.place<float>(q, a.Dv) + (16 * m + r) * a.Dv * 4, x[m][q][r]);
   }
   // in pieces, column-major, for the products that read it
-  __device__ __forceinline__ void publish(const Walk& k, bf16_t* Sp, int KP) {
+  __device__ __forceinline__ void publish(const Walk& k, bf16_t* Sp, int KP) const {
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -455,89 +509,57 @@ __device__ void zero_rest(T* out, long tok_ld, const DeltaArgs& a, const Walk& k
 // (and a quarter of the state's rows, which stay in its accumulators in float32);
 // what the next product needs of the other waves goes through LDS in pieces.
 // Waves 4-7 make Y beside them from the same pieces.  Three barriers a chunk.
-// The operands that do not depend on the state are loaded a chunk ahead.
+// The operands that do not depend on the state are loaded a chunk ahead, into
+// the other of two register sets.
 // ---------------------------------------------------------------------------
 template <typename T, int KS, int NL, bool SAVE>
 __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
   constexpr int NP = Pieces<T>::n, PP = NP == 1 ? 2 : 3, DP = 32 * KS, KP = DP + 8, NT = 16 * NL;
   constexpr int MT = KS == 4 ? 2 : 1;                  // 16-row tiles of the state per wave
-  // K^T a chunk ahead too, where the registers hold it
+  // T and K^T a chunk ahead too, where the registers hold them
   constexpr bool AHEAD = NP == 1;
   __shared__ __align__(16) bf16_t Sp[3 * NT * KP];     // state, column-major pieces
   __shared__ __align__(16) bf16_t Rp[3 * NT * RC], Up[3 * NT * RC], Uy[PP * NT * RC];
-  __shared__ float s_end;
   const Walk k(a, NT);
+  if (k.none) return;
   const int lo = k.lo, hi = k.hi;
-  T* const y0 = static_cast<T*>(a.y);
+  const long vrow = (long)a.B * a.v_ld, yrow = (long)a.B * a.Hv * a.Dv;
   if (threadIdx.x < 256) {
+    struct Ops {
+      uint4 rows[NP][KS], sq[3][2], kt[NP][MT][2];
+      float4 tok[4];
+      float end;
+      T v[4][NL];
+    };
     const bool own = k.w * MT * 16 < DP;               // this wave holds rows of the state
     State<MT, NL> S;
     S.load(k, a, a.S0 && own ? a.S0 + k.head : nullptr);
     if (own) S.publish(k, Sp, KP);
-    const T* kp = static_cast<const T*>(a.k) + ((long)k.arow * a.B + k.b) * a.k_ld + (long)k.hk * a.Dk + 8 * hi;
-    const T* vp = static_cast<const T*>(a.v) + ((long)k.crow * a.B + k.b) * a.v_ld + (long)k.h * a.Dv + k.c0 + lo;
-    const bf16_t* tp = a.tp + k.item0 * 3 * SQ + k.arow * CT + 8 * hi;
-    const bf16_t* ktp = a.ktp + (k.kitem0 * NP * DP + 16 * k.w * MT + lo) * CT + 8 * hi;
-    const float4* tkp = a.tok + k.item0 * CT + k.crow;
-    const long kstep = (long)CT * a.B * a.k_ld, vstep = (long)CT * a.B * a.v_ld, vrow = (long)a.B * a.v_ld;
-    Raw8<T> rows[KS];
-    uint4 sq[3][2], kt[NP][MT][2];
-    float4 tok[4];
-    T vraw[4][NL];
-    auto fetch = [&](int n) {
-      load_rows16<T, KS>(rows, kp, n * CT + k.arow < k.len, a.Dk, hi);
-      load_square16<3>(sq, tp);
-      if (AHEAD) load_transposed<NP, MT, DP>(kt, ktp, own);
+    auto squares = [&](Ops& o, int n) {
+      load_square16<3>(o.sq, a.tp + (k.item0 + n) * 3 * SQ, k);
+      load_transposed<NP, MT, DP>(o.kt, a.ktp + (k.kitem0 + n) * NP * DP * CT, k, own);
+    };
+    auto fetch = [&](Ops& o, int n) {
+      load_rows16<NP, KS>(o.rows, a.kp + (k.kitem0 + n) * NP * CT * DP, k);
+      const int t0 = n * CT + 16 * k.w;
+      const rsrc_t rt = make_rsrc(a.tok + (k.item0 + n) * CT, CT * 16);
+      const rsrc_t rv = rows_rsrc(static_cast<const T*>(a.v) + ((long)t0 * a.B + k.b) * a.v_ld + (long)k.h * a.Dv + k.c0,
+                                  min(16, k.len - t0), vrow, k.nc);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        tok[r] = tkp[r];
+        o.tok[r] = __builtin_bit_cast(float4, bload16(rt, (k.crow + r) * 16));
 #pragma unroll
         for (int q = 0; q < NL; ++q)
-          vraw[r][q] = n * CT + k.crow + r < k.len && k.c0 + 16 * q + lo < a.Dv ? vp[r * vrow + 16 * q] : (T)0;
+          o.v[r][q] = bload<T>(rv, k.place<T>(q, vrow) + (unsigned)(r * vrow * (long)sizeof(T)));
       }
-      kp += kstep;
-      vp += vstep;
-      tp += 3 * SQ;
-      tkp += CT;
-      if (AHEAD) ktp += (long)NP * DP * CT;
+      o.end = bload<float>(rt, (CT - 1) * 16);
+      if (AHEAD) squares(o, n);
     };
-    if (k.live > 0) fetch(0);
-    lds_barrier();
-    for (int n = 0; n < k.live; ++n) {
+    auto chunk = [&](int n, Ops& o, Ops& nxt) {
       const long item = k.item0 + n;
-      frag ra[KS][NP];
-      uint4 ta[3][2], ka[NP][MT][2];
-      float4 tk[4];
-      float v[4][NL];
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        uint4 p[NP];
-        rows[s].pieces(p);
-#pragma unroll
-        for (int e = 0; e < NP; ++e) ra[s][e] = as_frag(p[e]);
-      }
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-#pragma unroll
-        for (int e = 0; e < 3; ++e) ta[e][s] = sq[e][s];
-        if (AHEAD)
-#pragma unroll
-          for (int e = 0; e < NP; ++e)
-#pragma unroll
-            for (int m = 0; m < MT; ++m) ka[e][m][s] = kt[e][m][s];
-      }
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        tk[r] = tok[r];
-#pragma unroll
-        for (int q = 0; q < NL; ++q) v[r][q] = Op<T>::to_f32(vraw[r][q]);
-      }
-      if (k.w == 3 && hi == 3 && lo == 0) s_end = tk[3].x;
-      if (!AHEAD) {
-        load_transposed<NP, MT, DP>(ka, ktp, own);
-        ktp += (long)NP * DP * CT;
-      }
-      if (n + 1 < k.live) fetch(n + 1);
+      if (!AHEAD) squares(o, n);
+      fetch(nxt, min(n + 1, k.live - 1));
+      __builtin_amdgcn_sched_barrier(0);               // the loads go out first
       f32x4 ks[NL];
 #pragma unroll
       for (int q = 0; q < NL; ++q) ks[q] = zero_acc();
@@ -545,19 +567,22 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
       for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int q = 0; q < NL; ++q) {
-          frag sb[3];
+          frag sb[3], ra[NP];
           load_b<3>(sb, Sp + (16 * q + lo) * KP + 32 * s + 8 * hi, NT * KP);
-          mma<NP, 3, 2>(ra[s], sb, ks[q]);
+#pragma unroll
+          for (int e = 0; e < NP; ++e) ra[e] = as_frag(o.rows[e][s]);
+          mma<NP, 3, 2>(ra, sb, ks[q]);
         }
 #pragma unroll
       for (int q = 0; q < NL; ++q) {
         f32x4 rr;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) rr[r] = tk[r].z * (v[r][q] - tk[r].x * ks[q][r]);
+        for (int r = 0; r < 4; ++r) rr[r] = o.tok[r].z * (Op<T>::to_f32(o.v[r][q]) - o.tok[r].x * ks[q][r]);
         split4_store<3>(rr, Rp + (16 * q + lo) * RC + k.crow, NT * RC);
       }
-      if (SAVE && own) S.store(k, a, a.st + item * a.Dk * a.Dv);
+      if (SAVE) S.store(k, a, a.st + item * a.Dk * a.Dv);
       lds_barrier();
+      const rsrc_t ru = rows_rsrc(a.u + (item * CT + 16 * k.w) * a.Dv + k.c0, SAVE ? 16 : 0, a.Dv, k.nc);
 #pragma unroll
       for (int q = 0; q < NL; ++q) {
         f32x4 u = zero_acc(), us;
@@ -566,116 +591,110 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
           frag rb[3], tf[3];
           load_b<3>(rb, Rp + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
 #pragma unroll
-          for (int e = 0; e < 3; ++e) tf[e] = as_frag(ta[e][s]);
+          for (int e = 0; e < 3; ++e) tf[e] = as_frag(o.sq[e][s]);
           mma<3, 3, 2>(tf, rb, u);
         }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) us[r] = tk[r].y * u[r];
+        for (int r = 0; r < 4; ++r) us[r] = o.tok[r].y * u[r];
         split4_store<3>(us, Up + (16 * q + lo) * RC + k.crow, NT * RC);
         split4_store<PP>(u, Uy + (16 * q + lo) * RC + k.crow, NT * RC);
-        if (SAVE && k.c0 + 16 * q + lo < a.Dv) {
-          float* up = a.u + (item * CT + 16 * k.w) * a.Dv + k.c0 + 16 * q;
+        if (SAVE) {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) up[(unsigned)((4 * hi + r) * a.Dv + lo)] = u[r];
+          for (int r = 0; r < 4; ++r) bstore(ru, k.place<float>(q, a.Dv) + r * a.Dv * 4, u[r]);
         }
       }
       lds_barrier();
       if (own) {
-        const float e_end = s_end;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
           for (int q = 0; q < NL; ++q) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S.x[m][q][r] *= e_end;
+            for (int r = 0; r < 4; ++r) S.x[m][q][r] *= o.end;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
               frag ub[3], kf[NP];
               load_b<3>(ub, Up + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
 #pragma unroll
-              for (int e = 0; e < NP; ++e) kf[e] = as_frag(ka[e][m][s]);
+              for (int e = 0; e < NP; ++e) kf[e] = as_frag(o.kt[e][m][s]);
               mma<NP, 3, 2>(kf, ub, S.x[m][q]);
             }
           }
         S.publish(k, Sp, KP);
       }
       lds_barrier();
+    };
+    Ops A, B;
+    if (k.live > 0) fetch(A, 0);
+    lds_barrier();
+    for (int n = 0; n < k.live; n += 2) {
+      chunk(n, A, B);
+      if (n + 1 < k.live) chunk(n + 1, B, A);
     }
     if (own && a.ST) S.store(k, a, a.ST + k.head);
   } else {
-    const T* qp = static_cast<const T*>(a.q) + ((long)k.arow * a.B + k.b) * a.q_ld + (long)k.hk * a.Dk + 8 * hi;
-    const bf16_t* pp = a.pp + k.item0 * 3 * SQ + k.arow * CT + 8 * hi;
-    const float4* tkp = a.tok + k.item0 * CT + k.crow;
-    T* yp = y0 + (((long)k.crow * a.B + k.b) * a.Hv + k.h) * a.Dv + k.c0 + lo;
-    const long qstep = (long)CT * a.B * a.q_ld, yrow = (long)a.B * a.Hv * a.Dv;
-    Raw8<T> rows[KS];
-    uint4 sq[3][2];
-    float tok[4];
-    auto fetch = [&](int n) {
-      load_rows16<T, KS>(rows, qp, n * CT + k.arow < k.len, a.Dk, hi);
-      load_square16<PP>(sq, pp);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) tok[r] = tkp[r].x;
-      qp += qstep;
-      pp += 3 * SQ;
-      tkp += CT;
+    struct Ops {
+      uint4 rows[NP][KS], sq[PP][2];
+      float tok[4];
     };
-    if (k.live > 0) fetch(0);
-    lds_barrier();
-    for (int n = 0; n < k.live; ++n) {
-      uint4 pa[PP][2];
-      float tk[4];
+    auto fetch = [&](Ops& o, int n) {
+      load_rows16<NP, KS>(o.rows, a.qp + (k.kitem0 + n) * NP * CT * DP, k);
+      load_square16<PP>(o.sq, a.pp + (k.item0 + n) * 3 * SQ, k);
+      const rsrc_t rt = make_rsrc(a.tok + (k.item0 + n) * CT, CT * 16);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o.tok[r] = bload<float>(rt, (k.crow + r) * 16);
+    };
+    auto chunk = [&](int n, Ops& o, Ops& nxt) {
+      fetch(nxt, min(n + 1, k.live - 1));
+      __builtin_amdgcn_sched_barrier(0);               // the loads go out first
       f32x4 y[NL];
 #pragma unroll
       for (int q = 0; q < NL; ++q) y[q] = zero_acc();
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        frag ra[NP];
-        uint4 p[NP];
-        rows[s].pieces(p);
-#pragma unroll
-        for (int e = 0; e < NP; ++e) ra[e] = as_frag(p[e]);
+      for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int q = 0; q < NL; ++q) {
-          frag sb[PP];
+          frag sb[PP], ra[NP];
           load_b<PP>(sb, Sp + (16 * q + lo) * KP + 32 * s + 8 * hi, NT * KP);
+#pragma unroll
+          for (int e = 0; e < NP; ++e) ra[e] = as_frag(o.rows[e][s]);
           mma<NP, PP, PP - 1>(ra, sb, y[q]);
         }
-      }
 #pragma unroll
-      for (int e = 0; e < PP; ++e)
+      for (int q = 0; q < NL; ++q)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) pa[e][s] = sq[e][s];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) tk[r] = a.scale * tok[r];
-      if (n + 1 < k.live) fetch(n + 1);
+        for (int r = 0; r < 4; ++r) y[q][r] *= a.scale * o.tok[r];
       lds_barrier();
       lds_barrier();
+      const int t0 = n * CT + 16 * k.w;
+      const rsrc_t ry = rows_rsrc(static_cast<T*>(a.y) + ((long)t0 * a.B + k.b) * a.Hv * a.Dv + (long)k.h * a.Dv + k.c0,
+                                  min(16, a.T - t0), yrow, k.nc);
 #pragma unroll
       for (int q = 0; q < NL; ++q) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) y[q][r] *= tk[r];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           frag ub[PP], pf[PP];
           load_b<PP>(ub, Uy + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
 #pragma unroll
-          for (int e = 0; e < PP; ++e) pf[e] = as_frag(pa[e][s]);
+          for (int e = 0; e < PP; ++e) pf[e] = as_frag(o.sq[e][s]);
           mma<PP, PP, PP - 1>(pf, ub, y[q]);
         }
-        if (k.c0 + 16 * q + lo < a.Dv) {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int t = n * CT + k.crow + r;
-            if (t < a.T) yp[r * yrow + 16 * q] = Op<T>::from_f32(t < k.len ? y[q][r] : 0.f);
-          }
-        }
+        for (int r = 0; r < 4; ++r)
+          bstore(ry, k.place<T>(q, yrow) + (unsigned)(r * yrow * (long)sizeof(T)),
+                 Op<T>::from_f32(n * CT + k.crow + r < k.len ? y[q][r] : 0.f));
       }
-      yp += CT * yrow;
       lds_barrier();
+    };
+    Ops A, B;
+    if (k.live > 0) fetch(A, 0);
+    lds_barrier();
+    for (int n = 0; n < k.live; n += 2) {
+      chunk(n, A, B);
+      if (n + 1 < k.live) chunk(n + 1, B, A);
     }
   }
-  zero_rest<T, NT>(y0, (long)a.Hv * a.Dv, a, k);
+  zero_rest<T, NT>(static_cast<T*>(a.y), (long)a.Hv * a.Dv, a, k);
 }
 
 // ---------------------------------------------------------------------------
@@ -693,70 +712,38 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
   __shared__ __align__(16) bf16_t Rp[3 * NT * RC], Up[3 * NT * RC];
   __shared__ __align__(16) bf16_t Yp[NP * NT * RC], Ys[3 * NT * RC];   // dY, scale e^G dY of the next chunk
   __shared__ f32x4 mail[2][4][(MT + 1) * NL][64];
-  __shared__ float s_end;
   const Walk k(a, NT);
+  if (k.none) return;
   const int lo = k.lo, hi = k.hi, l = threadIdx.x & 63;
-  const bool rows_here = k.w * MT * 16 < DP;
-  const long last = k.live - 1;                          // the loop runs from here down
-  T* const dv0 = static_cast<T*>(a.dv);
+  const bool own = k.w * MT * 16 < DP;
+  const long vrow = (long)a.B * a.dv_ld, yrow = (long)a.B * a.Hv * a.Dv;
   if (threadIdx.x < 256) {
-    State<MT, NL> S;
-    S.load(k, a, a.dST && rows_here ? a.dST + k.head : nullptr);
-    if (rows_here) S.publish(k, Sp, KP);
-    const T* kp = static_cast<const T*>(a.k) + ((last * CT + k.arow) * a.B + k.b) * a.k_ld + (long)k.hk * a.Dk + 8 * hi;
-    const bf16_t* tp = a.ttp + (k.item0 + last) * 3 * SQ + k.arow * CT + 8 * hi;
-    const bf16_t* ktp = a.ktp + ((k.kitem0 + last) * NP * DP + 16 * k.w * MT + lo) * CT + 8 * hi;
-    const float4* tkp = a.tok + (k.item0 + last) * CT + k.crow;
-    T* vp = dv0 + ((last * CT + k.crow) * a.B + k.b) * a.dv_ld + (long)k.h * a.Dv + k.c0 + lo;
-    const long kstep = (long)CT * a.B * a.k_ld, vrow = (long)a.B * a.dv_ld;
-    Raw8<T> rows[KS];
-    uint4 sq[3][2], kt[NP][MT][2];
-    float4 tok[4];
-    auto fetch = [&](int n) {
-      load_rows16<T, KS>(rows, kp, n * CT + k.arow < k.len, a.Dk, hi);
-      load_square16<3>(sq, tp);
-      if (AHEAD) load_transposed<NP, MT, DP>(kt, ktp, rows_here);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) tok[r] = tkp[r];
-      kp -= kstep;
-      tp -= 3 * SQ;
-      tkp -= CT;
-      if (AHEAD) ktp -= (long)NP * DP * CT;
+    struct Ops {
+      uint4 rows[NP][KS], sq[3][2], kt[NP][MT][2];
+      float4 tok[4];
+      float end;
     };
-    if (k.live > 0) fetch(k.live - 1);
-    lds_barrier();
-    lds_barrier();
-    for (int n = k.live - 1; n >= 0; --n) {
+    State<MT, NL> S;
+    S.load(k, a, a.dST && own ? a.dST + k.head : nullptr);
+    if (own) S.publish(k, Sp, KP);
+    auto squares = [&](Ops& o, int n) {
+      load_square16<3>(o.sq, a.ttp + (k.item0 + n) * 3 * SQ, k);
+      load_transposed<NP, MT, DP>(o.kt, a.ktp + (k.kitem0 + n) * NP * DP * CT, k, own);
+    };
+    auto fetch = [&](Ops& o, int n) {
+      load_rows16<NP, KS>(o.rows, a.kp + (k.kitem0 + n) * NP * CT * DP, k);
+      const rsrc_t rt = make_rsrc(a.tok + (k.item0 + n) * CT, CT * 16);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o.tok[r] = __builtin_bit_cast(float4, bload16(rt, (k.crow + r) * 16));
+      o.end = bload<float>(rt, (CT - 1) * 16);
+      if (AHEAD) squares(o, n);
+    };
+    auto chunk = [&](int n, Ops& o, Ops& nxt) {
       const long item = k.item0 + n;
       const int slot = n & 1;
-      frag ra[KS][NP];
-      uint4 ta[3][2], ka[NP][MT][2];
-      float4 tk[4];
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        uint4 p[NP];
-        rows[s].pieces(p);
-#pragma unroll
-        for (int e = 0; e < NP; ++e) ra[s][e] = as_frag(p[e]);
-      }
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-#pragma unroll
-        for (int e = 0; e < 3; ++e) ta[e][s] = sq[e][s];
-        if (AHEAD)
-#pragma unroll
-          for (int e = 0; e < NP; ++e)
-#pragma unroll
-            for (int m = 0; m < MT; ++m) ka[e][m][s] = kt[e][m][s];
-      }
-#pragma unroll
-      for (int r = 0; r < 4; ++r) tk[r] = tok[r];
-      if (k.w == 3 && hi == 3 && lo == 0) s_end = tk[3].x;   // e^{G_end}
-      if (!AHEAD) {
-        load_transposed<NP, MT, DP>(ka, ktp, rows_here);
-        ktp -= (long)NP * DP * CT;
-      }
-      if (n > 0) fetch(n - 1);
+      if (!AHEAD) squares(o, n);
+      fetch(nxt, max(n - 1, 0));
+      __builtin_amdgcn_sched_barrier(0);
       f32x4 du[NL];
 #pragma unroll
       for (int q = 0; q < NL; ++q) du[q] = zero_acc();
@@ -764,19 +751,25 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
       for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int q = 0; q < NL; ++q) {
-          frag sb[3];
+          frag sb[3], ra[NP];
           load_b<3>(sb, Sp + (16 * q + lo) * KP + 32 * s + 8 * hi, NT * KP);
-          mma<NP, 3, 2>(ra[s], sb, du[q]);
+#pragma unroll
+          for (int e = 0; e < NP; ++e) ra[e] = as_frag(o.rows[e][s]);
+          mma<NP, 3, 2>(ra, sb, du[q]);
         }
 #pragma unroll
       for (int q = 0; q < NL; ++q) {
         const f32x4 x = mail[slot][k.w][q][l];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) du[q][r] = x[r] + tk[r].y * du[q][r];
+        for (int r = 0; r < 4; ++r) du[q][r] = x[r] + o.tok[r].y * du[q][r];
         split4_store<3>(du[q], Rp + (16 * q + lo) * RC + k.crow, NT * RC);
       }
-      if (rows_here) S.store(k, a, a.dst + item * a.Dk * a.Dv);
+      S.store(k, a, a.dst + item * a.Dk * a.Dv);
       lds_barrier();
+      const int t0 = n * CT + 16 * k.w;
+      const rsrc_t rr = rows_rsrc(a.dr + (item * CT + 16 * k.w) * a.Dv + k.c0, 16, a.Dv, k.nc);
+      const rsrc_t rv = rows_rsrc(static_cast<T*>(a.dv) + ((long)t0 * a.B + k.b) * a.dv_ld + (long)k.h * a.Dv + k.c0,
+                                  min(16, a.T - t0), vrow, k.nc);
 #pragma unroll
       for (int q = 0; q < NL; ++q) {
         f32x4 z = zero_acc(), zs;
@@ -785,90 +778,90 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
           frag rb[3], tf[3];
           load_b<3>(rb, Rp + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
 #pragma unroll
-          for (int e = 0; e < 3; ++e) tf[e] = as_frag(ta[e][s]);
+          for (int e = 0; e < 3; ++e) tf[e] = as_frag(o.sq[e][s]);
           mma<3, 3, 2>(tf, rb, z);
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          z[r] *= tk[r].z;                               // dR
-          zs[r] = -tk[r].x * z[r];
+          z[r] *= o.tok[r].z;                            // dR
+          zs[r] = -o.tok[r].x * z[r];
         }
         split4_store<3>(zs, Up + (16 * q + lo) * RC + k.crow, NT * RC);
-        if (k.c0 + 16 * q + lo < a.Dv) {
-          float* rp = a.dr + (item * CT + 16 * k.w) * a.Dv + k.c0 + 16 * q;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int t = n * CT + k.crow + r;
-            rp[(unsigned)((4 * hi + r) * a.Dv + lo)] = z[r];
-            if (t < a.T) vp[r * vrow + 16 * q] = Op<T>::from_f32(t < k.len ? z[r] : 0.f);
-          }
+        for (int r = 0; r < 4; ++r) {
+          bstore(rr, k.place<float>(q, a.Dv) + r * a.Dv * 4, z[r]);
+          bstore(rv, k.place<T>(q, vrow) + (unsigned)(r * vrow * (long)sizeof(T)),
+                 Op<T>::from_f32(n * CT + k.crow + r < k.len ? z[r] : 0.f));
         }
       }
-      vp -= CT * vrow;
       lds_barrier();
-      if (rows_here) {
-        const float e_end = s_end;
+      if (own) {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
           for (int q = 0; q < NL; ++q) {
             const f32x4 x = mail[slot][k.w][NL + m * NL + q][l];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S.x[m][q][r] = e_end * S.x[m][q][r] + x[r];
+            for (int r = 0; r < 4; ++r) S.x[m][q][r] = o.end * S.x[m][q][r] + x[r];
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
               frag ub[3], kf[NP];
               load_b<3>(ub, Up + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
 #pragma unroll
-              for (int e = 0; e < NP; ++e) kf[e] = as_frag(ka[e][m][s]);
+              for (int e = 0; e < NP; ++e) kf[e] = as_frag(o.kt[e][m][s]);
               mma<NP, 3, 2>(kf, ub, S.x[m][q]);
             }
           }
         S.publish(k, Sp, KP);
       }
       lds_barrier();
+    };
+    Ops A, B;
+    if (k.live > 0) fetch(A, k.live - 1);
+    lds_barrier();
+    lds_barrier();
+    for (int n = k.live - 1; n >= 0; n -= 2) {
+      chunk(n, A, B);
+      if (n > 0) chunk(n - 1, B, A);
     }
-    if (rows_here && a.dS0) S.store(k, a, a.dS0 + k.head);
+    if (own && a.dS0) S.store(k, a, a.dS0 + k.head);
   } else {
-    const bf16_t* tp = a.ptp + (k.item0 + last) * 3 * SQ + k.arow * CT + 8 * hi;
-    const bf16_t* qtp = a.qtp + ((k.kitem0 + last) * NP * DP + 16 * k.w * MT + lo) * CT + 8 * hi;
-    const float4* tkp = a.tok + (k.item0 + last) * CT + k.crow;
-    const T* yp = static_cast<const T*>(a.dy) + (((last * CT + k.crow) * a.B + k.b) * a.Hv + k.h) * a.Dv + k.c0 + lo;
-    const long yrow = (long)a.B * a.Hv * a.Dv;
-    uint4 sq[3][2], qt[NP][MT][2];
-    float tok[4];
-    T yraw[4][NL];
-    auto fetch = [&](int n) {
-      load_square16<3>(sq, tp);
-      load_transposed<NP, MT, DP>(qt, qtp, rows_here);
+    struct Ops {
+      uint4 sq[3][2], qt[NP][MT][2];
+      float tok[4];
+      T y[4][NL];
+    };
+    auto fetch = [&](Ops& o, int n) {
+      const int t0 = n * CT + 16 * k.w;
+      const rsrc_t rt = make_rsrc(a.tok + (k.item0 + n) * CT, CT * 16);
+      const rsrc_t ry = rows_rsrc(static_cast<const T*>(a.dy) + ((long)t0 * a.B + k.b) * a.Hv * a.Dv + (long)k.h * a.Dv + k.c0,
+                                  min(16, k.len - t0), yrow, k.nc);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        tok[r] = tkp[r].x;
+        o.tok[r] = bload<float>(rt, (k.crow + r) * 16);
 #pragma unroll
         for (int q = 0; q < NL; ++q)
-          yraw[r][q] = n * CT + k.crow + r < k.len && k.c0 + 16 * q + lo < a.Dv ? yp[r * yrow + 16 * q] : (T)0;
+          o.y[r][q] = bload<T>(ry, k.place<T>(q, yrow) + (unsigned)(r * yrow * (long)sizeof(T)));
       }
-      tp -= 3 * SQ;
-      qtp -= (long)NP * DP * CT;
-      tkp -= CT;
-      yp -= CT * yrow;
+      load_square16<3>(o.sq, a.ptp + (k.item0 + n) * 3 * SQ, k);
+      load_transposed<NP, MT, DP>(o.qt, a.qtp + (k.kitem0 + n) * NP * DP * CT, k, own);
     };
     // dY of the fetched chunk into LDS ..
-    auto lay_dy = [&]() {
+    auto lay_dy = [&](const Ops& o) {
 #pragma unroll
       for (int q = 0; q < NL; ++q) {
         f32x4 y, ys;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          y[r] = Op<T>::to_f32(yraw[r][q]);
-          ys[r] = a.scale * tok[r] * y[r];
+          y[r] = Op<T>::to_f32(o.y[r][q]);
+          ys[r] = a.scale * o.tok[r] * y[r];
         }
         split4_store<NP>(y, Yp + (16 * q + lo) * RC + k.crow, NT * RC);
         split4_store<3>(ys, Ys + (16 * q + lo) * RC + k.crow, NT * RC);
       }
     };
     // .. and the two products into the mailbox
-    auto products = [&](int slot) {
+    auto products = [&](int slot, const Ops& o) {
 #pragma unroll
       for (int q = 0; q < NL; ++q) {
         f32x4 x = zero_acc();
@@ -877,7 +870,7 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
           frag yb[NP], pa[3];
           load_b<NP>(yb, Yp + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
 #pragma unroll
-          for (int e = 0; e < 3; ++e) pa[e] = as_frag(sq[e][s]);
+          for (int e = 0; e < 3; ++e) pa[e] = as_frag(o.sq[e][s]);
           mma<3, NP, 2>(pa, yb, x);
         }
         mail[slot][k.w][q][l] = x;
@@ -889,31 +882,38 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
             frag yb[3], qa[NP];
             load_b<3>(yb, Ys + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
 #pragma unroll
-            for (int e = 0; e < NP; ++e) qa[e] = as_frag(qt[e][m][s]);
+            for (int e = 0; e < NP; ++e) qa[e] = as_frag(o.qt[e][m][s]);
             mma<NP, 3, 2>(qa, yb, z);
           }
           mail[slot][k.w][NL + m * NL + q][l] = z;
         }
       }
     };
+    // in the chain's chunk n: chunk n - 1's products (o), loads of chunk n - 2
+    auto chunk = [&](int n, Ops& o, Ops& nxt) {
+      fetch(nxt, max(n - 2, 0));
+      __builtin_amdgcn_sched_barrier(0);
+      lay_dy(o);
+      lds_barrier();
+      products((n - 1) & 1, o);
+      lds_barrier();
+      lds_barrier();
+    };
+    Ops A, B;
     if (k.live > 0) {
-      fetch(k.live - 1);
-      lay_dy();
+      fetch(A, k.live - 1);
+      fetch(B, max(k.live - 2, 0));
+      lay_dy(A);
     }
     lds_barrier();
-    if (k.live > 0) products((k.live - 1) & 1);
-    if (k.live > 1) fetch(k.live - 2);
+    if (k.live > 0) products((k.live - 1) & 1, A);
     lds_barrier();
-    for (int n = k.live - 1; n >= 0; --n) {
-      if (n > 0) lay_dy();                               // of chunk n - 1
-      lds_barrier();
-      if (n > 0) products((n - 1) & 1);
-      lds_barrier();
-      if (n > 1) fetch(n - 2);
-      lds_barrier();
+    for (int n = k.live - 1; n >= 0; n -= 2) {
+      chunk(n, B, A);
+      if (n > 0) chunk(n - 1, A, B);
     }
   }
-  zero_rest<T, NT>(dv0, a.dv_ld, a, k);
+  zero_rest<T, NT>(static_cast<T*>(a.dv), a.dv_ld, a, k);
 }
 
 // ---------------------------------------------------------------------------
@@ -1209,7 +1209,7 @@ int cols_of(const DeltaArgs& a, int cus) {
 
 template <typename T, int KS, int NL>
 void launch_state(const DeltaArgs& a, bool save, bool bwd, hipStream_t s) {
-  const dim3 grid((unsigned)((long)a.B * a.Hv * ((a.Dv + 16 * NL - 1) / (16 * NL))));
+  const dim3 grid((unsigned)(((long)a.B * a.Hv + 7) / 8 * 8 * ((a.Dv + 16 * NL - 1) / (16 * NL))));
   if (bwd) delta_state_bwd_kernel<T, KS, NL><<<grid, dim3(512), 0, s>>>(a);
   else if (save) delta_state_fwd_kernel<T, KS, NL, true><<<grid, dim3(512), 0, s>>>(a);
   else delta_state_fwd_kernel<T, KS, NL, false><<<grid, dim3(512), 0, s>>>(a);
