@@ -425,7 +425,7 @@ ll_status ll_eval_activations(int32_t device, const float* in, float* out, int64
  * h reads key head h / (Hv / Hk).
  *   T_max, B, Hk, Hv, Dk, Dv >= 1; Hv a multiple of Hk; Dk <= 128, Dv <= 512,
  *     both multiples of 8, a time step of v, y and dv (B tokens with their
- *     strides) at most 2^27 bytes (else LL_EUNSUPPORTED); dtype an ll_dtype, the type
+ *     strides) at most 2^26 bytes (else LL_EUNSUPPORTED); dtype an ll_dtype, the type
  *     of q, k, v, y and their gradients (g, beta, states and their gradients
  *     are float).  Inside, sums, states and everything between two products
  *     are held in float, products keep float's 24 bits.

@@ -140,8 +140,8 @@ ll_status validate(const ll_delta_desc* d, bool step) {
       return fail(LL_EINVAL, "%s = %lld must be 0, or at least %lld, at most 2^31 and a multiple of 16 bytes",
                   names[i], (long long)ld[i], (long long)need[i]);
   const int64_t widest = std::max({d->v_ld, step ? 0 : d->dv_ld, v});
-  if (!step && widest * d->B * es > (int64_t)1 << 27)
-    return fail(LL_EUNSUPPORTED, "a time step of v, y or dv spans %lld bytes (at most 2^27)",
+  if (!step && widest * d->B * es > (int64_t)1 << 26)
+    return fail(LL_EUNSUPPORTED, "a time step of v, y or dv spans %lld bytes (at most 2^26)",
                 (long long)(widest * d->B * es));
   const int64_t nch = (d->T_max + ll::kDeltaChunk - 1) / ll::kDeltaChunk;
   if ((int64_t)d->B * d->Hv > 1 << 24 || (int64_t)d->B * d->Hv * nch > 1 << 26)

@@ -180,11 +180,6 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
     for (int e = 0; e < NP; ++e) {
       *reinterpret_cast<uint4*>(kp + (e * CT + r) * KP + c) = p[e];
       *reinterpret_cast<uint4*>(qp + (e * CT + r) * KP + c) = q[e];
-      if (first) {
-        const long at = ((kitem * NP + e) * CT + r) * DP + c;
-        *reinterpret_cast<uint4*>(a.kp + at) = p[e];
-        *reinterpret_cast<uint4*>(a.qp + at) = q[e];
-      }
     }
   }
   if (tid < CT) {
@@ -230,23 +225,28 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
         mma<NP, NP, 2>(qa, kb, qk[m]);
       }
   }
-  if (first)
-    for (int i = tid; i < NP * DP * 8; i += 256) {
-      const int c = i % DP, j = (i / DP) % 8 * 8, e = i / (DP * 8);
+  if (first) {
+    // wave by wave one fragment: lane l has row 16 tile + lo, columns 32 step + 8 hi ..
+    const long base = kitem * NP * CT * DP + 8 * l;
+    for (int f = w; f < 4 * KS * NP; f += 4) {
+      const int e = f % NP, s = f / NP % KS, t = f / (NP * KS);
+      const int at = (e * CT + 16 * t + lo) * KP + 32 * s + 8 * hi;
+      *reinterpret_cast<uint4*>(a.kp + base + f * 512) = ld16(kp + at);
+      *reinterpret_cast<uint4*>(a.qp + base + f * 512) = ld16(qp + at);
+    }
+    for (int f = w; f < 4 * KS * NP; f += 4) {           // 2 KS row tiles of two steps
+      const int e = f % NP, s = f / NP % 2, t = f / (NP * 2);
       uint32_t x[4], y[4];
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
-        const bf16_t* k0 = kp + (e * CT + j + 2 * m) * KP + c;
-        x[m] = (uint32_t)k0[0] | (uint32_t)k0[KP] << 16;
-        if (SAVE) {
-          const bf16_t* q0 = qp + (e * CT + j + 2 * m) * KP + c;
-          y[m] = (uint32_t)q0[0] | (uint32_t)q0[KP] << 16;
-        }
+        const int at = (e * CT + 32 * s + 8 * hi + 2 * m) * KP + 16 * t + lo;
+        x[m] = (uint32_t)kp[at] | (uint32_t)kp[at + KP] << 16;
+        if (SAVE) y[m] = (uint32_t)qp[at] | (uint32_t)qp[at + KP] << 16;
       }
-      const long at = ((kitem * NP + e) * DP + c) * CT + j;
-      *reinterpret_cast<uint4*>(a.ktp + at) = make_uint4(x[0], x[1], x[2], x[3]);
-      if (SAVE) *reinterpret_cast<uint4*>(a.qtp + at) = make_uint4(y[0], y[1], y[2], y[3]);
+      *reinterpret_cast<uint4*>(a.ktp + base + f * 512) = make_uint4(x[0], x[1], x[2], x[3]);
+      if (SAVE) *reinterpret_cast<uint4*>(a.qtp + base + f * 512) = make_uint4(y[0], y[1], y[2], y[3]);
     }
+  }
   __syncthreads();
   float* am = reinterpret_cast<float*>(raw);
   float* pm = am + CT * SC;
@@ -302,39 +302,34 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
     wave_lds_fence();
   }
   __syncthreads();
-  for (int i = tid; i < CT * 8; i += 256) {
-    const int r = i / 8, j = i % 8 * 8;
+  // fragments (row tile, step) of T and P and, for the gradient, the transposes
+  for (int f = w; f < 8; f += 4) {
+    const int r = 16 * (f / 2) + lo, j = 32 * (f % 2) + 8 * hi;
+    const long at = item * 3 * SQ + (long)f * 3 * 512 + 8 * l;
     float x[8];
     uint4 p[3];
-    const long at = (long)r * CT + j;
+    auto put = [&](bf16_t* dst, int n) {
+      for (int e = 0; e < n; ++e) *reinterpret_cast<uint4*>(dst + at + e * 512) = p[e];
+    };
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = tm[r * SC + j + e];
     split8<3>(x, p);
-#pragma unroll
-    for (int e = 0; e < 3; ++e) *reinterpret_cast<uint4*>(a.tp + (item * 3 + e) * SQ + at) = p[e];
+    put(a.tp, 3);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = pm[r * SC + j + e];
     split8<PP>(x, p);
-#pragma unroll
-    for (int e = 0; e < PP; ++e) *reinterpret_cast<uint4*>(a.pp + (item * 3 + e) * SQ + at) = p[e];
-  }
-  if (SAVE)
-    for (int i = tid; i < CT * 8; i += 256) {
-      const int r = i % CT, j = i / CT * 8;              // row r of the transpose: column r
-      float x[8];
-      uint4 p[3];
-      const long at = (long)r * CT + j;
+    put(a.pp, PP);
+    if (SAVE) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = tm[(j + e) * SC + r];
       split8<3>(x, p);
-#pragma unroll
-      for (int e = 0; e < 3; ++e) *reinterpret_cast<uint4*>(a.ttp + (item * 3 + e) * SQ + at) = p[e];
+      put(a.ttp, 3);
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = pm[(j + e) * SC + r];
       split8<3>(x, p);
-#pragma unroll
-      for (int e = 0; e < 3; ++e) *reinterpret_cast<uint4*>(a.ptp + (item * 3 + e) * SQ + at) = p[e];
+      put(a.ptp, 3);
     }
+  }
 }
 
 namespace {
@@ -351,8 +346,8 @@ __device__ __forceinline__ void lds_barrier() {
 // chunk: what lies past a row's end, past Dk or past Dv is out of the buffer's
 // range (read as 0, not written), so there is no branch around any of them
 // and the wait for one counts exactly what was issued after it.  A lane that
-// has no place at all gets an offset past every range; rows span at most 2^27
-// bytes (validated), so 16 of them stay below it.
+// has no place at all gets an offset past every range; a time step spans at most
+// 2^26 bytes (validated), so the offsets of 32 of them stay below it.
 typedef __amdgpu_buffer_rsrc_t rsrc_t;
 constexpr unsigned kNowhere = 0x80000000u;
 
@@ -380,7 +375,7 @@ __device__ __forceinline__ void bstore(rsrc_t r, unsigned off, bf16_t v) {
 
 // One row and head's walk by a wave of the two loops.
 struct Walk {
-  int b, h, len, live, c0, nc, w, lo, hi, arow, crow;
+  int b, h, len, live, c0, nc, w, lane, lo, hi, crow;
   long head, item0, kitem0;
   bool none;                           // no head for this work-group
   __device__ Walk(const DeltaArgs& a, int NT) {
@@ -399,11 +394,10 @@ struct Walk {
     head = (long)bh * a.Dk * a.Dv;
     item0 = (long)bh * a.nch;
     kitem0 = ((long)b * a.Hk + h / (a.Hv / a.Hk)) * a.nch;
-    const int l = threadIdx.x & 63;
+    lane = threadIdx.x & 63;
     w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6) & 3);
-    lo = l & 15;
-    hi = l >> 4;
-    arow = 16 * w + lo;                // row of an A operand
+    lo = lane & 15;
+    hi = lane >> 4;
     crow = 16 * w + 4 * hi;            // first of the four rows of a result
   }
   // Byte offset of the lane's first row and column 16 q + lo in rows ld apart,
@@ -414,38 +408,41 @@ struct Walk {
   }
 };
 
-// Rows 16 w .. of K or Q of a chunk: piece, 32 elements a step.
+// A wave's fragments into registers: rows 16 w .. of K or Q of a chunk ..
 template <int NP, int KS>
 __device__ __forceinline__ void load_rows16(uint4 (*x)[KS], const bf16_t* base, const Walk& k) {
-  constexpr unsigned DP = 32 * KS;
-  const rsrc_t r = make_rsrc(base, NP * CT * DP * 2);
+  const rsrc_t r = make_rsrc(base, NP * CT * 32 * KS * 2);
 #pragma unroll
-  for (int e = 0; e < NP; ++e)
+  for (int s = 0; s < KS; ++s)
 #pragma unroll
-    for (int s = 0; s < KS; ++s) x[e][s] = bload16(r, (k.arow * DP + 8 * k.hi) * 2 + e * CT * DP * 2 + 64 * s);
+    for (int e = 0; e < NP; ++e)
+      x[e][s] = bload16(r, (frag_at(0, s, e, KS, NP) + k.w * KS * NP * 512) * 2 + k.lane * 16);
 }
 
-// Rows 16 w .. of a [64][64] in N pieces.
-template <int N>
+// .. of a 64 x 64 in three pieces, N of them (a triangular one: tiles 0 and 1
+// of a lower and 2 and 3 of an upper one have nothing in one of the steps) ..
+template <int N, bool LOW>
 __device__ __forceinline__ void load_square16(uint4 (*x)[2], const bf16_t* base, const Walk& k) {
-  const rsrc_t r = make_rsrc(base, 3 * SQ * 2);
 #pragma unroll
-  for (int e = 0; e < N; ++e)
+  for (int s = 0; s < 2; ++s) {
+    const bool some = LOW ? s == 0 || k.w >= 2 : s == 1 || k.w < 2;
+    const rsrc_t r = make_rsrc(base, some ? 3 * SQ * 2 : 0);
 #pragma unroll
-    for (int s = 0; s < 2; ++s) x[e][s] = bload16(r, (k.arow * CT + 8 * k.hi) * 2 + e * SQ * 2 + 64 * s);
+    for (int e = 0; e < N; ++e) x[e][s] = bload16(r, (frag_at(0, s, e, 2, 3) + k.w * 2 * 3 * 512) * 2 + k.lane * 16);
+  }
 }
 
-// The wave's MT tiles of 16 rows of K^T or Q^T (rows past the last read 0).
+// .. and the wave's MT row tiles of K^T or Q^T (tiles past the last read 0).
 template <int NP, int MT, int DP>
 __device__ __forceinline__ void load_transposed(uint4 (*x)[MT][2], const bf16_t* base, const Walk& k, bool own) {
   const rsrc_t r = make_rsrc(base, own ? NP * DP * CT * 2 : 0);
 #pragma unroll
-  for (int e = 0; e < NP; ++e)
+  for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-        x[e][m][s] = bload16(r, ((16 * k.w * MT + k.lo) * CT + 8 * k.hi) * 2 + (e * DP + 16 * m) * CT * 2 + 64 * s);
+      for (int e = 0; e < NP; ++e)
+        x[e][m][s] = bload16(r, (frag_at(m, s, e, 2, NP) + k.w * MT * 2 * NP * 512) * 2 + k.lane * 16);
 }
 
 // B operand: NN pieces of a column, from LDS [piece][NT][pitch].
@@ -536,7 +533,7 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
     S.load(k, a, a.S0 && own ? a.S0 + k.head : nullptr);
     if (own) S.publish(k, Sp, KP);
     auto squares = [&](Ops& o, int n) {
-      load_square16<3>(o.sq, a.tp + (k.item0 + n) * 3 * SQ, k);
+      load_square16<3, true>(o.sq, a.tp + (k.item0 + n) * 3 * SQ, k);
       load_transposed<NP, MT, DP>(o.kt, a.ktp + (k.kitem0 + n) * NP * DP * CT, k, own);
     };
     auto fetch = [&](Ops& o, int n) {
@@ -560,9 +557,9 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
       if (!AHEAD) squares(o, n);
       fetch(nxt, min(n + 1, k.live - 1));
       __builtin_amdgcn_sched_barrier(0);               // the loads go out first
-      f32x4 ks[NL];
+      f32x4 ks[NL][2];                                 // two sums: the products wait for each other less
 #pragma unroll
-      for (int q = 0; q < NL; ++q) ks[q] = zero_acc();
+      for (int q = 0; q < NL; ++q) ks[q][0] = ks[q][1] = zero_acc();
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll
@@ -571,13 +568,13 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
           load_b<3>(sb, Sp + (16 * q + lo) * KP + 32 * s + 8 * hi, NT * KP);
 #pragma unroll
           for (int e = 0; e < NP; ++e) ra[e] = as_frag(o.rows[e][s]);
-          mma<NP, 3, 2>(ra, sb, ks[q]);
+          mma<NP, 3, 2>(ra, sb, ks[q][s & 1]);
         }
 #pragma unroll
       for (int q = 0; q < NL; ++q) {
         f32x4 rr;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) rr[r] = o.tok[r].z * (Op<T>::to_f32(o.v[r][q]) - o.tok[r].x * ks[q][r]);
+        for (int r = 0; r < 4; ++r) rr[r] = o.tok[r].z * (Op<T>::to_f32(o.v[r][q]) - o.tok[r].x * (ks[q][0][r] + ks[q][1][r]));
         split4_store<3>(rr, Rp + (16 * q + lo) * RC + k.crow, NT * RC);
       }
       if (SAVE) S.store(k, a, a.st + item * a.Dk * a.Dv);
@@ -585,15 +582,16 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
       const rsrc_t ru = rows_rsrc(a.u + (item * CT + 16 * k.w) * a.Dv + k.c0, SAVE ? 16 : 0, a.Dv, k.nc);
 #pragma unroll
       for (int q = 0; q < NL; ++q) {
-        f32x4 u = zero_acc(), us;
+        f32x4 us, part[2] = {zero_acc(), zero_acc()};
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           frag rb[3], tf[3];
           load_b<3>(rb, Rp + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
 #pragma unroll
           for (int e = 0; e < 3; ++e) tf[e] = as_frag(o.sq[e][s]);
-          mma<3, 3, 2>(tf, rb, u);
+          mma<3, 3, 2>(tf, rb, part[s]);
         }
+        const f32x4 u = part[0] + part[1];
 #pragma unroll
         for (int r = 0; r < 4; ++r) us[r] = o.tok[r].y * u[r];
         split4_store<3>(us, Up + (16 * q + lo) * RC + k.crow, NT * RC);
@@ -639,7 +637,7 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
     };
     auto fetch = [&](Ops& o, int n) {
       load_rows16<NP, KS>(o.rows, a.qp + (k.kitem0 + n) * NP * CT * DP, k);
-      load_square16<PP>(o.sq, a.pp + (k.item0 + n) * 3 * SQ, k);
+      load_square16<PP, true>(o.sq, a.pp + (k.item0 + n) * 3 * SQ, k);
       const rsrc_t rt = make_rsrc(a.tok + (k.item0 + n) * CT, CT * 16);
 #pragma unroll
       for (int r = 0; r < 4; ++r) o.tok[r] = bload<float>(rt, (k.crow + r) * 16);
@@ -727,7 +725,7 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
     S.load(k, a, a.dST && own ? a.dST + k.head : nullptr);
     if (own) S.publish(k, Sp, KP);
     auto squares = [&](Ops& o, int n) {
-      load_square16<3>(o.sq, a.ttp + (k.item0 + n) * 3 * SQ, k);
+      load_square16<3, false>(o.sq, a.ttp + (k.item0 + n) * 3 * SQ, k);
       load_transposed<NP, MT, DP>(o.kt, a.ktp + (k.kitem0 + n) * NP * DP * CT, k, own);
     };
     auto fetch = [&](Ops& o, int n) {
@@ -744,9 +742,9 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
       if (!AHEAD) squares(o, n);
       fetch(nxt, max(n - 1, 0));
       __builtin_amdgcn_sched_barrier(0);
-      f32x4 du[NL];
+      f32x4 du[NL][2];
 #pragma unroll
-      for (int q = 0; q < NL; ++q) du[q] = zero_acc();
+      for (int q = 0; q < NL; ++q) du[q][0] = du[q][1] = zero_acc();
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll
@@ -755,14 +753,14 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
           load_b<3>(sb, Sp + (16 * q + lo) * KP + 32 * s + 8 * hi, NT * KP);
 #pragma unroll
           for (int e = 0; e < NP; ++e) ra[e] = as_frag(o.rows[e][s]);
-          mma<NP, 3, 2>(ra, sb, du[q]);
+          mma<NP, 3, 2>(ra, sb, du[q][s & 1]);
         }
 #pragma unroll
       for (int q = 0; q < NL; ++q) {
-        const f32x4 x = mail[slot][k.w][q][l];
+        f32x4 x = mail[slot][k.w][q][l];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) du[q][r] = x[r] + o.tok[r].y * du[q][r];
-        split4_store<3>(du[q], Rp + (16 * q + lo) * RC + k.crow, NT * RC);
+        for (int r = 0; r < 4; ++r) x[r] += o.tok[r].y * (du[q][0][r] + du[q][1][r]);
+        split4_store<3>(x, Rp + (16 * q + lo) * RC + k.crow, NT * RC);
       }
       S.store(k, a, a.dst + item * a.Dk * a.Dv);
       lds_barrier();
@@ -772,15 +770,16 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
                                   min(16, a.T - t0), vrow, k.nc);
 #pragma unroll
       for (int q = 0; q < NL; ++q) {
-        f32x4 z = zero_acc(), zs;
+        f32x4 zs, part[2] = {zero_acc(), zero_acc()};
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           frag rb[3], tf[3];
           load_b<3>(rb, Rp + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
 #pragma unroll
           for (int e = 0; e < 3; ++e) tf[e] = as_frag(o.sq[e][s]);
-          mma<3, 3, 2>(tf, rb, z);
+          mma<3, 3, 2>(tf, rb, part[s]);
         }
+        f32x4 z = part[0] + part[1];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           z[r] *= o.tok[r].z;                            // dR
@@ -843,7 +842,7 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
         for (int q = 0; q < NL; ++q)
           o.y[r][q] = bload<T>(ry, k.place<T>(q, yrow) + (unsigned)(r * yrow * (long)sizeof(T)));
       }
-      load_square16<3>(o.sq, a.ptp + (k.item0 + n) * 3 * SQ, k);
+      load_square16<3, false>(o.sq, a.ptp + (k.item0 + n) * 3 * SQ, k);
       load_transposed<NP, MT, DP>(o.qt, a.qtp + (k.kitem0 + n) * NP * DP * CT, k, own);
     };
     // dY of the fetched chunk into LDS ..
@@ -1132,15 +1131,15 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
 #pragma unroll
       for (int i = 0; i < ND; ++i) {
         const int d = 16 * (half * ND + i) + lo;
+        const long kt0 = kitem * NP * DP * CT + 8 * l + frag_at(half * ND + i, 0, 0, 2, NP);
         f32x4 x = zero_acc();
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           frag kb[NP], qb[NP], fa[3], ta[XP], ha[XP];
 #pragma unroll
           for (int e = 0; e < NP; ++e) {
-            const long at = ((kitem * NP + e) * DP + d) * CT + 32 * s + 8 * hi;
-            kb[e] = as_frag(ld16(a.ktp + at));
-            qb[e] = as_frag(ld16(a.qtp + at));
+            kb[e] = as_frag(ld16(a.ktp + kt0 + frag_at(0, s, e, 2, NP)));
+            qb[e] = as_frag(ld16(a.qtp + kt0 + frag_at(0, s, e, 2, NP)));
           }
 #pragma unroll
           for (int e = 0; e < 3; ++e) fa[e] = lds_frag(Fp + (e * CT + arow) * RC + 32 * s + 8 * hi);
@@ -1208,19 +1207,17 @@ int cols_of(const DeltaArgs& a, int cus) {
 }
 
 template <typename T, int KS, int NL>
-void launch_state(const DeltaArgs& a, bool save, bool bwd, hipStream_t s) {
+hipError_t launch_state(const DeltaArgs& a, bool save, bool bwd, hipStream_t s) {
   const dim3 grid((unsigned)(((long)a.B * a.Hv + 7) / 8 * 8 * ((a.Dv + 16 * NL - 1) / (16 * NL))));
   if (bwd) delta_state_bwd_kernel<T, KS, NL><<<grid, dim3(512), 0, s>>>(a);
   else if (save) delta_state_fwd_kernel<T, KS, NL, true><<<grid, dim3(512), 0, s>>>(a);
   else delta_state_fwd_kernel<T, KS, NL, false><<<grid, dim3(512), 0, s>>>(a);
+  return hipGetLastError();
 }
 
 template <typename T, int KS>
-void launch_cols(const DeltaArgs& a, bool save, bool bwd, int cus, hipStream_t s) {
-  switch (cols_of(a, cus)) {
-    case 1: launch_state<T, KS, 1>(a, save, bwd, s); break;
-    default: launch_state<T, KS, 2>(a, save, bwd, s); break;
-  }
+hipError_t launch_cols(const DeltaArgs& a, bool save, bool bwd, int cus, hipStream_t s) {
+  return cols_of(a, cus) == 2 ? launch_state<T, KS, 2>(a, save, bwd, s) : launch_state<T, KS, 1>(a, save, bwd, s);
 }
 
 template <typename T, int KS>
@@ -1230,14 +1227,12 @@ hipError_t launch_fwd(const DeltaArgs& a, bool save, int cus, hipStream_t s) {
   else delta_prep_kernel<T, KS, false><<<items, dim3(256), 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  launch_cols<T, KS>(a, save, false, cus, s);
-  return hipGetLastError();
+  return launch_cols<T, KS>(a, save, false, cus, s);
 }
 
 template <typename T, int KS>
 hipError_t launch_bwd(const DeltaArgs& a, int cus, hipStream_t s) {
-  launch_cols<T, KS>(a, true, true, cus, s);
-  hipError_t e = hipGetLastError();
+  hipError_t e = launch_cols<T, KS>(a, true, true, cus, s);
   if (e != hipSuccess) return e;
   delta_grads_kernel<T, KS><<<dim3((unsigned)((long)a.B * a.Hk * a.nch)), dim3(512), 0, s>>>(a);
   return hipGetLastError();
