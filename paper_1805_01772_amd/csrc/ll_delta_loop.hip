@@ -916,17 +916,19 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// grads: one work-group of eight waves per item of a key head; wave = 16 of the
-// 64 tokens x half of the columns.  The value columns are walked 32 at a time:
-// dY, U, dR and the two states go through LDS in pieces, F, H and the three
-// products with the states stay in accumulators.  The value heads of a key head
-// follow one another, so dQ and dK are summed in a fixed order.
+// grads: one work-group of eight waves per item of a key head; wave = 16 of the 64
+// tokens x half of the columns.  The value columns are walked 32 at a
+// time: dY, U, dR and the two states go through LDS in pieces (loaded a step
+// ahead into registers), F, H and the three products with the states stay in
+// accumulators.  The value heads of a key head follow one another, so dQ and dK
+// are summed in a fixed order.
 // ---------------------------------------------------------------------------
 template <typename T, int KS>
 __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
-  constexpr int NP = Pieces<T>::n, XP = NP == 1 ? 2 : 3;   // pieces where the result is only dK
-  constexpr int DP = 32 * KS, NC = 32, CP = NC + 8, NDT = DP / 16, ND = NDT / 2 > 0 ? NDT / 2 : 1;
+  constexpr int NP = Pieces<T>::n, XP = NP == 1 ? 2 : 3;   // XP pieces where the result is only dK
+  constexpr int DP = 32 * KS, NC = 32, CP = NC + 8, NDT = DP / 16, ND = NDT / 2;
   constexpr int kWalk = (NP * CT + 3 * CT + XP * CT + 6 * DP) * CP, kSq = (3 + XP + XP) * CT * RC;
+  constexpr int kLoads = KS > 2 ? KS : 2;                  // float4 pairs a thread loads a step
   __shared__ __align__(16) bf16_t pool[kWalk > kSq ? kWalk : kSq];
   __shared__ float4 tok[CT];
   __shared__ double G[CT];
@@ -942,8 +944,8 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
   const int n = blockIdx.x % a.nch, bk = blockIdx.x / a.nch;
   const int b = bk / a.Hk, hk = bk % a.Hk, grp = a.Hv / a.Hk;
   const int len = delta_len(a, b), t0 = n * CT;
-  const int tid = threadIdx.x, wave = tid >> 6, w = wave & 3, half = wave >> 2, l = tid & 63, lo = l & 15, hi = l >> 4;
-  const int arow = 16 * w + lo, crow = 16 * w + 4 * hi;
+  const int tid = threadIdx.x, l = tid & 63, lo_ = l & 15, hi_ = l >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), w = wave & 3, half = wave >> 2;
   T* dq = static_cast<T*>(a.dq);
   T* dk = static_cast<T*>(a.dk);
   if (t0 >= len) {
@@ -960,11 +962,67 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
     }
     return;
   }
-  const bool dcols = half * ND < NDT;  // (one 16-column tile: the second half has none)
   f32x4 tq[ND], tkk[ND];
 #pragma unroll
   for (int i = 0; i < ND; ++i) tq[i] = tkk[i] = zero_acc();
   const long kitem = bk * (long)a.nch + n;
+  // K and Q at the results' places (rows crow .. crow + 3 of a column), as the
+  // transposes hold them: four neighbours of one fragment
+  const rsrc_t rk = make_rsrc(a.ktp + kitem * NP * DP * CT, NP * DP * CT * 2);
+  const rsrc_t rq = make_rsrc(a.qtp + kitem * NP * DP * CT, NP * DP * CT * 2);
+  const unsigned kq = ((2 * (w & 1) + (hi_ >> 1)) * 16 + lo_) * 16 + 8 * (hi_ & 1);
+  auto column = [&](rsrc_t r, int i) {
+    f32x4 v = zero_acc();
+#pragma unroll
+    for (int e = 0; e < NP; ++e) {
+      const uint2 u = __builtin_bit_cast(
+          uint2, __builtin_amdgcn_raw_buffer_load_b64(r, kq, frag_at(half * ND + i, w >> 1, e, 2, NP) * 2, 0));
+      v += f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                 __uint_as_float(u.y & 0xffff0000u)};
+    }
+    return v;
+  };
+  // loads of a step: waves 0-3 four columns of two tokens a lane, the others
+  // four columns of KS rows of the states (descriptors as in the loops: uniform
+  // bases, so that few addresses live in registers)
+  const bool tokens = wave < 4;
+  const int row = (tid & 255) >> 3, rc = (tid & 7) * 4;
+  const long yrow = (long)a.B * a.Hv * a.Dv, vrow = (long)a.B * a.v_ld;
+  struct alignas(4 * sizeof(T)) Four { T x[4]; };
+  f32x4 x0[kLoads], x1[kLoads];
+  Four fy[2], fv[2];
+  auto load4 = [&](rsrc_t r, unsigned off, Four& f) {
+    if constexpr (NP == 1) f = __builtin_bit_cast(Four, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
+    else f = __builtin_bit_cast(Four, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+  };
+  auto fetch = [&](int h, int c0) {
+    const long item = ((long)b * a.Hv + h) * a.nch + n;
+    const bool in = c0 + rc < a.Dv;
+    if (tokens) {
+      const rsrc_t ru = make_rsrc(a.u + item * CT * a.Dv, CT * a.Dv * 4), rr = make_rsrc(a.dr + item * CT * a.Dv, CT * a.Dv * 4);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const unsigned off = in ? ((row + 32 * i) * a.Dv + c0 + rc) * 4 : kNowhere;
+        x0[i] = __builtin_bit_cast(f32x4, bload16(ru, off));
+        x1[i] = __builtin_bit_cast(f32x4, bload16(rr, off));
+        const int r0 = 8 * wave + 32 * i, tv = min(8, len - t0 - r0);   // the wave's first row, its tokens
+        const long tok0 = (long)(t0 + r0) * a.B + b;
+        const rsrc_t ry = rows_rsrc(static_cast<const T*>(a.dy) + (tok0 * a.Hv + h) * a.Dv, tv, yrow, a.Dv);
+        const rsrc_t rv = rows_rsrc(static_cast<const T*>(a.v) + tok0 * a.v_ld + (long)h * a.Dv, tv, vrow, a.Dv);
+        load4(ry, in ? (unsigned)(((row & 7) * yrow + c0 + rc) * (long)sizeof(T)) : kNowhere, fy[i]);
+        load4(rv, in ? (unsigned)(((row & 7) * vrow + c0 + rc) * (long)sizeof(T)) : kNowhere, fv[i]);
+      }
+    } else {
+      const rsrc_t rs = make_rsrc(a.st + item * a.Dk * a.Dv, a.Dk * a.Dv * 4), rd = make_rsrc(a.dst + item * a.Dk * a.Dv, a.Dk * a.Dv * 4);
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        const unsigned off = in ? ((row + 32 * i) * a.Dv + c0 + rc) * 4 : kNowhere;
+        x0[i] = __builtin_bit_cast(f32x4, bload16(rs, off));
+        x1[i] = __builtin_bit_cast(f32x4, bload16(rd, off));
+      }
+    }
+  };
+  fetch(hk * grp, 0);
   for (int hh = 0; hh < grp; ++hh) {
     const int h = hk * grp + hh;
     const long item = ((long)b * a.Hv + h) * a.nch + n;
@@ -972,56 +1030,41 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
 #pragma unroll
     for (int i = 0; i < ND; ++i) aq[i] = ku[i] = kr[i] = zero_acc();
     F[0] = F[1] = H[0] = H[1] = zero_acc();
-    float ss = 0.f, ub = 0.f, vr = 0.f;
-    const int row = tid >> 3, rc = (tid & 7) * 4;        // four of a row's 32 columns
-    __syncthreads();
-    if (tid < CT) {
-      tok[tid] = a.tok[item * CT + tid];
-      G[tid] = a.G[item * CT + tid];
-    }
+    float ss = 0.f, ub[2] = {0.f, 0.f}, vr[2] = {0.f, 0.f};
     for (int c0 = 0; c0 < a.Dv; c0 += NC) {
-      if (c0) __syncthreads();
-      {
-        const int t = t0 + row, c = c0 + rc;
-        const bool in = c < a.Dv;
-        f32x4 u = zero_acc(), r = zero_acc(), y = zero_acc(), v = zero_acc();
-        if (in) {
-          u = *reinterpret_cast<const f32x4*>(a.u + (item * CT + row) * a.Dv + c);
-          r = *reinterpret_cast<const f32x4*>(a.dr + (item * CT + row) * a.Dv + c);
-          if (t < len) {
-            const T* yp = static_cast<const T*>(a.dy) + (((long)t * a.B + b) * a.Hv + h) * a.Dv + c;
-            const T* vp = static_cast<const T*>(a.v) + ((long)t * a.B + b) * a.v_ld + (long)h * a.Dv + c;
-            struct alignas(4 * sizeof(T)) Four { T x[4]; };
-            const Four fy = *reinterpret_cast<const Four*>(yp), fv = *reinterpret_cast<const Four*>(vp);
+      __syncthreads();
+      if (c0 == 0 && tid < CT) {
+        tok[tid] = a.tok[item * CT + tid];
+        G[tid] = a.G[item * CT + tid];
+      }
+      if (tokens) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              y[e] = Op<T>::to_f32(fy.x[e]);
-              v[e] = Op<T>::to_f32(fv.x[e]);
-            }
+        for (int i = 0; i < 2; ++i) {
+          const int r = row + 32 * i;
+          f32x4 y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            y[e] = Op<T>::to_f32(fy[i].x[e]);
+            ub[i] += x1[i][e] * x0[i][e];
+            vr[i] += x1[i][e] * Op<T>::to_f32(fv[i].x[e]);
           }
+          split4_store<NP>(y, Yp + r * CP + rc, CT * CP);
+          split4_store<3>(x0[i], Up + r * CP + rc, CT * CP);
+          split4_store<XP>(x1[i], Rp + r * CP + rc, CT * CP);
         }
+      } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          ub += r[e] * u[e];
-          vr += r[e] * v[e];
-        }
-        split4_store<NP>(y, Yp + row * CP + rc, CT * CP);
-        split4_store<3>(u, Up + row * CP + rc, CT * CP);
-        split4_store<XP>(r, Rp + row * CP + rc, CT * CP);
-        for (int i = tid; i < DP * 8; i += 512) {
-          const int d = i >> 3, cc = (i & 7) * 4;
-          f32x4 s = zero_acc(), ds = zero_acc();
-          if (d < a.Dk && c0 + cc < a.Dv) {
-            s = *reinterpret_cast<const f32x4*>(a.st + (item * a.Dk + d) * a.Dv + c0 + cc);
-            ds = *reinterpret_cast<const f32x4*>(a.dst + (item * a.Dk + d) * a.Dv + c0 + cc);
-          }
+        for (int i = 0; i < KS; ++i) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) ss += s[e] * ds[e];
-          split4_store<3>(s, Sp + d * CP + cc, DP * CP);
-          split4_store<3>(ds, Dp + d * CP + cc, DP * CP);
+          for (int e = 0; e < 4; ++e) ss += x0[i][e] * x1[i][e];
+          split4_store<3>(x0[i], Sp + (row + 32 * i) * CP + rc, DP * CP);
+          split4_store<3>(x1[i], Dp + (row + 32 * i) * CP + rc, DP * CP);
         }
       }
       __syncthreads();
+      if (c0 + NC < a.Dv) fetch(h, c0 + NC);
+      else if (hh + 1 < grp) fetch(h + 1, 0);
+      const int lo = lo_, hi = hi_, arow = 16 * w + lo;
       frag ya[NP], ua[3], ra[XP];
 #pragma unroll
       for (int e = 0; e < NP; ++e) ya[e] = lds_frag(Yp + (e * CT + arow) * CP + 8 * hi);
@@ -1040,7 +1083,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
           mma<XP, XP, XP - 1>(ra, un, H[m]);
         }
       }
-      if (dcols) {
+      {
 #pragma unroll
         for (int i = 0; i < ND; ++i) {
           const int d = 16 * (half * ND + i) + lo;
@@ -1056,18 +1099,35 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
         }
       }
     }
+    // K^T and Q^T by column tiles, one ahead
+    frag kb[2][2][NP], qb[2][2][NP];
+    auto load_kq = [&](int i) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int e = 0; e < NP; ++e) {
+          const int at = frag_at(half * ND + i, s, e, 2, NP) * 2;
+          kb[i & 1][s][e] = as_frag(__builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rk, 16 * l, at, 0)));
+          qb[i & 1][s][e] = as_frag(__builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rq, 16 * l, at, 0)));
+        }
+    };
+    load_kq(0);
+    // (places computed anew for every head: kept over the walk they would spill)
+    int lo = lo_, hi = hi_;
+    asm volatile("" : "+v"(lo), "+v"(hi));
+    const int arow = 16 * w + lo, crow = 16 * w + 4 * hi;
     __syncthreads();
-    // F, F^T and H + H^T in pieces (F_ij of tile (w, j), j <= w; zero above)
+    // F, F^T and H + H^T in pieces (F_ij of tile (w, jt), jt <= w; zero above)
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      const int j = 16 * (2 * half + m) + lo;
-      f32x4 f, hh4;
+      const int jt = 2 * half + m, j = 16 * jt + lo;
+      f32x4 f, hm;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int i = crow + r;
         const float d = j <= i ? expf((float)(G[i] - G[j])) : 0.f;
         f[r] = j <= i ? a.scale * d * F[m][r] : 0.f;
-        hh4[r] = j < i ? -d * H[m][r] : 0.f;
+        hm[r] = j < i ? -d * H[m][r] : 0.f;
       }
       // rows i .. i + 3 of column j: consecutive in the transpose
       split4_store<XP>(f, Ft + j * RC + crow, CT * RC);
@@ -1082,12 +1142,12 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
         x[2 * RC] = (bf16_t)p1[e];
         x[3 * RC] = (bf16_t)(p1[e] >> 16);
       }
-      // H below the diagonal, its mirror above (the diagonal is 0): tile (w, j)
-      // with j < w writes both, a diagonal tile its lower entries and mirrors
-      if (2 * half + m < w) split4_store<XP>(hh4, Hp + j * RC + crow, CT * RC);
-      if (2 * half + m <= w) {
-        split2<XP>(hh4[0], hh4[1], p0);
-        split2<XP>(hh4[2], hh4[3], p1);
+      // H below the diagonal, its mirror above (the diagonal is 0): a tile below
+      // writes both, a diagonal one its lower entries and their mirrors
+      if (jt < w) split4_store<XP>(hm, Hp + j * RC + crow, CT * RC);
+      if (jt <= w) {
+        split2<XP>(hm[0], hm[1], p0);
+        split2<XP>(hm[2], hm[3], p1);
 #pragma unroll
         for (int e = 0; e < XP; ++e) {
           const bf16_t q[4] = {(bf16_t)p0[e], (bf16_t)(p0[e] >> 16), (bf16_t)p1[e], (bf16_t)(p1[e] >> 16)};
@@ -1096,7 +1156,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
             const int i = crow + r;
             if (j <= i) {
               Hp[(e * CT + i) * RC + j] = q[r];
-              if (2 * half + m == w) Hp[(e * CT + j) * RC + i] = q[r];
+              if (jt == w) Hp[(e * CT + j) * RC + i] = q[r];
             }
           }
         }
@@ -1104,43 +1164,44 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
     }
     ss *= tok[CT - 1].x;
     float dots[4] = {0.f, 0.f, 0.f, 0.f};
-    // K and Q at the result's places (row, column), for the dots
-#pragma unroll
-    for (int i = 0; i < ND; ++i)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int c = 16 * (half * ND + i) + lo, t = t0 + crow + r;
-        ku[i][r] *= tok[crow + r].y;
-        aq[i][r] *= a.scale * tok[crow + r].x;
-        kr[i][r] *= tok[crow + r].x;
-        if (dcols && t < len && c < a.Dk)
-          ss += ku[i][r] * Op<T>::to_f32(static_cast<const T*>(a.k)[((long)t * a.B + b) * a.k_ld + (long)hk * a.Dk + c]);
-      }
-    for (int d = 1; d < 64; d <<= 1) ss += __shfl_xor(ss, d, 64);
-    if (l == 0) part[wave] = ss;
-    for (int d = 1; d < 8; d <<= 1) {
-      ub += __shfl_xor(ub, d, 64);
-      vr += __shfl_xor(vr, d, 64);
-    }
-    if ((tid & 7) == 0) {
-      sub[row] = vr;
-      sbeta[row] = ub;
-    }
-    __syncthreads();
-    if (dcols) {
+    {
 #pragma unroll
       for (int i = 0; i < ND; ++i) {
-        const int d = 16 * (half * ND + i) + lo;
-        const long kt0 = kitem * NP * DP * CT + 8 * l + frag_at(half * ND + i, 0, 0, 2, NP);
+        const f32x4 kc = column(rk, i);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float4 tk = tok[crow + r];
+          ku[i][r] *= tk.y;
+          aq[i][r] *= a.scale * tk.x;
+          kr[i][r] *= tk.x;
+          ss += ku[i][r] * kc[r];
+        }
+      }
+    }
+    for (int d = 1; d < 64; d <<= 1) ss += __shfl_xor(ss, d, 64);
+    if (l == 0) part[wave] = ss;
+    if (tokens) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        for (int d = 1; d < 8; d <<= 1) {
+          ub[i] += __shfl_xor(ub[i], d, 64);
+          vr[i] += __shfl_xor(vr[i], d, 64);
+        }
+        if ((tid & 7) == 0) {
+          sub[row + 32 * i] = vr[i];
+          sbeta[row + 32 * i] = ub[i];
+        }
+      }
+    }
+    __syncthreads();
+    {
+#pragma unroll
+      for (int i = 0; i < ND; ++i) {
         f32x4 x = zero_acc();
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-          frag kb[NP], qb[NP], fa[3], ta[XP], ha[XP];
-#pragma unroll
-          for (int e = 0; e < NP; ++e) {
-            kb[e] = as_frag(ld16(a.ktp + kt0 + frag_at(0, s, e, 2, NP)));
-            qb[e] = as_frag(ld16(a.qtp + kt0 + frag_at(0, s, e, 2, NP)));
-          }
+          frag fa[3], ta[XP], ha[XP];
+          if (s == 0 && i + 1 < ND) load_kq(i + 1);
 #pragma unroll
           for (int e = 0; e < 3; ++e) fa[e] = lds_frag(Fp + (e * CT + arow) * RC + 32 * s + 8 * hi);
 #pragma unroll
@@ -1148,15 +1209,14 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
             ta[e] = lds_frag(Ft + (e * CT + arow) * RC + 32 * s + 8 * hi);
             ha[e] = lds_frag(Hp + (e * CT + arow) * RC + 32 * s + 8 * hi);
           }
-          mma<3, NP, 2>(fa, kb, aq[i]);
-          mma<XP, NP, XP - 1>(ta, qb, x);
-          mma<XP, NP, XP - 1>(ha, kb, x);
+          mma<3, NP, 2>(fa, kb[i & 1][s], aq[i]);
+          mma<XP, NP, XP - 1>(ta, qb[i & 1][s], x);
+          mma<XP, NP, XP - 1>(ha, kb[i & 1][s], x);
         }
+        const f32x4 qc = column(rq, i);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int t = t0 + crow + r;
-          if (t < len && d < a.Dk)
-            dots[r] += aq[i][r] * Op<T>::to_f32(static_cast<const T*>(a.q)[((long)t * a.B + b) * a.q_ld + (long)hk * a.Dk + d]);
+          dots[r] += aq[i][r] * qc[r];
           tq[i][r] += aq[i][r];
           tkk[i][r] += x[r] + ku[i][r] - kr[i][r];
         }
@@ -1184,7 +1244,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
       if (t0 + at < a.T) a.dg[((long)(t0 + at) * a.B + b) * a.Hv + h] = t0 + at < len ? s + all : 0.f;
     }
   }
-  if (!dcols) return;
+  const int lo = lo_, crow = 16 * w + 4 * hi_;
 #pragma unroll
   for (int i = 0; i < ND; ++i)
 #pragma unroll
