@@ -133,6 +133,10 @@ __device__ __forceinline__ unsigned long long key_of(float x, int index) {
   return (unsigned long long)u << 32 | (uint32_t)~index;
 }
 __device__ __forceinline__ int key_index(unsigned long long k) { return (int)~(uint32_t)k; }
+__device__ __forceinline__ float key_value(unsigned long long k) {
+  const uint32_t u = (uint32_t)(k >> 32);
+  return __uint_as_float(u == 0 ? 0x7fc00000u : u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
 __device__ __forceinline__ unsigned long long shfl_xor_u64(unsigned long long v, int d) {
   const uint32_t lo = __shfl_xor((int)(uint32_t)v, d, 64), hi = __shfl_xor((int)(uint32_t)(v >> 32), d, 64);
   return (unsigned long long)hi << 32 | lo;
@@ -161,8 +165,12 @@ __device__ __forceinline__ Stats join_group(Stats a, float (*st)[NTHR / 64]) {
     st[2][w] = a.t;
   }
   __syncthreads();
-  a = Stats{st[0][0], st[1][0], st[2][0]};
-  for (int i = 1; i < NTHR / 64; ++i) a = join(a, Stats{st[0][i], st[1][i], st[2][i]});
+  constexpr int NW = NTHR / 64;
+  const int i = tid & (NW - 1);
+  a = Stats{st[0][i], st[1][i], st[2][i]};
+#pragma unroll
+  for (int d = 1; d < NW; d <<= 1)
+    a = join(a, Stats{__shfl_xor(a.m, d, 64), __shfl_xor(a.s, d, 64), __shfl_xor(a.t, d, 64)});
   return a;
 }
 
@@ -177,6 +185,7 @@ __device__ void rank_buffer(Shared<NTHR>& sh, int n, int top) {
     for (int e = tid; e < n; e += NTHR) {
       const unsigned long long k = sh.buf[e];
       int rank = 0;
+#pragma unroll 8
       for (int j = 0; j < n; ++j) rank += sh.buf[j] > k;
       if (rank < top) sh.top[rank] = k;
     }
@@ -202,16 +211,17 @@ __device__ void rank_buffer(Shared<NTHR>& sh, int n, int top) {
   __syncthreads();
 }
 
-// The `top` largest keys of the part's span into sh.top.  (own: the largest
-// value of this thread's chunks, found first in chunk own_c, -1: no chunk.)
+// The `top` largest keys of the part's span into sh.top.  (own: the chunk of this
+// thread's that holds its largest value, the first of them; own_c: which one,
+// -1: the thread has none.)
 template <typename T, int NTHR>
-__device__ void select_top(const T* row, const Span& sp, int V, int top, float own, int own_c, Shared<NTHR>& sh) {
+__device__ void select_top(const T* row, const Span& sp, int V, int top, uint4 own, int own_c, Shared<NTHR>& sh) {
   constexpr int E = Op<T>::kPerChunk, G = NTHR / 64, CAP = NTHR == 256 ? 1024 : 4096;
   const int tid = threadIdx.x, w = tid >> 6, l = tid & 63;
   unsigned long long key = 0;
   if (own_c >= 0) {
     float f[E];
-    unpack<T>(ld16(row + sp.head + (long)own_c * E), f);
+    unpack<T>(own, f);
 #pragma unroll
     for (int e = 0; e < E; ++e) key = max(key, key_of(f[e], sp.head + own_c * E + e));
   }
@@ -227,6 +237,7 @@ __device__ void select_top(const T* row, const Span& sp, int V, int top, float o
   if (w == 0) {
     const unsigned long long mine = sh.group[l];
     int rank = 0;
+#pragma unroll 16
     for (int i = 0; i < 64; ++i) rank += sh.group[i] > mine;
     // (groups without a chunk have key 0 and share a rank: then every element
     // counts, and there are few)
@@ -246,12 +257,26 @@ __device__ void select_top(const T* row, const Span& sp, int V, int top, float o
   if (sp.last && tid < V - sp.tail0) offer(Op<T>::to_f32(row[sp.tail0 + tid]), sp.tail0 + tid);
   __syncthreads();
   const int nc = sh.cands;
-  for (int j = w; j < nc; j += NTHR / 64)
-    for (long c = sp.c0 + sh.cand[j] + (long)l * NTHR; c < sp.c1; c += 64L * NTHR) {
-      float f[E];
-      unpack<T>(ld16(row + sp.head + c * E), f);
+  // a wave per candidate, its chunks over the lanes; four candidates' loads at once
+  const int per = (sp.c1 - sp.c0 + NTHR - 1) / NTHR;     // chunks of a thread at most
+  for (int j = w; j < nc; j += 4 * (NTHR / 64))
+    for (int i = l; i < per; i += 64) {
+      uint4 u[4];
+      int c[4];
 #pragma unroll
-      for (int e = 0; e < E; ++e) offer(f[e], sp.head + (int)c * E + e);
+      for (int q = 0; q < 4; ++q) {
+        const int jq = j + q * (NTHR / 64);
+        c[q] = jq < nc ? sp.c0 + sh.cand[jq] + i * NTHR : sp.c1;
+        u[q] = ld16(row + sp.head + (long)min(c[q], sp.c1 - 1) * E);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (c[q] < sp.c1) {
+          float f[E];
+          unpack<T>(u[q], f);
+#pragma unroll
+          for (int e = 0; e < E; ++e) offer(f[e], sp.head + c[q] * E + e);
+        }
     }
   __syncthreads();
   const int n = sh.count;
@@ -289,14 +314,18 @@ __device__ void select_top(const T* row, const Span& sp, int V, int top, float o
   __syncthreads();
 }
 
-// The part's sums (per thread), and with TOP its thread's largest chunk.
-template <typename T, int NTHR, bool TOP>
-__device__ __forceinline__ Stats walk(const T* row, const Span& sp, int V, float* own, int* own_c) {
+// The part's sums (per thread), and with TOP its thread's largest chunk.  With
+// KEEP the thread's first chunks stay in LDS (keep[i][tid]).  Chunks are loaded
+// four at a time, past the end the last one again: one wait for four.
+template <typename T, int NTHR, bool TOP, int KEEP = 0>
+__device__ __forceinline__ Stats walk(const T* row, const Span& sp, int V, uint4* own, int* own_c,
+                                      uint4 (*keep)[NTHR] = nullptr) {
   constexpr int E = Op<T>::kPerChunk;
   const int tid = threadIdx.x;
   Stats a{kLowest, 0.f, 0.f};
   float best = -__builtin_inff();
-  int best_c = sp.c0 + tid < sp.c1 ? sp.c0 + tid : -1;
+  int best_c = -1;
+  uint4 best_u = zero4();
   auto eat = [&](uint4 u, int c) {
     float f[E];
     unpack<T>(u, f);
@@ -304,9 +333,10 @@ __device__ __forceinline__ Stats walk(const T* row, const Span& sp, int V, float
 #pragma unroll
     for (int e = 1; e < E; ++e) cm = fmaxf(cm, f[e]);
     if (cm > a.m) rebase(a, cm);
-    if (TOP && cm > best) {
-      best = cm;
+    if (TOP && (cm > best || best_c < 0)) {
+      best = cm > best ? cm : best;    // (a first chunk of NaN: anything is more)
       best_c = c;
+      best_u = u;
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -316,18 +346,27 @@ __device__ __forceinline__ Stats walk(const T* row, const Span& sp, int V, float
     }
   };
   const T* body = row + sp.head;
-  int c = sp.c0 + tid;
-  for (; c + 3 * NTHR < sp.c1; c += 4 * NTHR) {
+  float single = 0.f;
+  const bool in_head = sp.first && tid < sp.head, in_tail = sp.last && tid < V - sp.tail0;
+  if (in_head) single = Op<T>::to_f32(row[tid]);
+  float single2 = 0.f;
+  if (in_tail) single2 = Op<T>::to_f32(row[sp.tail0 + tid]);
+  int slot = 0;
+  for (int c = sp.c0 + tid; c < sp.c1; c += 4 * NTHR) {
     uint4 u[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = ld16(body + (long)(c + i * NTHR) * E);
+    for (int i = 0; i < 4; ++i) u[i] = ld16(body + (long)min(c + i * NTHR, sp.c1 - 1) * E);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) eat(u[i], c + i * NTHR);
+    for (int i = 0; i < 4; ++i)
+      if (c + i * NTHR < sp.c1) {
+        if (KEEP && slot + i < KEEP) keep[slot + i][tid] = u[i];
+        eat(u[i], c + i * NTHR);
+      }
+    slot += 4;
   }
-  for (; c < sp.c1; c += NTHR) eat(ld16(body + (long)c * E), c);
-  if (sp.first && tid < sp.head) add_one(a, Op<T>::to_f32(row[tid]));
-  if (sp.last && tid < V - sp.tail0) add_one(a, Op<T>::to_f32(row[sp.tail0 + tid]));
-  *own = best;
+  if (in_head) add_one(a, single);
+  if (in_tail) add_one(a, single2);
+  *own = best_u;
   *own_c = best_c;
   return a;
 }
@@ -336,9 +375,23 @@ struct RowResult {
   float lse, ent;
 };
 
-// The row's outputs from its sums (one thread writes).
+// The row's target and its logit, read while the row is (thread 0's are used).
+struct Target {
+  int id;
+  float x;
+};
 template <typename T>
-__device__ __forceinline__ RowResult row_result(const LogprobArgs& a, const T* row, long r, Stats st) {
+__device__ __forceinline__ Target target_of(const LogprobArgs& a, const T* row, long r) {
+  Target t{-1, 0.f};
+  if (a.targets && threadIdx.x == 0) {
+    t.id = a.targets[r];
+    if (t.id >= 0 && t.id < a.V) t.x = Op<T>::to_f32(row[t.id]);
+  }
+  return t;
+}
+
+// The row's outputs from its sums (one thread writes).
+__device__ __forceinline__ RowResult row_result(const LogprobArgs& a, long r, Stats st, Target t) {
   RowResult res;
   if (st.s == 0.f) {
     res.lse = -__builtin_inff();
@@ -352,12 +405,10 @@ __device__ __forceinline__ RowResult row_result(const LogprobArgs& a, const T* r
     if (a.lse) a.lse[r] = res.lse;
     if (a.entropy) a.entropy[r] = res.ent;
     if (a.targets && a.logp) {
-      const int t = a.targets[r];
       float lp = 0.f;
-      if (t >= 0 && t < a.V) {
-        const float x = Op<T>::to_f32(row[t]);
-        lp = x == -__builtin_inff() && res.lse == res.lse ? x : x - res.lse;
-      } else if (t != -1) {
+      if (t.id >= 0 && t.id < a.V) {
+        lp = t.x == -__builtin_inff() && res.lse == res.lse ? t.x : t.x - res.lse;
+      } else if (t.id != -1) {
         atomicOr(a.err, LL_DEVERR_TARGET);
       }
       a.logp[r] = lp;
@@ -374,11 +425,21 @@ __global__ __launch_bounds__(NTHR) void logprob_fwd_kernel(LogprobArgs a) {
   const int part = blockIdx.x % a.parts;
   const T* row = static_cast<const T*>(a.x) + r * a.ld;
   const Span sp = span_of(row, a.V, part, a.parts);
-  float own;
+  const Target target = target_of(a, row, r);
+  uint4 own;
   int own_c;
   Stats st = walk<T, NTHR, TOP>(row, sp, a.V, &own, &own_c);
   st = join_group<NTHR>(st, sh.st);
-  if (TOP) select_top<T, NTHR>(row, sp, a.V, a.top, own, own_c, sh);
+  if (TOP) {
+    if (st.s == 0.f) {
+      // nothing is allowed here: all equal, the first ones
+      const int first = sp.first ? 0 : sp.head + sp.c0 * Op<T>::kPerChunk;
+      if (tid < a.top) sh.top[tid] = key_of(-__builtin_inff(), first + tid);
+      __syncthreads();
+    } else {
+      select_top<T, NTHR>(row, sp, a.V, a.top, own, own_c, sh);
+    }
+  }
   if (a.parts > 1) {
     // the last work-group of the row to arrive joins the parts
     const long at = r * a.parts + part;
@@ -402,20 +463,19 @@ __global__ __launch_bounds__(NTHR) void logprob_fwd_kernel(LogprobArgs a) {
       rank_buffer<NTHR>(sh, n, a.top);
     }
   }
-  const RowResult res = row_result(a, row, r, st);
+  const RowResult res = row_result(a, r, st, target);
   if (TOP && tid < a.top) {
-    const int i = key_index(sh.top[tid]);
-    const float x = Op<T>::to_f32(row[i]);
-    a.top_ids[r * a.top + tid] = i;
+    const float x = key_value(sh.top[tid]);
+    a.top_ids[r * a.top + tid] = key_index(sh.top[tid]);
     a.top_logp[r * a.top + tid] = x == -__builtin_inff() && res.lse == res.lse ? x : x - res.lse;
   }
 }
 
 // The gradient of one part of a row: everything but the marked entries in a
 // pass, those after it.
-template <typename T, int NTHR>
+template <typename T, int NTHR, int KEEP = 0>
 __device__ void row_gradient(const LogprobArgs& a, const T* row, T* out, long r, const Span& sp, float lse,
-                             float ent, int* mark, float* add, float* val) {
+                             float ent, int* mark, float* add, float* val, const uint4 (*keep)[NTHR] = nullptr) {
   constexpr int E = Op<T>::kPerChunk;
   const int tid = threadIdx.x;
   const int t = a.targets ? a.targets[r] : -1;
@@ -460,15 +520,20 @@ __device__ void row_gradient(const LogprobArgs& a, const T* row, T* out, long r,
     for (int e = 0; e < E; ++e) f[e] = grad(f[e]);
     *reinterpret_cast<uint4*>(out + sp.head + (long)k * E) = pack<T>(f);
   };
-  int k = sp.c0 + tid;
-  for (; k + 3 * NTHR < sp.c1; k += 4 * NTHR) {
+  // last chunks first: read most recently, they are the nearest still; the
+  // thread's first KEEP chunks are in LDS
+  const int mine = sp.c1 - sp.c0 > tid ? (sp.c1 - sp.c0 - tid + NTHR - 1) / NTHR : 0;
+  const int k0 = sp.c0 + tid;
+  for (int i = mine - 1; i >= KEEP; i -= 4) {
     uint4 u[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = ld16(row + sp.head + (long)(k + i * NTHR) * E);
+    for (int j = 0; j < 4; ++j) u[j] = ld16(row + sp.head + (long)(k0 + max(i - j, KEEP) * NTHR) * E);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) one(u[i], k + i * NTHR);
+    for (int j = 0; j < 4; ++j)
+      if (i - j >= KEEP) one(u[j], k0 + (i - j) * NTHR);
   }
-  for (; k < sp.c1; k += NTHR) one(ld16(row + sp.head + (long)k * E), k);
+  if (KEEP)
+    for (int i = min(mine, KEEP) - 1; i >= 0; --i) one(keep[i][tid], k0 + i * NTHR);
   if (sp.first && tid < sp.head) out[tid] = Op<T>::from_f32(grad(Op<T>::to_f32(row[tid])));
   if (sp.last && tid < a.V - sp.tail0)
     out[sp.tail0 + tid] = Op<T>::from_f32(grad(Op<T>::to_f32(row[sp.tail0 + tid])));
@@ -492,21 +557,26 @@ __global__ __launch_bounds__(NTHR) void logprob_bwd_kernel(LogprobArgs a) {
                         a.dentropy ? a.ent_in[r] : 0.f, mark, add, val);
 }
 
-template <typename T, int NTHR>
-__global__ __launch_bounds__(NTHR) void logprob_fwd_bwd_kernel(LogprobArgs a) {
+// Both.  Work-groups of 1024 threads for long rows, two a compute unit: few
+// enough rows are under way that what is read a second time comes from the
+// last-level cache, and 64 KB a row stay in LDS.
+template <typename T, int NTHR, int KEEP>
+__global__ __launch_bounds__(NTHR, NTHR == 1024 ? 8 : 1) void logprob_fwd_bwd_kernel(LogprobArgs a) {
   __shared__ float sts[3][NTHR / 64];
   __shared__ int mark[kTopMax + 1];
   __shared__ float add[kTopMax + 1], val[kTopMax + 1];
+  __shared__ uint4 keep[KEEP ? KEEP : 1][NTHR];
   const long r = blockIdx.x;
   const T* row = static_cast<const T*>(a.x) + r * a.ld;
   const Span sp = span_of(row, a.V, 0, 1);
-  float own;
+  const Target target = target_of(a, row, r);
+  uint4 own;
   int own_c;
-  Stats st = walk<T, NTHR, false>(row, sp, a.V, &own, &own_c);
+  Stats st = walk<T, NTHR, false, KEEP>(row, sp, a.V, &own, &own_c, keep);
   st = join_group<NTHR>(st, sts);
-  const RowResult res = row_result(a, row, r, st);
+  const RowResult res = row_result(a, r, st, target);
   __syncthreads();                     // the target's logit is read before the row is overwritten
-  row_gradient<T, NTHR>(a, row, static_cast<T*>(a.dx) + r * a.ld, r, sp, res.lse, res.ent, mark, add, val);
+  row_gradient<T, NTHR, KEEP>(a, row, static_cast<T*>(a.dx) + r * a.ld, r, sp, res.lse, res.ent, mark, add, val, keep);
 }
 
 }  // namespace ll
@@ -520,11 +590,12 @@ struct ll_logprob_plan {
 namespace {
 
 // Work-groups per row: enough to fill the chip where the rows alone do not,
-// each with at least 16 KiB of its row.
+// each with at least 256 KiB of its row (one work-group reads that in about the
+// time that the join takes).
 int parts_of(const ll_logprob_plan* p, int rows) {
   const long bytes = (long)p->d.V * (p->d.dtype == LL_BF16 ? 2 : 4);
   const long want = (p->cus + rows - 1) / rows;
-  return (int)std::max(1L, std::min({want, bytes >> 14, (long)ll::kPartsMax}));
+  return (int)std::max(1L, std::min({want, bytes >> 18, (long)ll::kPartsMax}));
 }
 
 void release(ll_logprob_plan* p) {
@@ -676,8 +747,14 @@ ll_status ll_logprob_fwd_bwd(ll_logprob_plan* p, void* stream, int32_t rows, con
   a.entropy = entropy; a.lse = lse; a.dx = dlogits;
   a.parts = 1;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  if (p->d.dtype == LL_BF16) ll::logprob_fwd_bwd_kernel<bf16_t, 256><<<dim3(rows), dim3(256), 0, s>>>(a);
-  else ll::logprob_fwd_bwd_kernel<float, 256><<<dim3(rows), dim3(256), 0, s>>>(a);
+  const bool wide = (long)p->d.V * (p->d.dtype == LL_BF16 ? 2 : 4) >= 64 << 10;
+  if (p->d.dtype == LL_BF16) {
+    if (wide) ll::logprob_fwd_bwd_kernel<bf16_t, 1024, 4><<<dim3(rows), dim3(1024), 0, s>>>(a);
+    else ll::logprob_fwd_bwd_kernel<bf16_t, 256, 4><<<dim3(rows), dim3(256), 0, s>>>(a);
+  } else {
+    if (wide) ll::logprob_fwd_bwd_kernel<float, 1024, 4><<<dim3(rows), dim3(1024), 0, s>>>(a);
+    else ll::logprob_fwd_bwd_kernel<float, 256, 4><<<dim3(rows), dim3(256), 0, s>>>(a);
+  }
   LL_HIP(hipGetLastError());
   return LL_OK;
 }

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import atexit
 import ctypes
+import functools
 import os
 import weakref
 from typing import Optional, Sequence
@@ -224,9 +225,10 @@ def _ptr_array(ts):
 
 
 def _stream(stream) -> Optional[int]:
-    import torch
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return s.cuda_stream
+    if stream is None:
+        import torch
+        stream = torch.cuda.current_stream()
+    return stream.cuda_stream
 
 
 class Plan:
@@ -375,34 +377,41 @@ def ll_plan_stack_bytes(plan: Plan):
 # --------------------------------------------------------------------------
 # the operators beside the loops
 # --------------------------------------------------------------------------
-def _op_name(dtype) -> str:
-    name = str(dtype)
-    return {"torch.bfloat16": "bf16", "torch.float32": "f32"}.get(name, name)
+@functools.lru_cache(maxsize=None)
+def _dtype(name: str):
+    """torch's type of a dtype or element type name."""
+    import torch
+    return getattr(torch, {"f32": "float32", "bf16": "bfloat16"}.get(name, name))
 
 
-def _want(t, name: str, shape, dtype: str, optional: bool = False):
-    """The tensor's address; shape and type are what the call says."""
-    if t is None and optional:
-        return None
-    if tuple(t.shape) != tuple(shape) or str(t.dtype) != "torch." + dtype:
-        raise ValueError(f"{name}: {tuple(shape)} {dtype} is wanted, got {tuple(t.shape)} {t.dtype}")
-    return _ptr(t)
-
-
-def _tokens(t, name: str, shape, ld: int, dtype: str):
-    """Address of a token array whose tokens are ld elements apart."""
-    if tuple(t.shape) != tuple(shape) or str(t.dtype) != "torch." + dtype:
+def _refuse(t, name: str, shape, dtype):
+    if tuple(t.shape) != tuple(shape) or t.dtype is not dtype:
         raise ValueError(f"{name}: {tuple(shape)} {dtype} is wanted, got {tuple(t.shape)} {t.dtype}")
     if not t.is_cuda:
         raise ValueError("tensors passed to the library must live on the GPU")
-    want = [ld, shape[-1], 1] if len(shape) == 3 else [shape[1] * ld, ld, shape[-1], 1]
-    if any(s != w and n > 1 for s, w, n in zip(t.stride(), want, shape)):
-        raise ValueError(f"{name}: strides {tuple(t.stride())}, {tuple(want)} are wanted "
-                         f"(tokens {ld} elements apart)")
+
+
+def _want(t, name: str, shape: tuple, dtype, optional: bool = False):
+    """Address of a contiguous tensor whose shape and type are what the call says."""
+    if t is None and optional:
+        return None
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
+        _refuse(t, name, shape, dtype)
+    if not t.is_contiguous():
+        raise ValueError("tensors passed to the library must be contiguous")
     return t.data_ptr()
 
 
-_TORCH = {"f32": "float32", "bf16": "bfloat16"}
+def _tokens(t, name: str, shape: tuple, ld: int, dtype):
+    """Address of a token array ([T, B, heads, size] or [B, heads, size]) whose
+    tokens are ld elements apart."""
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
+        _refuse(t, name, shape, dtype)
+    want = (ld, shape[-1], 1) if len(shape) == 3 else (shape[1] * ld, ld, shape[-1], 1)
+    if t.stride() != want and any(s != w and n > 1 for s, w, n in zip(t.stride(), want, shape)):
+        raise ValueError(f"{name}: strides {tuple(t.stride())}, {want} are wanted "
+                         f"(tokens {ld} elements apart)")
+    return t.data_ptr()
 
 
 class _OpPlan:
@@ -461,6 +470,7 @@ class DeltaPlan(_OpPlan):
         self.desc = d = make_delta_desc(T_max, B, Hk, Hv, Dk, Dv, dtype, inference, q_ld, k_ld,
                                         v_ld, dq_ld, dk_ld, dv_ld, scale)
         self.dtype = dtype
+        self._t = _dtype(dtype)
         self._create("ll_delta_plan_create", d, device)
         qk, v = Hk * Dk, Hv * Dv
         self._ld = dict(q=q_ld or qk, k=k_ld or qk, v=v_ld or v, dq=dq_ld or qk, dk=dk_ld or qk,
@@ -469,35 +479,35 @@ class DeltaPlan(_OpPlan):
         self._gate, self._state = (T_max, B, Hv), (B, Hv, Dk, Dv)
 
     def _inputs(self, q, k, v, g, beta, seq_len):
-        t = _TORCH[self.dtype]
+        t, f = self._t, _dtype("float32")
         return (_tokens(q, "q", self._qk, self._ld["q"], t),
                 _tokens(k, "k", self._qk, self._ld["k"], t),
                 _tokens(v, "v", self._v, self._ld["v"], t),
-                _want(g, "g", self._gate, "float32"), _want(beta, "beta", self._gate, "float32"),
-                _want(seq_len, "seq_len", self._qk[1:2], "int32", optional=True))
+                _want(g, "g", self._gate, f), _want(beta, "beta", self._gate, f),
+                _want(seq_len, "seq_len", self._qk[1:2], _dtype("int32"), optional=True))
 
     def fwd(self, q, k, v, g, beta, seq_len, S0, y, ST, save_for_backward: bool = True,
             stream=None) -> None:
         """delta_loop_fwd (asynchronous on `stream`, default: torch's current)."""
+        f = _dtype("float32")
         _check(self._lib.delta_loop_fwd(
             self._h, _stream(stream), *self._inputs(q, k, v, g, beta, seq_len),
-            _want(S0, "S0", self._state, "float32", optional=True),
-            _want(y, "y", self._v, _TORCH[self.dtype]),
-            _want(ST, "ST", self._state, "float32", optional=True), 1 if save_for_backward else 0))
+            _want(S0, "S0", self._state, f, optional=True), _want(y, "y", self._v, self._t),
+            _want(ST, "ST", self._state, f, optional=True), 1 if save_for_backward else 0))
 
     def bwd(self, q, k, v, g, beta, seq_len, dy, dST, dq, dk, dv, dg, dbeta, dS0=None,
             stream=None) -> None:
         """delta_loop_bwd (asynchronous on `stream`); q .. seq_len are the
         tensors the saved forward was given."""
-        t = _TORCH[self.dtype]
+        t, f = self._t, _dtype("float32")
         _check(self._lib.delta_loop_bwd(
             self._h, _stream(stream), *self._inputs(q, k, v, g, beta, seq_len),
-            _want(dy, "dy", self._v, t), _want(dST, "dST", self._state, "float32", optional=True),
+            _want(dy, "dy", self._v, t), _want(dST, "dST", self._state, f, optional=True),
             _tokens(dq, "dq", self._qk, self._ld["dq"], t),
             _tokens(dk, "dk", self._qk, self._ld["dk"], t),
             _tokens(dv, "dv", self._v, self._ld["dv"], t),
-            _want(dg, "dg", self._gate, "float32"), _want(dbeta, "dbeta", self._gate, "float32"),
-            _want(dS0, "dS0", self._state, "float32", optional=True)))
+            _want(dg, "dg", self._gate, f), _want(dbeta, "dbeta", self._gate, f),
+            _want(dS0, "dS0", self._state, f, optional=True)))
 
     def bytes(self) -> int:
         """ll_delta_plan_bytes: device memory that the plan holds."""
@@ -523,20 +533,29 @@ def delta_loop_step(q, k, v, g, beta, S, y, slots=None, scale: float = 0.0, devi
     """delta_loop_step: one token for the B rows of q [B, Hk, Dk], k, v [B, Hv, Dv]
     (rows may be slices of a projection's), states S [n_slots, Hv, Dk, Dv]
     updated in place (asynchronous on `stream`)."""
-    (B, Hk, Dk), (Hv, Dv) = q.shape, v.shape[1:]
-    dtype = _op_name(q.dtype)
-    if dtype not in _TORCH:
-        raise ValueError(f"q: float32 or bfloat16 is wanted, got {q.dtype}")
-    t = _TORCH[dtype]
-    ld = [a.stride(0) if B > 1 else a.shape[1] * a.shape[2] for a in (q, k, v)]
-    desc = make_delta_desc(1, B, Hk, Hv, Dk, Dv, dtype, True, *ld, scale=scale)
+    (B, Hk, Dk), (_, Hv, Dv) = q.shape, v.shape
+    t, f = q.dtype, _dtype("float32")
+    lq, lk, lv = (q.stride(0), k.stride(0), v.stride(0)) if B > 1 else (Hk * Dk, Hk * Dk, Hv * Dv)
+    if t is f:
+        name = "f32"
+    elif t is _dtype("bfloat16"):
+        name = "bf16"
+    else:
+        raise ValueError(f"q: float32 or bfloat16 is wanted, got {t}")
     _check(load_library().delta_loop_step(
-        ctypes.byref(desc), _stream(stream), _tokens(q, "q", (B, Hk, Dk), ld[0], t),
-        _tokens(k, "k", (B, Hk, Dk), ld[1], t), _tokens(v, "v", (B, Hv, Dv), ld[2], t),
-        _want(g, "g", (B, Hv), "float32"), _want(beta, "beta", (B, Hv), "float32"),
-        _want(S, "S", (S.shape[0], Hv, Dk, Dv), "float32"),
-        _want(slots, "slots", (B,), "int32", optional=True), S.shape[0],
-        _want(y, "y", (B, Hv, Dv), t), _want(device_error, "device_error", (1,), "int32", optional=True)))
+        _step_desc(B, Hk, Hv, Dk, Dv, name, lq, lk, lv, scale), _stream(stream),
+        _tokens(q, "q", (B, Hk, Dk), lq, t), _tokens(k, "k", (B, Hk, Dk), lk, t),
+        _tokens(v, "v", (B, Hv, Dv), lv, t), _want(g, "g", (B, Hv), f),
+        _want(beta, "beta", (B, Hv), f), _want(S, "S", (S.shape[0], Hv, Dk, Dv), f),
+        _want(slots, "slots", (B,), _dtype("int32"), optional=True), S.shape[0],
+        _want(y, "y", (B, Hv, Dv), t),
+        _want(device_error, "device_error", (1,), _dtype("int32"), optional=True)))
+
+
+@functools.lru_cache(maxsize=256)
+def _step_desc(B, Hk, Hv, Dk, Dv, dtype, q_ld, k_ld, v_ld, scale):
+    return ctypes.byref(make_delta_desc(1, B, Hk, Hv, Dk, Dv, dtype, True, q_ld, k_ld, v_ld,
+                                        scale=scale))
 
 
 class LogprobPlan(_OpPlan):
@@ -548,17 +567,19 @@ class LogprobPlan(_OpPlan):
     def __init__(self, N: int, V: int, dtype: str = "f32", top_k: int = 0, ld: int = 0,
                  device: int = 0):
         d = ll_logprob_desc(N, V, LL_BF16 if dtype == "bf16" else LL_F32, top_k, ld)
-        if dtype not in _TORCH:
+        if dtype not in ("f32", "bf16"):
             raise ValueError(f"dtype {dtype!r} is neither 'f32' nor 'bf16'")
         self.desc, self.dtype, self.top_k, self.V = d, dtype, top_k, V
+        self._t = _dtype(dtype)
         self.ld = ld or V
         self._create("ll_logprob_plan_create", d, device)
 
     def _rows(self, x, name: str, n: int):
-        if (tuple(x.shape) != (n, self.V) or str(x.dtype) != "torch." + _TORCH[self.dtype]
-                or (self.V > 1 and x.stride(1) != 1) or (n > 1 and x.stride(0) != self.ld)):
-            raise ValueError(f"{name}: [rows, {self.V}] {_TORCH[self.dtype]} with rows {self.ld} apart "
-                             f"is wanted, got {tuple(x.shape)} {x.dtype} strides {tuple(x.stride())}")
+        sh, st = x.shape, x.stride()
+        if (sh != (n, self.V) or x.dtype is not self._t or (self.V > 1 and st[1] != 1)
+                or (n > 1 and st[0] != self.ld)):
+            raise ValueError(f"{name}: [rows, {self.V}] {self._t} with rows {self.ld} apart is "
+                             f"wanted, got {tuple(sh)} {x.dtype} strides {tuple(st)}")
         if not x.is_cuda:
             raise ValueError("tensors passed to the library must live on the GPU")
         return x.data_ptr()
@@ -566,43 +587,43 @@ class LogprobPlan(_OpPlan):
     def fwd(self, logits, targets, logp, entropy=None, lse=None, top_ids=None, top_logp=None,
             stream=None) -> None:
         """ll_logprob_fwd (asynchronous on `stream`)."""
-        n = logits.shape[0]
+        n, f = logits.shape[0], _dtype("float32")
         _check(self._lib.ll_logprob_fwd(
             self._h, _stream(stream), n, self._rows(logits, "logits", n),
-            _want(targets, "targets", (n,), "int32", optional=True),
-            _want(logp, "logp", (n,), "float32", optional=True),
-            _want(entropy, "entropy", (n,), "float32", optional=True),
-            _want(lse, "lse", (n,), "float32", optional=True),
-            _want(top_ids, "top_ids", (n, self.top_k), "int32", optional=True),
-            _want(top_logp, "top_logp", (n, self.top_k), "float32", optional=True)))
+            _want(targets, "targets", (n,), _dtype("int32"), optional=True),
+            _want(logp, "logp", (n,), f, optional=True),
+            _want(entropy, "entropy", (n,), f, optional=True),
+            _want(lse, "lse", (n,), f, optional=True),
+            _want(top_ids, "top_ids", (n, self.top_k), _dtype("int32"), optional=True),
+            _want(top_logp, "top_logp", (n, self.top_k), f, optional=True)))
 
     def bwd(self, logits, targets, lse, entropy, top_ids, dlogp, dentropy, dtop, dlogits,
             stream=None) -> None:
         """ll_logprob_bwd (asynchronous on `stream`); dlogits may be logits."""
-        n = logits.shape[0]
+        n, f = logits.shape[0], _dtype("float32")
         _check(self._lib.ll_logprob_bwd(
             self._h, _stream(stream), n, self._rows(logits, "logits", n),
-            _want(targets, "targets", (n,), "int32", optional=True),
-            _want(lse, "lse", (n,), "float32"),
-            _want(entropy, "entropy", (n,), "float32", optional=True),
-            _want(top_ids, "top_ids", (n, self.top_k), "int32", optional=True),
-            _want(dlogp, "dlogp", (n,), "float32", optional=True),
-            _want(dentropy, "dentropy", (n,), "float32", optional=True),
-            _want(dtop, "dtop", (n, self.top_k), "float32", optional=True),
+            _want(targets, "targets", (n,), _dtype("int32"), optional=True),
+            _want(lse, "lse", (n,), f),
+            _want(entropy, "entropy", (n,), f, optional=True),
+            _want(top_ids, "top_ids", (n, self.top_k), _dtype("int32"), optional=True),
+            _want(dlogp, "dlogp", (n,), f, optional=True),
+            _want(dentropy, "dentropy", (n,), f, optional=True),
+            _want(dtop, "dtop", (n, self.top_k), f, optional=True),
             self._rows(dlogits, "dlogits", n)))
 
     def fwd_bwd(self, logits, targets, dlogp, dentropy, logp, entropy, lse, dlogits,
                 stream=None) -> None:
         """ll_logprob_fwd_bwd (asynchronous on `stream`); dlogits may be logits."""
-        n = logits.shape[0]
+        n, f = logits.shape[0], _dtype("float32")
         _check(self._lib.ll_logprob_fwd_bwd(
             self._h, _stream(stream), n, self._rows(logits, "logits", n),
-            _want(targets, "targets", (n,), "int32", optional=True),
-            _want(dlogp, "dlogp", (n,), "float32", optional=True),
-            _want(dentropy, "dentropy", (n,), "float32", optional=True),
-            _want(logp, "logp", (n,), "float32", optional=True),
-            _want(entropy, "entropy", (n,), "float32", optional=True),
-            _want(lse, "lse", (n,), "float32", optional=True),
+            _want(targets, "targets", (n,), _dtype("int32"), optional=True),
+            _want(dlogp, "dlogp", (n,), f, optional=True),
+            _want(dentropy, "dentropy", (n,), f, optional=True),
+            _want(logp, "logp", (n,), f, optional=True),
+            _want(entropy, "entropy", (n,), f, optional=True),
+            _want(lse, "lse", (n,), f, optional=True),
             self._rows(dlogits, "dlogits", n)))
 
     def status_sync(self) -> int:
@@ -625,7 +646,7 @@ class AdamWPlan(_OpPlan):
                  copies=None, weight_decay=0.0, grad_dtype: str = "f32", device: int = 0):
         n = len(params)
         q8 = m_scale is not None
-        if grad_dtype not in _TORCH:
+        if grad_dtype not in ("f32", "bf16"):
             raise ValueError(f"grad_dtype {grad_dtype!r} is neither 'f32' nor 'bf16'")
         if q8 != (v_scale is not None):
             raise ValueError("m_scale and v_scale go together")
@@ -636,20 +657,20 @@ class AdamWPlan(_OpPlan):
         if any(len(x) != n for x in lists):
             raise ValueError(f"{n} params, but lists of {[len(x) for x in lists]} for them")
         recs = (ll_adamw_tensor * n)()
-        mt, vt = ("int8", "uint8") if q8 else ("float32", "float32")
+        f = _dtype("float32")
+        mt, vt = (_dtype("int8"), _dtype("uint8")) if q8 else (f, f)
         for i, p in enumerate(params):
             shape, rows = tuple(p.shape), (-(-p.numel() // ADAMW_ROW),)
             recs[i] = ll_adamw_tensor(
-                _want(p, f"params[{i}]", shape, "float32"),
-                _want(copies[i] if copies is not None else None, f"copies[{i}]", shape, "bfloat16",
+                _want(p, f"params[{i}]", shape, f),
+                _want(copies[i] if copies is not None else None, f"copies[{i}]", shape, _dtype("bfloat16"),
                       optional=True),
                 _want(m[i], f"m[{i}]", shape, mt), _want(v[i], f"v[{i}]", shape, vt),
-                _want(m_scale[i], f"m_scale[{i}]", rows, "float32") if q8 else None,
-                _want(v_scale[i], f"v_scale[{i}]", rows, "float32") if q8 else None,
+                _want(m_scale[i], f"m_scale[{i}]", rows, f) if q8 else None,
+                _want(v_scale[i], f"v_scale[{i}]", rows, f) if q8 else None,
                 p.numel(), wd[i], 0)
         self._keep = (list(params), list(m), list(v), m_scale, v_scale, copies)
-        import torch
-        self._grad_type = getattr(torch, _TORCH[grad_dtype])
+        self._grad_type = _dtype(grad_dtype)
         self._sizes = [p.numel() for p in params]
         self._ptrs = (ctypes.c_void_p * n)()
         desc = ll_adamw_desc(n, 8 if q8 else 32, LL_BF16 if grad_dtype == "bf16" else LL_F32, 0)
@@ -673,4 +694,4 @@ class AdamWPlan(_OpPlan):
         hyper = ll_adamw_hyper(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFF, 0)
         _check(self._lib.ll_adamw_step(
             self._h, _stream(stream), self._ptrs, ctypes.byref(hyper),
-            _want(grad_scale, "grad_scale", (1,), "float32", optional=True)))
+            _want(grad_scale, "grad_scale", (1,), _dtype("float32"), optional=True)))
