@@ -308,26 +308,29 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
     const long at = item * 3 * SQ + (long)f * 3 * 512 + 8 * l;
     float x[8];
     uint4 p[3];
-    auto put = [&](bf16_t* dst, int n) {
-      for (int e = 0; e < n; ++e) *reinterpret_cast<uint4*>(dst + at + e * 512) = p[e];
+    // (the fragments right of a lower and left of an upper triangle are never read)
+    const bool low = f % 2 == 0 || f / 2 >= 2, up = f % 2 == 1 || f / 2 < 2;
+    auto put = [&](bf16_t* dst, int n, bool some) {
+      if (some)
+        for (int e = 0; e < n; ++e) *reinterpret_cast<uint4*>(dst + at + e * 512) = p[e];
     };
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = tm[r * SC + j + e];
     split8<3>(x, p);
-    put(a.tp, 3);
+    put(a.tp, 3, low);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = pm[r * SC + j + e];
     split8<PP>(x, p);
-    put(a.pp, PP);
+    put(a.pp, PP, low);
     if (SAVE) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = tm[(j + e) * SC + r];
       split8<3>(x, p);
-      put(a.ttp, 3);
+      put(a.ttp, 3, up);
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = pm[(j + e) * SC + r];
       split8<3>(x, p);
-      put(a.ptp, 3);
+      put(a.ptp, 3, up);
     }
   }
 }

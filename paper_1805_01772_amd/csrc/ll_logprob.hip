@@ -44,6 +44,7 @@ struct LogprobArgs {
   const float *lse_in, *ent_in, *dlogp, *dentropy, *dtop;
   const int* ids_in;
   void* dx;
+  bool stream;                         // dx goes past the caches
   int* err;
   // rows split over work-groups: m, s, t per part, its keys, arrivals per row
   float4* part;
@@ -518,7 +519,8 @@ __device__ void row_gradient(const LogprobArgs& a, const T* row, T* out, long r,
     unpack<T>(u, f);
 #pragma unroll
     for (int e = 0; e < E; ++e) f[e] = grad(f[e]);
-    *reinterpret_cast<uint4*>(out + sp.head + (long)k * E) = pack<T>(f);
+    if (a.stream) st16_stream(out + sp.head + (long)k * E, pack<T>(f));
+    else *reinterpret_cast<uint4*>(out + sp.head + (long)k * E) = pack<T>(f);
   };
   // last chunks first: read most recently, they are the nearest still; the
   // thread's first KEEP chunks are in LDS
@@ -589,14 +591,18 @@ struct ll_logprob_plan {
 
 namespace {
 
+long row_bytes(const ll_logprob_plan* p) { return (long)p->d.V * (p->d.dtype == LL_BF16 ? 2 : 4); }
+
 // Work-groups per row: enough to fill the chip where the rows alone do not,
-// each with at least 256 KiB of its row (one work-group reads that in about the
-// time that the join takes).
-int parts_of(const ll_logprob_plan* p, int rows) {
-  const long bytes = (long)p->d.V * (p->d.dtype == LL_BF16 ? 2 : 4);
+// each with at least `least` bytes of its row.
+int parts_of(const ll_logprob_plan* p, int rows, long least) {
   const long want = (p->cus + rows - 1) / rows;
-  return (int)std::max(1L, std::min({want, bytes >> 18, (long)ll::kPartsMax}));
+  return (int)std::max(1L, std::min({want, row_bytes(p) / least, (long)ll::kPartsMax}));
 }
+
+// A gradient larger than the last-level cache goes past it (4096 x 131072
+// bfloat16: 478 -> 447 us in the call that makes both).
+bool past_caches(const ll_logprob_plan* p, int rows) { return row_bytes(p) * rows > ll::kLastLevelBytes; }
 
 void release(ll_logprob_plan* p) {
   void* all[] = {p->a.part, p->a.keys, p->a.arrived, p->a.err};
@@ -698,7 +704,8 @@ ll_status ll_logprob_fwd(ll_logprob_plan* p, void* stream, int32_t rows, const v
   ll::LogprobArgs a = p->a;
   a.x = logits; a.targets = targets; a.logp = logp; a.entropy = entropy; a.lse = lse;
   a.top_ids = top_ids; a.top_logp = top_logp;
-  a.parts = parts_of(p, rows);
+  // (one work-group reads 256 KiB in about the time that a join takes)
+  a.parts = parts_of(p, rows, 256 << 10);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const bool wide = (long)rows * a.parts <= 2L * p->cus;
   if (p->d.dtype == LL_BF16) launch_fwd<bf16_t>(a, rows, wide, s);
@@ -722,7 +729,8 @@ ll_status ll_logprob_bwd(ll_logprob_plan* p, void* stream, int32_t rows, const v
   ll::LogprobArgs a = p->a;
   a.x = logits; a.targets = targets; a.lse_in = lse; a.ent_in = entropy; a.ids_in = top_ids;
   a.dlogp = dlogp; a.dentropy = dentropy; a.dtop = dtop; a.dx = dlogits;
-  a.parts = parts_of(p, rows);
+  a.parts = parts_of(p, rows, 16 << 10);
+  a.stream = past_caches(p, rows);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const dim3 grid((unsigned)(rows * a.parts));
   if (p->d.dtype == LL_BF16) ll::logprob_bwd_kernel<bf16_t, 256><<<grid, dim3(256), 0, s>>>(a);
@@ -746,8 +754,9 @@ ll_status ll_logprob_fwd_bwd(ll_logprob_plan* p, void* stream, int32_t rows, con
   a.x = logits; a.targets = targets; a.dlogp = dlogp; a.dentropy = dentropy; a.logp = logp;
   a.entropy = entropy; a.lse = lse; a.dx = dlogits;
   a.parts = 1;
+  a.stream = past_caches(p, rows);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  const bool wide = (long)p->d.V * (p->d.dtype == LL_BF16 ? 2 : 4) >= 64 << 10;
+  const bool wide = row_bytes(p) >= 64 << 10;
   if (p->d.dtype == LL_BF16) {
     if (wide) ll::logprob_fwd_bwd_kernel<bf16_t, 1024, 4><<<dim3(rows), dim3(1024), 0, s>>>(a);
     else ll::logprob_fwd_bwd_kernel<bf16_t, 256, 4><<<dim3(rows), dim3(256), 0, s>>>(a);
