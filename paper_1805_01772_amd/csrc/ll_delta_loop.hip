@@ -920,30 +920,32 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
 
 // ---------------------------------------------------------------------------
 // grads: one work-group of eight waves per item of a key head; wave = 16 of the 64
-// tokens x half of the columns.  The value columns are walked 32 at a
-// time: dY, U, dR and the two states go through LDS in pieces (loaded a step
-// ahead into registers), F, H and the three products with the states stay in
-// accumulators.  The value heads of a key head follow one another, so dQ and dK
-// are summed in a fixed order.
+// tokens x half of the columns.  The value columns are walked 32 at a time, the
+// states' rows 64 at a time within: dY, U, dR and the two states go through LDS
+// in pieces.  A step's products read one of two buffers while the next step is
+// split into the other and the one after it is on its way into registers.  F, H
+// and the three products with the states stay in accumulators.  The value heads
+// of a key head follow one another, so dQ and dK are summed in a fixed order.
 // ---------------------------------------------------------------------------
 template <typename T, int KS>
 __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
   constexpr int NP = Pieces<T>::n, XP = NP == 1 ? 2 : 3;   // XP pieces where the result is only dK
-  constexpr int DP = 32 * KS, NC = 32, CP = NC + 8, NDT = DP / 16, ND = NDT / 2;
-  constexpr int kWalk = (NP * CT + 3 * CT + XP * CT + 6 * DP) * CP, kSq = (3 + XP + XP) * CT * RC;
-  constexpr int kLoads = KS > 2 ? KS : 2;                  // float4 pairs a thread loads a step
-  __shared__ __align__(16) bf16_t pool[kWalk > kSq ? kWalk : kSq];
+  constexpr int DP = 32 * KS, NC = 32, CP = NC + 8, ND = DP / 32;
+  constexpr int TPS = ND < 2 ? ND : 2, HS = ND / TPS, DR = 32 * TPS;   // column tiles of a wave, row halves, rows a step
+  constexpr int kTok = (NP + 3 + XP) * CT * CP, kState = 6 * DR * CP, kSq = (3 + XP + XP) * CT * RC;
+  constexpr int kPool = 2 * (kTok + kState);
+  __shared__ __align__(16) bf16_t pool[kPool > kSq ? kPool : kSq];
   __shared__ float4 tok[CT];
   __shared__ double G[CT];
   __shared__ float dG[2][CT], part[8], sub[CT], sbeta[CT];
-  bf16_t* Yp = pool;                   // [NP][64][CP] dY
-  bf16_t* Up = Yp + NP * CT * CP;      // [3][64][CP]
-  bf16_t* Rp = Up + 3 * CT * CP;       // [XP][64][CP] dR
-  bf16_t* Sp = Rp + XP * CT * CP;      // [3][DP][CP]
-  bf16_t* Dp = Sp + 3 * DP * CP;       // [3][DP][CP] dS
+  // tokens' buffer: dY [NP][64][CP], U [3][64][CP], dR [XP][64][CP]; states': S
+  // [3][DR][CP], dS [3][DR][CP]
+  constexpr int kU = NP * CT * CP, kR = kU + 3 * CT * CP, kD = 3 * DR * CP;
   bf16_t* Fp = pool;                   // [3][64][RC] F, rows i          (after the walk)
   bf16_t* Ft = Fp + 3 * CT * RC;       // [XP][64][RC] F^T
   bf16_t* Hp = Ft + XP * CT * RC;      // [XP][64][RC] H + H^T
+  // the wave's column tile i of the results
+  auto tile = [](int i, int half) { return i / TPS * 2 * TPS + half * TPS + i % TPS; };
   const int n = blockIdx.x % a.nch, bk = blockIdx.x / a.nch;
   const int b = bk / a.Hk, hk = bk % a.Hk, grp = a.Hv / a.Hk;
   const int len = delta_len(a, b), t0 = n * CT;
@@ -979,53 +981,45 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
 #pragma unroll
     for (int e = 0; e < NP; ++e) {
       const uint2 u = __builtin_bit_cast(
-          uint2, __builtin_amdgcn_raw_buffer_load_b64(r, kq, frag_at(half * ND + i, w >> 1, e, 2, NP) * 2, 0));
+          uint2, __builtin_amdgcn_raw_buffer_load_b64(r, kq, frag_at(tile(i, half), w >> 1, e, 2, NP) * 2, 0));
       v += f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
                  __uint_as_float(u.y & 0xffff0000u)};
     }
     return v;
   };
-  // loads of a step: waves 0-3 four columns of two tokens a lane, the others
-  // four columns of KS rows of the states (descriptors as in the loops: uniform
-  // bases, so that few addresses live in registers)
-  const bool tokens = wave < 4;
-  const int row = (tid & 255) >> 3, rc = (tid & 7) * 4;
+  // loads of a step, four columns a thread: a row of each state and, with the
+  // first rows, a token (descriptors as in the loops: uniform bases, so that few
+  // addresses live in registers)
+  const int row = tid >> 3, rc = (tid & 7) * 4;
   const long yrow = (long)a.B * a.Hv * a.Dv, vrow = (long)a.B * a.v_ld;
   struct alignas(4 * sizeof(T)) Four { T x[4]; };
-  f32x4 x0[kLoads], x1[kLoads];
-  Four fy[2], fv[2];
+  f32x4 fs, fd, fu, fr;
+  Four fy, fv;
   auto load4 = [&](rsrc_t r, unsigned off, Four& f) {
     if constexpr (NP == 1) f = __builtin_bit_cast(Four, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
     else f = __builtin_bit_cast(Four, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
   };
-  auto fetch = [&](int h, int c0) {
+  auto fetch = [&](int h, int c0, int hs) {
     const long item = ((long)b * a.Hv + h) * a.nch + n;
     const bool in = c0 + rc < a.Dv;
-    if (tokens) {
+    const rsrc_t rs = make_rsrc(a.st + item * a.Dk * a.Dv, a.Dk * a.Dv * 4), rd = make_rsrc(a.dst + item * a.Dk * a.Dv, a.Dk * a.Dv * 4);
+    const unsigned at = in && row < DR ? ((hs * DR + row) * a.Dv + c0 + rc) * 4 : kNowhere;
+    fs = __builtin_bit_cast(f32x4, bload16(rs, at));
+    fd = __builtin_bit_cast(f32x4, bload16(rd, at));
+    if (hs == 0) {
       const rsrc_t ru = make_rsrc(a.u + item * CT * a.Dv, CT * a.Dv * 4), rr = make_rsrc(a.dr + item * CT * a.Dv, CT * a.Dv * 4);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const unsigned off = in ? ((row + 32 * i) * a.Dv + c0 + rc) * 4 : kNowhere;
-        x0[i] = __builtin_bit_cast(f32x4, bload16(ru, off));
-        x1[i] = __builtin_bit_cast(f32x4, bload16(rr, off));
-        const int r0 = 8 * wave + 32 * i, tv = min(8, len - t0 - r0);   // the wave's first row, its tokens
-        const long tok0 = (long)(t0 + r0) * a.B + b;
-        const rsrc_t ry = rows_rsrc(static_cast<const T*>(a.dy) + (tok0 * a.Hv + h) * a.Dv, tv, yrow, a.Dv);
-        const rsrc_t rv = rows_rsrc(static_cast<const T*>(a.v) + tok0 * a.v_ld + (long)h * a.Dv, tv, vrow, a.Dv);
-        load4(ry, in ? (unsigned)(((row & 7) * yrow + c0 + rc) * (long)sizeof(T)) : kNowhere, fy[i]);
-        load4(rv, in ? (unsigned)(((row & 7) * vrow + c0 + rc) * (long)sizeof(T)) : kNowhere, fv[i]);
-      }
-    } else {
-      const rsrc_t rs = make_rsrc(a.st + item * a.Dk * a.Dv, a.Dk * a.Dv * 4), rd = make_rsrc(a.dst + item * a.Dk * a.Dv, a.Dk * a.Dv * 4);
-#pragma unroll
-      for (int i = 0; i < KS; ++i) {
-        const unsigned off = in ? ((row + 32 * i) * a.Dv + c0 + rc) * 4 : kNowhere;
-        x0[i] = __builtin_bit_cast(f32x4, bload16(rs, off));
-        x1[i] = __builtin_bit_cast(f32x4, bload16(rd, off));
-      }
+      const unsigned off = in ? (row * a.Dv + c0 + rc) * 4 : kNowhere;
+      fu = __builtin_bit_cast(f32x4, bload16(ru, off));
+      fr = __builtin_bit_cast(f32x4, bload16(rr, off));
+      const int tv = min(8, len - t0 - 8 * wave);          // the wave's eight rows: its tokens
+      const long tok0 = (long)(t0 + 8 * wave) * a.B + b;
+      const rsrc_t ry = rows_rsrc(static_cast<const T*>(a.dy) + (tok0 * a.Hv + h) * a.Dv, tv, yrow, a.Dv);
+      const rsrc_t rv = rows_rsrc(static_cast<const T*>(a.v) + tok0 * a.v_ld + (long)h * a.Dv, tv, vrow, a.Dv);
+      load4(ry, in ? (unsigned)(((row & 7) * yrow + c0 + rc) * (long)sizeof(T)) : kNowhere, fy);
+      load4(rv, in ? (unsigned)(((row & 7) * vrow + c0 + rc) * (long)sizeof(T)) : kNowhere, fv);
     }
   };
-  fetch(hk * grp, 0);
+  fetch(hk * grp, 0, 0);
   for (int hh = 0; hh < grp; ++hh) {
     const int h = hk * grp + hh;
     const long item = ((long)b * a.Hv + h) * a.nch + n;
@@ -1033,72 +1027,90 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
 #pragma unroll
     for (int i = 0; i < ND; ++i) aq[i] = ku[i] = kr[i] = zero_acc();
     F[0] = F[1] = H[0] = H[1] = zero_acc();
-    float ss = 0.f, ub[2] = {0.f, 0.f}, vr[2] = {0.f, 0.f};
-    for (int c0 = 0; c0 < a.Dv; c0 += NC) {
-      __syncthreads();
-      if (c0 == 0 && tid < CT) {
-        tok[tid] = a.tok[item * CT + tid];
-        G[tid] = a.G[item * CT + tid];
+    float ss = 0.f, ub = 0.f, vr = 0.f;
+    // the fetched step into the buffers (cb: of the tokens, sb: of the states)
+    auto split = [&](int hs, int cb, int sb) {
+      bf16_t* S = pool + 2 * kTok + sb * kState;
+      if (row < DR) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ss += fs[e] * fd[e];
+        split4_store<3>(fs, S + row * CP + rc, DR * CP);
+        split4_store<3>(fd, S + kD + row * CP + rc, DR * CP);
       }
-      if (tokens) {
+      if (hs == 0) {
+        bf16_t* X = pool + cb * kTok;
+        f32x4 y;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int r = row + 32 * i;
-          f32x4 y;
+        for (int e = 0; e < 4; ++e) {
+          y[e] = Op<T>::to_f32(fy.x[e]);
+          ub += fr[e] * fu[e];
+          vr += fr[e] * Op<T>::to_f32(fv.x[e]);
+        }
+        split4_store<NP>(y, X + row * CP + rc, CT * CP);
+        split4_store<3>(fu, X + kU + row * CP + rc, CT * CP);
+        split4_store<XP>(fr, X + kR + row * CP + rc, CT * CP);
+      }
+    };
+    __syncthreads();
+    if (tid < CT) {
+      tok[tid] = a.tok[item * CT + tid];
+      G[tid] = a.G[item * CT + tid];
+    }
+    split(0, 0, 0);
+    if (HS > 1) fetch(h, 0, 1);
+    else if (NC < a.Dv) fetch(h, NC, 0);
+    else if (hh + 1 < grp) fetch(h + 1, 0, 0);
+    for (int ct = 0; ct * NC < a.Dv; ++ct) {
+      const int c0 = ct * NC;
+      const bool more = c0 + NC < a.Dv;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            y[e] = Op<T>::to_f32(fy[i].x[e]);
-            ub[i] += x1[i][e] * x0[i][e];
-            vr[i] += x1[i][e] * Op<T>::to_f32(fv[i].x[e]);
+      for (int hs = 0; hs < HS; ++hs) {
+        const int sb = HS == 2 ? hs : ct & 1, cb = ct & 1;
+        __syncthreads();
+        // the next step's pieces, the loads of the one after it
+        if (hs + 1 < HS) {
+          split(1, cb, 1 - sb);
+          if (more) fetch(h, c0 + NC, 0);
+          else if (hh + 1 < grp) fetch(h + 1, 0, 0);
+        } else if (more) {
+          split(0, 1 - cb, 1 - sb);
+          if (HS == 2) fetch(h, c0 + NC, 1);
+          else if (c0 + 2 * NC < a.Dv) fetch(h, c0 + 2 * NC, 0);
+          else if (hh + 1 < grp) fetch(h + 1, 0, 0);
+        }
+        const bf16_t* X = pool + cb * kTok + (16 * w + lo_) * CP + 8 * hi_;
+        const bf16_t* S = pool + 2 * kTok + sb * kState + lo_ * CP + 8 * hi_;
+        frag ya[NP], ua[3], ra[XP];
+#pragma unroll
+        for (int e = 0; e < NP; ++e) ya[e] = lds_frag(X + e * CT * CP);
+#pragma unroll
+        for (int e = 0; e < 3; ++e) ua[e] = lds_frag(X + kU + e * CT * CP);
+#pragma unroll
+        for (int e = 0; e < XP; ++e) ra[e] = lds_frag(X + kR + e * CT * CP);
+        if (hs == 0) {
+#pragma unroll
+          for (int m = 0; m < 2; ++m) {
+            const int j = 2 * half + m;
+            if (j <= w) {
+              frag un[3];
+#pragma unroll
+              for (int e = 0; e < 3; ++e) un[e] = lds_frag(pool + cb * kTok + kU + (e * CT + 16 * j + lo_) * CP + 8 * hi_);
+              mma<NP, 3, 2>(ya, un, F[m]);
+              mma<XP, XP, XP - 1>(ra, un, H[m]);
+            }
           }
-          split4_store<NP>(y, Yp + r * CP + rc, CT * CP);
-          split4_store<3>(x0[i], Up + r * CP + rc, CT * CP);
-          split4_store<XP>(x1[i], Rp + r * CP + rc, CT * CP);
         }
-      } else {
 #pragma unroll
-        for (int i = 0; i < KS; ++i) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) ss += x0[i][e] * x1[i][e];
-          split4_store<3>(x0[i], Sp + (row + 32 * i) * CP + rc, DP * CP);
-          split4_store<3>(x1[i], Dp + (row + 32 * i) * CP + rc, DP * CP);
-        }
-      }
-      __syncthreads();
-      if (c0 + NC < a.Dv) fetch(h, c0 + NC);
-      else if (hh + 1 < grp) fetch(h + 1, 0);
-      const int lo = lo_, hi = hi_, arow = 16 * w + lo;
-      frag ya[NP], ua[3], ra[XP];
-#pragma unroll
-      for (int e = 0; e < NP; ++e) ya[e] = lds_frag(Yp + (e * CT + arow) * CP + 8 * hi);
-#pragma unroll
-      for (int e = 0; e < 3; ++e) ua[e] = lds_frag(Up + (e * CT + arow) * CP + 8 * hi);
-#pragma unroll
-      for (int e = 0; e < XP; ++e) ra[e] = lds_frag(Rp + (e * CT + arow) * CP + 8 * hi);
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const int j = 2 * half + m;
-        if (j <= w) {
-          frag un[3];
-#pragma unroll
-          for (int e = 0; e < 3; ++e) un[e] = lds_frag(Up + (e * CT + 16 * j + lo) * CP + 8 * hi);
-          mma<NP, 3, 2>(ya, un, F[m]);
-          mma<XP, XP, XP - 1>(ra, un, H[m]);
-        }
-      }
-      {
-#pragma unroll
-        for (int i = 0; i < ND; ++i) {
-          const int d = 16 * (half * ND + i) + lo;
-          frag sb[3], db[3];
+        for (int i = 0; i < TPS; ++i) {
+          frag sf[3], df[3];
 #pragma unroll
           for (int e = 0; e < 3; ++e) {
-            sb[e] = lds_frag(Sp + (e * DP + d) * CP + 8 * hi);
-            db[e] = lds_frag(Dp + (e * DP + d) * CP + 8 * hi);
+            sf[e] = lds_frag(S + (e * DR + 16 * (half * TPS + i)) * CP);
+            df[e] = lds_frag(S + kD + (e * DR + 16 * (half * TPS + i)) * CP);
           }
-          mma<NP, 3, 2>(ya, sb, aq[i]);
-          mma<3, 3, 2>(ua, db, ku[i]);
-          mma<XP, XP, XP - 1>(ra, sb, kr[i]);
+          mma<NP, 3, 2>(ya, sf, aq[hs * TPS + i]);
+          mma<3, 3, 2>(ua, df, ku[hs * TPS + i]);
+          mma<XP, XP, XP - 1>(ra, sf, kr[hs * TPS + i]);
         }
       }
     }
@@ -1109,7 +1121,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
       for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int e = 0; e < NP; ++e) {
-          const int at = frag_at(half * ND + i, s, e, 2, NP) * 2;
+          const int at = frag_at(tile(i, half), s, e, 2, NP) * 2;
           kb[i & 1][s][e] = as_frag(__builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rk, 16 * l, at, 0)));
           qb[i & 1][s][e] = as_frag(__builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rq, 16 * l, at, 0)));
         }
@@ -1183,18 +1195,13 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
     }
     for (int d = 1; d < 64; d <<= 1) ss += __shfl_xor(ss, d, 64);
     if (l == 0) part[wave] = ss;
-    if (tokens) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        for (int d = 1; d < 8; d <<= 1) {
-          ub[i] += __shfl_xor(ub[i], d, 64);
-          vr[i] += __shfl_xor(vr[i], d, 64);
-        }
-        if ((tid & 7) == 0) {
-          sub[row + 32 * i] = vr[i];
-          sbeta[row + 32 * i] = ub[i];
-        }
-      }
+    for (int d = 1; d < 8; d <<= 1) {
+      ub += __shfl_xor(ub, d, 64);
+      vr += __shfl_xor(vr, d, 64);
+    }
+    if ((tid & 7) == 0) {
+      sub[row] = vr;
+      sbeta[row] = ub;
     }
     __syncthreads();
     {
@@ -1252,7 +1259,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
   for (int i = 0; i < ND; ++i)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int t = t0 + crow + r, c = 16 * (half * ND + i) + lo;
+      const int t = t0 + crow + r, c = 16 * tile(i, half) + lo;
       if (t < a.T && c < a.Dk) {
         const long at = (long)t * a.B + b;
         dq[at * a.dq_ld + (long)hk * a.Dk + c] = Op<T>::from_f32(t < len ? tq[i][r] : 0.f);
