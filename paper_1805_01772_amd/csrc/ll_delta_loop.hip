@@ -128,6 +128,14 @@ template <> struct Pieces<bf16_t> { static constexpr int n = 1; };
 
 __device__ __forceinline__ frag lds_frag(const bf16_t* p) { return as_frag(ld16(p)); }
 
+// Barrier of the work-group that orders LDS only: loads and stores of global
+// memory stay in flight across it.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // LDS written by other lanes of the same wave is read next.
 __device__ __forceinline__ void wave_lds_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -203,7 +211,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
     if (SAVE) a.G[item * CT + tid] = s;
     a.tok[item * CT + tid] = make_float4(expf((float)s), expf((float)(end - s)), bt, 0.f);
   }
-  __syncthreads();
+  lds_barrier();
   f32x4 kk[4], qk[4];
 #pragma unroll
   for (int m = 0; m < 4; ++m) kk[m] = qk[m] = zero_acc();
@@ -247,7 +255,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
       if (SAVE) *reinterpret_cast<uint4*>(a.qtp + base + f * 512) = make_uint4(y[0], y[1], y[2], y[3]);
     }
   }
-  __syncthreads();
+  lds_barrier();
   float* am = reinterpret_cast<float*>(raw);
   float* pm = am + CT * SC;
 #pragma unroll
@@ -259,7 +267,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
       am[i * SC + j] = j < i ? be[i] * d * kk[m][r] : 0.f;
       pm[i * SC + j] = j <= i ? a.scale * d * qk[m][r] : 0.f;
     }
-  __syncthreads();
+  lds_barrier();
   {
     // diagonal block w: column lo by substitution, in registers
     const float* A = am + 16 * w * SC + 16 * w;
@@ -280,7 +288,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) tm[(16 * m + 4 * hi + r) * SC + 16 * w + lo] = 0.f;
   }
-  __syncthreads();
+  lds_barrier();
   for (int r = w + 1; r < 4; ++r) {
     f32x4 x = zero_acc(), z = zero_acc();
     for (int k = w; k < r; ++k)
@@ -301,7 +309,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
     for (int e = 0; e < 4; ++e) blk[(4 * hi + e) * SC + lo] = z[e];
     wave_lds_fence();
   }
-  __syncthreads();
+  lds_barrier();
   // fragments (row tile, step) of T and P and, for the gradient, the transposes
   for (int f = w; f < 8; f += 4) {
     const int r = 16 * (f / 2) + lo, j = 32 * (f % 2) + 8 * hi;
@@ -336,14 +344,6 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
 }
 
 namespace {
-
-// Barrier of the work-group that orders LDS only: loads and stores of global
-// memory stay in flight across it.
-__device__ __forceinline__ void lds_barrier() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
 
 // The loops' loads and stores go through buffer descriptors made for each
 // chunk: what lies past a row's end, past Dk or past Dv is out of the buffer's
@@ -1051,7 +1051,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
         split4_store<XP>(fr, X + kR + row * CP + rc, CT * CP);
       }
     };
-    __syncthreads();
+    lds_barrier();
     if (tid < CT) {
       tok[tid] = a.tok[item * CT + tid];
       G[tid] = a.G[item * CT + tid];
@@ -1066,7 +1066,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
 #pragma unroll
       for (int hs = 0; hs < HS; ++hs) {
         const int sb = HS == 2 ? hs : ct & 1, cb = ct & 1;
-        __syncthreads();
+        lds_barrier();
         // the next step's pieces, the loads of the one after it
         if (hs + 1 < HS) {
           split(1, cb, 1 - sb);
@@ -1131,7 +1131,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
     int lo = lo_, hi = hi_;
     asm volatile("" : "+v"(lo), "+v"(hi));
     const int arow = 16 * w + lo, crow = 16 * w + 4 * hi;
-    __syncthreads();
+    lds_barrier();
     // F, F^T and H + H^T in pieces (F_ij of tile (w, jt), jt <= w; zero above)
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
@@ -1203,7 +1203,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
       sub[row] = vr;
       sbeta[row] = ub;
     }
-    __syncthreads();
+    lds_barrier();
     {
 #pragma unroll
       for (int i = 0; i < ND; ++i) {
@@ -1237,7 +1237,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
       for (int d = 1; d < 16; d <<= 1) dots[r] += __shfl_xor(dots[r], d, 64);
       if (lo == 0) dG[half][crow + r] = dots[r];
     }
-    __syncthreads();
+    lds_barrier();
     if (tid < CT) {
       const float bt = tok[tid].z;
       if (t0 + tid < a.T)
