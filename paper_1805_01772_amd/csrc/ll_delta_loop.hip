@@ -128,6 +128,12 @@ template <> struct Pieces<bf16_t> { static constexpr int n = 1; };
 
 __device__ __forceinline__ frag lds_frag(const bf16_t* p) { return as_frag(ld16(p)); }
 
+// A fragment's read of 16 bytes a lane serves lanes 0-3, 12-15, 20-27 together
+// (4-11, 16-19, 28-31; the same from 32), each from 64 banks: rows 4-11 of every 16
+// hold their neighbouring groups of eight columns exchanged, so that with an odd
+// number of groups to a row the 16 lanes meet different banks.
+__device__ __forceinline__ int swap8(int row) { return ((row >> 2) ^ (row >> 3)) & 1 ? 8 : 0; }
+
 // Barrier of the work-group that orders LDS only: loads and stores of global
 // memory stay in flight across it.
 __device__ __forceinline__ void lds_barrier() {
@@ -489,7 +495,7 @@ struct State {
     for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int q = 0; q < NL; ++q)
-        split4_store<3>(x[m][q], Sp + (16 * q + k.lo) * KP + 16 * (k.w * MT + m) + 4 * k.hi, 16 * NL * KP);
+        split4_store<3>(x[m][q], Sp + (16 * q + k.lo) * KP + ((16 * (k.w * MT + m) + 4 * k.hi) ^ swap8(k.lo)), 16 * NL * KP);
   }
 };
 
@@ -522,7 +528,7 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
   __shared__ __align__(16) bf16_t Rp[3 * NT * RC], Up[3 * NT * RC], Uy[PP * NT * RC];
   const Walk k(a, NT);
   if (k.none) return;
-  const int lo = k.lo, hi = k.hi;
+  const int lo = k.lo, h8 = 8 * k.hi ^ swap8(k.lo), wc = k.crow ^ swap8(k.lo);   // columns read, written in LDS
   const long vrow = (long)a.B * a.v_ld, yrow = (long)a.B * a.Hv * a.Dv;
   if (threadIdx.x < 256) {
     struct Ops {
@@ -567,7 +573,7 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
 #pragma unroll
         for (int q = 0; q < NL; ++q) {
           frag sb[3], ra[NP];
-          load_b<3>(sb, Sp + (16 * q + lo) * KP + 32 * s + 8 * hi, NT * KP);
+          load_b<3>(sb, Sp + (16 * q + lo) * KP + 32 * s + h8, NT * KP);
 #pragma unroll
           for (int e = 0; e < NP; ++e) ra[e] = as_frag(o.rows[e][s]);
           mma<NP, 3, 2>(ra, sb, ks[q][s & 1]);
@@ -578,7 +584,7 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
         f32x4 rr;
 #pragma unroll
         for (int r = 0; r < 4; ++r) rr[r] = o.tok[r].z * (Op<T>::to_f32(o.v[r][q]) - o.tok[r].x * (ks[q][0][r] + ks[q][1][r]));
-        split4_store<3>(rr, Rp + (16 * q + lo) * RC + k.crow, NT * RC);
+        split4_store<3>(rr, Rp + (16 * q + lo) * RC + wc, NT * RC);
       }
       if (SAVE) S.store(k, a, a.st + item * a.Dk * a.Dv);
       lds_barrier();
@@ -589,7 +595,7 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           frag rb[3], tf[3];
-          load_b<3>(rb, Rp + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
+          load_b<3>(rb, Rp + (16 * q + lo) * RC + 32 * s + h8, NT * RC);
 #pragma unroll
           for (int e = 0; e < 3; ++e) tf[e] = as_frag(o.sq[e][s]);
           mma<3, 3, 2>(tf, rb, part[s]);
@@ -597,8 +603,8 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
         const f32x4 u = part[0] + part[1];
 #pragma unroll
         for (int r = 0; r < 4; ++r) us[r] = o.tok[r].y * u[r];
-        split4_store<3>(us, Up + (16 * q + lo) * RC + k.crow, NT * RC);
-        split4_store<PP>(u, Uy + (16 * q + lo) * RC + k.crow, NT * RC);
+        split4_store<3>(us, Up + (16 * q + lo) * RC + wc, NT * RC);
+        split4_store<PP>(u, Uy + (16 * q + lo) * RC + wc, NT * RC);
         if (SAVE) {
 #pragma unroll
           for (int r = 0; r < 4; ++r) bstore(ru, k.place<float>(q, a.Dv) + r * a.Dv * 4, u[r]);
@@ -618,7 +624,7 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
               frag ub[3], kf[NP];
-              load_b<3>(ub, Up + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
+              load_b<3>(ub, Up + (16 * q + lo) * RC + 32 * s + h8, NT * RC);
 #pragma unroll
               for (int e = 0; e < NP; ++e) kf[e] = as_frag(o.kt[e][m][s]);
               mma<NP, 3, 2>(kf, ub, S.x[m][q]);
@@ -661,7 +667,7 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
 #pragma unroll
         for (int q = 0; q < NL; ++q) {
           frag sb[PP], ra[NP];
-          load_b<PP>(sb, Sp + (16 * q + lo) * KP + 32 * s + 8 * hi, NT * KP);
+          load_b<PP>(sb, Sp + (16 * q + lo) * KP + 32 * s + h8, NT * KP);
 #pragma unroll
           for (int e = 0; e < NP; ++e) ra[e] = as_frag(o.rows[e][s]);
           mma<NP, PP, PP - 1>(ra, sb, y[q]);
@@ -681,7 +687,7 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           frag ub[PP], pf[PP];
-          load_b<PP>(ub, Uy + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
+          load_b<PP>(ub, Uy + (16 * q + lo) * RC + 32 * s + h8, NT * RC);
 #pragma unroll
           for (int e = 0; e < PP; ++e) pf[e] = as_frag(o.sq[e][s]);
           mma<PP, PP, PP - 1>(pf, ub, y[q]);
@@ -721,7 +727,8 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
   __shared__ f32x4 mail[2][4][(MT + 1) * NL][64];
   const Walk k(a, NT);
   if (k.none) return;
-  const int lo = k.lo, hi = k.hi, l = threadIdx.x & 63;
+  const int lo = k.lo, l = threadIdx.x & 63;
+  const int h8 = 8 * k.hi ^ swap8(lo), wc = k.crow ^ swap8(lo);   // columns read, written in LDS
   const bool own = k.w * MT * 16 < DP;
   const long vrow = (long)a.B * a.dv_ld, yrow = (long)a.B * a.Hv * a.Dv;
   if (threadIdx.x < 256) {
@@ -757,7 +764,7 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
 #pragma unroll
         for (int q = 0; q < NL; ++q) {
           frag sb[3], ra[NP];
-          load_b<3>(sb, Sp + (16 * q + lo) * KP + 32 * s + 8 * hi, NT * KP);
+          load_b<3>(sb, Sp + (16 * q + lo) * KP + 32 * s + h8, NT * KP);
 #pragma unroll
           for (int e = 0; e < NP; ++e) ra[e] = as_frag(o.rows[e][s]);
           mma<NP, 3, 2>(ra, sb, du[q][s & 1]);
@@ -768,7 +775,7 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
         f32x4 x = mail[slot][k.w][q][l];
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[r] += o.tok[r].y * (du[q][0][r] + du[q][1][r]);
-        split4_store<3>(x, Rp + (16 * q + lo) * RC + k.crow, NT * RC);
+        split4_store<3>(x, Rp + (16 * q + lo) * RC + wc, NT * RC);
       }
       S.store(k, a, a.dst + item * a.Dk * a.Dv);
       lds_barrier();
@@ -782,7 +789,7 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           frag rb[3], tf[3];
-          load_b<3>(rb, Rp + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
+          load_b<3>(rb, Rp + (16 * q + lo) * RC + 32 * s + h8, NT * RC);
 #pragma unroll
           for (int e = 0; e < 3; ++e) tf[e] = as_frag(o.sq[e][s]);
           mma<3, 3, 2>(tf, rb, part[s]);
@@ -793,7 +800,7 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
           z[r] *= o.tok[r].z;                            // dR
           zs[r] = -o.tok[r].x * z[r];
         }
-        split4_store<3>(zs, Up + (16 * q + lo) * RC + k.crow, NT * RC);
+        split4_store<3>(zs, Up + (16 * q + lo) * RC + wc, NT * RC);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           bstore(rr, k.place<float>(q, a.Dv) + r * a.Dv * 4, z[r]);
@@ -816,7 +823,7 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
               frag ub[3], kf[NP];
-              load_b<3>(ub, Up + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
+              load_b<3>(ub, Up + (16 * q + lo) * RC + 32 * s + h8, NT * RC);
 #pragma unroll
               for (int e = 0; e < NP; ++e) kf[e] = as_frag(o.kt[e][m][s]);
               mma<NP, 3, 2>(kf, ub, S.x[m][q]);
@@ -871,8 +878,8 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
           y[r] = Op<T>::to_f32(o.y[r][q]);
           ys[r] = a.scale * o.tok[r] * y[r];
         }
-        split4_store<NP>(y, Yp + (16 * q + lo) * RC + k.crow, NT * RC);
-        split4_store<3>(ys, Ys + (16 * q + lo) * RC + k.crow, NT * RC);
+        split4_store<NP>(y, Yp + (16 * q + lo) * RC + wc, NT * RC);
+        split4_store<3>(ys, Ys + (16 * q + lo) * RC + wc, NT * RC);
       }
     };
     // .. and the two products into the mailbox
@@ -883,7 +890,7 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           frag yb[NP], pa[3];
-          load_b<NP>(yb, Yp + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
+          load_b<NP>(yb, Yp + (16 * q + lo) * RC + 32 * s + h8, NT * RC);
 #pragma unroll
           for (int e = 0; e < 3; ++e) pa[e] = as_frag(o.sq[e][s]);
           mma<3, NP, 2>(pa, yb, x);
@@ -895,7 +902,7 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
             frag yb[3], qa[NP];
-            load_b<3>(yb, Ys + (16 * q + lo) * RC + 32 * s + 8 * hi, NT * RC);
+            load_b<3>(yb, Ys + (16 * q + lo) * RC + 32 * s + h8, NT * RC);
 #pragma unroll
             for (int e = 0; e < NP; ++e) qa[e] = as_frag(o.qt[e][m][s]);
             mma<NP, 3, 2>(qa, yb, z);
@@ -1004,7 +1011,8 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
   // loads of a step, four columns a thread: a row of each state and, with the
   // first rows, a token (descriptors as in the loops: uniform bases, so that few
   // addresses live in registers)
-  const int row = tid >> 3, rc = (tid & 7) * 4;
+  const int h8 = 8 * hi_ ^ swap8(lo_);
+  const int row = tid >> 3, rc = (tid & 7) * 4, wc = rc ^ swap8(row);
   const long yrow = (long)a.B * a.Hv * a.Dv, vrow = (long)a.B * a.v_ld;
   struct alignas(4 * sizeof(T)) Four { T x[4]; };
   f32x4 fs, fd, fu, fr;
@@ -1048,8 +1056,8 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
       if (row < DR) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) ss += fs[e] * fd[e];
-        split4_store<3>(fs, S + row * CP + rc, DR * CP);
-        split4_store<3>(fd, S + kD + row * CP + rc, DR * CP);
+        split4_store<3>(fs, S + row * CP + wc, DR * CP);
+        split4_store<3>(fd, S + kD + row * CP + wc, DR * CP);
       }
       if (hs == 0) {
         bf16_t* X = pool + cb * kTok;
@@ -1060,9 +1068,9 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
           ub += fr[e] * fu[e];
           vr += fr[e] * Op<T>::to_f32(fv.x[e]);
         }
-        split4_store<NP>(y, X + row * CP + rc, CT * CP);
-        split4_store<3>(fu, X + kU + row * CP + rc, CT * CP);
-        split4_store<XP>(fr, X + kR + row * CP + rc, CT * CP);
+        split4_store<NP>(y, X + row * CP + wc, CT * CP);
+        split4_store<3>(fu, X + kU + row * CP + wc, CT * CP);
+        split4_store<XP>(fr, X + kR + row * CP + wc, CT * CP);
       }
     };
     lds_barrier();
@@ -1092,8 +1100,8 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
           else if (c0 + 2 * NC < a.Dv) fetch(h, c0 + 2 * NC, 0);
           else if (hh + 1 < grp) fetch(h + 1, 0, 0);
         }
-        const bf16_t* X = pool + cb * kTok + (16 * w + lo_) * CP + 8 * hi_;
-        const bf16_t* S = pool + 2 * kTok + sb * kState + lo_ * CP + 8 * hi_;
+        const bf16_t* X = pool + cb * kTok + (16 * w + lo_) * CP + h8;
+        const bf16_t* S = pool + 2 * kTok + sb * kState + lo_ * CP + h8;
         frag ya[NP], ua[3], ra[XP];
 #pragma unroll
         for (int e = 0; e < NP; ++e) ya[e] = lds_frag(X + e * CT * CP);
@@ -1108,7 +1116,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
             if (j <= w) {
               frag un[3];
 #pragma unroll
-              for (int e = 0; e < 3; ++e) un[e] = lds_frag(pool + cb * kTok + kU + (e * CT + 16 * j + lo_) * CP + 8 * hi_);
+              for (int e = 0; e < 3; ++e) un[e] = lds_frag(pool + cb * kTok + kU + (e * CT + 16 * j + lo_) * CP + h8);
               mma<NP, 3, 2>(ya, un, F[m]);
               mma<XP, XP, XP - 1>(ra, un, H[m]);
             }
@@ -1159,13 +1167,13 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
         hm[r] = j < i ? -d * H[m][r] : 0.f;
       }
       // rows i .. i + 3 of column j: consecutive in the transpose
-      split4_store<XP>(f, Ft + j * RC + crow, CT * RC);
+      split4_store<XP>(f, Ft + j * RC + (crow ^ swap8(lo)), CT * RC);
       uint32_t p0[3], p1[3];
       split2<3>(f[0], f[1], p0);
       split2<3>(f[2], f[3], p1);
 #pragma unroll
       for (int e = 0; e < 3; ++e) {
-        bf16_t* x = Fp + (e * CT + crow) * RC + j;
+        bf16_t* x = Fp + (e * CT + crow) * RC + (j ^ swap8(4 * hi));
         x[0] = (bf16_t)p0[e];
         x[RC] = (bf16_t)(p0[e] >> 16);
         x[2 * RC] = (bf16_t)p1[e];
@@ -1173,7 +1181,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
       }
       // H below the diagonal, its mirror above (the diagonal is 0): a tile below
       // writes both, a diagonal one its lower entries and their mirrors
-      if (jt < w) split4_store<XP>(hm, Hp + j * RC + crow, CT * RC);
+      if (jt < w) split4_store<XP>(hm, Hp + j * RC + (crow ^ swap8(lo)), CT * RC);
       if (jt <= w) {
         split2<XP>(hm[0], hm[1], p0);
         split2<XP>(hm[2], hm[3], p1);
@@ -1184,8 +1192,8 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
           for (int r = 0; r < 4; ++r) {
             const int i = crow + r;
             if (j <= i) {
-              Hp[(e * CT + i) * RC + j] = q[r];
-              if (jt == w) Hp[(e * CT + j) * RC + i] = q[r];
+              Hp[(e * CT + i) * RC + (j ^ swap8(4 * hi))] = q[r];
+              if (jt == w) Hp[(e * CT + j) * RC + (i ^ swap8(lo))] = q[r];
             }
           }
         }
@@ -1227,11 +1235,11 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
           frag fa[3], ta[XP], ha[XP];
           if (s == 0 && i + 1 < ND) load_kq(i + 1);
 #pragma unroll
-          for (int e = 0; e < 3; ++e) fa[e] = lds_frag(Fp + (e * CT + arow) * RC + 32 * s + 8 * hi);
+          for (int e = 0; e < 3; ++e) fa[e] = lds_frag(Fp + (e * CT + arow) * RC + 32 * s + (8 * hi ^ swap8(lo)));
 #pragma unroll
           for (int e = 0; e < XP; ++e) {
-            ta[e] = lds_frag(Ft + (e * CT + arow) * RC + 32 * s + 8 * hi);
-            ha[e] = lds_frag(Hp + (e * CT + arow) * RC + 32 * s + 8 * hi);
+            ta[e] = lds_frag(Ft + (e * CT + arow) * RC + 32 * s + (8 * hi ^ swap8(lo)));
+            ha[e] = lds_frag(Hp + (e * CT + arow) * RC + 32 * s + (8 * hi ^ swap8(lo)));
           }
           mma<3, NP, 2>(fa, kb[i & 1][s], aq[i]);
           mma<XP, NP, XP - 1>(ta, qb[i & 1][s], x);
