@@ -134,6 +134,41 @@ __device__ __forceinline__ frag lds_frag(const bf16_t* p) { return as_frag(ld16(
 // number of groups to a row the 16 lanes meet different banks.
 __device__ __forceinline__ int swap8(int row) { return ((row >> 2) ^ (row >> 3)) & 1 ? 8 : 0; }
 
+// Sums over the 8 or 16 neighbouring lanes that hold a row, in every one of them,
+// by moves inside the rows of 16 lanes.
+template <int CTRL>
+__device__ __forceinline__ float moved(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float sum8(float x) {
+  x += moved<0xb1>(x);                                   // pairs
+  x += moved<0x4e>(x);                                   // quads
+  return x + moved<0x141>(x);                            // the half row mirrored
+}
+__device__ __forceinline__ float sum16(float x) {
+  x = sum8(x);
+  return x + moved<0x128>(x);                            // the row turned by 8
+}
+
+// Rows crow .. crow + 3 of column lo (a tile of the accumulators) to dst: float as
+// they are, bfloat16 two columns a store, even lanes the even rows.
+template <typename T>
+__device__ __forceinline__ void store_tile(T* dst, long pitch, f32x4 x, int lo, int rows) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (r < rows) dst[r * pitch + lo] = x[r];
+  } else {
+    const bool odd = lo & 1;
+#pragma unroll
+    for (int r = 0; r < 4; r += 2) {
+      const float got = moved<0xb1>(odd ? x[r] : x[r + 1]);
+      const uint32_t two = odd ? pack2(got, x[r + 1]) : pack2(x[r], got);
+      if (r + odd < rows) *reinterpret_cast<uint32_t*>(dst + (r + odd) * pitch + (lo & ~1)) = two;
+    }
+  }
+}
+
 // Barrier of the work-group that orders LDS only: loads and stores of global
 // memory stay in flight across it.
 __device__ __forceinline__ void lds_barrier() {
@@ -954,17 +989,22 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
   constexpr int DP = 32 * KS, NC = 32, CP = NC + 8, ND = DP / 32;
   constexpr int TPS = ND < 2 ? ND : 2, HS = ND / TPS, DR = 32 * TPS;   // column tiles of a wave, row halves, rows a step
   constexpr int kTok = (NP + 3 + XP) * CT * CP, kState = 6 * DR * CP, kSq = (3 + XP + XP) * CT * RC;
-  constexpr int kPool = 2 * (kTok + kState);
-  __shared__ __align__(16) bf16_t pool[kPool > kSq ? kPool : kSq];
+  // after the walk: F and H, K^T and Q^T (all of them, or half the column tiles at a
+  // time where LDS does not hold them)
+  constexpr int NS = NP == 3 && KS == 4 ? 2 : 1, kTr = NP * DP * CT / NS;
+  constexpr int kPool = 2 * (kTok + kState), kEnd = kSq + 2 * kTr;
+  __shared__ __align__(16) bf16_t pool[kPool > kEnd ? kPool : kEnd];
   __shared__ float4 tok[CT];
   __shared__ double G[CT];
-  __shared__ float dG[2][CT], part[8], sub[CT], sbeta[CT];
+  __shared__ float dG[2][CT], part[8][4], sub[CT], sbeta[CT];
   // tokens' buffer: dY [NP][64][CP], U [3][64][CP], dR [XP][64][CP]; states': S
   // [3][DR][CP], dS [3][DR][CP]
   constexpr int kU = NP * CT * CP, kR = kU + 3 * CT * CP, kD = 3 * DR * CP;
   bf16_t* Fp = pool;                   // [3][64][RC] F, rows i          (after the walk)
   bf16_t* Ft = Fp + 3 * CT * RC;       // [XP][64][RC] F^T
   bf16_t* Hp = Ft + XP * CT * RC;      // [XP][64][RC] H + H^T
+  bf16_t* Kt = Hp + XP * CT * RC;      // K^T, Q^T in fragments
+  bf16_t* Qt = Kt + kTr;
   // the wave's column tile i of the results
   auto tile = [](int i, int half) { return i / TPS * 2 * TPS + half * TPS + i % TPS; };
   const int n = blockIdx.x % a.nch, bk = blockIdx.x / a.nch;
@@ -992,17 +1032,16 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
 #pragma unroll
   for (int i = 0; i < ND; ++i) tq[i] = tkk[i] = zero_acc();
   const long kitem = bk * (long)a.nch + n;
-  // K and Q at the results' places (rows crow .. crow + 3 of a column), as the
-  // transposes hold them: four neighbours of one fragment
   const rsrc_t rk = make_rsrc(a.ktp + kitem * NP * DP * CT, NP * DP * CT * 2);
   const rsrc_t rq = make_rsrc(a.qtp + kitem * NP * DP * CT, NP * DP * CT * 2);
-  const unsigned kq = ((2 * (w & 1) + (hi_ >> 1)) * 16 + lo_) * 16 + 8 * (hi_ & 1);
-  auto column = [&](rsrc_t r, int i) {
+  // K or Q at the results' places (rows crow .. crow + 3 of a column), as the
+  // transposes hold them: four neighbours of one fragment
+  auto column = [&](const bf16_t* tr, int i) {
     f32x4 v = zero_acc();
 #pragma unroll
     for (int e = 0; e < NP; ++e) {
-      const uint2 u = __builtin_bit_cast(
-          uint2, __builtin_amdgcn_raw_buffer_load_b64(r, kq, frag_at(tile(i, half), w >> 1, e, 2, NP) * 2, 0));
+      const uint2 u = *reinterpret_cast<const uint2*>(tr + frag_at(i, w >> 1, e, 2, NP) +
+                                                      ((2 * (w & 1) + (hi_ >> 1)) * 16 + lo_) * 8 + 4 * (hi_ & 1));
       v += f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
                  __uint_as_float(u.y & 0xffff0000u)};
     }
@@ -1136,16 +1175,23 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
         }
       }
     }
-    // K^T and Q^T by column tiles, one ahead
-    frag kb[2][2][NP], qb[2][2][NP];
-    auto load_kq = [&](int i) {
+    // K^T and Q^T on their way while F and H are made
+    constexpr int NL = (kTr / 8 + 511) / 512;
+    uint4 kraw[NL], qraw[NL];
+    auto load_kq = [&](int st) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+      for (int x = 0; x < NL; ++x) {
+        const unsigned at = (tid + 512 * x) * 8 < kTr ? (st * kTr + (tid + 512 * x) * 8) * 2 : kNowhere;
+        kraw[x] = bload16(rk, at);
+        qraw[x] = bload16(rq, at);
+      }
+    };
+    auto lay_kq = [&]() {
 #pragma unroll
-        for (int e = 0; e < NP; ++e) {
-          const int at = frag_at(tile(i, half), s, e, 2, NP) * 2;
-          kb[i & 1][s][e] = as_frag(__builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rk, 16 * l, at, 0)));
-          qb[i & 1][s][e] = as_frag(__builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rq, 16 * l, at, 0)));
+      for (int x = 0; x < NL; ++x)
+        if ((tid + 512 * x) * 8 < kTr) {
+          *reinterpret_cast<uint4*>(Kt + (tid + 512 * x) * 8) = kraw[x];
+          *reinterpret_cast<uint4*>(Qt + (tid + 512 * x) * 8) = qraw[x];
         }
     };
     load_kq(0);
@@ -1201,39 +1247,40 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
     }
     ss *= tok[CT - 1].x;
     float dots[4] = {0.f, 0.f, 0.f, 0.f};
-    {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float4 tk = tok[crow + r];
 #pragma unroll
       for (int i = 0; i < ND; ++i) {
-        const f32x4 kc = column(rk, i);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float4 tk = tok[crow + r];
-          ku[i][r] *= tk.y;
-          aq[i][r] *= a.scale * tk.x;
-          kr[i][r] *= tk.x;
-          ss += ku[i][r] * kc[r];
-        }
+        ku[i][r] *= tk.y;
+        aq[i][r] *= a.scale * tk.x;
+        kr[i][r] *= tk.x;
       }
     }
-    for (int d = 1; d < 64; d <<= 1) ss += __shfl_xor(ss, d, 64);
-    if (l == 0) part[wave] = ss;
-    for (int d = 1; d < 8; d <<= 1) {
-      ub += __shfl_xor(ub, d, 64);
-      vr += __shfl_xor(vr, d, 64);
-    }
+    ub = sum8(ub);
+    vr = sum8(vr);
     if ((tid & 7) == 0) {
       sub[row] = vr;
       sbeta[row] = ub;
     }
-    lds_barrier();
-    {
 #pragma unroll
-      for (int i = 0; i < ND; ++i) {
+    for (int st = 0; st < NS; ++st) {
+      if (st > 0) lds_barrier();
+      lay_kq();
+      lds_barrier();
+      if (st + 1 < NS) load_kq(st + 1);
+#pragma unroll
+      for (int i = st * ND / NS; i < (st + 1) * ND / NS; ++i) {
+        const int ti = tile(i, half) - st * (2 * KS / NS);
         f32x4 x = zero_acc();
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-          frag fa[3], ta[XP], ha[XP];
-          if (s == 0 && i + 1 < ND) load_kq(i + 1);
+          frag fa[3], ta[XP], ha[XP], kb[NP], qb[NP];
+#pragma unroll
+          for (int e = 0; e < NP; ++e) {
+            kb[e] = lds_frag(Kt + frag_at(ti, s, e, 2, NP) + 8 * (16 * hi + lo));
+            qb[e] = lds_frag(Qt + frag_at(ti, s, e, 2, NP) + 8 * (16 * hi + lo));
+          }
 #pragma unroll
           for (int e = 0; e < 3; ++e) fa[e] = lds_frag(Fp + (e * CT + arow) * RC + 32 * s + (8 * hi ^ swap8(lo)));
 #pragma unroll
@@ -1241,22 +1288,26 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
             ta[e] = lds_frag(Ft + (e * CT + arow) * RC + 32 * s + (8 * hi ^ swap8(lo)));
             ha[e] = lds_frag(Hp + (e * CT + arow) * RC + 32 * s + (8 * hi ^ swap8(lo)));
           }
-          mma<3, NP, 2>(fa, kb[i & 1][s], aq[i]);
-          mma<XP, NP, XP - 1>(ta, qb[i & 1][s], x);
-          mma<XP, NP, XP - 1>(ha, kb[i & 1][s], x);
+          mma<3, NP, 2>(fa, kb, aq[i]);
+          mma<XP, NP, XP - 1>(ta, qb, x);
+          mma<XP, NP, XP - 1>(ha, kb, x);
         }
-        const f32x4 qc = column(rq, i);
+        const f32x4 kc = column(Kt, ti), qc = column(Qt, ti);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
+          ss += ku[i][r] * kc[r];
           dots[r] += aq[i][r] * qc[r];
           tq[i][r] += aq[i][r];
           tkk[i][r] += x[r] + ku[i][r] - kr[i][r];
         }
+        __builtin_amdgcn_sched_barrier(0);               // (tiles mixed by the compiler would spill)
       }
     }
+    ss = sum16(ss);
+    if (lo == 0) part[wave][hi] = ss;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      for (int d = 1; d < 16; d <<= 1) dots[r] += __shfl_xor(dots[r], d, 64);
+      dots[r] = sum16(dots[r]);
       if (lo == 0) dG[half][crow + r] = dots[r];
     }
     lds_barrier();
@@ -1272,22 +1323,22 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
       }
       float all = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) all += part[i];
+      for (int i = 0; i < 8; ++i) all += (part[i][0] + part[i][1]) + (part[i][2] + part[i][3]);
       if (t0 + at < a.T) a.dg[((long)(t0 + at) * a.B + b) * a.Hv + h] = t0 + at < len ? s + all : 0.f;
     }
   }
-  const int lo = lo_, crow = 16 * w + 4 * hi_;
+  const int crow = 16 * w + 4 * hi_, rows = a.T - t0 - crow;
+  const long at = (long)(t0 + crow) * a.B + b;
 #pragma unroll
-  for (int i = 0; i < ND; ++i)
+  for (int i = 0; i < ND; ++i) {
+    const int c = 16 * tile(i, half);
+    if (c + lo_ >= a.Dk) continue;                       // (Dk is even: pairs of lanes agree)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int t = t0 + crow + r, c = 16 * tile(i, half) + lo;
-      if (t < a.T && c < a.Dk) {
-        const long at = (long)t * a.B + b;
-        dq[at * a.dq_ld + (long)hk * a.Dk + c] = Op<T>::from_f32(t < len ? tq[i][r] : 0.f);
-        dk[at * a.dk_ld + (long)hk * a.Dk + c] = Op<T>::from_f32(t < len ? tkk[i][r] : 0.f);
-      }
-    }
+    for (int r = 0; r < 4; ++r)
+      if (t0 + crow + r >= len) tq[i][r] = tkk[i][r] = 0.f;
+    store_tile(dq + at * a.dq_ld + (long)hk * a.Dk + c, (long)a.B * a.dq_ld, tq[i], lo_, rows);
+    store_tile(dk + at * a.dk_ld + (long)hk * a.Dk + c, (long)a.B * a.dk_ld, tkk[i], lo_, rows);
+  }
 }
 
 namespace {
