@@ -579,6 +579,7 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
     auto load_t = [&](Ops& o, int n) { load_square16<3, true>(o.sq, a.tp + (k.item0 + n) * 3 * SQ, k); };
     auto load_kt = [&](Ops& o, int n) {
       load_transposed<NP, MT, DP>(o.kt, a.ktp + (k.kitem0 + n) * NP * DP * CT, k, own);
+      o.end = bload<float>(make_rsrc(a.tok + (k.item0 + n) * CT, CT * 16), (CT - 1) * 16);
     };
     auto load_k = [&](Ops& o, int n) {
       load_rows16<NP, KS>(o.rows, a.kp + (k.kitem0 + n) * NP * CT * DP, k);
@@ -595,7 +596,6 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
         for (int q = 0; q < NL; ++q)
           o.v[r][q] = bload<T>(rv, k.place<T>(q, vrow) + (unsigned)(r * vrow * (long)sizeof(T)));
       }
-      o.end = bload<float>(rt, (CT - 1) * 16);
     };
     auto chunk = [&](int n, Ops& o) {
       const long item = k.item0 + n;
@@ -621,7 +621,6 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
         for (int r = 0; r < 4; ++r) rr[r] = o.tok[r].z * (Op<T>::to_f32(o.v[r][q]) - o.tok[r].x * (ks[q][0][r] + ks[q][1][r]));
         split4_store<3>(rr, Rp + (16 * q + lo) * RC + wc, NT * RC);
       }
-      if (SAVE) S.store(k, a, a.st + item * a.Dk * a.Dv);
       lds_barrier();
       const rsrc_t ru = rows_rsrc(a.u + (item * CT + 16 * k.w) * a.Dv + k.c0, SAVE ? 16 : 0, a.Dv, k.nc);
 #pragma unroll
@@ -645,7 +644,7 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
           for (int r = 0; r < 4; ++r) bstore(ru, k.place<float>(q, a.Dv) + r * a.Dv * 4, u[r]);
         }
       }
-      const float end = o.end;
+      if (SAVE) S.store(k, a, a.st + item * a.Dk * a.Dv);
       load_t(o, next);
       load_v(o, next);
       lds_barrier();
@@ -655,7 +654,7 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
 #pragma unroll
           for (int q = 0; q < NL; ++q) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S.x[m][q][r] *= end;
+            for (int r = 0; r < 4; ++r) S.x[m][q][r] *= o.end;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
               frag ub[3], kf[NP];
@@ -711,8 +710,8 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
       for (int q = 0; q < NL; ++q)
 #pragma unroll
         for (int r = 0; r < 4; ++r) y[q][r] *= a.scale * o.tok[r];
-      load_q(o, next);
       lds_barrier();
+      load_q(o, next);
       lds_barrier();
       const int t0 = n * CT + 16 * k.w;
       const rsrc_t ry = rows_rsrc(static_cast<T*>(a.y) + ((long)t0 * a.B + k.b) * a.Hv * a.Dv + (long)k.h * a.Dv + k.c0,
@@ -778,6 +777,7 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
     auto load_t = [&](Ops& o, int n) { load_square16<3, false>(o.sq, a.ttp + (k.item0 + n) * 3 * SQ, k); };
     auto load_kt = [&](Ops& o, int n) {
       load_transposed<NP, MT, DP>(o.kt, a.ktp + (k.kitem0 + n) * NP * DP * CT, k, own);
+      o.end = bload<float>(make_rsrc(a.tok + (k.item0 + n) * CT, CT * 16), (CT - 1) * 16);
     };
     auto load_k = [&](Ops& o, int n) {
       load_rows16<NP, KS>(o.rows, a.kp + (k.kitem0 + n) * NP * CT * DP, k);
@@ -786,7 +786,6 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
       const rsrc_t rt = make_rsrc(a.tok + (k.item0 + n) * CT, CT * 16);
 #pragma unroll
       for (int r = 0; r < 4; ++r) o.tok[r] = __builtin_bit_cast(float4, bload16(rt, (k.crow + r) * 16));
-      o.end = bload<float>(rt, (CT - 1) * 16);
     };
     auto chunk = [&](int n, Ops& o) {
       const long item = k.item0 + n;
@@ -843,7 +842,6 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
                  Op<T>::from_f32(n * CT + k.crow + r < k.len ? z[r] : 0.f));
         }
       }
-      const float end = o.end;
       load_t(o, next);
       load_tok(o, next);
       lds_barrier();
@@ -854,7 +852,7 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
           for (int q = 0; q < NL; ++q) {
             const f32x4 x = mail[slot][k.w][NL + m * NL + q][l];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S.x[m][q][r] = end * S.x[m][q][r] + x[r];
+            for (int r = 0; r < 4; ++r) S.x[m][q][r] = o.end * S.x[m][q][r] + x[r];
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
               frag ub[3], kf[NP];
@@ -966,8 +964,8 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
       load_dy(A, next);
       lds_barrier();
       products((n - 1) & 1, A);
-      load_sq(A, next);
       lds_barrier();
+      load_sq(A, next);
       lds_barrier();
     }
   }
