@@ -444,15 +444,23 @@ __global__ __launch_bounds__(NTHR) void logprob_fwd_kernel(LogprobArgs a) {
   if (a.parts > 1) {
     // the last work-group of the row to arrive joins the parts
     const long at = r * a.parts + part;
-    if (tid == 0) a.part[at] = make_float4(st.m, st.s, st.t, 0.f);
-    if (TOP && tid < a.top) a.keys[at * kTopMax + tid] = sh.top[tid];
-    __threadfence();
-    __syncthreads();
-    if (tid == 0) sh.last = atomicAdd(&a.arrived[r], 1u) == (unsigned)a.parts - 1;
+    // (the first wave writes and arrives, and it alone fences: a fence writes back
+    // or drops the L2 of the XCD, and one from each of 16 waves took 50 us more where
+    // 64 rows were split in two)
+    if (tid < 64) {
+      if (tid == 0) a.part[at] = make_float4(st.m, st.s, st.t, 0.f);
+      if (TOP && tid < a.top) a.keys[at * kTopMax + tid] = sh.top[tid];
+      __threadfence();
+      if (tid == 0) {
+        sh.last = atomicAdd(&a.arrived[r], 1u) == (unsigned)a.parts - 1;
+        if (sh.last) {
+          __threadfence();
+          a.arrived[r] = 0;            // for the next call
+        }
+      }
+    }
     __syncthreads();
     if (!sh.last) return;
-    __threadfence();
-    if (tid == 0) a.arrived[r] = 0;    // for the next call
     const volatile float* ps = reinterpret_cast<const volatile float*>(a.part + r * a.parts);
     st = Stats{ps[0], ps[1], ps[2]};
     for (int i = 1; i < a.parts; ++i) st = join(st, Stats{ps[4 * i], ps[4 * i + 1], ps[4 * i + 2]});
@@ -729,7 +737,7 @@ ll_status ll_logprob_bwd(ll_logprob_plan* p, void* stream, int32_t rows, const v
   ll::LogprobArgs a = p->a;
   a.x = logits; a.targets = targets; a.lse_in = lse; a.ent_in = entropy; a.ids_in = top_ids;
   a.dlogp = dlogp; a.dentropy = dentropy; a.dtop = dtop; a.dx = dlogits;
-  a.parts = parts_of(p, rows, 16 << 10);
+  a.parts = parts_of(p, rows, 4 << 10);
   a.stream = past_caches(p, rows);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const dim3 grid((unsigned)(rows * a.parts));
