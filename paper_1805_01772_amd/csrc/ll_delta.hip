@@ -39,6 +39,9 @@ constexpr int kStepCols = 32;
 // group r = tid / 8, column group tid % 8) holds rows r, r + 32, .. and four
 // columns of them in registers.  Two sums over the rows (S^T k, then S^T q)
 // are all that the columns exchange.
+// Bound: HBM, the state read and written: 256 rows, 32 heads of 128 x 128 in 225 us,
+// 1.08 GB, 4.8 TB/s (a copy of that size: 5.2).  A few rows: the launch, 4 rows of 4
+// heads of 32 x 32 in 4 us.
 template <typename T>
 __global__ __launch_bounds__(256) void delta_step_kernel(DeltaStepArgs a) {
   __shared__ float ks[kDeltaMaxDk], qs[kDeltaMaxDk];

@@ -26,7 +26,12 @@
 // pieces (24 bits, exactly), a bfloat16 one is its own piece, and a product of
 // pieces i and j is taken while i + j <= 2: what is dropped is below 2^-24 of the
 // term.  Results that leave the call as bfloat16 and feed nothing else take two
-// pieces (2^-16 against the rounding's 2^-9).  Sums are float32.
+// pieces (2^-17 of the value against the rounding's 2^-8).  Sums are float32.
+//
+// Sizes that the figures below are for: "8 rows", lengths 256 to 2048, and "one
+// row" of 16384 tokens, 16 value heads of 128 x 128 in bfloat16 (8 and 16 key
+// heads), forward and gradient; "prompts", 4 rows of 100 to 1000 tokens, the same
+// heads, inference.
 #include "ll_delta.h"
 #include "ll_exchange.h"
 #include "ll_kernels.h"
@@ -191,6 +196,8 @@ __device__ __forceinline__ void wave_lds_fence() {
 // blocks below by float32 products: T_rc = -T_rr sum_k A_rk T_kc, a wave per
 // block column), then everything the loops read in the order in which a lane
 // reads it, 16 bytes at a time.
+// Bound: HBM, for what it writes (K, Q, T and P, plain and transposed, in pieces):
+// 8 rows 103 us, 0.6 GB; one row 132 us; prompts 27 us.
 // ---------------------------------------------------------------------------
 template <typename T, int KS, bool SAVE>
 __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
@@ -552,8 +559,14 @@ __device__ void zero_rest(T* out, long tok_ld, const DeltaArgs& a, const Walk& k
 // Waves 4-7 make Y beside them from the same pieces.  Three barriers a chunk.
 // The operands that do not depend on the state are loaded a chunk ahead, each into
 // its own registers as soon as the last product that reads them has been issued
-// (two register sets in turn need 60 registers more and measured 54 us against 45
-// for the ragged prompts, 240 against 224 for 16 rows of 2048 tokens).
+// (two register sets in turn need 60 registers more: prompts 54 us against 45, 8
+// rows 240 against 224).  The waves that make Y load in the phase in which they
+// have nothing to multiply, and S and U are stored in the second phase: 8 rows 226
+// -> 215 us, one row 657 -> 630.
+// Bound: with few heads a chunk's three products one after the other, 2.5 us a chunk
+// with 16 columns (1.5 of them when nothing else runs on the compute unit): one
+// row 630 us for 256 chunks; with many the traffic of the operands and of what is
+// kept for the gradient: 8 rows 215 us, 0.85 GB, 4 TB/s; prompts 42 us.
 // ---------------------------------------------------------------------------
 template <typename T, int KS, int NL, bool SAVE>
 __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
@@ -749,7 +762,7 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
 // state_bwd: the gradient loop, the same split.  Waves 0-3 carry dS: K dS, T^T dU,
 // K^T dR.  Waves 4-7 make what does not depend on it, P^T dY and Q^T (scale e^G
 // dY), one chunk ahead, each for the chain wave of its rows (through LDS, in the
-// accumulators' order).
+// accumulators' order).  Bound as state_fwd: 8 rows 235 us, one row 630 us.
 // ---------------------------------------------------------------------------
 template <typename T, int KS, int NL>
 __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
@@ -980,6 +993,11 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
 // split into the other and the one after it is on its way into registers.  F, H
 // and the three products with the states stay in accumulators.  The value heads
 // of a key head follow one another, so dQ and dK are summed in a fixed order.
+// After the walk K^T and Q^T come through LDS once for all eight waves: read by each
+// wave for itself from global memory they took 10 of 52 thousand cycles a head's
+// chunk.  Bound: HBM in the walk (U, dR and both states of every chunk, 5 TB/s),
+// which stands still while F, H and what follows are made, since LDS holds one
+// work-group: 8 rows 317 us, 1.2 GB, 3.8 TB/s; one row 357 us.
 // ---------------------------------------------------------------------------
 template <typename T, int KS>
 __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
@@ -1342,7 +1360,10 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
 namespace {
 
 // Columns of the state per work-group, in 16s: 32 where that still gives every
-// compute unit a work-group (16 read the chunk's operands twice as often).
+// compute unit a work-group (16 read the chunk's operands twice as often): inference
+// over 1000 tokens with 16 heads of 128 columns, 32 against 16 columns, takes 276
+// against 305 us for 16 rows, 1016 against 1162 for 64; for 2 rows
+// it is 59 against 48, for one row of 16384, forward and gradient, 1578 against 1290.
 int cols_of(const DeltaArgs& a, int cus) {
   return a.Dv > 16 && (long)a.B * a.Hv * ((a.Dv + 31) / 32) >= cus ? 2 : 1;
 }
