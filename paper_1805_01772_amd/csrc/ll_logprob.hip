@@ -466,9 +466,14 @@ __global__ __launch_bounds__(NTHR) void logprob_fwd_kernel(LogprobArgs a) {
     }
     __syncthreads();
     if (!sh.last) return;
-    const volatile float* ps = reinterpret_cast<const volatile float*>(a.part + r * a.parts);
+    static_assert(kPartsMax == 32, "a part for each of 32 lanes");
+    const int i = tid & 31;
+    const volatile float* ps = reinterpret_cast<const volatile float*>(a.part + r * a.parts + min(i, a.parts - 1));
     st = Stats{ps[0], ps[1], ps[2]};
-    for (int i = 1; i < a.parts; ++i) st = join(st, Stats{ps[4 * i], ps[4 * i + 1], ps[4 * i + 2]});
+    if (i >= a.parts) st = Stats{kLowest, 0.f, 0.f};
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1)
+      st = join(st, Stats{__shfl_xor(st.m, d, 32), __shfl_xor(st.s, d, 32), __shfl_xor(st.t, d, 32)});
     if (TOP) {
       const int n = a.parts * a.top;
       const volatile unsigned long long* keys = a.keys + r * a.parts * kTopMax;
@@ -717,9 +722,9 @@ ll_status ll_logprob_fwd(ll_logprob_plan* p, void* stream, int32_t rows, const v
   ll::LogprobArgs a = p->a;
   a.x = logits; a.targets = targets; a.logp = logp; a.entropy = entropy; a.lse = lse;
   a.top_ids = top_ids; a.top_logp = top_logp;
-  // (8 rows of 400000 floats: 18 us in parts of 256 KiB, 25 in parts of 64, 44 whole;
-  // 8 rows of 131072 bfloat16, 256 KiB, 17.5 whole and 14 in four)
-  a.parts = parts_of(p, rows, 256 << 10);
+  // (8 rows of 131072 bfloat16: 13.5 us in parts of 64 KiB, 15.7 of 128, 17.4 whole; 8 rows
+  // of 400000 floats: 17.5, 15.6 and 44)
+  a.parts = parts_of(p, rows, 64 << 10);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   // 1024 threads a work-group where there is at most one for a compute unit, else 256
   // (256 rows of 50001 floats: 15.0 us against 19.4; 512 rows: 28.2 against 22.3)
