@@ -453,6 +453,11 @@ ll_status ll_delta_plan_create(const ll_delta_desc* desc, int device, ll_delta_p
 ll_status ll_delta_plan_destroy(ll_delta_plan* plan);
 /* Bytes of device memory that the plan holds. */
 ll_status ll_delta_plan_bytes(const ll_delta_plan* plan, int64_t* device_bytes);
+/* Distances of the tokens from the next call on: ld[6] for q, k, v, dq, dk, dv, as
+ * the descriptor's fields and under its rules (no buffer depends on them).  Another
+ * distance for q, k or v than before drops a saved forward.  Refused values leave
+ * the plan as it was. */
+ll_status ll_delta_plan_set_ld(ll_delta_plan* plan, const int64_t* ld);
 
 /*
  * Forward loop.

@@ -254,6 +254,19 @@ ll_status ll_delta_plan_destroy(ll_delta_plan* p) {
   return LL_OK;
 }
 
+ll_status ll_delta_plan_set_ld(ll_delta_plan* p, const int64_t* ld) {
+  if (!p || !ld) return fail(LL_EINVAL, "plan and ld are required");
+  ll_delta_desc d = p->d;
+  d.q_ld = ld[0]; d.k_ld = ld[1]; d.v_ld = ld[2]; d.dq_ld = ld[3]; d.dk_ld = ld[4]; d.dv_ld = ld[5];
+  LL_STATUS(validate(&d, false));
+  const DeltaArgs z = sizes(d);
+  if (z.q_ld != p->a.q_ld || z.k_ld != p->a.k_ld || z.v_ld != p->a.v_ld) p->saved = false;
+  p->d = d;
+  p->a.q_ld = z.q_ld; p->a.k_ld = z.k_ld; p->a.v_ld = z.v_ld;
+  p->a.dq_ld = z.dq_ld; p->a.dk_ld = z.dk_ld; p->a.dv_ld = z.dv_ld;
+  return LL_OK;
+}
+
 ll_status ll_delta_plan_bytes(const ll_delta_plan* p, int64_t* device_bytes) {
   if (!p || !device_bytes) return fail(LL_EINVAL, "plan and device_bytes are required");
   *device_bytes = p->bytes;

@@ -32,7 +32,7 @@ EXPORTED = ("ll_plan_create", "ll_plan_destroy", "ll_plan_stack_bytes",
             "ll_status_sync", "ll_last_error", "ll_version",
             "ll_plan_set_timing", "ll_plan_set_timing_stages", "ll_plan_read_timing",
             "ll_measure_mfma_peak", "ll_eval_activations", "lstm_loop_fwd_noalloc",
-            "ll_delta_plan_create", "ll_delta_plan_destroy", "ll_delta_plan_bytes",
+            "ll_delta_plan_create", "ll_delta_plan_destroy", "ll_delta_plan_bytes", "ll_delta_plan_set_ld",
             "delta_loop_fwd", "delta_loop_bwd", "delta_loop_step", "ll_delta_status_sync",
             "ll_logprob_plan_create", "ll_logprob_plan_destroy", "ll_logprob_fwd",
             "ll_logprob_bwd", "ll_logprob_fwd_bwd", "ll_logprob_status_sync",
@@ -145,6 +145,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.ll_delta_plan_create.argtypes = [ctypes.POINTER(ll_delta_desc), ctypes.c_int, pvp]
     lib.ll_delta_plan_destroy.argtypes = [vp]
     lib.ll_delta_plan_bytes.argtypes = [vp, ctypes.POINTER(i64)]
+    lib.ll_delta_plan_set_ld.argtypes = [vp, ctypes.POINTER(i64)]
     lib.delta_loop_fwd.argtypes = [vp] * 11 + [i32]
     lib.delta_loop_bwd.argtypes = [vp] * 16
     lib.delta_loop_step.argtypes = [ctypes.POINTER(ll_delta_desc)] + [vp] * 8 + [i32, vp, vp]
@@ -165,7 +166,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                  "lstm_loop_fwd", "lstm_loop_bwd", "ll_status_sync", "ll_plan_set_timing",
                  "ll_plan_set_timing_stages", "ll_plan_read_timing", "ll_measure_mfma_peak",
                  "ll_eval_activations", "lstm_loop_fwd_noalloc", "ll_delta_plan_create",
-                 "ll_delta_plan_destroy", "ll_delta_plan_bytes", "delta_loop_fwd",
+                 "ll_delta_plan_destroy", "ll_delta_plan_bytes", "ll_delta_plan_set_ld", "delta_loop_fwd",
                  "delta_loop_bwd", "delta_loop_step", "ll_delta_status_sync",
                  "ll_logprob_plan_create", "ll_logprob_plan_destroy", "ll_logprob_fwd",
                  "ll_logprob_bwd", "ll_logprob_fwd_bwd", "ll_logprob_status_sync",
@@ -478,8 +479,24 @@ class DeltaPlan(_OpPlan):
         self._qk, self._v = (T_max, B, Hk, Dk), (T_max, B, Hv, Dv)
         self._gate, self._state = (T_max, B, Hv), (B, Hv, Dk, Dv)
 
+    def _follow(self, **tokens):
+        """The tokens of a single row are stride(0) apart; stride(1), of a dimension
+        of one, says nothing (a view may hold any number there), and a distance
+        taken from it is put right here."""
+        T, B = self._qk[:2]
+        if B != 1 or T == 1:
+            return
+        new = {n: t.stride(0) for n, t in tokens.items()
+               if t.dim() == 4 and t.stride(0) > 0 and t.stride(0) != self._ld[n]}
+        if new:
+            ld = {**self._ld, **new}
+            _check(self._lib.ll_delta_plan_set_ld(
+                self._h, (ctypes.c_int64 * 6)(*(ld[n] for n in ("q", "k", "v", "dq", "dk", "dv")))))
+            self._ld = ld
+
     def _inputs(self, q, k, v, g, beta, seq_len):
         t, f = self._t, _dtype("float32")
+        self._follow(q=q, k=k, v=v)
         return (_tokens(q, "q", self._qk, self._ld["q"], t),
                 _tokens(k, "k", self._qk, self._ld["k"], t),
                 _tokens(v, "v", self._v, self._ld["v"], t),
@@ -500,6 +517,7 @@ class DeltaPlan(_OpPlan):
         """delta_loop_bwd (asynchronous on `stream`); q .. seq_len are the
         tensors the saved forward was given."""
         t, f = self._t, _dtype("float32")
+        self._follow(dq=dq, dk=dk, dv=dv)
         _check(self._lib.delta_loop_bwd(
             self._h, _stream(stream), *self._inputs(q, k, v, g, beta, seq_len),
             _want(dy, "dy", self._v, t), _want(dST, "dST", self._state, f, optional=True),

@@ -39,3 +39,8 @@ def test_one_token_has_no_such_limit():
     lib = _lib()
     # null operands are what this call is refused for
     assert lib.delta_loop_step(ctypes.byref(d), *[None] * 8, 4, None, None) == ll.LL_EINVAL
+
+
+def test_distances_need_a_plan_and_values():
+    lib = _lib()
+    assert lib.ll_delta_plan_set_ld(None, (ctypes.c_int64 * 6)()) == ll.LL_EINVAL
