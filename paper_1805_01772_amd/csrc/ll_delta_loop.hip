@@ -1332,15 +1332,18 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
       if (t0 + tid < a.T)
         a.dbeta[((long)(t0 + tid) * a.B + b) * a.Hv + h] = t0 + tid < len ? sbeta[tid] / (bt * bt) : 0.f;
       const int at = CT - 1 - tid;
-      float s = dG[0][at] + dG[1][at] - sub[at];         // sums from the chunk's end
+      // sums from the chunk's end, in double: terms of both signs
+      double s = ((double)dG[0][at] + dG[1][at]) - sub[at];
       for (int d = 1; d < 64; d <<= 1) {
-        const float o = __shfl_up(s, d, 64);
+        const double o = __shfl_up(s, d, 64);
         if (tid >= d) s += o;
       }
-      float all = 0.f;
+      double all = 0.;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) all += (part[i][0] + part[i][1]) + (part[i][2] + part[i][3]);
-      if (t0 + at < a.T) a.dg[((long)(t0 + at) * a.B + b) * a.Hv + h] = t0 + at < len ? s + all : 0.f;
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) all += part[i][j];
+      if (t0 + at < a.T) a.dg[((long)(t0 + at) * a.B + b) * a.Hv + h] = t0 + at < len ? (float)(s + all) : 0.f;
     }
   }
   const int crow = 16 * w + 4 * hi_, rows = a.T - t0 - crow;
