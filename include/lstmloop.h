@@ -565,6 +565,9 @@ ll_status ll_logprob_fwd(ll_logprob_plan* plan, void* stream, int32_t rows, cons
  *     sum_i dlogp_i logp_i + dentropy_i entropy_i + sum_j dtop_ij top_logp_ij
  * from the forward's lse, entropy and top_ids.  dlogp, dentropy, dtop may be
  * NULL (zero).  entropy is read only with dentropy, top_ids only with dtop.
+ * Where an lse is 32 or more in magnitude, what its rounding to a float took
+ * away is found again from the row (read once more); an lse that is further
+ * off than that (of a vocabulary in several parts, say) is taken as it is.
  */
 ll_status ll_logprob_bwd(ll_logprob_plan* plan, void* stream, int32_t rows, const void* logits,
                          const int32_t* targets, const float* lse, const float* entropy,

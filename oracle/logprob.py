@@ -16,7 +16,9 @@ def logprob_forward(x, targets=None, top_k=0):
     with np.errstate(divide="ignore"):
         lse = np.where(empty, -np.inf, m + np.log(np.where(empty, 1.0, s)))
     p = np.where(empty[:, None], 0.0, e / np.where(empty, 1.0, s)[:, None])
-    lp = np.where(np.isneginf(x), -np.inf, x - np.where(empty, 0.0, lse)[:, None])
+    # (x - m) - log s: their sum loses log s where m is as large as a type's lowest value
+    lp = np.where(np.isneginf(x), -np.inf,
+                  (x - np.where(empty, 0.0, m)[:, None]) - np.log(np.where(empty, 1.0, s))[:, None])
     plp = p * np.where(p > 0, lp, 0.0)
     out = dict(lse=lse, p=p, lp=lp, entropy=-plp.sum(1), empty=empty)
     if targets is not None:

@@ -3,7 +3,9 @@
 //
 // One pass over a row keeps, per thread, the running maximum m, s = sum e^{x-m}
 // and t = sum (x - m) e^{x-m}; joined over the work-group
-//     lse = m + log s,  logp = x_target - lse,  entropy = log s - t / s.
+//     lse = m + log s,  logp = (x_target - m) - log s,  entropy = log s - t / s.
+// m and log s stay apart wherever both are at hand: their sum as one float loses log s
+// where |m| is large (of a row at the type's lowest value all of it).
 // Alternatives: each of 64 thread groups knows its largest (value, index); the
 // top_k-th largest of those bounds the row's top_k-th from below, so only the
 // threads that hold at least that much are read again (about top_k of them),
@@ -11,7 +13,9 @@
 // all keys differ.
 // Gradient, with c = dlogp (if there is a target) + sum_j dtop_j:
 //     dx = -p (c + dentropy (log p + entropy)) + dlogp [target] + dtop_j [id_j]
-// the marked entries are few and written after the row.
+// the marked entries are few and written after the row.  The call of its own has lse
+// as a float: where that is 32 or more in magnitude it sums the row again first
+// (lse_rest).
 //
 // Rows are walked in 16-byte chunks from the first aligned element; up to 7
 // elements before and after are done singly.
@@ -55,6 +59,7 @@ struct LogprobArgs {
   float4* part;
   unsigned long long* keys;
   unsigned* arrived;
+  float* rest;                         // lse_rest by row, where a kernel of its own made it
 };
 
 // The chunks of a row that a part walks, and its single elements.
@@ -378,7 +383,11 @@ __device__ __forceinline__ Stats walk(const T* row, const Span& sp, int V, uint4
 }
 
 struct RowResult {
-  float lse, ent;
+  float m, ls, ent;                    // log p = (x - m) - ls
+  bool empty, sound;                   // nothing is allowed; no NaN
+  __device__ __forceinline__ float logp(float x) const {
+    return x == -__builtin_inff() && sound ? x : (x - m) - ls;
+  }
 };
 
 // The row's target and its logit, read while the row is (thread 0's are used).
@@ -399,21 +408,19 @@ __device__ __forceinline__ Target target_of(const LogprobArgs& a, const T* row, 
 // The row's outputs from its sums (one thread writes).
 __device__ __forceinline__ RowResult row_result(const LogprobArgs& a, long r, Stats st, Target t) {
   RowResult res;
-  if (st.s == 0.f) {
-    res.lse = -__builtin_inff();
-    res.ent = 0.f;
-  } else {
-    const float ls = logf(st.s);
-    res.lse = st.m + ls;
-    res.ent = ls - st.t / st.s;
-  }
+  res.empty = st.s == 0.f;
+  res.m = res.empty ? 0.f : st.m;
+  res.ls = res.empty ? -__builtin_inff() : logf(st.s);
+  res.ent = res.empty ? 0.f : res.ls - st.t / st.s;
+  const float lse = res.m + res.ls;
+  res.sound = lse == lse;
   if (threadIdx.x == 0) {
-    if (a.lse) a.lse[r] = res.lse;
+    if (a.lse) a.lse[r] = lse;
     if (a.entropy) a.entropy[r] = res.ent;
     if (a.targets && a.logp) {
       float lp = 0.f;
       if (t.id >= 0 && t.id < a.V) {
-        lp = t.x == -__builtin_inff() && res.lse == res.lse ? t.x : t.x - res.lse;
+        lp = res.logp(t.x);
       } else if (t.id != -1) {
         atomicOr(a.err, LL_DEVERR_TARGET);
       }
@@ -484,32 +491,86 @@ __global__ __launch_bounds__(NTHR) void logprob_fwd_kernel(LogprobArgs a) {
   }
   const RowResult res = row_result(a, r, st, target);
   if (TOP && tid < a.top) {
-    const float x = key_value(sh.top[tid]);
     a.top_ids[r * a.top + tid] = key_index(sh.top[tid]);
-    a.top_logp[r * a.top + tid] = x == -__builtin_inff() && res.lse == res.lse ? x : x - res.lse;
+    a.top_logp[r * a.top + tid] = res.logp(key_value(sh.top[tid]));
   }
 }
 
+// log sum e^{x - lse} of a row: what the rounding of its lse to a float took away, at
+// most a unit of lse.  More than that is no rounding (the lse of more logits than these,
+// a vocabulary in several parts): 0, lse is taken as it is.
+template <typename T, int NTHR>
+__device__ float lse_rest(const T* row, int V, float lse, float* part) {
+  constexpr int E = Op<T>::kPerChunk, NW = NTHR / 64;
+  const int tid = threadIdx.x;
+  const Span sp = span_of(row, V, 0, 1);
+  float s = 0.f;
+  if (tid < sp.head) s += exp_diff(Op<T>::to_f32(row[tid]) - lse);
+  if (tid < V - sp.tail0) s += exp_diff(Op<T>::to_f32(row[sp.tail0 + tid]) - lse);
+  for (int c = tid; c < sp.c1; c += 4 * NTHR) {
+    uint4 u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = ld16(row + sp.head + (long)min(c + i * NTHR, sp.c1 - 1) * E);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c + i * NTHR < sp.c1) {
+        float f[E];
+        unpack<T>(u[i], f);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s += exp_diff(f[e] - lse);
+      }
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) s += __shfl_xor(s, d, 64);
+  if ((tid & 63) == 0) part[tid >> 6] = s;
+  __syncthreads();
+  s = 0.f;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) s += part[i];
+  const float z = logf(s);
+  return __builtin_fabsf(z) <= __builtin_fabsf(lse) * 0x1p-22f ? z : 0.f;
+}
+
+// Below this an lse's rounding is at most 2^-20 of p, of the size that the exponent's
+// own rounding leaves, and the row is not read again (4096 rows of 131072 bfloat16: 423
+// us, 560 where it is; 1024 of 100000 floats 166 and 201).
+__device__ __forceinline__ bool lse_is_short(float lse) {
+  return __builtin_fabsf(lse) >= 32.f && lse != -__builtin_inff();
+}
+
+// lse_rest for rows that are split and overwritten, before them: a part would read what
+// another has written (3 us for rows that need nothing; 8 rows of 400000 floats that do
+// 90 us in all, 84 where every part sums the row for itself).
+template <typename T>
+__global__ __launch_bounds__(256) void logprob_rest_kernel(LogprobArgs a) {
+  __shared__ float part[4];
+  const long r = blockIdx.x;
+  const float lse = a.lse_in[r];
+  const float z = lse_is_short(lse) ? lse_rest<T, 256>(static_cast<const T*>(a.x) + r * a.ld, a.V, lse, part) : 0.f;
+  if (threadIdx.x == 0) a.rest[r] = z;
+}
+
 // The gradient of one part of a row: everything but the marked entries in a
-// pass, those after it.
+// pass, those after it.  log p = (x - m) - ls.
 template <typename T, int NTHR, int KEEP = 0>
-__device__ void row_gradient(const LogprobArgs& a, const T* row, T* out, long r, const Span& sp, float lse,
-                             float ent, int* mark, float* add, float* val, const uint4 (*keep)[NTHR] = nullptr) {
+__device__ void row_gradient(const LogprobArgs& a, const T* row, T* out, long r, const Span& sp, float m, float ls,
+                             float ent, bool empty, int* mark, float* add, float* val,
+                             const uint4 (*keep)[NTHR] = nullptr) {
   constexpr int E = Op<T>::kPerChunk;
   const int tid = threadIdx.x;
   const int t = a.targets ? a.targets[r] : -1;
   const bool has = t >= 0 && t < a.V;
   const float dl = has && a.dlogp ? a.dlogp[r] : 0.f;
   const float dh = a.dentropy ? a.dentropy[r] : 0.f;
-  const bool empty = lse == -__builtin_inff();
   const int ntop = a.dtop ? a.top : 0;
   float c = 0.f;
   for (int j = 0; j < ntop; ++j) c += a.dtop[r * a.top + j];
   c += dl;
-  const float h = ent, cl = -c, dhn = -dh;
+  // log p and log p + entropy from x - m: their other terms are the row's
+  const float h = ent - ls, l2 = -ls * kLog2e, cl = -c, dhn = -dh;
   auto grad = [&](float x) {
-    const float lp = x - lse, p = __builtin_amdgcn_exp2f(lp * kLog2e);
-    return p * (cl + dhn * (fmaxf(lp, -1e30f) + h));
+    const float d = x - m, p = __builtin_amdgcn_exp2f(__builtin_fmaf(d, kLog2e, l2));
+    return p * (cl + dhn * (fmaxf(d, -1e30f) + h));
   };
   // marked entries of this part (they are read before anything is written:
   // out may be the row itself)
@@ -569,12 +630,14 @@ __device__ void row_gradient(const LogprobArgs& a, const T* row, T* out, long r,
 template <typename T, int NTHR>
 __global__ __launch_bounds__(NTHR) void logprob_bwd_kernel(LogprobArgs a) {
   __shared__ int mark[kTopMax + 1];
-  __shared__ float add[kTopMax + 1], val[kTopMax + 1];
+  __shared__ float add[kTopMax + 1], val[kTopMax + 1], sums[NTHR / 64];
   const long r = blockIdx.x / a.parts;
   const T* row = static_cast<const T*>(a.x) + r * a.ld;
   const Span sp = span_of(row, a.V, blockIdx.x % a.parts, a.parts);
-  row_gradient<T, NTHR>(a, row, static_cast<T*>(a.dx) + r * a.ld, r, sp, a.lse_in[r],
-                        a.dentropy ? a.ent_in[r] : 0.f, mark, add, val);
+  const float lse = a.lse_in[r];
+  const float rest = a.rest ? a.rest[r] : lse_is_short(lse) ? lse_rest<T, NTHR>(row, a.V, lse, sums) : 0.f;
+  row_gradient<T, NTHR>(a, row, static_cast<T*>(a.dx) + r * a.ld, r, sp, lse, rest,
+                        a.dentropy ? a.ent_in[r] : 0.f, lse == -__builtin_inff(), mark, add, val);
 }
 
 // Both.  Work-groups of 1024 threads for long rows, two a compute unit: few
@@ -596,7 +659,8 @@ __global__ __launch_bounds__(NTHR, NTHR == 1024 ? 8 : 1) void logprob_fwd_bwd_ke
   st = join_group<NTHR>(st, sts);
   const RowResult res = row_result(a, r, st, target);
   __syncthreads();                     // the target's logit is read before the row is overwritten
-  row_gradient<T, NTHR, KEEP>(a, row, static_cast<T*>(a.dx) + r * a.ld, r, sp, res.lse, res.ent, mark, add, val, keep);
+  row_gradient<T, NTHR, KEEP>(a, row, static_cast<T*>(a.dx) + r * a.ld, r, sp, res.m, res.ls, res.ent, res.empty, mark,
+                              add, val, keep);
 }
 
 }  // namespace ll
@@ -605,6 +669,7 @@ struct ll_logprob_plan {
   ll_logprob_desc d;
   int device = 0, cus = 0;
   ll::LogprobArgs a{};
+  float* rest = nullptr;               // [split rows]
 };
 
 namespace {
@@ -623,7 +688,7 @@ int parts_of(const ll_logprob_plan* p, int rows, long least) {
 bool past_caches(const ll_logprob_plan* p, int rows) { return row_bytes(p) * rows > ll::kLastLevelBytes; }
 
 void release(ll_logprob_plan* p) {
-  void* all[] = {p->a.part, p->a.keys, p->a.arrived, p->a.err};
+  void* all[] = {p->a.part, p->a.keys, p->a.arrived, p->a.err, p->rest};
   for (void* m : all)
     if (m) (void)hipFree(m);
 }
@@ -686,6 +751,7 @@ ll_status ll_logprob_plan_create(const ll_logprob_desc* d, int device, ll_logpro
   if (st == LL_OK)
     st = ll::dalloc((void**)&p->a.keys, d->top_k ? 8 * split * ll::kPartsMax * ll::kTopMax : 0, "the parts' keys");
   if (st == LL_OK) st = ll::dalloc((void**)&p->a.arrived, sizeof(unsigned) * split, "the arrivals");
+  if (st == LL_OK) st = ll::dalloc((void**)&p->rest, sizeof(float) * split, "what the rows' lse leave");
   if (st == LL_OK) st = ll::dalloc((void**)&p->a.err, sizeof(int), "the error word");
   if (st == LL_OK && (hipMemset(p->a.arrived, 0, sizeof(unsigned) * split) != hipSuccess ||
                       hipMemset(p->a.err, 0, sizeof(int)) != hipSuccess))
@@ -755,6 +821,12 @@ ll_status ll_logprob_bwd(ll_logprob_plan* p, void* stream, int32_t rows, const v
   a.parts = parts_of(p, rows, 4 << 10);
   a.stream = past_caches(p, rows);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (a.parts > 1 && logits == dlogits) {
+    a.rest = p->rest;
+    if (p->d.dtype == LL_BF16) ll::logprob_rest_kernel<bf16_t><<<dim3(rows), dim3(256), 0, s>>>(a);
+    else ll::logprob_rest_kernel<float><<<dim3(rows), dim3(256), 0, s>>>(a);
+    LL_HIP(hipGetLastError());
+  }
   const dim3 grid((unsigned)(rows * a.parts));
   if (p->d.dtype == LL_BF16) ll::logprob_bwd_kernel<bf16_t, 256><<<grid, dim3(256), 0, s>>>(a);
   else ll::logprob_bwd_kernel<float, 256><<<grid, dim3(256), 0, s>>>(a);
