@@ -25,8 +25,9 @@
 // the float32 ones, so a float operand is taken as the sum of three bfloat16
 // pieces (24 bits, exactly), a bfloat16 one is its own piece, and a product of
 // pieces i and j is taken while i + j <= 2: what is dropped is below 2^-24 of the
-// term.  Results that leave the call as bfloat16 and feed nothing else take two
-// pieces (2^-17 of the value against the rounding's 2^-8).  Sums are float32.
+// term.  Sums are float32.  (Two pieces, 17 bits, of what only y and dK read would
+// round one bfloat16 result in five hundred the other way and lose small differences of
+// large terms; they save 2 to 6 %: 8 rows, forward and gradient, 784 us against 818.)
 //
 // Sizes that the figures below are for: "8 rows", lengths 256 to 2048, and "one
 // row" of 16384 tokens, 16 value heads of 128 x 128 in bfloat16 (8 and 16 key
@@ -201,7 +202,7 @@ __device__ __forceinline__ void wave_lds_fence() {
 // ---------------------------------------------------------------------------
 template <typename T, int KS, bool SAVE>
 __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
-  constexpr int NP = Pieces<T>::n, DP = 32 * KS, KP = DP + 8, PP = NP == 1 ? 2 : 3;
+  constexpr int NP = Pieces<T>::n, DP = 32 * KS, KP = DP + 8;
   constexpr int kOps = 2 * NP * CT * KP * 2, kMats = 2 * CT * SC * 4;
   __shared__ __align__(16) unsigned char raw[kOps > kMats ? kOps : kMats];
   __shared__ __align__(16) float tm[CT * SC];
@@ -376,8 +377,8 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
     put(a.tp, 3, low);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = pm[r * SC + j + e];
-    split8<PP>(x, p);
-    put(a.pp, PP, low);
+    split8<3>(x, p);
+    put(a.pp, 3, low);
     if (SAVE) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = tm[(j + e) * SC + r];
@@ -570,10 +571,10 @@ __device__ void zero_rest(T* out, long tok_ld, const DeltaArgs& a, const Walk& k
 // ---------------------------------------------------------------------------
 template <typename T, int KS, int NL, bool SAVE>
 __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
-  constexpr int NP = Pieces<T>::n, PP = NP == 1 ? 2 : 3, DP = 32 * KS, KP = DP + 8, NT = 16 * NL;
+  constexpr int NP = Pieces<T>::n, DP = 32 * KS, KP = DP + 8, NT = 16 * NL;
   constexpr int MT = KS == 4 ? 2 : 1;                  // 16-row tiles of the state per wave
   __shared__ __align__(16) bf16_t Sp[3 * NT * KP];     // state, column-major pieces
-  __shared__ __align__(16) bf16_t Rp[3 * NT * RC], Up[3 * NT * RC], Uy[PP * NT * RC];
+  __shared__ __align__(16) bf16_t Rp[3 * NT * RC], Up[3 * NT * RC], Uy[3 * NT * RC];
   const Walk k(a, NT);
   if (k.none) return;
   const int lo = k.lo, h8 = 8 * k.hi ^ swap8(k.lo), wc = k.crow ^ swap8(k.lo);   // columns read, written in LDS
@@ -651,7 +652,7 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) us[r] = o.tok[r].y * u[r];
         split4_store<3>(us, Up + (16 * q + lo) * RC + wc, NT * RC);
-        split4_store<PP>(u, Uy + (16 * q + lo) * RC + wc, NT * RC);
+        split4_store<3>(u, Uy + (16 * q + lo) * RC + wc, NT * RC);
         if (SAVE) {
 #pragma unroll
           for (int r = 0; r < 4; ++r) bstore(ru, k.place<float>(q, a.Dv) + r * a.Dv * 4, u[r]);
@@ -694,10 +695,10 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
     if (own && a.ST) S.store(k, a, a.ST + k.head);
   } else {
     struct Ops {
-      uint4 rows[NP][KS], sq[PP][2];
+      uint4 rows[NP][KS], sq[3][2];
       float tok[4];
     };
-    auto load_p = [&](Ops& o, int n) { load_square16<PP, true>(o.sq, a.pp + (k.item0 + n) * 3 * SQ, k); };
+    auto load_p = [&](Ops& o, int n) { load_square16<3, true>(o.sq, a.pp + (k.item0 + n) * 3 * SQ, k); };
     auto load_q = [&](Ops& o, int n) {
       load_rows16<NP, KS>(o.rows, a.qp + (k.kitem0 + n) * NP * CT * DP, k);
       const rsrc_t rt = make_rsrc(a.tok + (k.item0 + n) * CT, CT * 16);
@@ -713,11 +714,11 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
       for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int q = 0; q < NL; ++q) {
-          frag sb[PP], ra[NP];
-          load_b<PP>(sb, Sp + (16 * q + lo) * KP + 32 * s + h8, NT * KP);
+          frag sb[3], ra[NP];
+          load_b<3>(sb, Sp + (16 * q + lo) * KP + 32 * s + h8, NT * KP);
 #pragma unroll
           for (int e = 0; e < NP; ++e) ra[e] = as_frag(o.rows[e][s]);
-          mma<NP, PP, PP - 1>(ra, sb, y[q]);
+          mma<NP, 3, 2>(ra, sb, y[q]);
         }
 #pragma unroll
       for (int q = 0; q < NL; ++q)
@@ -733,11 +734,11 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
       for (int q = 0; q < NL; ++q) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-          frag ub[PP], pf[PP];
-          load_b<PP>(ub, Uy + (16 * q + lo) * RC + 32 * s + h8, NT * RC);
+          frag ub[3], pf[3];
+          load_b<3>(ub, Uy + (16 * q + lo) * RC + 32 * s + h8, NT * RC);
 #pragma unroll
-          for (int e = 0; e < PP; ++e) pf[e] = as_frag(o.sq[e][s]);
-          mma<PP, PP, PP - 1>(pf, ub, y[q]);
+          for (int e = 0; e < 3; ++e) pf[e] = as_frag(o.sq[e][s]);
+          mma<3, 3, 2>(pf, ub, y[q]);
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r)
@@ -1001,10 +1002,10 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
 // ---------------------------------------------------------------------------
 template <typename T, int KS>
 __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
-  constexpr int NP = Pieces<T>::n, XP = NP == 1 ? 2 : 3;   // XP pieces where the result is only dK
+  constexpr int NP = Pieces<T>::n;
   constexpr int DP = 32 * KS, NC = 32, CP = NC + 8, ND = DP / 32;
   constexpr int TPS = ND < 2 ? ND : 2, HS = ND / TPS, DR = 32 * TPS;   // column tiles of a wave, row halves, rows a step
-  constexpr int kTok = (NP + 3 + XP) * CT * CP, kState = 6 * DR * CP, kSq = (3 + XP + XP) * CT * RC;
+  constexpr int kTok = (NP + 6) * CT * CP, kState = 6 * DR * CP, kSq = 9 * CT * RC;
   // after the walk: F and H, K^T and Q^T (all of them, or half the column tiles at a
   // time where LDS does not hold them)
   constexpr int NS = NP == 3 && KS == 4 ? 2 : 1, kTr = NP * DP * CT / NS;
@@ -1013,13 +1014,13 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
   __shared__ float4 tok[CT];
   __shared__ double G[CT];
   __shared__ float dG[2][CT], part[8][4], sub[CT], sbeta[CT];
-  // tokens' buffer: dY [NP][64][CP], U [3][64][CP], dR [XP][64][CP]; states': S
+  // tokens' buffer: dY [NP][64][CP], U [3][64][CP], dR [3][64][CP]; states': S
   // [3][DR][CP], dS [3][DR][CP]
   constexpr int kU = NP * CT * CP, kR = kU + 3 * CT * CP, kD = 3 * DR * CP;
   bf16_t* Fp = pool;                   // [3][64][RC] F, rows i          (after the walk)
-  bf16_t* Ft = Fp + 3 * CT * RC;       // [XP][64][RC] F^T
-  bf16_t* Hp = Ft + XP * CT * RC;      // [XP][64][RC] H + H^T
-  bf16_t* Kt = Hp + XP * CT * RC;      // K^T, Q^T in fragments
+  bf16_t* Ft = Fp + 3 * CT * RC;       // [3][64][RC] F^T
+  bf16_t* Hp = Ft + 3 * CT * RC;      // [3][64][RC] H + H^T
+  bf16_t* Kt = Hp + 3 * CT * RC;      // K^T, Q^T in fragments
   bf16_t* Qt = Kt + kTr;
   // the wave's column tile i of the results
   auto tile = [](int i, int half) { return i / TPS * 2 * TPS + half * TPS + i % TPS; };
@@ -1125,7 +1126,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
         }
         split4_store<NP>(y, X + row * CP + wc, CT * CP);
         split4_store<3>(fu, X + kU + row * CP + wc, CT * CP);
-        split4_store<XP>(fr, X + kR + row * CP + wc, CT * CP);
+        split4_store<3>(fr, X + kR + row * CP + wc, CT * CP);
       }
     };
     lds_barrier();
@@ -1157,13 +1158,13 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
         }
         const bf16_t* X = pool + cb * kTok + (16 * w + lo_) * CP + h8;
         const bf16_t* S = pool + 2 * kTok + sb * kState + lo_ * CP + h8;
-        frag ya[NP], ua[3], ra[XP];
+        frag ya[NP], ua[3], ra[3];
 #pragma unroll
         for (int e = 0; e < NP; ++e) ya[e] = lds_frag(X + e * CT * CP);
 #pragma unroll
         for (int e = 0; e < 3; ++e) ua[e] = lds_frag(X + kU + e * CT * CP);
 #pragma unroll
-        for (int e = 0; e < XP; ++e) ra[e] = lds_frag(X + kR + e * CT * CP);
+        for (int e = 0; e < 3; ++e) ra[e] = lds_frag(X + kR + e * CT * CP);
         if (hs == 0) {
 #pragma unroll
           for (int m = 0; m < 2; ++m) {
@@ -1173,7 +1174,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
 #pragma unroll
               for (int e = 0; e < 3; ++e) un[e] = lds_frag(pool + cb * kTok + kU + (e * CT + 16 * j + lo_) * CP + h8);
               mma<NP, 3, 2>(ya, un, F[m]);
-              mma<XP, XP, XP - 1>(ra, un, H[m]);
+              mma<3, 3, 2>(ra, un, H[m]);
             }
           }
         }
@@ -1187,7 +1188,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
           }
           mma<NP, 3, 2>(ya, sf, aq[hs * TPS + i]);
           mma<3, 3, 2>(ua, df, ku[hs * TPS + i]);
-          mma<XP, XP, XP - 1>(ra, sf, kr[hs * TPS + i]);
+          mma<3, 3, 2>(ra, sf, kr[hs * TPS + i]);
         }
       }
     }
@@ -1229,7 +1230,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
         hm[r] = j < i ? -d * H[m][r] : 0.f;
       }
       // rows i .. i + 3 of column j: consecutive in the transpose
-      split4_store<XP>(f, Ft + j * RC + (crow ^ swap8(lo)), CT * RC);
+      split4_store<3>(f, Ft + j * RC + (crow ^ swap8(lo)), CT * RC);
       uint32_t p0[3], p1[3];
       split2<3>(f[0], f[1], p0);
       split2<3>(f[2], f[3], p1);
@@ -1243,12 +1244,12 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
       }
       // H below the diagonal, its mirror above (the diagonal is 0): a tile below
       // writes both, a diagonal one its lower entries and their mirrors
-      if (jt < w) split4_store<XP>(hm, Hp + j * RC + (crow ^ swap8(lo)), CT * RC);
+      if (jt < w) split4_store<3>(hm, Hp + j * RC + (crow ^ swap8(lo)), CT * RC);
       if (jt <= w) {
-        split2<XP>(hm[0], hm[1], p0);
-        split2<XP>(hm[2], hm[3], p1);
+        split2<3>(hm[0], hm[1], p0);
+        split2<3>(hm[2], hm[3], p1);
 #pragma unroll
-        for (int e = 0; e < XP; ++e) {
+        for (int e = 0; e < 3; ++e) {
           const bf16_t q[4] = {(bf16_t)p0[e], (bf16_t)(p0[e] >> 16), (bf16_t)p1[e], (bf16_t)(p1[e] >> 16)};
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
@@ -1291,7 +1292,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
         f32x4 x = zero_acc();
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-          frag fa[3], ta[XP], ha[XP], kb[NP], qb[NP];
+          frag fa[3], ta[3], ha[3], kb[NP], qb[NP];
 #pragma unroll
           for (int e = 0; e < NP; ++e) {
             kb[e] = lds_frag(Kt + frag_at(ti, s, e, 2, NP) + 8 * (16 * hi + lo));
@@ -1300,13 +1301,13 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
 #pragma unroll
           for (int e = 0; e < 3; ++e) fa[e] = lds_frag(Fp + (e * CT + arow) * RC + 32 * s + (8 * hi ^ swap8(lo)));
 #pragma unroll
-          for (int e = 0; e < XP; ++e) {
+          for (int e = 0; e < 3; ++e) {
             ta[e] = lds_frag(Ft + (e * CT + arow) * RC + 32 * s + (8 * hi ^ swap8(lo)));
             ha[e] = lds_frag(Hp + (e * CT + arow) * RC + 32 * s + (8 * hi ^ swap8(lo)));
           }
           mma<3, NP, 2>(fa, kb, aq[i]);
-          mma<XP, NP, XP - 1>(ta, qb, x);
-          mma<XP, NP, XP - 1>(ha, kb, x);
+          mma<3, NP, 2>(ta, qb, x);
+          mma<3, NP, 2>(ha, kb, x);
         }
         const f32x4 kc = column(Kt, ti), qc = column(Qt, ti);
 #pragma unroll
