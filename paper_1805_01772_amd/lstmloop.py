@@ -408,6 +408,9 @@ def _tokens(t, name: str, shape: tuple, ld: int, dtype):
     tokens are ld elements apart."""
     if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
         _refuse(t, name, shape, dtype)
+    if ld < shape[-2] * shape[-1]:
+        raise ValueError(f"{name}: tokens {ld} elements apart overlap ({shape[-2]} heads of {shape[-1]}); "
+                         "an expanded tensor has to be copied")
     want = (ld, shape[-1], 1) if len(shape) == 3 else (shape[1] * ld, ld, shape[-1], 1)
     if t.stride() != want and any(s != w and n > 1 for s, w, n in zip(t.stride(), want, shape)):
         raise ValueError(f"{name}: strides {tuple(t.stride())}, {want} are wanted "
