@@ -454,9 +454,9 @@ ll_status ll_delta_plan_destroy(ll_delta_plan* plan);
 /* Bytes of device memory that the plan holds. */
 ll_status ll_delta_plan_bytes(const ll_delta_plan* plan, int64_t* device_bytes);
 /* Distances of the tokens from the next call on: ld[6] for q, k, v, dq, dk, dv, as
- * the descriptor's fields and under its rules (no buffer depends on them).  Another
- * distance for q, k or v than before drops a saved forward.  Refused values leave
- * the plan as it was. */
+ * the descriptor's fields and under its rules (no buffer depends on them).  A saved
+ * forward stays, but its gradient needs the distances of q, k and v that it had
+ * (else LL_ESTATE).  Refused values leave the plan as it was. */
 ll_status ll_delta_plan_set_ld(ll_delta_plan* plan, const int64_t* ld);
 
 /*
@@ -481,9 +481,9 @@ ll_status delta_loop_fwd(ll_delta_plan* plan, void* stream, const void* q, const
                          int32_t save_for_backward);
 
 /*
- * Gradient loop of the last saved forward (LL_ESTATE if there is none;
- * LL_EINVAL, with the saved forward kept, if q .. seq_len are not its
- * pointers).  Consumes the saved forward.
+ * Gradient loop of the last saved forward (LL_ESTATE if there is none, or if
+ * the plan's distances of q, k and v are not its; LL_EINVAL if q .. seq_len are
+ * not its pointers; a refused call keeps it).  Consumes the saved forward.
  *   dy       [T_max,B,Hv,Dv] dtype; entries at t >= seq_len[b] are not used.
  *   dST      [B,Hv,Dk,Dv] float, or NULL (zero).
  *   dq, dk   [T_max,B,Hk,Dk], dv [T_max,B,Hv,Dv] dtype, dg, dbeta [T_max,B,Hv]

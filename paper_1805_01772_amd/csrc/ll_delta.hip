@@ -17,6 +17,7 @@ struct ll_delta_plan {
   DeltaArgs a{};                       // sizes and the plan's buffers
   int64_t bytes = 0;
   bool saved = false;
+  long saved_ld[3] = {0, 0, 0};        // of the saved forward's q, k and v
 };
 
 namespace ll {
@@ -260,7 +261,6 @@ ll_status ll_delta_plan_set_ld(ll_delta_plan* p, const int64_t* ld) {
   d.q_ld = ld[0]; d.k_ld = ld[1]; d.v_ld = ld[2]; d.dq_ld = ld[3]; d.dk_ld = ld[4]; d.dv_ld = ld[5];
   LL_STATUS(validate(&d, false));
   const DeltaArgs z = sizes(d);
-  if (z.q_ld != p->a.q_ld || z.k_ld != p->a.k_ld || z.v_ld != p->a.v_ld) p->saved = false;
   p->d = d;
   p->a.q_ld = z.q_ld; p->a.k_ld = z.k_ld; p->a.v_ld = z.v_ld;
   p->a.dq_ld = z.dq_ld; p->a.dk_ld = z.dk_ld; p->a.dv_ld = z.dv_ld;
@@ -291,6 +291,7 @@ ll_status delta_loop_fwd(ll_delta_plan* p, void* stream, const void* q, const vo
                                : ll::delta_launch_fwd<float>(a, save_for_backward != 0, p->cus, s));
   if (save_for_backward) {
     p->saved = true;
+    p->saved_ld[0] = a.q_ld; p->saved_ld[1] = a.k_ld; p->saved_ld[2] = a.v_ld;
     p->a.q = q; p->a.k = k; p->a.v = v; p->a.g = g; p->a.beta = beta; p->a.seq_len = seq_len;
   }
   return LL_OK;
@@ -303,6 +304,8 @@ ll_status delta_loop_bwd(ll_delta_plan* p, void* stream, const void* q, const vo
   if (!p) return fail(LL_EINVAL, "plan is NULL");
   if (!p->saved)
     return fail(LL_ESTATE, "no saved forward on this plan (call delta_loop_fwd with save_for_backward=1 first)");
+  if (p->a.q_ld != p->saved_ld[0] || p->a.k_ld != p->saved_ld[1] || p->a.v_ld != p->saved_ld[2])
+    return fail(LL_ESTATE, "the saved forward's q, k or v had their tokens at other distances than the plan now");
   if (q != p->a.q || k != p->a.k || v != p->a.v || g != p->a.g || beta != p->a.beta || seq_len != p->a.seq_len)
     return fail(LL_EINVAL, "q, k, v, g, beta or seq_len differs from the saved forward's");
   if (!dy || !dq || !dk || !dv || !dg || !dbeta)

@@ -477,32 +477,48 @@ class DeltaPlan(_OpPlan):
         self._t = _dtype(dtype)
         self._create("ll_delta_plan_create", d, device)
         qk, v = Hk * Dk, Hv * Dv
-        self._ld = dict(q=q_ld or qk, k=k_ld or qk, v=v_ld or v, dq=dq_ld or qk, dk=dk_ld or qk,
-                        dv=dv_ld or v)
+        self._note(dict(q=q_ld or qk, k=k_ld or qk, v=v_ld or v, dq=dq_ld or qk, dk=dk_ld or qk,
+                        dv=dv_ld or v))
         self._qk, self._v = (T_max, B, Hk, Dk), (T_max, B, Hv, Dv)
         self._gate, self._state = (T_max, B, Hv), (B, Hv, Dk, Dv)
 
-    def _follow(self, **tokens):
-        """The tokens of a single row are stride(0) apart; stride(1), of a dimension
-        of one, says nothing (a view may hold any number there), and a distance
-        taken from it is put right here."""
+    def _distances(self, **tokens):
+        """The plan's distances as these tensors have them.  The tokens of a single
+        row are stride(0) apart; stride(1), of a dimension of one, says nothing (a
+        view may hold any number there)."""
         T, B = self._qk[:2]
         if B != 1 or T == 1:
-            return
+            return self._ld
         new = {n: t.stride(0) for n, t in tokens.items()
                if t.dim() == 4 and t.stride(0) > 0 and t.stride(0) != self._ld[n]}
-        if new:
-            ld = {**self._ld, **new}
-            _check(self._lib.ll_delta_plan_set_ld(
-                self._h, (ctypes.c_int64 * 6)(*(ld[n] for n in ("q", "k", "v", "dq", "dk", "dv")))))
-            self._ld = ld
+        return {**self._ld, **new} if new else self._ld
 
-    def _inputs(self, q, k, v, g, beta, seq_len):
+    def _set_distances(self, ld):
+        names = ("q", "k", "v", "dq", "dk", "dv")
+        _check(self._lib.ll_delta_plan_set_ld(self._h, (ctypes.c_int64 * 6)(*(ld[n] for n in names))))
+        self._note(ld)
+
+    def _note(self, ld):
+        self._ld = ld
+        for n in ld:
+            setattr(self.desc, n + "_ld", ld[n])
+
+    def _call(self, ld, fn, *args):
+        """One call with the tokens ld apart; a refused one leaves the plan as it was."""
+        old = self._ld
+        if ld is not old:
+            self._set_distances(ld)
+        try:
+            _check(fn(self._h, *args))
+        except LoopError:
+            if ld is not old:
+                self._set_distances(old)
+            raise
+
+    def _inputs(self, q, k, v, g, beta, seq_len, ld):
         t, f = self._t, _dtype("float32")
-        self._follow(q=q, k=k, v=v)
-        return (_tokens(q, "q", self._qk, self._ld["q"], t),
-                _tokens(k, "k", self._qk, self._ld["k"], t),
-                _tokens(v, "v", self._v, self._ld["v"], t),
+        return (_tokens(q, "q", self._qk, ld["q"], t), _tokens(k, "k", self._qk, ld["k"], t),
+                _tokens(v, "v", self._v, ld["v"], t),
                 _want(g, "g", self._gate, f), _want(beta, "beta", self._gate, f),
                 _want(seq_len, "seq_len", self._qk[1:2], _dtype("int32"), optional=True))
 
@@ -510,25 +526,26 @@ class DeltaPlan(_OpPlan):
             stream=None) -> None:
         """delta_loop_fwd (asynchronous on `stream`, default: torch's current)."""
         f = _dtype("float32")
-        _check(self._lib.delta_loop_fwd(
-            self._h, _stream(stream), *self._inputs(q, k, v, g, beta, seq_len),
-            _want(S0, "S0", self._state, f, optional=True), _want(y, "y", self._v, self._t),
-            _want(ST, "ST", self._state, f, optional=True), 1 if save_for_backward else 0))
+        ld = self._distances(q=q, k=k, v=v)
+        self._call(ld, self._lib.delta_loop_fwd,
+                   _stream(stream), *self._inputs(q, k, v, g, beta, seq_len, ld),
+                   _want(S0, "S0", self._state, f, optional=True), _want(y, "y", self._v, self._t),
+                   _want(ST, "ST", self._state, f, optional=True), 1 if save_for_backward else 0)
 
     def bwd(self, q, k, v, g, beta, seq_len, dy, dST, dq, dk, dv, dg, dbeta, dS0=None,
             stream=None) -> None:
-        """delta_loop_bwd (asynchronous on `stream`); q .. seq_len are the
-        tensors the saved forward was given."""
+        """delta_loop_bwd (asynchronous on `stream`); q .. seq_len are the tensors the
+        saved forward was given.  (q, k or v with tokens at other distances than
+        that one's: LL_ESTATE, no forward of such tensors is saved.)"""
         t, f = self._t, _dtype("float32")
-        self._follow(dq=dq, dk=dk, dv=dv)
-        _check(self._lib.delta_loop_bwd(
-            self._h, _stream(stream), *self._inputs(q, k, v, g, beta, seq_len),
-            _want(dy, "dy", self._v, t), _want(dST, "dST", self._state, f, optional=True),
-            _tokens(dq, "dq", self._qk, self._ld["dq"], t),
-            _tokens(dk, "dk", self._qk, self._ld["dk"], t),
-            _tokens(dv, "dv", self._v, self._ld["dv"], t),
-            _want(dg, "dg", self._gate, f), _want(dbeta, "dbeta", self._gate, f),
-            _want(dS0, "dS0", self._state, f, optional=True)))
+        ld = self._distances(q=q, k=k, v=v, dq=dq, dk=dk, dv=dv)
+        args = (*self._inputs(q, k, v, g, beta, seq_len, ld),
+                _want(dy, "dy", self._v, t), _want(dST, "dST", self._state, f, optional=True),
+                _tokens(dq, "dq", self._qk, ld["dq"], t), _tokens(dk, "dk", self._qk, ld["dk"], t),
+                _tokens(dv, "dv", self._v, ld["dv"], t),
+                _want(dg, "dg", self._gate, f), _want(dbeta, "dbeta", self._gate, f),
+                _want(dS0, "dS0", self._state, f, optional=True))
+        self._call(ld, self._lib.delta_loop_bwd, _stream(stream), *args)
 
     def bytes(self) -> int:
         """ll_delta_plan_bytes: device memory that the plan holds."""
