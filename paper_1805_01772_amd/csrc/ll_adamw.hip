@@ -19,8 +19,8 @@
 #include <new>
 #include <vector>
 
-#include "ll_device.h"
 #include "ll_host.h"
+#include "ll_stream.h"
 
 using ll::bf16_t;
 using ll::fail;

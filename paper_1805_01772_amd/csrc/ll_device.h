@@ -92,18 +92,6 @@ __device__ __forceinline__ uint4 ld16(const void* p) {
   return *reinterpret_cast<const uint4*>(p);
 }
 
-// 16 bytes that nothing reads again soon: past the caches (arrays larger than
-// the last-level cache, kLastLevelBytes, which they would only sweep).
-constexpr long kLastLevelBytes = 256L << 20;
-typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
-__device__ __forceinline__ void st16_stream(void* p, uint4 v) {
-  __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4*>(p));
-}
-__device__ __forceinline__ uint4 ld16_stream(const void* p) {
-  const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
-  return make_uint4(v[0], v[1], v[2], v[3]);
-}
-
 // ------------------------------------------------------ grid barrier
 // All work-groups of a cooperative launch arrive on a monotonically growing
 // counter; barrier number k (0-based) completes when the counter reaches

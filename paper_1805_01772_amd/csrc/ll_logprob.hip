@@ -28,8 +28,8 @@
 #include <algorithm>
 #include <new>
 
-#include "ll_device.h"
 #include "ll_host.h"
+#include "ll_stream.h"
 
 using ll::bf16_t;
 using ll::fail;
