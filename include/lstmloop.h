@@ -409,7 +409,9 @@ ll_status ll_eval_activations(int32_t device, const float* in, float* out, int64
  * time and its calls do not overlap; checkable errors come back at once and
  * enqueue nothing, data-dependent ones set bits of a device error word).  They
  * need no co-resident work-groups and allocate only when a plan is created, so
- * they may run beside the loops and be captured into graphs.
+ * they may run beside the loops and be captured into graphs.  A replay repeats
+ * the captured call with what it was given by value: pointers, sizes, and all of
+ * ll_adamw_hyper (see ll_adamw_step).
  */
 
 /* More device error word bits. */
@@ -644,6 +646,11 @@ ll_status ll_adamw_plan_destroy(ll_adamw_plan* plan);
  *   grad_scale  device float that multiplies every gradient (a clip factor, a
  *            loss scale's inverse), or NULL for 1.  If it is not finite the
  *            call changes nothing.
+ * hyper and the gradients' pointers are read during the call.  A captured step
+ * therefore repeats one step number, rate and seed on every replay: the bias
+ * corrections stand still, and so do the random bits of state_bits 8, whose
+ * codes no longer keep the mean.  Replays of it are not training steps; make
+ * each step's call anew, beside the graph of the rest.
  */
 ll_status ll_adamw_step(ll_adamw_plan* plan, void* stream, const void* const* grads,
                         const ll_adamw_hyper* hyper, const float* grad_scale);

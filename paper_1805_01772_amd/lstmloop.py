@@ -717,7 +717,9 @@ class AdamWPlan(_OpPlan):
     def step(self, grads: Sequence, lr: float, beta1: float = 0.9, beta2: float = 0.999,
              eps: float = 1e-8, step: int = 1, seed: int = 0, grad_scale=None, stream=None) -> None:
         """ll_adamw_step (asynchronous on `stream`): grads has a tensor, or None,
-        for each parameter; grad_scale a float32 tensor of one value, or None."""
+        for each parameter; grad_scale a float32 tensor of one value, or None.
+        Captured into a graph it repeats this lr, step and seed: call it anew for
+        every step instead."""
         if len(grads) != len(self._sizes):
             raise ValueError(f"{len(self._sizes)} tensors, but {len(grads)} gradients")
         ptrs, dtype = self._ptrs, self._grad_type
