@@ -466,7 +466,8 @@ ll_status ll_delta_plan_set_ld(ll_delta_plan* plan, const int64_t* ld);
  *   q, k     [T_max,B,Hk,Dk], v [T_max,B,Hv,Dv] dtype, tokens q_ld, k_ld, v_ld
  *            apart.  Entries at t >= seq_len[b] may hold anything (NaN).
  *   g, beta  [T_max,B,Hv] float.  g is the logarithm of the decay (minus
- *            infinity forgets the state).
+ *            infinity forgets a state of finite values; its gradient is 0 where
+ *            the decay is 0 in float, below -104).
  *   seq_len  [B] int32 in [0, T_max], or NULL: every row has T_max tokens.  A
  *            length outside counts as 0 and sets LL_DEVERR_SEQ_LEN.
  *   S0       [B,Hv,Dk,Dv] float, or NULL for zeros.

@@ -13,7 +13,8 @@
 //   dQ = scale diag(e^G) dY S0^T + F K
 //   dK = F^T Q + diag(e^{G_end - G}) U dS'^T - diag(e^G) dR S0^T + (H + H^T) K
 //   dbeta_i = Z_i.U_i / beta_i
-//   dg_t = sum_{i >= t} (dq_i.q_i - dv_i.v_i) + <dS', S'>   (i within the chunk)
+//   dg_t = sum_{i >= t} (dq_i.q_i - dv_i.v_i) + <dS', S'>   (i within the chunk);
+//   0 where e^{g_t} is 0 in float32: the sum's terms cancel there
 // beta counts as at least 2^-40 in magnitude, so that U_i / beta_i exists.
 //
 // Kernels: prep (T, P and the transposes of every chunk at once), state_fwd (S,
@@ -1344,7 +1345,8 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
       for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) all += part[i][j];
-      if (t0 + at < a.T) a.dg[((long)(t0 + at) * a.B + b) * a.Hv + h] = t0 + at < len ? (float)(s + all) : 0.f;
+      const bool kept = G[at] - (at ? G[at - 1] : 0.) >= -104.;     // e^-104 < 2^-150
+      if (t0 + at < a.T) a.dg[((long)(t0 + at) * a.B + b) * a.Hv + h] = t0 + at < len && kept ? (float)(s + all) : 0.f;
     }
   }
   const int crow = 16 * w + 4 * hi_, rows = a.T - t0 - crow;
