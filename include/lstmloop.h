@@ -427,7 +427,8 @@ ll_status ll_eval_activations(int32_t device, const float* in, float* out, int64
  * h reads key head h / (Hv / Hk).
  *   T_max, B, Hk, Hv, Dk, Dv >= 1; Hv a multiple of Hk; Dk <= 128, Dv <= 512,
  *     both multiples of 8, a time step of v, y and dv (B tokens with their
- *     strides) at most 2^26 bytes (else LL_EUNSUPPORTED); dtype an ll_dtype, the type
+ *     strides) at most 2^26 bytes, B Hv ceil(T_max / 64) < 2^23 (one token: B Hv
+ *     ceil(Dv / 32) < 2^24; else LL_EUNSUPPORTED); dtype an ll_dtype, the type
  *     of q, k, v, y and their gradients (g, beta, states and their gradients
  *     are float).  Inside, sums, states and everything between two products
  *     are held in float, products keep float's 24 bits.
@@ -523,7 +524,7 @@ ll_status delta_loop_step(const ll_delta_desc* desc, void* stream, const void* q
 /*
  * Log probabilities of given tokens under softmax(logits), with the entropy
  * and the most likely alternatives, and their gradient.
- *   N rows at most, V columns >= 1; dtype the logits' type; top_k in [0, 32],
+ *   N rows at most, N < 2^24, V columns in [1, 2^28]; dtype the logits' type; top_k in [0, 32],
  *   at most V; ld: elements from row to row (0: V; any ld >= V, rows need the
  *   alignment of an element only).
  */
@@ -614,7 +615,7 @@ typedef struct {
   void* v;
   float* m_scale;    /* state_bits 8 only */
   float* v_scale;
-  int64_t n;         /* elements, >= 0 */
+  int64_t n;         /* elements, >= 0; in all < 2^36 */
   float weight_decay;
   int32_t reserved;  /* must be 0 */
 } ll_adamw_tensor;

@@ -300,8 +300,9 @@ ll_status build(ll_adamw_plan* p, const ll_adamw_tensor* ts) {
     if (q8 && (((uintptr_t)t.m_scale | (uintptr_t)t.v_scale) & 3))
       return fail(LL_EINVAL, "tensor %d: the scales are not 4-byte aligned", i);
     const long c = (long)((t.n + ll::kAdamChunk - 1) / ll::kAdamChunk);
-    if (chunks + c > (long)1 << 30)
-      return fail(LL_EUNSUPPORTED, "more than 2^42 elements in one plan (at tensor %d)", i);
+    if (chunks + c > ll::max_groups(256))
+      return fail(LL_EUNSUPPORTED, "more than 2^24 - 1 chunks of %d elements in one plan (at tensor %d)",
+                  ll::kAdamChunk, i);
     recs.push_back(ll::AdamTensor{t.p, static_cast<bf16_t*>(t.copy), t.m, t.v, t.m_scale, t.v_scale, (long)t.n,
                                   (int)chunks, t.weight_decay});
     p->chunk0.push_back((int)chunks);

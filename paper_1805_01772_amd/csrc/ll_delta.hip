@@ -148,9 +148,13 @@ ll_status validate(const ll_delta_desc* d, bool step) {
     return fail(LL_EUNSUPPORTED, "a time step of v, y or dv spans %lld bytes (at most 2^26)",
                 (long long)(widest * d->B * es));
   const int64_t nch = (d->T_max + ll::kDeltaChunk - 1) / ll::kDeltaChunk;
-  if ((int64_t)d->B * d->Hv > 1 << 24 || (int64_t)d->B * d->Hv * nch > 1 << 26)
-    return fail(LL_EUNSUPPORTED, "B * Hv = %lld (at most 2^24) with T_max = %d: more than 2^26 chunks",
-                (long long)d->B * d->Hv, d->T_max);
+  // work-groups of the largest launch: a chunk and head each (512 threads), or the step's column tiles
+  const int64_t groups = step ? (int64_t)d->B * d->Hv * ((d->Dv + ll::kStepCols - 1) / ll::kStepCols)
+                              : (int64_t)d->B * d->Hv * nch;
+  const int64_t most = ll::max_groups(step ? 256 : 512);
+  if ((int64_t)d->B * d->Hv > 1 << 24 || groups > most)
+    return fail(LL_EUNSUPPORTED, "B * Hv = %lld with T_max = %d and Dv = %d: %lld work-groups, a launch holds %lld",
+                (long long)d->B * d->Hv, d->T_max, d->Dv, (long long)groups, (long long)most);
   return LL_OK;
 }
 

@@ -21,6 +21,9 @@ ll_status check_device(int device);
 // NULL) and clears it.
 ll_status read_error_word(int* word, int32_t* out);
 
+// Work-items of a launch are counted in 32 bits: work-groups of `threads` that one holds.
+constexpr int64_t max_groups(int threads) { return (((int64_t)1 << 32) - 1) / threads; }
+
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 class DeviceGuard {

@@ -724,8 +724,8 @@ ll_status ll_logprob_plan_create(const ll_logprob_desc* d, int device, ll_logpro
   if (!out) return fail(LL_EINVAL, "out is NULL");
   *out = nullptr;
   if (!d) return fail(LL_EINVAL, "desc is NULL");
-  if (d->N < 1 || d->N > 1 << 24 || d->V < 1 || d->V > 1 << 28)
-    return fail(LL_EINVAL, "N = %d must be 1 .. 2^24 and V = %d 1 .. 2^28", d->N, d->V);
+  if (d->N < 1 || d->N > ll::max_groups(256) || d->V < 1 || d->V > 1 << 28)
+    return fail(LL_EINVAL, "N = %d must be 1 .. 2^24 - 1 and V = %d 1 .. 2^28", d->N, d->V);
   if (d->dtype != LL_F32 && d->dtype != LL_BF16) return fail(LL_EINVAL, "dtype must be LL_F32 or LL_BF16");
   if (d->top_k < 0 || d->top_k > ll::kTopMax || d->top_k > d->V)
     return fail(LL_EINVAL, "top_k = %d must be 0 .. %d and at most V", d->top_k, ll::kTopMax);
@@ -853,7 +853,7 @@ ll_status ll_logprob_fwd_bwd(ll_logprob_plan* p, void* stream, int32_t rows, con
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   // 1024 threads and 64 KB of a row in LDS, or 256 and 16 (4096 rows of bfloat16: 50000
   // take 188 us against 199, 32000 133 against 132, 10000 63 against 41)
-  const bool wide = row_bytes(p) >= 64 << 10;
+  const bool wide = row_bytes(p) >= 64 << 10 && rows <= ll::max_groups(1024);
   if (p->d.dtype == LL_BF16) {
     if (wide) ll::logprob_fwd_bwd_kernel<bf16_t, 1024, 4><<<dim3(rows), dim3(1024), 0, s>>>(a);
     else ll::logprob_fwd_bwd_kernel<bf16_t, 256, 4><<<dim3(rows), dim3(256), 0, s>>>(a);
