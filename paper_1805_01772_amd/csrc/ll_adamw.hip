@@ -15,6 +15,7 @@
 // largest magnitude by six exchanges.  Everything that a code depends on is
 // rounded operation by operation (no contraction), so that the same state and
 // gradient give the same codes on any path that does the same.
+#include <algorithm>
 #include <cmath>
 #include <new>
 #include <vector>
@@ -46,6 +47,7 @@ struct AdamArgs {
   const float* grad_scale;
   int chunk0, tensor0;                 // of this launch
   float b1, c1, b2, c2, r1, r2, eps, lr;
+  float lift;                          // power of two that makes eps a normal number
   uint32_t seed;
   const void* grads[kGradsPerLaunch];
 };
@@ -59,8 +61,14 @@ __device__ __forceinline__ Adam1 adam_one(const AdamArgs& a, float p, float m, f
   Adam1 r;
   r.m = m * a.b1 + g * a.c1;
   r.v = v * a.b2 + (g * g) * a.c2;
-  const float den = __builtin_amdgcn_sqrtf(r.v) * a.r2 + a.eps;
-  const float step = (r.m * a.r1) * __builtin_amdgcn_rcpf(den);
+  // Root and reciprocal by the instructions, one unit off at most.  They take subnormal
+  // numbers for 0, so v is lifted out of them, and den where eps is that small.  (The
+  // exact root and quotient: 920 us against 837 of the large 8-bit case.)
+  const bool sub = r.v < 0x1p-126f;
+  float root = __builtin_amdgcn_sqrtf(sub ? r.v * 0x1p24f : r.v);
+  root = sub ? root * 0x1p-12f : root;
+  const float den = root * a.r2 + a.eps;
+  const float step = (r.m * a.r1 * a.lift) * __builtin_amdgcn_rcpf(den * a.lift);
   r.p = p * keep - step * a.lr;
   return r;
 }
@@ -387,8 +395,9 @@ ll_status ll_adamw_step(ll_adamw_plan* p, void* stream, const void* const* grads
   a.c2 = (float)(1.0 - h->beta2);
   a.r1 = (float)(1.0 / (1.0 - std::pow(h->beta1, (double)h->step)));
   a.r2 = (float)(1.0 / std::sqrt(1.0 - std::pow(h->beta2, (double)h->step)));
-  a.eps = (float)h->eps;
+  a.eps = std::max((float)h->eps, 0x1p-149f);
   a.lr = (float)h->lr;
+  a.lift = a.eps < 0x1p-100f ? 0x1p48f : 1.f;
   a.seed = h->seed;
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
   for (int t0 = 0; t0 < n; t0 += ll::kGradsPerLaunch) {
