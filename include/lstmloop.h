@@ -439,6 +439,8 @@ ll_status ll_eval_activations(int32_t device, const float* in, float* out, int64
  *     and dv) may be slices of the rows of one projection; a token's stride is
  *     a multiple of 16 bytes.
  *   scale  0 means 1 / sqrt(Dk).
+ * g, beta, their gradients, seq_len, slots and device_error need 4 bytes'
+ * alignment, every other array 16.
  */
 typedef struct {
   int32_t T_max, B, Hk, Hv, Dk, Dv;
@@ -525,8 +527,10 @@ ll_status delta_loop_step(const ll_delta_desc* desc, void* stream, const void* q
  * Log probabilities of given tokens under softmax(logits), with the entropy
  * and the most likely alternatives, and their gradient.
  *   N rows at most, N < 2^24, V columns in [1, 2^28]; dtype the logits' type; top_k in [0, 32],
- *   at most V; ld: elements from row to row (0: V; any ld >= V, rows need the
- *   alignment of an element only).
+ *   at most V; ld: elements from row to row (0: V; any ld >= V).
+ *   logits and dlogits need the alignment of an element only, every other
+ *   array 4 bytes.  (A gradient is written an element at a time where dlogits
+ *   and logits differ modulo 16 bytes.)
  */
 typedef struct {
   int32_t N, V;

@@ -179,15 +179,6 @@ void release(ll_delta_plan* p) {
     if (m) (void)hipFree(m);
 }
 
-ll_status misaligned(const char* name, const void* p) {
-  return fail(LL_EINVAL, "%s = %p is not 16-byte aligned", name, p);
-}
-
-#define LL_ALIGNED(p) \
-  do {                \
-    if (!ll::aligned16(p)) return misaligned(#p, p); \
-  } while (0)
-
 }  // namespace
 
 extern "C" {
@@ -284,8 +275,8 @@ ll_status delta_loop_fwd(ll_delta_plan* p, void* stream, const void* q, const vo
   if (!q || !k || !v || !g || !beta || !y) return fail(LL_EINVAL, "q, k, v, g, beta and y are required");
   if (save_for_backward && p->d.inference)
     return fail(LL_EINVAL, "the plan was created for inference: it keeps nothing for the gradient");
-  LL_ALIGNED(q); LL_ALIGNED(k); LL_ALIGNED(v); LL_ALIGNED(g); LL_ALIGNED(beta); LL_ALIGNED(seq_len);
-  LL_ALIGNED(S0); LL_ALIGNED(y); LL_ALIGNED(ST);
+  LL_ALIGNED(q, 16); LL_ALIGNED(k, 16); LL_ALIGNED(v, 16); LL_ALIGNED(y, 16); LL_ALIGNED(S0, 16); LL_ALIGNED(ST, 16);
+  LL_ALIGNED(g, 4); LL_ALIGNED(beta, 4); LL_ALIGNED(seq_len, 4);
   ll::DeviceGuard guard(p->device);
   DeltaArgs a = p->a;
   a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta; a.seq_len = seq_len; a.S0 = S0; a.y = y; a.ST = ST;
@@ -314,8 +305,9 @@ ll_status delta_loop_bwd(ll_delta_plan* p, void* stream, const void* q, const vo
     return fail(LL_EINVAL, "q, k, v, g, beta or seq_len differs from the saved forward's");
   if (!dy || !dq || !dk || !dv || !dg || !dbeta)
     return fail(LL_EINVAL, "dy, dq, dk, dv, dg and dbeta are required");
-  LL_ALIGNED(dy); LL_ALIGNED(dST); LL_ALIGNED(dq); LL_ALIGNED(dk); LL_ALIGNED(dv); LL_ALIGNED(dg);
-  LL_ALIGNED(dbeta); LL_ALIGNED(dS0);
+  LL_ALIGNED(dy, 16); LL_ALIGNED(dST, 16); LL_ALIGNED(dq, 16); LL_ALIGNED(dk, 16); LL_ALIGNED(dv, 16);
+  LL_ALIGNED(dS0, 16);
+  LL_ALIGNED(dg, 4); LL_ALIGNED(dbeta, 4);
   ll::DeviceGuard guard(p->device);
   DeltaArgs a = p->a;
   a.dy = dy; a.dST = dST; a.dq = dq; a.dk = dk; a.dv = dv; a.dg = dg; a.dbeta = dbeta; a.dS0 = dS0;
@@ -340,8 +332,8 @@ ll_status delta_loop_step(const ll_delta_desc* desc, void* stream, const void* q
     return fail(LL_EINVAL, "q, k, v, g, beta, S and y are required");
   if (n_slots < 1 || (!slots && n_slots < desc->B))
     return fail(LL_EINVAL, "n_slots = %d is too small for B = %d rows", n_slots, desc->B);
-  LL_ALIGNED(q); LL_ALIGNED(k); LL_ALIGNED(v); LL_ALIGNED(g); LL_ALIGNED(beta); LL_ALIGNED(S);
-  LL_ALIGNED(slots); LL_ALIGNED(y); LL_ALIGNED(device_error);
+  LL_ALIGNED(q, 16); LL_ALIGNED(k, 16); LL_ALIGNED(v, 16); LL_ALIGNED(y, 16); LL_ALIGNED(S, 16);
+  LL_ALIGNED(g, 4); LL_ALIGNED(beta, 4); LL_ALIGNED(slots, 4); LL_ALIGNED(device_error, 4);
   const DeltaArgs z = sizes(*desc);
   ll::DeltaStepArgs a{};
   a.B = z.B; a.Hk = z.Hk; a.Hv = z.Hv; a.Dk = z.Dk; a.Dv = z.Dv; a.n_slots = n_slots;

@@ -24,7 +24,8 @@ ll_status read_error_word(int* word, int32_t* out);
 // Work-items of a launch are counted in 32 bits: work-groups of `threads` that one holds.
 constexpr int64_t max_groups(int threads) { return (((int64_t)1 << 32) - 1) / threads; }
 
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+inline bool aligned_to(const void* p, unsigned bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+inline bool aligned16(const void* p) { return aligned_to(p, 16); }
 
 class DeviceGuard {
  public:
@@ -48,6 +49,13 @@ class DeviceGuard {
     hipError_t e_ = (call);                                                       \
     if (e_ != hipSuccess)                                                         \
       return ll::fail(LL_EHIP, "%s failed: %s", #call, hipGetErrorString(e_));    \
+  } while (0)
+
+// Refuses an argument that is not aligned to `bytes`.
+#define LL_ALIGNED(p, bytes)                                                      \
+  do {                                                                            \
+    if (!ll::aligned_to(p, bytes))                                                \
+      return ll::fail(LL_EINVAL, "%s = %p is not %d-byte aligned", #p, (const void*)(p), (int)(bytes)); \
   } while (0)
 
 #define LL_STATUS(call)         \
