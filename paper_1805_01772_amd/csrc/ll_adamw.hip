@@ -325,7 +325,7 @@ ll_status build(ll_adamw_plan* p, const ll_adamw_tensor* ts) {
   LL_STATUS(ll::dalloc((void**)&p->tensor_of, sizeof(int) * of.size(), "the chunk table"));
   LL_HIP(hipMemcpy(p->tensors, recs.data(), sizeof(ll::AdamTensor) * recs.size(), hipMemcpyHostToDevice));
   if (!of.empty()) LL_HIP(hipMemcpy(p->tensor_of, of.data(), sizeof(int) * of.size(), hipMemcpyHostToDevice));
-  return LL_OK;
+  return ll::wait_created();
 }
 
 }  // namespace

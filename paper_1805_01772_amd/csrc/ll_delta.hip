@@ -237,6 +237,11 @@ ll_status ll_delta_plan_create(const ll_delta_desc* desc, int device, ll_delta_p
     delete p;
     return fail(LL_EHIP, "hipMemset of the error word failed");
   }
+  if (const ll_status s = ll::wait_created(); s != LL_OK) {
+    release(p);
+    delete p;
+    return s;
+  }
   *out = p;
   return LL_OK;
 }

@@ -21,6 +21,13 @@ ll_status check_device(int device);
 // NULL) and clears it.
 ll_status read_error_word(int* word, int32_t* out);
 
+// What a plan's creation wrote (on the default stream) is there for calls on any stream,
+// also for those that do not wait for the default one.
+inline ll_status wait_created() {
+  const hipError_t e = hipStreamSynchronize(nullptr);
+  return e == hipSuccess ? LL_OK : fail(LL_EHIP, "waiting for the plan's memory failed: %s", hipGetErrorString(e));
+}
+
 // Work-items of a launch are counted in 32 bits: work-groups of `threads` that one holds.
 constexpr int64_t max_groups(int threads) { return (((int64_t)1 << 32) - 1) / threads; }
 

@@ -687,7 +687,8 @@ namespace {
 int elem_bytes(const ll_logprob_plan* p) { return p->d.dtype == LL_BF16 ? 2 : 4; }
 long row_bytes(const ll_logprob_plan* p) { return (long)p->d.V * elem_bytes(p); }
 
-// Rows of the two start at different places between 16-byte borders.
+// Rows of the two start at different places between 16-byte borders: stores by elements
+// (4096 rows of 131072 bfloat16 813 us against 425, 1024 of 100000 floats 174 and 167).
 bool lie_apart(const void* x, const void* y) {
   return ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(y)) & 15) != 0;
 }
@@ -767,6 +768,7 @@ ll_status ll_logprob_plan_create(const ll_logprob_desc* d, int device, ll_logpro
   if (st == LL_OK && (hipMemset(p->a.arrived, 0, sizeof(unsigned) * split) != hipSuccess ||
                       hipMemset(p->a.err, 0, sizeof(int)) != hipSuccess))
     st = fail(LL_EHIP, "hipMemset of the arrivals or the error word failed");
+  if (st == LL_OK) st = ll::wait_created();
   if (st != LL_OK) {
     release(p);
     delete p;
