@@ -506,7 +506,8 @@ ll_status delta_loop_bwd(ll_delta_plan* plan, void* stream, const void* q, const
 ll_status ll_delta_status_sync(ll_delta_plan* plan, int32_t* device_error);
 
 /*
- * One token for B rows, states updated in place, no plan (serving).
+ * One token for B rows, states updated in place, no plan (serving).  Launches on
+ * the calling thread's current device, whose tensors these have to be.
  *   desc     as above with T_max = 1; inference and dq_ld .. dv_ld are ignored.
  *   q, k     [B,Hk,Dk], v [B,Hv,Dv] dtype (rows q_ld, k_ld, v_ld apart),
  *            g, beta [B,Hv] float, y [B,Hv,Dv] dtype.
@@ -608,7 +609,9 @@ ll_status ll_logprob_status_sync(ll_logprob_plan* plan, int32_t* device_error);
  * codes are rounded up or down at random, so that their mean is the value (a
  * slow average would stand still otherwise), from a hash of the element's
  * place, the tensor's number and `seed`; a positive v never becomes 0.  Zeroed
- * codes and scales are the state before the first step.
+ * codes and scales are the state before the first step.  A moment that is not
+ * finite makes its row's scale so, and with the next step all 256 elements of
+ * the row NaN; a row whose largest v is below 5e-29 loses bits of it.
  */
 #define LL_ADAMW_ROW 256
 

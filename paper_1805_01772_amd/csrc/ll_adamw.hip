@@ -7,8 +7,8 @@
 // elements in flight.  Gradients move from step to step, so their pointers
 // travel in the kernel's arguments, kGradsPerLaunch of them a launch.
 // Measured: 247 million parameters in 40 tensors, 32-bit states and the copy 1355 us
-// (7.4 GB, 5.5 TB/s, as a copy of that size), 8-bit states and bfloat16 gradients 855 us
-// (4.0 GB, 4.6 TB/s; the roots and hashes of the codes keep it from the rest); 48 tensors
+// (7.4 GB, 5.5 TB/s; a copy of 8 GB reaches 4.7), 8-bit states and bfloat16 gradients 837 us
+// (4.0 GB, 4.7 TB/s; the roots and hashes of the codes keep it from the rest); 48 tensors
 // of 0.4 million in 7 us.
 //
 // An 8-bit row of 256 elements is one wave's: four elements a lane, the row's

@@ -199,7 +199,8 @@ __device__ __forceinline__ void wave_lds_fence() {
 // block column), then everything the loops read in the order in which a lane
 // reads it, 16 bytes at a time.
 // Bound: HBM, for what it writes (K, Q, T and P, plain and transposed, in pieces):
-// 8 rows 103 us, 0.6 GB; one row 132 us; prompts 27 us.
+// 8 rows 107 us, 0.6 GB; one row 134 us; prompts 27 us.  (float32 keeps k and q in LDS in
+// pieces, 73 KB at 64 columns and 122 KB at 128: two work-groups and one a compute unit.)
 // ---------------------------------------------------------------------------
 template <typename T, int KS, bool SAVE>
 __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
@@ -565,10 +566,10 @@ __device__ void zero_rest(T* out, long tok_ld, const DeltaArgs& a, const Walk& k
 // rows 240 against 224).  The waves that make Y load in the phase in which they
 // have nothing to multiply, and S and U are stored in the second phase: 8 rows 226
 // -> 215 us, one row 657 -> 630.
-// Bound: with few heads a chunk's three products one after the other, 2.5 us a chunk
+// Bound: with few heads a chunk's three products one after the other, 2.6 us a chunk
 // with 16 columns (1.5 of them when nothing else runs on the compute unit): one
-// row 630 us for 256 chunks; with many the traffic of the operands and of what is
-// kept for the gradient: 8 rows 215 us, 0.85 GB, 4 TB/s; prompts 42 us.
+// row 655 us for 256 chunks, on half of the compute units; with many the traffic of the operands and of what is
+// kept for the gradient: 8 rows 228 us, 0.85 GB, 3.7 TB/s; prompts 45 us.
 // ---------------------------------------------------------------------------
 template <typename T, int KS, int NL, bool SAVE>
 __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
@@ -764,7 +765,7 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
 // state_bwd: the gradient loop, the same split.  Waves 0-3 carry dS: K dS, T^T dU,
 // K^T dR.  Waves 4-7 make what does not depend on it, P^T dY and Q^T (scale e^G
 // dY), one chunk ahead, each for the chain wave of its rows (through LDS, in the
-// accumulators' order).  Bound as state_fwd: 8 rows 235 us, one row 630 us.
+// accumulators' order).  Bound as state_fwd: 8 rows 233 us, one row 650 us.
 // ---------------------------------------------------------------------------
 template <typename T, int KS, int NL>
 __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
@@ -999,7 +1000,7 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
 // wave for itself from global memory they took 10 of 52 thousand cycles a head's
 // chunk.  Bound: HBM in the walk (U, dR and both states of every chunk, 5 TB/s),
 // which stands still while F, H and what follows are made, since LDS holds one
-// work-group: 8 rows 317 us, 1.2 GB, 3.8 TB/s; one row 357 us.
+// work-group (133 KB): 8 rows 326 to 345 us, 1.2 GB, 3.6 TB/s; one row 376 us.
 // ---------------------------------------------------------------------------
 template <typename T, int KS>
 __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
@@ -1366,10 +1367,12 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
 namespace {
 
 // Columns of the state per work-group, in 16s: 32 where that still gives every
-// compute unit a work-group (16 read the chunk's operands twice as often): inference
-// over 1000 tokens with 16 heads of 128 columns, 32 against 16 columns, takes 276
-// against 305 us for 16 rows, 1016 against 1162 for 64; for 2 rows
-// it is 59 against 48, for one row of 16384, forward and gradient, 1578 against 1290.
+// compute unit a work-group (16 read the chunk's operands twice as often).  32 against
+// 16 columns, 16 heads of 128 columns: inference over 1000 tokens takes 280 against 322
+// us for 16 whole rows and 800 against 920 for 64 of 100 to 1000 tokens (8 of those:
+// 105 against 95), 8 rows' forward and gradient 816 against 897, as many of 2048 tokens
+// 990 against 1215; for 2 rows' inference it is 59 against 46, for one row of 16384,
+// forward and gradient, 2127 against 1800.
 int cols_of(const DeltaArgs& a, int cus) {
   return a.Dv > 16 && (long)a.B * a.Hv * ((a.Dv + 31) / 32) >= cus ? 2 : 1;
 }

@@ -19,11 +19,12 @@
 //
 // Rows are walked in 16-byte chunks from the first aligned element; up to 7
 // elements before and after are done singly.
-// Bound: HBM.  Forward: one pass, 2047 rows of 50001 floats with 16 alternatives in
-// 97 us with the launch (4.2 TB/s; the selection is 17 us of it).  Gradient in a call of its own: two
-// passes.  Both in one: the first 64 KB of a long row (16 KB of a short one) stay in
-// LDS, the rest is read again from the last-level cache on the whole; 4096 rows of
-// 131072 bfloat16 in 450 us, 2.1 GB of traffic that cannot be saved at 4.8 TB/s.
+// Bound: HBM.  Forward: one pass, 2047 rows of 50001 floats in 72 us (5.7 TB/s), with 16
+// alternatives in 97.  Gradient in a call of its own: two passes, 4096 rows of 131072
+// bfloat16 in 423 us (5.1 TB/s), 1024 of 100000 floats in 166 (4.9).  Both in one: the
+// first 64 KB of a long row (16 KB of a short one) stay in LDS, the rest is read again
+// from the last-level cache on the whole; 4096 rows of 131072 bfloat16 in 445 to 461 us,
+// 2.1 GB of traffic that cannot be saved at 4.7 TB/s, 4096 of 32000 floats in 193 (5.4).
 // A few rows: latency, 8 rows of 32000 bfloat16 with 8 alternatives in 10 us.
 #include <algorithm>
 #include <new>
@@ -535,7 +536,7 @@ __device__ float lse_rest(const T* row, int V, float lse, float* part) {
 // Below this an lse's rounding is at most 2^-20 of p, of the size that the exponent's
 // own rounding leaves, and the row is not read again (4096 rows of 131072 bfloat16: 423
 // us, 560 where it is; 1024 of 100000 floats 166 and 201).
-__device__ __forceinline__ bool lse_is_short(float lse) {
+__device__ __forceinline__ bool lse_is_coarse(float lse) {
   return __builtin_fabsf(lse) >= 32.f && lse != -__builtin_inff();
 }
 
@@ -547,7 +548,7 @@ __global__ __launch_bounds__(256) void logprob_rest_kernel(LogprobArgs a) {
   __shared__ float part[4];
   const long r = blockIdx.x;
   const float lse = a.lse_in[r];
-  const float z = lse_is_short(lse) ? lse_rest<T, 256>(static_cast<const T*>(a.x) + r * a.ld, a.V, lse, part) : 0.f;
+  const float z = lse_is_coarse(lse) ? lse_rest<T, 256>(static_cast<const T*>(a.x) + r * a.ld, a.V, lse, part) : 0.f;
   if (threadIdx.x == 0) a.rest[r] = z;
 }
 
@@ -645,7 +646,7 @@ __global__ __launch_bounds__(NTHR) void logprob_bwd_kernel(LogprobArgs a) {
   const T* row = static_cast<const T*>(a.x) + r * a.ld;
   const Span sp = span_of(row, a.V, blockIdx.x % a.parts, a.parts);
   const float lse = a.lse_in[r];
-  const float rest = a.rest ? a.rest[r] : lse_is_short(lse) ? lse_rest<T, NTHR>(row, a.V, lse, sums) : 0.f;
+  const float rest = a.rest ? a.rest[r] : lse_is_coarse(lse) ? lse_rest<T, NTHR>(row, a.V, lse, sums) : 0.f;
   row_gradient<T, NTHR>(a, row, static_cast<T*>(a.dx) + r * a.ld, r, sp, lse, rest,
                         a.dentropy ? a.ent_in[r] : 0.f, lse == -__builtin_inff(), mark, add, val);
 }
@@ -866,6 +867,9 @@ ll_status ll_logprob_fwd_bwd(ll_logprob_plan* p, void* stream, int32_t rows, con
   a.stream = past_caches(p, rows);
   a.apart = lie_apart(logits, dlogits);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  // One work-group a row, however few the rows: a part of a row would have to wait for the
+  // others' sums before it writes.  Few long rows are faster in the two calls (8 of 400000
+  // floats 13 + 10 us against 64, 8 of 131072 bfloat16 9 + 10 against 28).
   // 1024 threads and 64 KB of a row in LDS, or 256 and 16 (4096 rows of bfloat16: 50000
   // take 188 us against 199, 32000 133 against 132, 10000 63 against 41)
   const bool wide = row_bytes(p) >= 64 << 10 && rows <= ll::max_groups(1024);
