@@ -6,6 +6,7 @@
 namespace ll {
 
 constexpr int kDeltaChunk = 64;      // tokens per chunk
+constexpr int kDeltaDots = 10 * 2 * 256;   // products of a chunk's q and k on and below the diagonal, tiles of 16
 constexpr int kDeltaMaxDk = 128;
 constexpr int kDeltaMaxDv = 512;
 
@@ -41,6 +42,9 @@ struct DeltaArgs {
   // per item of a key head, zeros past the row's end and Dk: K and Q, 64 x
   // (32 ksteps), and their transposes
   bf16_t *kp, *qp, *ktp, *qtp;
+  // per item of a key head, kept for the gradient: q_i.k_j and k_i.k_j, tile by tile
+  // (row tile w, column tile m <= w: number w (w + 1) / 2 + m) as the accumulators hold them
+  float* dots;
   // per item, kept for the gradient
   float *st, *u;                     // entering state [Dk][Dv], U [64][Dv]
   float *dst, *dr;                   // gradient of the leaving state, of R

@@ -174,7 +174,7 @@ DeltaArgs sizes(const ll_delta_desc& d) {
 }
 
 void release(ll_delta_plan* p) {
-  void* all[] = {p->a.tp, p->a.pp, p->a.ttp, p->a.ptp, p->a.kp, p->a.qp, p->a.ktp, p->a.qtp, p->a.G, p->a.tok, p->a.st, p->a.u, p->a.dst, p->a.dr, p->a.err};
+  void* all[] = {p->a.tp, p->a.pp, p->a.ttp, p->a.ptp, p->a.kp, p->a.qp, p->a.ktp, p->a.qtp, p->a.dots, p->a.G, p->a.tok, p->a.st, p->a.u, p->a.dst, p->a.dr, p->a.err};
   for (void* m : all)
     if (m) (void)hipFree(m);
 }
@@ -214,6 +214,7 @@ ll_status ll_delta_plan_create(const ll_delta_desc* desc, int device, ll_delta_p
       {(void**)&p->a.ttp, sq, "the chunks' T^T", true},
       {(void**)&p->a.ptp, sq, "the chunks' P^T", true},
       {(void**)&p->a.qtp, tr, "the chunks' Q^T", true},
+      {(void**)&p->a.dots, sizeof(float) * ll::kDeltaDots * desc->B * desc->Hk * p->a.nch, "the chunks' products", true},
       {(void**)&p->a.G, sizeof(double) * items * C, "the sums of g", true},
       {(void**)&p->a.tok, sizeof(float4) * items * C, "the tokens' decays", false},
       {(void**)&p->a.err, sizeof(int), "the error word", false},

@@ -13,8 +13,11 @@
 //   dQ = scale diag(e^G) dY S0^T + F K
 //   dK = F^T Q + diag(e^{G_end - G}) U dS'^T - diag(e^G) dR S0^T + (H + H^T) K
 //   dbeta_i = Z_i.U_i / beta_i
-//   dg_t = sum_{i >= t} (dq_i.q_i - dv_i.v_i) + <dS', S'>   (i within the chunk);
-//   0 where e^{g_t} is 0 in float32: the sum's terms cancel there
+//   X_ij = F_ij q_i.k_j + H_ij k_i.k_j  (j < i),  what the pair's decay is worth
+//   dg_t = sum_{i >= t > j} X_ij + sum_{i >= t} (q_i.(scale e^{G_i} S0 dY_i) - k_i.(e^{G_i} S0 dR_i))
+//          + sum_{j < t} k_j.(e^{G_end - G_j} dS' U_j) + e^{G_end} <dS', S0>
+// and nothing that does not straddle t is in the sum, to be taken out again: it would leave
+// its rounding where e^{g_t} is small
 // beta counts as at least 2^-40 in magnitude, so that U_i / beta_i exists.
 //
 // Kernels: prep (T, P and the transposes of every chunk at once), state_fwd (S,
@@ -157,6 +160,48 @@ __device__ __forceinline__ float sum16(float x) {
   return x + moved<0x128>(x);                            // the row turned by 8
 }
 
+// The same in double, by two moves of 32 bits.
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ double moved2(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t a = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xf, false);
+  const uint32_t b = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)b << 32 | a);
+}
+__device__ __forceinline__ double sum16(double x) {
+  x += moved2<0xb1>(x);
+  x += moved2<0x4e>(x);
+  x += moved2<0x141>(x);
+  return x + moved2<0x128>(x);
+}
+// Sum over the lanes lo, lo + 16, lo + 32, lo + 48, in every one of them.
+__device__ __forceinline__ float sum_rows(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t v = __float_as_uint(__uint_as_float(a[0]) + __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+// Sums over the lanes up to this one: of its row of 16, of all 64.
+constexpr int kUpOne = 0x111;                            // the lane below's, 0 in a row's first
+__device__ __forceinline__ float scan16(float x) {
+  x += moved<kUpOne>(x);
+  x += moved<0x112>(x);                                  // by 2, 4, 8
+  x += moved<0x114>(x);
+  return x + moved<0x118>(x);
+}
+__device__ __forceinline__ double scan16(double x) {
+  x += moved2<kUpOne>(x);
+  x += moved2<0x112>(x);
+  x += moved2<0x114>(x);
+  return x + moved2<0x118>(x);
+}
+__device__ __forceinline__ double scan64(double x) {
+  x = scan16(x);
+  x += moved2<0x142, 0xa>(x);                            // a row's last lane to the next row, odd rows
+  return x + moved2<0x143, 0xc>(x);                      // lane 31 to the upper half
+}
+
 // Rows crow .. crow + 3 of column lo (a tile of the accumulators) to dst: float as
 // they are, bfloat16 two columns a store, even lanes the even rows.
 template <typename T>
@@ -282,6 +327,15 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
         for (int e = 0; e < NP; ++e) kb[e] = lds_frag(kp + (e * CT + 16 * m + lo) * KP + 32 * s + 8 * hi);
         mma<NP, NP, 2>(ka, kb, kk[m]);
         mma<NP, NP, 2>(qa, kb, qk[m]);
+      }
+  }
+  if (SAVE && first) {
+    f32x4* x = reinterpret_cast<f32x4*>(a.dots + kitem * kDeltaDots) + w * (w + 1) * 64 + l;
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+      if (m <= w) {
+        x[m * 128] = qk[m];
+        x[m * 128 + 64] = kk[m];
       }
   }
   if (first) {
@@ -1015,7 +1069,11 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
   __shared__ __align__(16) bf16_t pool[kPool > kEnd ? kPool : kEnd];
   __shared__ float4 tok[CT];
   __shared__ double G[CT];
-  __shared__ float dG[2][CT], part[8][4], sub[CT], sbeta[CT];
+  __shared__ float part[8][4], sbeta[CT];
+  // sums of X: of row i over column tile jt < its own; for column t over the rows >= t of
+  // row tile w and the columns below t of t's tile
+  __shared__ float rowsX[3][CT], colsX[4][CT];
+  __shared__ float nearS[2][CT], farS[2][CT];            // the tokens' terms with S0, with dS'
   // tokens' buffer: dY [NP][64][CP], U [3][64][CP], dR [3][64][CP]; states': S
   // [3][DR][CP], dS [3][DR][CP]
   constexpr int kU = NP * CT * CP, kR = kU + 3 * CT * CP, kD = 3 * DR * CP;
@@ -1053,6 +1111,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
   const long kitem = bk * (long)a.nch + n;
   const rsrc_t rk = make_rsrc(a.ktp + kitem * NP * DP * CT, NP * DP * CT * 2);
   const rsrc_t rq = make_rsrc(a.qtp + kitem * NP * DP * CT, NP * DP * CT * 2);
+  const rsrc_t rx = make_rsrc(a.dots + kitem * kDeltaDots, kDeltaDots * 4);
   // K or Q at the results' places (rows crow .. crow + 3 of a column), as the
   // transposes hold them: four neighbours of one fragment
   auto column = [&](const bf16_t* tr, int i) {
@@ -1071,10 +1130,10 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
   // addresses live in registers)
   const int h8 = 8 * hi_ ^ swap8(lo_);
   const int row = tid >> 3, rc = (tid & 7) * 4, wc = rc ^ swap8(row);
-  const long yrow = (long)a.B * a.Hv * a.Dv, vrow = (long)a.B * a.v_ld;
+  const long yrow = (long)a.B * a.Hv * a.Dv;
   struct alignas(4 * sizeof(T)) Four { T x[4]; };
   f32x4 fs, fd, fu, fr;
-  Four fy, fv;
+  Four fy;
   auto load4 = [&](rsrc_t r, unsigned off, Four& f) {
     if constexpr (NP == 1) f = __builtin_bit_cast(Four, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
     else f = __builtin_bit_cast(Four, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
@@ -1094,9 +1153,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
       const int tv = min(8, len - t0 - 8 * wave);          // the wave's eight rows: its tokens
       const long tok0 = (long)(t0 + 8 * wave) * a.B + b;
       const rsrc_t ry = rows_rsrc(static_cast<const T*>(a.dy) + (tok0 * a.Hv + h) * a.Dv, tv, yrow, a.Dv);
-      const rsrc_t rv = rows_rsrc(static_cast<const T*>(a.v) + tok0 * a.v_ld + (long)h * a.Dv, tv, vrow, a.Dv);
       load4(ry, in ? (unsigned)(((row & 7) * yrow + c0 + rc) * (long)sizeof(T)) : kNowhere, fy);
-      load4(rv, in ? (unsigned)(((row & 7) * vrow + c0 + rc) * (long)sizeof(T)) : kNowhere, fv);
     }
   };
   fetch(hk * grp, 0, 0);
@@ -1107,7 +1164,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
 #pragma unroll
     for (int i = 0; i < ND; ++i) aq[i] = ku[i] = kr[i] = zero_acc();
     F[0] = F[1] = H[0] = H[1] = zero_acc();
-    float ss = 0.f, ub = 0.f, vr = 0.f;
+    float ss = 0.f, ub = 0.f;
     // the fetched step into the buffers (cb: of the tokens, sb: of the states)
     auto split = [&](int hs, int cb, int sb) {
       bf16_t* S = pool + 2 * kTok + sb * kState;
@@ -1124,7 +1181,6 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
         for (int e = 0; e < 4; ++e) {
           y[e] = Op<T>::to_f32(fy.x[e]);
           ub += fr[e] * fu[e];
-          vr += fr[e] * Op<T>::to_f32(fv.x[e]);
         }
         split4_store<NP>(y, X + row * CP + wc, CT * CP);
         split4_store<3>(fu, X + kU + row * CP + wc, CT * CP);
@@ -1213,6 +1269,14 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
           *reinterpret_cast<uint4*>(Qt + (tid + 512 * x) * 8) = qraw[x];
         }
     };
+    // q_i.k_j and k_i.k_j at F's and H's places
+    f32x4 qk[2], kk[2];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const unsigned at = 2 * half + m <= w ? (w * (w + 1) / 2 + 2 * half + m) * 2048 + l * 16 : kNowhere;
+      qk[m] = __builtin_bit_cast(f32x4, bload16(rx, at));
+      kk[m] = __builtin_bit_cast(f32x4, bload16(rx, at + 1024));
+    }
     load_kq(0);
     // (places computed anew for every head: kept over the walk they would spill)
     int lo = lo_, hi = hi_;
@@ -1230,6 +1294,17 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
         const float d = j <= i ? expf((float)(G[i] - G[j])) : 0.f;
         f[r] = j <= i ? a.scale * d * F[m][r] : 0.f;
         hm[r] = j < i ? -d * H[m][r] : 0.f;
+      }
+      {
+        float below = 0.f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float x = scan16(j < crow + r ? f[r] * qk[m][r] + hm[r] * kk[m][r] : 0.f);
+          if (jt < w && lo == 15) rowsX[jt][crow + r] = x;
+          below += j <= crow + r ? moved<kUpOne>(x) : 0.f;
+        }
+        below = sum_rows(below);
+        if (hi == 0) colsX[w][j] = below;
       }
       // rows i .. i + 3 of column j: consecutive in the transpose
       split4_store<3>(f, Ft + j * RC + (crow ^ swap8(lo)), CT * RC);
@@ -1265,7 +1340,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
       }
     }
     ss *= tok[CT - 1].x;
-    float dots[4] = {0.f, 0.f, 0.f, 0.f};
+    float nr[4] = {0.f, 0.f, 0.f, 0.f}, fs4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const float4 tk = tok[crow + r];
@@ -1277,11 +1352,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
       }
     }
     ub = sum8(ub);
-    vr = sum8(vr);
-    if ((tid & 7) == 0) {
-      sub[row] = vr;
-      sbeta[row] = ub;
-    }
+    if ((tid & 7) == 0) sbeta[row] = ub;
 #pragma unroll
     for (int st = 0; st < NS; ++st) {
       if (st > 0) lds_barrier();
@@ -1291,6 +1362,12 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
 #pragma unroll
       for (int i = st * ND / NS; i < (st + 1) * ND / NS; ++i) {
         const int ti = tile(i, half) - st * (2 * KS / NS);
+        const f32x4 kc = column(Kt, ti), qc = column(Qt, ti);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          nr[r] += aq[i][r] * qc[r] - kr[i][r] * kc[r];
+          fs4[r] += ku[i][r] * kc[r];
+        }
         f32x4 x = zero_acc();
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
@@ -1311,11 +1388,8 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
           mma<3, NP, 2>(ta, qb, x);
           mma<3, NP, 2>(ha, kb, x);
         }
-        const f32x4 kc = column(Kt, ti), qc = column(Qt, ti);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          ss += ku[i][r] * kc[r];
-          dots[r] += aq[i][r] * qc[r];
           tq[i][r] += aq[i][r];
           tkk[i][r] += x[r] + ku[i][r] - kr[i][r];
         }
@@ -1326,28 +1400,36 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
     if (lo == 0) part[wave][hi] = ss;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      dots[r] = sum16(dots[r]);
-      if (lo == 0) dG[half][crow + r] = dots[r];
+      nr[r] = sum16(nr[r]);
+      fs4[r] = sum16(fs4[r]);
+      if (lo == 0) {
+        nearS[half][crow + r] = nr[r];
+        farS[half][crow + r] = fs4[r];
+      }
     }
     lds_barrier();
     if (tid < CT) {
       const float bt = tok[tid].z;
       if (t0 + tid < a.T)
         a.dbeta[((long)(t0 + tid) * a.B + b) * a.Hv + h] = t0 + tid < len ? sbeta[tid] / (bt * bt) : 0.f;
-      const int at = CT - 1 - tid;
-      // sums from the chunk's end, in double: terms of both signs
-      double s = ((double)dG[0][at] + dG[1][at]) - sub[at];
-      for (int d = 1; d < 64; d <<= 1) {
-        const double o = __shfl_up(s, d, 64);
-        if (tid >= d) s += o;
-      }
-      double all = 0.;
+      // lane by lane from the chunk's end: token at, of tile jt
+      const int at = CT - 1 - tid, jt = at >> 4;
+      double all = scan64((double)nearS[0][at] + nearS[1][at]);
+      const double c = scan64((double)farS[0][tid] + farS[1][tid]), before = __shfl(c, at - 1, 64);
+      if (at > 0) all += before;
+      // pairs in t's column tile, then those of the tiles before it: rows of t's own tile, of later ones
+      for (int i = jt; i < 4; ++i) all += colsX[i][at];
+      const double r0 = jt > 0 ? rowsX[0][at] : 0., r1 = jt > 1 ? rowsX[1][at] : 0., r2 = jt > 2 ? rowsX[2][at] : 0.;
+      all += scan16(r0 + r1 + r2);
+      const double s0 = sum16(r0), s1 = sum16(r1);
+      const double s03 = __shfl(s0, 0, 64), s02 = __shfl(s0, 16, 64), s13 = __shfl(s1, 0, 64);
+      if (jt == 1) all += s02 + s03;
+      if (jt == 2) all += s03 + s13;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) all += part[i][j];
-      const bool kept = G[at] - (at ? G[at - 1] : 0.) >= -104.;     // e^-104 < 2^-150
-      if (t0 + at < a.T) a.dg[((long)(t0 + at) * a.B + b) * a.Hv + h] = t0 + at < len && kept ? (float)(s + all) : 0.f;
+      if (t0 + at < a.T) a.dg[((long)(t0 + at) * a.B + b) * a.Hv + h] = t0 + at < len ? (float)all : 0.f;
     }
   }
   const int crow = 16 * w + 4 * hi_, rows = a.T - t0 - crow;
