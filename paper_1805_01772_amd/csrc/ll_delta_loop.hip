@@ -31,7 +31,7 @@
 // pieces i and j is taken while i + j <= 2: what is dropped is below 2^-24 of the
 // term.  Sums are float32.  (Two pieces, 17 bits, of what only y and dK read would
 // round one bfloat16 result in five hundred the other way and lose small differences of
-// large terms; they save 2 to 6 %: 8 rows, forward and gradient, 784 us against 818.)
+// large terms; they save 2 to 6 %: 8 rows, forward and gradient, 784 us against 818 when measured.)
 //
 // Sizes that the figures below are for: "8 rows", lengths 256 to 2048, and "one
 // row" of 16384 tokens, 16 value heads of 128 x 128 in bfloat16 (8 and 16 key
@@ -244,7 +244,7 @@ __device__ __forceinline__ void wave_lds_fence() {
 // block column), then everything the loops read in the order in which a lane
 // reads it, 16 bytes at a time.
 // Bound: HBM, for what it writes (K, Q, T and P, plain and transposed, in pieces):
-// 8 rows 107 us, 0.6 GB; one row 134 us; prompts 27 us.  (float32 keeps k and q in LDS in
+// 8 rows 110 us, 0.6 GB; one row 146 us; prompts 27 us.  (float32 keeps k and q in LDS in
 // pieces, 73 KB at 64 columns and 122 KB at 128: two work-groups and one a compute unit.)
 // ---------------------------------------------------------------------------
 template <typename T, int KS, bool SAVE>
@@ -623,7 +623,7 @@ __device__ void zero_rest(T* out, long tok_ld, const DeltaArgs& a, const Walk& k
 // Bound: with few heads a chunk's three products one after the other, 2.6 us a chunk
 // with 16 columns (1.5 of them when nothing else runs on the compute unit): one
 // row 655 us for 256 chunks, on half of the compute units; with many the traffic of the operands and of what is
-// kept for the gradient: 8 rows 228 us, 0.85 GB, 3.7 TB/s; prompts 45 us.
+// kept for the gradient: 8 rows 227 us, 0.85 GB, 3.7 TB/s; prompts 46 us.
 // ---------------------------------------------------------------------------
 template <typename T, int KS, int NL, bool SAVE>
 __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
@@ -819,7 +819,7 @@ __global__ __launch_bounds__(512) void delta_state_fwd_kernel(DeltaArgs a) {
 // state_bwd: the gradient loop, the same split.  Waves 0-3 carry dS: K dS, T^T dU,
 // K^T dR.  Waves 4-7 make what does not depend on it, P^T dY and Q^T (scale e^G
 // dY), one chunk ahead, each for the chain wave of its rows (through LDS, in the
-// accumulators' order).  Bound as state_fwd: 8 rows 233 us, one row 650 us.
+// accumulators' order).  Bound as state_fwd: 8 rows 231 us, one row 650 us.
 // ---------------------------------------------------------------------------
 template <typename T, int KS, int NL>
 __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
@@ -1054,7 +1054,7 @@ __global__ __launch_bounds__(512) void delta_state_bwd_kernel(DeltaArgs a) {
 // wave for itself from global memory they took 10 of 52 thousand cycles a head's
 // chunk.  Bound: HBM in the walk (U, dR and both states of every chunk, 5 TB/s),
 // which stands still while F, H and what follows are made, since LDS holds one
-// work-group (133 KB): 8 rows 326 to 345 us, 1.2 GB, 3.6 TB/s; one row 376 us.
+// work-group (139 KB): 8 rows 330 to 346 us, 1.2 GB, 3.5 TB/s; one row 379 us.
 // ---------------------------------------------------------------------------
 template <typename T, int KS>
 __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaArgs a) {
