@@ -401,9 +401,10 @@ ll_status ll_measure_mfma_peak(int32_t device, int32_t dtype, int32_t shape, dou
 ll_status ll_eval_activations(int32_t device, const float* in, float* out, int64_t n, int32_t fn);
 
 /* ===========================================================================
- * Operators of sequence models beside the loops: a recurrence whose state is
- * a matrix (the gated delta rule), the log probabilities a model is trained
- * and scored by, and the AdamW step that applies the gradients.  They follow
+ * Operators of sequence models beside the loops: recurrences whose state is
+ * a matrix (the gated delta rule, linear attention), the embedding that makes the
+ * inputs, the log probabilities a model is trained and scored by, beam search,
+ * and the AdamW step that applies the gradients.  They follow
  * the conventions above (device pointers, 16-byte aligned unless an argument
  * says otherwise; asynchronous on `stream`; a plan serves one stream at a
  * time and its calls do not overlap; checkable errors come back at once and
@@ -417,6 +418,9 @@ ll_status ll_eval_activations(int32_t device, const float* in, float* out, int64
 /* More device error word bits. */
 #define LL_DEVERR_SLOT 4     /* a state slot >= n_slots                       */
 #define LL_DEVERR_TARGET 8   /* a target < -1 or >= V                         */
+#define LL_DEVERR_TOKEN 16   /* a token < -1 or >= V                          */
+#define LL_DEVERR_BEAM 32    /* a parent outside [0, K); NaN among a beam's   */
+                             /* logits or scores                              */
 
 /*
  * The gated delta rule, a loop with a state S [Dk, Dv] per row and value head:
@@ -525,6 +529,92 @@ ll_status delta_loop_step(const ll_delta_desc* desc, void* stream, const void* q
                           int32_t* device_error);
 
 /*
+ * Linear attention with a decay for each head, a loop with a state S [Dk, Dv] per
+ * row and value head:
+ *     S_t = e^{g_h} S_{t-1} + k_t v_t^T,   y_t = scale S_t^T q_t
+ * Rows keep their state at t >= seq_len[b] and output y = 0 there.  Value head
+ * h reads key head h / (Hv / Hk).
+ *   T_max, B, Hk, Hv, Dk, Dv >= 1; Hv a multiple of Hk; Dk and Dv multiples of
+ *     8, at most 128, T_max <= 2^30, B Hv < 2^21 (one token: B Hv ceil(Dv / 32) <
+ *     2^24; else LL_EUNSUPPORTED); dtype an ll_dtype, the type of q, k, v, y and
+ *     their gradients (decays, states and their gradients are float).  Inside, sums
+ *     and states are float, products keep float's 24 bits.
+ *   inference, q_ld .. dv_ld, scale  as for ll_delta_desc.
+ * The decays are constants of the layer: they get no gradient.  A token that holds
+ * NaN or infinity may reach y from up to 63 tokens before it on (what it leaves in
+ * the state stays there).  Outputs overlap no input, but for ST, which may be S0.
+ * g, seq_len, slots and device_error need 4 bytes' alignment, every other array 16.
+ */
+typedef struct {
+  int32_t T_max, B, Hk, Hv, Dk, Dv;
+  int32_t dtype;
+  int32_t inference;
+  int64_t q_ld, k_ld, v_ld, dq_ld, dk_ld, dv_ld;
+  float scale;
+  int32_t reserved;   /* must be 0 */
+} ll_linattn_desc;
+
+typedef struct ll_linattn_plan ll_linattn_plan;
+
+ll_status ll_linattn_plan_create(const ll_linattn_desc* desc, int device, ll_linattn_plan** out);
+/* Waits for the device's work.  NULL is accepted. */
+ll_status ll_linattn_plan_destroy(ll_linattn_plan* plan);
+/* Bytes of device memory that the plan holds. */
+ll_status ll_linattn_plan_bytes(const ll_linattn_plan* plan, int64_t* device_bytes);
+/* Distances of the tokens from the next call on, as ll_delta_plan_set_ld. */
+ll_status ll_linattn_plan_set_ld(ll_linattn_plan* plan, const int64_t* ld);
+
+/*
+ * Forward loop.
+ *   q, k     [T_max,B,Hk,Dk], v [T_max,B,Hv,Dv] dtype, tokens q_ld, k_ld, v_ld
+ *            apart.  Entries at t >= seq_len[b] may hold anything (NaN).
+ *   g        [Hv] float, the logarithm of each head's decay, at most 0 (minus
+ *            infinity: nothing is kept; below -200 counts as -200).
+ *   seq_len  [B] int32 in [0, T_max], or NULL: every row has T_max tokens.  A
+ *            length outside counts as 0 and sets LL_DEVERR_SEQ_LEN.
+ *   S0       [B,Hv,Dk,Dv] float, or NULL for zeros.
+ *   y        [T_max,B,Hv,Dv] dtype.
+ *   ST       [B,Hv,Dk,Dv] float, the state after the last token, or NULL; may
+ *            be S0 itself.
+ *   save_for_backward  nonzero: the plan keeps what linattn_loop_bwd needs, and the
+ *            pointers q, k, v, g, seq_len, whose contents must stay as they are
+ *            until the gradient has been enqueued.
+ */
+ll_status linattn_loop_fwd(ll_linattn_plan* plan, void* stream, const void* q, const void* k,
+                           const void* v, const float* g, const int32_t* seq_len, const float* S0,
+                           void* y, float* ST, int32_t save_for_backward);
+
+/*
+ * Gradient loop of the last saved forward (LL_ESTATE if there is none, or if
+ * the plan's distances of q, k and v are not its; LL_EINVAL if q .. seq_len are
+ * not its pointers; a refused call keeps it).  Consumes the saved forward.
+ *   dy       [T_max,B,Hv,Dv] dtype; entries at t >= seq_len[b] are not used.
+ *   dST      [B,Hv,Dk,Dv] float, or NULL (zero).
+ *   dq, dk   [T_max,B,Hk,Dk], dv [T_max,B,Hv,Dv] dtype: overwritten, 0 at
+ *            t >= seq_len[b].  dq and dk are summed over the value heads that share
+ *            a key head, in their order.
+ *   dS0      [B,Hv,Dk,Dv] float, or NULL; not dST.
+ */
+ll_status linattn_loop_bwd(ll_linattn_plan* plan, void* stream, const void* q, const void* k,
+                           const void* v, const float* g, const int32_t* seq_len, const void* dy,
+                           const float* dST, void* dq, void* dk, void* dv, float* dS0);
+
+/* Wait for the device's work, then read and clear the plan's error word. */
+ll_status ll_linattn_status_sync(ll_linattn_plan* plan, int32_t* device_error);
+
+/*
+ * One token for B rows, states updated in place, no plan (serving).  Launches on
+ * the calling thread's current device, whose tensors these have to be.
+ *   desc     as above with T_max = 1; inference and dq_ld .. dv_ld are ignored.
+ *   q, k     [B,Hk,Dk], v [B,Hv,Dv] dtype (rows q_ld, k_ld, v_ld apart),
+ *            g [Hv] float, y [B,Hv,Dv] dtype.
+ *   S, slots, n_slots, device_error  as for delta_loop_step.
+ */
+ll_status linattn_loop_step(const ll_linattn_desc* desc, void* stream, const void* q, const void* k,
+                            const void* v, const float* g, float* S, const int32_t* slots,
+                            int32_t n_slots, void* y, int32_t* device_error);
+
+/*
  * Log probabilities of given tokens under softmax(logits), with the entropy
  * and the most likely alternatives, and their gradient.
  *   N rows at most, N < 2^24, V columns in [1, 2^28]; dtype the logits' type; top_k in [0, 32],
@@ -593,6 +683,137 @@ ll_status ll_logprob_fwd_bwd(ll_logprob_plan* plan, void* stream, int32_t rows,
                              void* dlogits);
 
 ll_status ll_logprob_status_sync(ll_logprob_plan* plan, int32_t* device_error);
+
+/*
+ * Embedding: the rows of a table [V, D] that a batch of tokens names, and the
+ * gradient of the table.
+ *     x_n = scale W[tokens_n],     dW_r = scale sum over {n : tokens_n = r} of dx_n
+ *   N tokens at most, N <= 2^24, V in [1, 2^30), D in [1, 2^16] (ceil(N / 64)
+ *     ceil(D / 512) < 2^24, else LL_EUNSUPPORTED); the four types are ll_dtypes of
+ *     their own; sums are float and rounded once.
+ *   inference  nonzero: lookups only (no buffers for the gradient).
+ *   table_ld .. grad_ld  elements from row to row (0: D; any ld >= D).
+ *   scale    0 means 1.
+ * Arrays need the alignment of an element only; outputs overlap no input.
+ */
+typedef struct {
+  int32_t N, V, D;
+  int32_t table_dtype, x_dtype, dx_dtype, grad_dtype;
+  int32_t inference;
+  int64_t table_ld, x_ld, dx_ld, grad_ld;
+  float scale;
+  int32_t reserved;   /* must be 0 */
+} ll_embed_desc;
+
+typedef struct ll_embed_plan ll_embed_plan;
+
+ll_status ll_embed_plan_create(const ll_embed_desc* desc, int device, ll_embed_plan** out);
+ll_status ll_embed_plan_destroy(ll_embed_plan* plan);
+/* Bytes of device memory that the plan holds. */
+ll_status ll_embed_plan_bytes(const ll_embed_plan* plan, int64_t* device_bytes);
+
+/*
+ *   n        tokens of this call, 0 .. N.
+ *   tokens   [n] int32; -1: no token (x = 0).  Others outside [0, V) count as -1 and
+ *            set LL_DEVERR_TOKEN.
+ */
+ll_status ll_embed_fwd(ll_embed_plan* plan, void* stream, int32_t n, const void* table,
+                       const int32_t* tokens, void* x);
+
+/*
+ *   dx       [n, D]; rows without a token are not read.
+ *   dtable   [V, D]: overwritten, or, with accumulate, added to (rows that no token
+ *            names stay as they are and are not read; grad_dtype bfloat16: the sum with
+ *            the old value is rounded once).
+ * A row's terms are added in an order that the tokens alone decide: the same call
+ * gives the same bits.
+ */
+ll_status ll_embed_bwd(ll_embed_plan* plan, void* stream, int32_t n, const int32_t* tokens,
+                       const void* dx, void* dtable, int32_t accumulate);
+
+ll_status ll_embed_status_sync(ll_embed_plan* plan, int32_t* device_error);
+
+/*
+ * Beam search: one step of B searches with K beams each.  Token v after beam k has
+ *     score = scores_k + log softmax(logits_k)_v,   length = lengths_k + 1
+ * a finished beam goes on as one candidate, with its score and length, and the K
+ * candidates of a search with the largest
+ *     score / ((5 + length) / 6)^length_penalty
+ * are its next beams, best first (equal ones: lower beam, then lower token).
+ *   B >= 1, K in [1, 32], B K <= 2^20, V in [1, 2^28]; dtype the logits' type; ld:
+ *     elements from row to row (0: V; any ld >= V).
+ *   eos      the token that finishes a beam, or -1: none does.
+ *   length_penalty  in [-16, 16]; 0: scores are compared as they are.
+ * Scores are made and compared in double.  logits need the alignment of an element
+ * only, every other array 4 bytes.
+ */
+#define LL_BEAM_MAX 32
+#define LL_BEAM_TENSORS 256
+
+typedef struct {
+  int32_t B, K, V;
+  int32_t dtype;
+  int64_t ld;
+  int32_t eos;
+  float length_penalty;
+  int32_t reserved[2];   /* must be 0 */
+} ll_beam_desc;
+
+typedef struct ll_beam_plan ll_beam_plan;
+
+ll_status ll_beam_plan_create(const ll_beam_desc* desc, int device, ll_beam_plan** out);
+ll_status ll_beam_plan_destroy(ll_beam_plan* plan);
+
+/*
+ *   searches of this call, 0 .. B.
+ *   logits   [searches K, V] dtype.  Minus infinity: a token that is not allowed.
+ *            Rows of finished beams, and of beams that do not count, are not read.
+ *   scores   [searches,K] float; minus infinity: a beam that does not count (all but
+ *            one at a search's first step).
+ *   finished [searches,K] int32, nonzero: this beam is finished; NULL: none is.
+ *   lengths  [searches,K] int32, or NULL (length_penalty 0 only).
+ *   parents  [searches,K] int32: the beam that each next one continues, 0 .. K - 1.
+ *   tokens   [searches,K] int32: its token (eos for a beam that was finished, also
+ *            where that is -1).
+ *   scores_out, finished_out, lengths_out  [searches,K]: may be scores, finished,
+ *            lengths themselves; finished_out and lengths_out may be NULL.
+ * Where fewer than K candidates have a score above minus infinity, the places k left
+ * over get parent k, token -1, score minus infinity, finished 0 and their old length.
+ * A beam with NaN for a score, or with NaN or plus infinity among its logits, offers
+ * nothing and sets LL_DEVERR_BEAM.
+ */
+ll_status ll_beam_select(ll_beam_plan* plan, void* stream, int32_t searches, const void* logits,
+                         const float* scores, const int32_t* finished, const int32_t* lengths,
+                         int32_t* parents, int32_t* tokens, float* scores_out,
+                         int32_t* finished_out, int32_t* lengths_out);
+
+typedef struct {
+  void* data;
+  int64_t row_bytes;   /* 1 .. 2^36; rows lie one after the other */
+} ll_beam_tensor;
+
+/*
+ * The beams' states (of the loops, of a pool, their tokens so far) in the order of
+ * the next beams, in place, no plan.  Launches on the calling thread's current device.
+ *   parents  [searches,K] as above; one outside [0, K) counts as its own place and
+ *            sets LL_DEVERR_BEAM.
+ *   tensors  host array of n_tensors (0 .. LL_BEAM_TENSORS) that do not overlap.
+ *   slots    NULL: a tensor has searches K rows, and row (b, k) gets what row (b,
+ *            parents[b,k]) held.
+ *            Else [searches,K] int32 into tensors of n_slots rows, and slots_out
+ *            [searches,K], another array, required: the slot of each next beam.  A
+ *            beam's first successor keeps its slot; the state is copied for the further
+ *            ones only, into the slots of beams without a successor.  Slots are
+ *            distinct; -1: no state (nothing is copied from or to it); < -1 or >=
+ *            n_slots: the same, and sets LL_DEVERR_SLOT.
+ *   device_error  device int32 whose bits are set (never cleared), or NULL.
+ */
+ll_status ll_beam_reorder(void* stream, int32_t searches, int32_t K, const int32_t* parents,
+                          int32_t n_tensors, const ll_beam_tensor* tensors,
+                          const int32_t* slots, int32_t n_slots, int32_t* slots_out,
+                          int32_t* device_error);
+
+ll_status ll_beam_status_sync(ll_beam_plan* plan, int32_t* device_error);
 
 /*
  * AdamW over many tensors in one call:

@@ -1,0 +1,878 @@
+// Linear attention with a decay for each head: forward, gradient, one-token step.
+//
+//   S_t = l S_{t-1} + k_t v_t^T,  y_t = scale S_t^T q_t,  l = e^g of the head
+// and, with D_t = dL/dS_t (all of it), D_t = l D_{t+1} + scale q_t dy_t^T,
+//   dq_t = scale S_t dy_t,  dk_t = D_t v_t,  dv_t = D_t^T k_t,  dS0 = l D_1
+// are the same recurrence four times (LinPass): rows a ask, rows b and c make the state
+//   out_i = w_P sum_{j <= i} l^{i-j} (a_i.b_j) c_j + w_A l^{i+e} a_i S
+//   S'    = l^m S + w_U sum_j l^{m-j-e} b_j c_j^T          over m tokens, S entering
+//   y:  a, b, c = q, k, v     dq: dy, v, k (state S^T)           e = 1
+//   dv: a, b, c = k, q, dy    dk: v, dy, q (state D^T)   e = 0, tokens from the last on
+#include <algorithm>
+#include <cmath>
+#include <new>
+
+#include "ll_host.h"
+#include "ll_kernels.h"
+#include "ll_pieces.h"
+
+using ll::bf16_t;
+using ll::fail;
+
+namespace ll {
+
+constexpr int kLinMaxD = 128;
+constexpr int kLinStepCols = 32;
+
+// Tokens of a chunk: 16 KB of 128 columns in either type.
+template <typename T> struct LinChunk { static constexpr int n = 64; };
+template <> struct LinChunk<float> { static constexpr int n = 32; };
+
+struct LinPass {
+  const void *a, *b, *c;
+  void* out;                           // NULL: this pass is not made
+  long a_ld, b_ld, c_ld, o_ld;         // elements from token to token
+  int ag, bg, cg, og;                  // value heads to a head of the array
+  int Dr, Dc;                          // sizes of a and b, of c and out
+  const float* st;                     // entering states, part by part; NULL: zeros
+  float* keep;                         // a copy of them is written here, or NULL
+  float* last;                         // the state after the last token, or NULL
+  int rs, cs;                          // distances of a state's rows (Dr) and columns (Dc)
+  float wP, wA, wU;
+  int e, rev;
+  int wide;                            // out is float whatever the call's type
+};
+
+struct LinArgs {
+  LinPass p[3];
+  int T, B, H, Dk, Dv;                 // H: value heads
+  int parts, per, npass, ctiles;       // parts of a row, chunks of a part
+  const float* g;
+  const int* seq_len;
+  float* local;                        // [row, head, part] states
+  int* err;
+};
+
+__device__ __forceinline__ int lin_len(const LinArgs& a, int b) {
+  const int L = a.seq_len ? a.seq_len[b] : a.T;
+  return L < 0 || L > a.T ? 0 : L;
+}
+// The logarithm of a decay: l^n is 0 in float well before -200, and l^0 stays 1.
+__device__ __forceinline__ float lin_log(const float* g, int h) {
+  const float x = g[h];
+  return x < -200.f ? -200.f : x;
+}
+
+// Operands over 32 of what a product sums over: a lane holds the four of its group hi
+// in each of two tiles of 16, the four that an accumulator tile gives it.  So states and
+// the chunk's products go from accumulators into the next product as they lie.
+template <typename T> struct Lin;
+
+// bfloat16: an operand of the call is its own piece, a float one the sum of three (24
+// bits, exactly), so that a product drops nothing but what a float cannot hold.
+template <> struct Lin<bf16_t> {
+  typedef uint4 Raw;
+  static constexpr int NP = 3;
+  struct Split { uint4 p[NP]; };
+  __device__ static __forceinline__ Raw rows(const bf16_t* p) {
+    const uint2 x = *reinterpret_cast<const uint2*>(p), y = *reinterpret_cast<const uint2*>(p + 16);
+    return make_uint4(x.x, x.y, y.x, y.y);
+  }
+  // Columns of [32 rows][pitch]: lane lo has the column that element lo % 4 of chunk lo / 4
+  // is (the transposing load takes four rows' chunks from 16 lanes); chunks q apart.
+  __device__ static __forceinline__ Raw cols(const bf16_t* p, int pitch, int lo, int hi, int q) {
+    typedef __attribute__((ext_vector_type(4))) short s4;
+    typedef __attribute__((address_space(3))) s4* lds4;
+    const bf16_t* at = p + (4 * hi + (lo >> 2)) * pitch + q * (lo & 3);
+    const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at);
+    const s4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 16 * pitch));
+    const uint2 u = __builtin_bit_cast(uint2, x), v = __builtin_bit_cast(uint2, y);
+    return make_uint4(u.x, u.y, v.x, v.y);
+  }
+  __device__ static __forceinline__ Split split(f32x4 x, f32x4 y) {
+    const float f[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+    Split s;
+    split8<NP>(f, s.p);
+    return s;
+  }
+  __device__ static __forceinline__ void floats(Raw r, f32x4& x, f32x4& y) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      y[2 * i] = __uint_as_float(w[2 + i] << 16);
+      y[2 * i + 1] = __uint_as_float(w[2 + i] & 0xffff0000u);
+    }
+  }
+  __device__ static __forceinline__ f32x4 mm(Raw a, Raw b, f32x4 c) { return mfma(as_frag(a), as_frag(b), c); }
+  __device__ static __forceinline__ f32x4 mm(Raw a, const Split& b, f32x4 c) {
+#pragma unroll
+    for (int i = NP - 1; i >= 0; --i) c = mfma(as_frag(a), as_frag(b.p[i]), c);
+    return c;
+  }
+  __device__ static __forceinline__ f32x4 mm(const Split& a, Raw b, f32x4 c) {
+#pragma unroll
+    for (int i = NP - 1; i >= 0; --i) c = mfma(as_frag(a.p[i]), as_frag(b), c);
+    return c;
+  }
+};
+
+// float: the float32 matrix instructions take it as it is, a sixteenth of the rate.
+template <> struct Lin<float> {
+  struct Raw { f32x4 x, y; };
+  typedef Raw Split;
+  __device__ static __forceinline__ Raw rows(const float* p) {
+    return Raw{*reinterpret_cast<const f32x4*>(p), *reinterpret_cast<const f32x4*>(p + 16)};
+  }
+  __device__ static __forceinline__ Raw cols(const float* p, int pitch, int lo, int hi, int q) {
+    const float* at = p + 4 * hi * pitch + q * (lo >> 2) + (lo & 3);
+    Raw r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      r.x[i] = at[i * pitch];
+      r.y[i] = at[(16 + i) * pitch];
+    }
+    return r;
+  }
+  __device__ static __forceinline__ Split split(f32x4 x, f32x4 y) { return Raw{x, y}; }
+  __device__ static __forceinline__ void floats(Raw r, f32x4& x, f32x4& y) {
+    x = r.x;
+    y = r.y;
+  }
+  __device__ static __forceinline__ f32x4 mm(const Raw& a, const Raw& b, f32x4 c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[i], b.x[i], c, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.y[i], b.y[i], c, 0, 0, 0);
+    return c;
+  }
+};
+
+// N floats, neighbours, to dst as the call's type or as floats.
+template <typename T, int N>
+__device__ __forceinline__ void lin_store(void* dst, long at, const float* x, bool wide) {
+  if (sizeof(T) == 4 || wide) {
+    f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(dst) + at);
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) p[i] = f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+  } else {
+    uint32_t w[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) w[i] = pack2(x[2 * i], x[2 * i + 1]);
+    bf16_t* p = static_cast<bf16_t*>(dst) + at;
+    if (N == 8) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[N / 2 - 2], w[N / 2 - 1]);
+    else *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// One part of a row, head and pass, 64 NV columns of the state: chunk after chunk.  A
+// wave has 16 NV columns of the state in its accumulators and makes the chunk's products
+// a_i.b_j for itself (a sixth of its matrix instructions), so that nothing but the
+// operands goes through LDS.  LOCAL: only the state of the part's tokens alone.
+// KD: rows of the state in steps of 32.
+// ---------------------------------------------------------------------------
+template <typename T, int KD, int NV, bool LOCAL>
+__global__ __launch_bounds__(256) void lin_kernel(LinArgs args) {
+  typedef Lin<T> L;
+  constexpr int CT = LinChunk<T>::n, NI = CT / 16, NM = CT / 32, NC = 64 * NV, Q = 4 * NV;
+  constexpr int E = 16 / sizeof(T), PR = 32 * KD + E, PC = NC + E;
+  constexpr int UR = 32 * KD / E, UC = NC / E;           // 16-byte units of a row
+  constexpr int LR = CT * UR / 256, LC = CT * UC / 256;  // loads of a thread
+  __shared__ __align__(16) T as[LOCAL ? 8 : CT * PR];
+  __shared__ __align__(16) T bs[CT * PR];
+  __shared__ __align__(16) T cs[CT * PC];
+  // items that read the same tokens (columns and passes) lie 8 work-groups apart: on one
+  // XCD, one after the other
+  const int sub = args.ctiles * args.npass, items = args.B * args.H * args.parts;
+  int id = blockIdx.x;
+  const int full = items / 8 * 8 * sub;
+  int item, which;
+  if (id < full) {
+    item = id / (8 * sub) * 8 + id % 8;
+    which = id / 8 % sub;
+  } else {
+    id -= full;
+    item = items / 8 * 8 + id % (items % 8);
+    which = id / (items % 8);
+  }
+  const LinPass& p = args.p[which / args.ctiles];
+  const int c0 = which % args.ctiles * NC;
+  if (c0 >= p.Dc) return;
+  const int part = item % args.parts, bh = item / args.parts, h = bh % args.H, b = bh / args.H;
+  const int len = lin_len(args, b), per = args.per * CT;
+  const int t_lo = part * per, t_hi = min(args.T, t_lo + per);
+  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, lo = l & 15, hi = l >> 4;
+  if (!LOCAL && h == 0 && part == 0 && which == 0 && tid == 0 && args.seq_len &&
+      (args.seq_len[b] < 0 || args.seq_len[b] > args.T))
+    atomicOr(args.err, LL_DEVERR_SEQ_LEN_BIT);
+  // token number i of the pass is token len - 1 - i where it runs backwards
+  auto token = [&](int i) { return ((long)(p.rev && i < len ? len - 1 - i : i)) * args.B + b; };
+  const int cw = c0 + 16 * NV * w;                       // the wave's columns; a lane's: cw + 4 NV hi + ..
+  const int mine = cw + Q * hi;
+  const T* pa = static_cast<const T*>(p.a) + (long)(h / p.ag) * p.Dr;
+  const T* pb = static_cast<const T*>(p.b) + (long)(h / p.bg) * p.Dr;
+  const T* pc = static_cast<const T*>(p.c) + (long)(h / p.cg) * p.Dc;
+  const long oh = (long)(h / p.og) * p.Dc;
+
+  // the state: rows 16 d + 4 hi + r, column of tile t: cw + 4 NV (lo / 4) + 4 t + lo % 4
+  f32x4 S[2 * KD][NV];
+  const long stride = (long)args.Dk * args.Dv;
+  const float* st = LOCAL || !p.st ? nullptr : p.st + (long)item * stride;
+  auto each_state = [&](auto f) {
+#pragma unroll
+    for (int d = 0; d < 2 * KD; ++d)
+#pragma unroll
+      for (int t = 0; t < NV; ++t) {
+        const int r = 16 * d + 4 * hi, c = cw + Q * (lo >> 2) + 4 * t + (lo & 3);
+        f(S[d][t], r, (long)r * p.rs + (long)c * p.cs, r < p.Dr && c < p.Dc);
+      }
+  };
+  each_state([&](f32x4& s, int, long at, bool in) {
+    s = zero_acc();
+    if (!st || !in) return;
+    if (p.rs == 1) s = *reinterpret_cast<const f32x4*>(st + at);
+    else
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] = st[at + (long)e * p.rs];
+  });
+  auto put_state = [&](float* to) {
+    each_state([&](f32x4& s, int, long at, bool in) {
+      if (!in) return;
+      if (p.rs == 1) *reinterpret_cast<f32x4*>(to + at) = s;
+      else
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[at + (long)e * p.rs] = s[e];
+    });
+  };
+  if (!LOCAL && p.keep) put_state(p.keep + (long)item * stride);
+
+  const float g = lin_log(args.g, h);
+  // weights: of pairs on the diagonal tiles, of pairs one tile apart (more apart: times
+  // l^16 each), of a token's place in its tile, and of what a full chunk's tokens leave
+  f32x4 near, far, leave;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int d = lo - 4 * hi - r;
+    near[r] = d < 0 ? 0.f : p.wP * expf(g * d);
+    far[r] = p.wP * expf(g * (16 + d));
+    leave[r] = p.wU * expf(g * (16 - 4 * hi - r - p.e));
+  }
+  const float place = p.wA * expf(g * (lo + p.e));
+  float l16[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) l16[i] = expf(g * (16 * i));
+
+  uint4 ra[LR], rb[LR], rc[LC];
+  auto load = [&](int t0) {
+#pragma unroll
+    for (int i = 0; i < LR; ++i) {
+      const int u = tid + 256 * i, row = u / UR, col = u % UR * E;
+      const bool in = t0 + row < len && col < p.Dr;
+      const long tok = token(t0 + row);
+      if (!LOCAL) ra[i] = in ? ld16(pa + tok * p.a_ld + col) : zero4();
+      rb[i] = in ? ld16(pb + tok * p.b_ld + col) : zero4();
+    }
+#pragma unroll
+    for (int i = 0; i < LC; ++i) {
+      const int u = tid + 256 * i, row = u / UC, col = c0 + u % UC * E;
+      rc[i] = t0 + row < len && col < p.Dc ? ld16(pc + token(t0 + row) * p.c_ld + col) : zero4();
+    }
+  };
+  const int t_end = min(t_hi, len);
+  if (t_lo < t_end) load(t_lo);
+  for (int t0 = t_lo; t0 < t_end; t0 += CT) {
+    lds_barrier();                                       // the chunk before has been read
+#pragma unroll
+    for (int i = 0; i < LR; ++i) {
+      const int u = tid + 256 * i, at = u / UR * PR + u % UR * E;
+      if (!LOCAL) *reinterpret_cast<uint4*>(as + at) = ra[i];
+      *reinterpret_cast<uint4*>(bs + at) = rb[i];
+    }
+#pragma unroll
+    for (int i = 0; i < LC; ++i) {
+      const int u = tid + 256 * i;
+      *reinterpret_cast<uint4*>(cs + u / UC * PC + u % UC * E) = rc[i];
+    }
+    lds_barrier();
+    if (t0 + CT < t_end) load(t0 + CT);
+    const int m = min(CT, len - t0);
+    typename L::Raw cf[NM][NV];
+#pragma unroll
+    for (int j = 0; j < NM; ++j)
+#pragma unroll
+      for (int t = 0; t < NV; ++t) cf[j][t] = L::cols(cs + 32 * j * PC + 16 * NV * w + 4 * t, PC, lo, hi, Q);
+    if constexpr (!LOCAL) {
+      f32x4 P[NI][NI], y[NI][NV];
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j) P[i][j] = zero_acc();
+#pragma unroll
+        for (int t = 0; t < NV; ++t) y[i][t] = zero_acc();
+      }
+#pragma unroll
+      for (int k = 0; k < KD; ++k) {
+        typename L::Raw fa[NI], fb[NI];
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          fa[i] = L::rows(as + (16 * i + lo) * PR + 32 * k + 4 * hi);
+          fb[i] = L::rows(bs + (16 * i + lo) * PR + 32 * k + 4 * hi);
+        }
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int j = 0; j <= i; ++j) P[i][j] = L::mm(fb[j], fa[i], P[i][j]);
+#pragma unroll
+        for (int t = 0; t < NV; ++t) {
+          const typename L::Split s = L::split(S[2 * k][t], S[2 * k + 1][t]);
+#pragma unroll
+          for (int i = 0; i < NI; ++i) y[i][t] = L::mm(s, fa[i], y[i][t]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const float f = place * l16[i];
+#pragma unroll
+        for (int t = 0; t < NV; ++t) y[i][t] *= f;
+#pragma unroll
+        for (int j = 0; j <= i; ++j) {
+          const f32x4 x = P[i][j];
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            P[i][j][r] = i == j ? (lo >= 4 * hi + r ? x[r] * near[r] : 0.f) : x[r] * (far[r] * l16[i - j - 1]);
+        }
+#pragma unroll
+        for (int j = 0; j <= i / 2; ++j) {
+          const typename L::Split s = L::split(P[i][2 * j], 2 * j + 1 <= i ? P[i][2 * j + 1] : zero_acc());
+#pragma unroll
+          for (int t = 0; t < NV; ++t) y[i][t] = L::mm(cf[j][t], s, y[i][t]);
+        }
+        const int tok = t0 + 16 * i + lo;
+        if (tok < t_hi && mine < p.Dc) {
+          float o[4 * NV];
+#pragma unroll
+          for (int t = 0; t < NV; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[4 * t + r] = tok < len ? y[i][t][r] : 0.f;
+          lin_store<T, 4 * NV>(p.out, token(tok) * p.o_ld + oh + mine, o, p.wide);
+        }
+      }
+    }
+    // S' = l^m S + ..; as S + (l^m - 1) S, because a rounded l^m would err the same way in
+    // every chunk
+    const float grow = expm1f(g * m);
+#pragma unroll
+    for (int d = 0; d < 2 * KD; ++d)
+#pragma unroll
+      for (int t = 0; t < NV; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[d][t][r] = __builtin_fmaf(S[d][t][r], grow, S[d][t][r]);
+    typename L::Split cv[NM][NV];
+#pragma unroll
+    for (int j = 0; j < NM; ++j) {
+      f32x4 wx, wy;
+      if (m == CT) {
+        wx = leave * l16[NI - 1 - 2 * j];
+        wy = leave * l16[NI - 2 - 2 * j];
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {                    // (tokens past the end are zeros)
+          const int at = 32 * j + 4 * hi + r + p.e;
+          wx[r] = p.wU * expf(g * max(0, m - at));
+          wy[r] = p.wU * expf(g * max(0, m - at - 16));
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < NV; ++t) {
+        f32x4 x, y;
+        L::floats(cf[j][t], x, y);
+        cv[j][t] = L::split(x * wx, y * wy);
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < 2 * KD; ++d)
+#pragma unroll
+      for (int j = 0; j < NM; ++j) {
+        const typename L::Raw f = L::cols(bs + 32 * j * PR + 16 * d, PR, lo, hi, 4);
+#pragma unroll
+        for (int t = 0; t < NV; ++t) S[d][t] = L::mm(f, cv[j][t], S[d][t]);
+      }
+  }
+  if constexpr (LOCAL) {
+    put_state(args.local + (long)item * stride);
+  } else {
+    // tokens past the row's end, in whole chunks
+    const int first = max(t_lo, (len + CT - 1) / CT * CT);
+    if (mine < p.Dc) {
+      const float zero[4 * NV] = {};
+      for (int t = first + lo; t < t_hi; t += 16) lin_store<T, 4 * NV>(p.out, token(t) * p.o_ld + oh + mine, zero, p.wide);
+    }
+    // the part that holds the last token has the last state (the first one of an empty row)
+    if (p.last && (part == 0 || t_lo < len) && t_lo + per >= len) put_state(p.last + (long)bh * stride);
+  }
+}
+
+// The parts' states from their tokens' own: E_0 as given, E_{p+1} = l^n E_p + local_p.
+__global__ __launch_bounds__(256) void lin_scan_kernel(LinArgs a, const float* S0, int chunk) {
+  const long size = (long)a.Dk * a.Dv;
+  const int blocks = (int)((size / 4 + 255) / 256);
+  const int bh = blockIdx.x / blocks;
+  const long at = ((long)(blockIdx.x % blocks) * 256 + threadIdx.x) * 4;
+  if (at >= size) return;
+  const int len = lin_len(a, bh / a.H), per = a.per * chunk;
+  const float g = lin_log(a.g, bh % a.H);
+  f32x4 e = S0 ? *reinterpret_cast<const f32x4*>(S0 + bh * size + at) : zero_acc();
+  float* st = a.local + (long)bh * a.parts * size + at;
+  for (int p = 0; p < a.parts; ++p) {
+    const f32x4 own = *reinterpret_cast<const f32x4*>(st + p * size);
+    *reinterpret_cast<f32x4*>(st + p * size) = e;
+    const float grow = expm1f(g * min(per, max(0, len - p * per)));
+#pragma unroll
+    for (int r = 0; r < 4; ++r) e[r] = __builtin_fmaf(e[r], grow, e[r]) + own[r];
+  }
+}
+
+// Sums over the r value heads that share a key head: two gradients of a token, [Hk r][D]
+// floats each, to [Hk][D] of the call's type, in the heads' order.
+struct LinSum {
+  const float* from[2];
+  void* to[2];
+  long ld[2];
+  long tokens;
+  int Hk, r, D;
+};
+template <typename T>
+__global__ __launch_bounds__(256) void lin_sum_kernel(LinSum a) {
+  const int per = a.Hk * a.D / 4;                        // groups of four of a token
+  const long i = (long)blockIdx.x * 256 + threadIdx.x;
+  const long tok = i / per;
+  if (tok >= a.tokens) return;
+  const int u = (int)(i % per) * 4, h = u / a.D, c = u % a.D;
+  const float* x = a.from[blockIdx.y] + (tok * a.Hk + h) * a.r * a.D + c;
+  f32x4 s = *reinterpret_cast<const f32x4*>(x);
+  for (int j = 1; j < a.r; ++j) s += *reinterpret_cast<const f32x4*>(x + (long)j * a.D);
+  const float o[4] = {s[0], s[1], s[2], s[3]};
+  lin_store<T, 4>(a.to[blockIdx.y], tok * a.ld[blockIdx.y] + u, o, false);
+}
+
+// One token.  A work-group has 32 columns of one head's state: thread (row group tid / 8,
+// column group tid % 8) holds rows r, r + 32, .. and four columns of them.
+struct LinStepArgs {
+  int B, Hk, H, Dk, Dv, n_slots;
+  float scale;
+  long q_ld, k_ld, v_ld;
+  const void *q, *k, *v;
+  const float* g;
+  float* S;
+  const int* slots;
+  void* y;
+  int* err;
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void lin_step_kernel(LinStepArgs a) {
+  __shared__ float4 red[4][8];
+  const int ntile = (a.Dv + kLinStepCols - 1) / kLinStepCols;
+  const int ct = blockIdx.x % ntile, bh = blockIdx.x / ntile;
+  const int b = bh / a.H, h = bh % a.H, hk = h / (a.H / a.Hk);
+  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63;
+  const int c = ct * kLinStepCols + (tid & 7) * 4, r0 = tid >> 3;
+  const bool in = c < a.Dv;                              // Dv is a multiple of 8: all four columns or none
+  const long yat = ((long)b * a.H + h) * a.Dv + c;
+  const int slot = a.slots ? a.slots[b] : b;
+  if (slot < 0 || slot >= a.n_slots) {
+    const float zero[4] = {};
+    if (in && r0 == 0) lin_store<T, 4>(a.y, yat, zero, false);
+    if ((slot < -1 || slot >= a.n_slots) && a.err && h == 0 && ct == 0 && tid == 0) atomicOr(a.err, LL_DEVERR_SLOT);
+    return;
+  }
+  const T* k = static_cast<const T*>(a.k) + b * a.k_ld + (long)hk * a.Dk;
+  const T* q = static_cast<const T*>(a.q) + b * a.q_ld + (long)hk * a.Dk;
+  const T* v = static_cast<const T*>(a.v) + b * a.v_ld + (long)h * a.Dv + c;
+  float* S = a.S + ((long)slot * a.H + h) * a.Dk * a.Dv + c;
+  const float grow = expm1f(lin_log(a.g, h));
+  f32x4 s[4];
+  float kd[4], qd[4], vc[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int d = r0 + 32 * i;
+    const bool has = in && d < a.Dk;
+    s[i] = has ? *reinterpret_cast<const f32x4*>(S + (long)d * a.Dv) : zero_acc();
+    kd[i] = has ? Op<T>::to_f32(k[d]) : 0.f;
+    qd[i] = has ? Op<T>::to_f32(q[d]) : 0.f;
+    vc[i] = in ? Op<T>::to_f32(v[i]) : 0.f;
+  }
+  f32x4 o = zero_acc();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int d = r0 + 32 * i;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      // (l S as S + (l - 1) S: a rounded l would err the same way at every token)
+      s[i][e] = __builtin_fmaf(kd[i], vc[e], __builtin_fmaf(s[i][e], grow, s[i][e]));
+      o[e] = __builtin_fmaf(qd[i], s[i][e], o[e]);
+    }
+    if (in && d < a.Dk) *reinterpret_cast<f32x4*>(S + (long)d * a.Dv) = s[i];
+  }
+#pragma unroll
+  for (int m = 8; m < 64; m <<= 1)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], m, 64);
+  if (l < 8) red[w][l] = make_float4(o[0], o[1], o[2], o[3]);
+  __syncthreads();
+  if (in && r0 == 0) {
+    const float4 x = red[0][tid], y = red[1][tid], z = red[2][tid], u = red[3][tid];
+    const float f[4] = {a.scale * ((x.x + y.x) + (z.x + u.x)), a.scale * ((x.y + y.y) + (z.y + u.y)),
+                        a.scale * ((x.z + y.z) + (z.z + u.z)), a.scale * ((x.w + y.w) + (z.w + u.w))};
+    lin_store<T, 4>(a.y, yat, f, false);
+  }
+}
+
+}  // namespace ll
+
+struct ll_linattn_plan {
+  ll_linattn_desc d;
+  int device = 0, cus = 0;
+  ll::LinArgs a{};                     // sizes and the error word
+  long ld[6] = {};                     // q, k, v, dq, dk, dv
+  float scale = 0.f;
+  float *st = nullptr, *dst = nullptr, *wide = nullptr;
+  int64_t bytes = 0;
+  bool saved = false, has_state = false;
+  const void *q = nullptr, *k = nullptr, *v = nullptr;
+  const float* g = nullptr;
+  const int* seq_len = nullptr;
+  long saved_ld[3] = {};
+};
+
+namespace {
+
+ll_status validate(const ll_linattn_desc* d, bool step) {
+  if (!d) return fail(LL_EINVAL, "desc is NULL");
+  if (d->T_max < 1 || d->B < 1 || d->Hk < 1 || d->Hv < 1 || d->Dk < 1 || d->Dv < 1)
+    return fail(LL_EINVAL, "T_max, B, Hk, Hv, Dk and Dv must be at least 1 (got %d, %d, %d, %d, %d, %d)",
+                d->T_max, d->B, d->Hk, d->Hv, d->Dk, d->Dv);
+  if (step && d->T_max != 1) return fail(LL_EINVAL, "the step takes one token: T_max must be 1 (got %d)", d->T_max);
+  if (d->dtype != LL_F32 && d->dtype != LL_BF16) return fail(LL_EINVAL, "dtype must be LL_F32 or LL_BF16");
+  if (d->Hv % d->Hk) return fail(LL_EINVAL, "Hv = %d is not a multiple of Hk = %d", d->Hv, d->Hk);
+  if (d->reserved) return fail(LL_EINVAL, "reserved must be 0");
+  if (!std::isfinite(d->scale)) return fail(LL_EINVAL, "scale is not finite");
+  if (d->Dk % 8 || d->Dv % 8 || d->Dk > ll::kLinMaxD || d->Dv > ll::kLinMaxD)
+    return fail(LL_EUNSUPPORTED, "Dk = %d and Dv = %d must be multiples of 8, at most %d", d->Dk, d->Dv, ll::kLinMaxD);
+  const int es = d->dtype == LL_BF16 ? 2 : 4;
+  const int64_t qk = (int64_t)d->Hk * d->Dk, v = (int64_t)d->Hv * d->Dv;
+  const int64_t ld[6] = {d->q_ld, d->k_ld, d->v_ld, d->dq_ld, d->dk_ld, d->dv_ld};
+  const int64_t need[6] = {qk, qk, v, qk, qk, v};
+  const char* names[6] = {"q_ld", "k_ld", "v_ld", "dq_ld", "dk_ld", "dv_ld"};
+  for (int i = 0; i < (step ? 3 : 6); ++i)
+    if (ld[i] && (ld[i] < need[i] || ld[i] * es % 16 || ld[i] > (int64_t)1 << 31))
+      return fail(LL_EINVAL, "%s = %lld must be 0, or at least %lld, at most 2^31 and a multiple of 16 bytes",
+                  names[i], (long long)ld[i], (long long)need[i]);
+  if (d->T_max > 1 << 30) return fail(LL_EUNSUPPORTED, "T_max = %d is more than 2^30", d->T_max);
+  // work-groups: at most six a head and part (three passes of two column tiles), and the
+  // sums of shared heads' gradients; the step's column tiles
+  const int64_t heads = (int64_t)d->B * d->Hv;
+  const int64_t groups = step ? heads * ((d->Dv + ll::kLinStepCols - 1) / ll::kLinStepCols) : 6 * heads + (1 << 14);
+  const int64_t most = ll::max_groups(256);
+  if (heads > 1 << 24 || groups > most)
+    return fail(LL_EUNSUPPORTED, "B * Hv = %lld: %lld work-groups, a launch holds %lld", (long long)heads,
+                (long long)groups, (long long)most);
+  if (!step && (int64_t)d->T_max * d->B * qk / 4 > most * 256)
+    return fail(LL_EUNSUPPORTED, "T_max * B * Hk * Dk = %lld is too large for one launch",
+                (long long)d->T_max * d->B * (long long)qk);
+  return LL_OK;
+}
+
+void distances(ll_linattn_plan* p) {
+  const ll_linattn_desc& d = p->d;
+  const long qk = (long)d.Hk * d.Dk, v = (long)d.Hv * d.Dv;
+  p->ld[0] = d.q_ld ? d.q_ld : qk;
+  p->ld[1] = d.k_ld ? d.k_ld : qk;
+  p->ld[2] = d.v_ld ? d.v_ld : v;
+  p->ld[3] = d.dq_ld ? d.dq_ld : qk;
+  p->ld[4] = d.dk_ld ? d.dk_ld : qk;
+  p->ld[5] = d.dv_ld ? d.dv_ld : v;
+}
+
+float scale_of(const ll_linattn_desc& d) { return d.scale != 0.f ? d.scale : (float)(1.0 / std::sqrt((double)d.Dk)); }
+int chunk_of(const ll_linattn_desc& d) { return d.dtype == LL_BF16 ? ll::LinChunk<bf16_t>::n : ll::LinChunk<float>::n; }
+
+void release(ll_linattn_plan* p) {
+  void* all[] = {p->st, p->dst, p->wide, p->a.err};
+  for (void* m : all)
+    if (m) (void)hipFree(m);
+}
+
+template <typename T, int KD>
+void launch(const ll::LinArgs& a, int nv, bool local, unsigned grid, hipStream_t s) {
+  if (local) {
+    if (nv == 1) ll::lin_kernel<T, KD, 1, true><<<dim3(grid), dim3(256), 0, s>>>(a);
+    else ll::lin_kernel<T, KD, 2, true><<<dim3(grid), dim3(256), 0, s>>>(a);
+  } else {
+    if (nv == 1) ll::lin_kernel<T, KD, 1, false><<<dim3(grid), dim3(256), 0, s>>>(a);
+    else ll::lin_kernel<T, KD, 2, false><<<dim3(grid), dim3(256), 0, s>>>(a);
+  }
+}
+
+// The passes a.p[0 .. npass) over all parts.
+hipError_t launch_passes(ll::LinArgs a, bool bf16, bool local, hipStream_t s) {
+  int dr = 0, dc = 0;
+  for (int i = 0; i < a.npass; ++i) {
+    dr = std::max(dr, a.p[i].Dr);
+    dc = std::max(dc, a.p[i].Dc);
+  }
+  const int nv = dc > 64 ? 2 : 1;
+  a.ctiles = 1;
+  const unsigned grid = (unsigned)a.B * a.H * a.parts * a.ctiles * a.npass;
+  const int kd = (dr + 31) / 32;
+  if (bf16) {
+    if (kd == 1) launch<bf16_t, 1>(a, nv, local, grid, s);
+    else if (kd == 2) launch<bf16_t, 2>(a, nv, local, grid, s);
+    else if (kd == 3) launch<bf16_t, 3>(a, nv, local, grid, s);
+    else launch<bf16_t, 4>(a, nv, local, grid, s);
+  } else {
+    if (kd == 1) launch<float, 1>(a, nv, local, grid, s);
+    else if (kd == 2) launch<float, 2>(a, nv, local, grid, s);
+    else if (kd == 3) launch<float, 3>(a, nv, local, grid, s);
+    else launch<float, 4>(a, nv, local, grid, s);
+  }
+  return hipGetLastError();
+}
+
+// The parts' entering states into `to` from the first one; a.p[0] says what makes them.
+hipError_t launch_states(ll::LinArgs a, float* to, const float* first, bool bf16, int chunk, hipStream_t s) {
+  a.local = to;
+  a.npass = 1;
+  if (hipError_t e = launch_passes(a, bf16, true, s); e != hipSuccess) return e;
+  const long blocks = ((long)a.Dk * a.Dv / 4 + 255) / 256;
+  ll::lin_scan_kernel<<<dim3((unsigned)(blocks * a.B * a.H)), dim3(256), 0, s>>>(a, first, chunk);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+extern "C" {
+
+ll_status ll_linattn_plan_create(const ll_linattn_desc* desc, int device, ll_linattn_plan** out) {
+  if (!out) return fail(LL_EINVAL, "out is NULL");
+  *out = nullptr;
+  LL_STATUS(validate(desc, false));
+  LL_STATUS(ll::check_device(device));
+  ll::DeviceGuard guard(device);
+  ll_linattn_plan* p = new (std::nothrow) ll_linattn_plan();
+  if (!p) return fail(LL_ENOMEM, "host allocation of the plan failed");
+  p->d = *desc;
+  p->device = device;
+  distances(p);
+  p->scale = scale_of(*desc);
+  hipDeviceProp_t prop;
+  if (hipGetDeviceProperties(&prop, device) != hipSuccess) {
+    delete p;
+    return fail(LL_EHIP, "hipGetDeviceProperties failed");
+  }
+  p->cus = prop.multiProcessorCount;
+  ll::LinArgs& a = p->a;
+  a.T = desc->T_max; a.B = desc->B; a.H = desc->Hv; a.Dk = desc->Dk; a.Dv = desc->Dv;
+  const int chunk = chunk_of(*desc), nch = (desc->T_max + chunk - 1) / chunk;
+  const long heads = (long)desc->B * desc->Hv;
+  // parts of a row: two work-groups for a compute unit, each with four chunks at least
+  const int want = (int)std::min<long>((2L * p->cus + heads - 1) / heads, std::max(1, nch / 4));
+  a.per = (nch + want - 1) / want;
+  a.parts = (nch + a.per - 1) / a.per;
+  const size_t st = sizeof(float) * heads * a.parts * desc->Dk * desc->Dv;
+  const size_t wide = sizeof(float) * 2 * (size_t)desc->T_max * heads * desc->Dk;
+  const bool train = !desc->inference;
+  struct { void** at; size_t bytes; const char* what; bool want; } bufs[] = {
+      {(void**)&p->st, st, "the parts' states", train || a.parts > 1},
+      {(void**)&p->dst, st, "the gradients of the parts' states", train && a.parts > 1},
+      {(void**)&p->wide, wide, "the heads' gradients of q and k", train && desc->Hv > desc->Hk},
+      {(void**)&a.err, sizeof(int), "the error word", true},
+  };
+  ll_status status = LL_OK;
+  for (auto& b : bufs)
+    if (b.want && status == LL_OK) {
+      status = ll::dalloc(b.at, b.bytes, b.what);
+      p->bytes += (int64_t)b.bytes;
+    }
+  if (status == LL_OK && hipMemset(a.err, 0, sizeof(int)) != hipSuccess)
+    status = fail(LL_EHIP, "hipMemset of the error word failed");
+  if (status == LL_OK) status = ll::wait_created();
+  if (status != LL_OK) {
+    release(p);
+    delete p;
+    return status;
+  }
+  *out = p;
+  return LL_OK;
+}
+
+ll_status ll_linattn_plan_destroy(ll_linattn_plan* p) {
+  if (!p) return LL_OK;
+  ll::DeviceGuard guard(p->device);
+  (void)hipDeviceSynchronize();
+  release(p);
+  delete p;
+  return LL_OK;
+}
+
+ll_status ll_linattn_plan_bytes(const ll_linattn_plan* p, int64_t* device_bytes) {
+  if (!p || !device_bytes) return fail(LL_EINVAL, "plan and device_bytes are required");
+  *device_bytes = p->bytes;
+  return LL_OK;
+}
+
+ll_status ll_linattn_plan_set_ld(ll_linattn_plan* p, const int64_t* ld) {
+  if (!p || !ld) return fail(LL_EINVAL, "plan and ld are required");
+  ll_linattn_desc d = p->d;
+  d.q_ld = ld[0]; d.k_ld = ld[1]; d.v_ld = ld[2]; d.dq_ld = ld[3]; d.dk_ld = ld[4]; d.dv_ld = ld[5];
+  LL_STATUS(validate(&d, false));
+  p->d = d;
+  distances(p);
+  return LL_OK;
+}
+
+ll_status linattn_loop_fwd(ll_linattn_plan* p, void* stream, const void* q, const void* k, const void* v,
+                           const float* g, const int32_t* seq_len, const float* S0, void* y, float* ST,
+                           int32_t save_for_backward) {
+  if (!p) return fail(LL_EINVAL, "plan is NULL");
+  if (!q || !k || !v || !g || !y) return fail(LL_EINVAL, "q, k, v, g and y are required");
+  if (save_for_backward && p->d.inference)
+    return fail(LL_EINVAL, "the plan was created for inference: it keeps nothing for the gradient");
+  LL_ALIGNED(q, 16); LL_ALIGNED(k, 16); LL_ALIGNED(v, 16); LL_ALIGNED(y, 16); LL_ALIGNED(S0, 16); LL_ALIGNED(ST, 16);
+  LL_ALIGNED(g, 4); LL_ALIGNED(seq_len, 4);
+  ll::DeviceGuard guard(p->device);
+  const ll_linattn_desc& d = p->d;
+  const int r = d.Hv / d.Hk;
+  ll::LinArgs a = p->a;
+  a.g = g; a.seq_len = seq_len; a.npass = 1;
+  ll::LinPass& f = a.p[0];
+  f.a = q; f.b = k; f.c = v; f.out = y;
+  f.a_ld = p->ld[0]; f.b_ld = p->ld[1]; f.c_ld = p->ld[2]; f.o_ld = (long)d.Hv * d.Dv;
+  f.ag = f.bg = r; f.cg = f.og = 1;
+  f.Dr = d.Dk; f.Dc = d.Dv; f.rs = d.Dv; f.cs = 1;
+  f.wP = f.wA = p->scale; f.wU = 1.f; f.e = 1;
+  f.last = ST;
+  p->saved = false;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  const bool bf16 = d.dtype == LL_BF16;
+  if (a.parts > 1) {
+    LL_HIP(launch_states(a, p->st, S0, bf16, chunk_of(d), s));
+    f.st = p->st;
+  } else {
+    f.st = S0;
+    f.keep = save_for_backward && S0 ? p->st : nullptr;
+  }
+  LL_HIP(launch_passes(a, bf16, false, s));
+  if (save_for_backward) {
+    p->saved = true;
+    p->has_state = f.st != nullptr;
+    p->q = q; p->k = k; p->v = v; p->g = g; p->seq_len = seq_len;
+    for (int i = 0; i < 3; ++i) p->saved_ld[i] = p->ld[i];
+  }
+  return LL_OK;
+}
+
+ll_status linattn_loop_bwd(ll_linattn_plan* p, void* stream, const void* q, const void* k, const void* v,
+                           const float* g, const int32_t* seq_len, const void* dy, const float* dST, void* dq,
+                           void* dk, void* dv, float* dS0) {
+  if (!p) return fail(LL_EINVAL, "plan is NULL");
+  if (!p->saved)
+    return fail(LL_ESTATE, "no saved forward on this plan (call linattn_loop_fwd with save_for_backward=1 first)");
+  for (int i = 0; i < 3; ++i)
+    if (p->ld[i] != p->saved_ld[i])
+      return fail(LL_ESTATE, "the saved forward's q, k or v had their tokens at other distances than the plan now");
+  if (q != p->q || k != p->k || v != p->v || g != p->g || seq_len != p->seq_len)
+    return fail(LL_EINVAL, "q, k, v, g or seq_len differs from the saved forward's");
+  if (!dy || !dq || !dk || !dv) return fail(LL_EINVAL, "dy, dq, dk and dv are required");
+  if (dS0 && dS0 == dST) return fail(LL_EINVAL, "dS0 must be another array than dST");
+  LL_ALIGNED(dy, 16); LL_ALIGNED(dST, 16); LL_ALIGNED(dq, 16); LL_ALIGNED(dk, 16); LL_ALIGNED(dv, 16);
+  LL_ALIGNED(dS0, 16);
+  ll::DeviceGuard guard(p->device);
+  const ll_linattn_desc& d = p->d;
+  const int r = d.Hv / d.Hk;
+  const bool bf16 = d.dtype == LL_BF16;
+  const long qw = (long)d.Hv * d.Dk, y_ld = (long)d.Hv * d.Dv;
+  ll::LinArgs a = p->a;
+  a.g = g; a.seq_len = seq_len;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  p->saved = false;
+  float* wide_k = p->wide ? p->wide + (long)d.T_max * d.B * qw : nullptr;
+  ll::LinPass v_, q_, k_;
+  v_ = ll::LinPass{};
+  v_.a = k; v_.b = q; v_.c = dy; v_.out = dv;
+  v_.a_ld = p->ld[1]; v_.b_ld = p->ld[0]; v_.c_ld = y_ld; v_.o_ld = p->ld[5];
+  v_.ag = v_.bg = r; v_.cg = v_.og = 1;
+  v_.Dr = d.Dk; v_.Dc = d.Dv; v_.rs = d.Dv; v_.cs = 1;
+  v_.wP = v_.wU = p->scale; v_.wA = 1.f; v_.e = 0; v_.rev = 1;
+  v_.last = dS0;
+  v_.st = dST;
+  if (a.parts > 1) {
+    a.p[0] = v_;
+    LL_HIP(launch_states(a, p->dst, dST, bf16, chunk_of(d), s));
+    v_.st = p->dst;
+  }
+  k_ = v_;
+  k_.a = v; k_.b = dy; k_.c = q;
+  k_.a_ld = p->ld[2]; k_.b_ld = y_ld; k_.c_ld = p->ld[0];
+  k_.ag = k_.bg = 1; k_.cg = r;
+  k_.Dr = d.Dv; k_.Dc = d.Dk; k_.rs = 1; k_.cs = d.Dv;
+  k_.last = nullptr;
+  k_.out = r > 1 ? wide_k : dk; k_.o_ld = r > 1 ? qw : p->ld[4]; k_.og = 1; k_.wide = r > 1;
+  q_ = k_;
+  q_.a = dy; q_.b = v; q_.c = k;
+  q_.a_ld = y_ld; q_.b_ld = p->ld[2]; q_.c_ld = p->ld[1];
+  q_.wP = q_.wA = p->scale; q_.wU = 1.f; q_.e = 1; q_.rev = 0;
+  q_.st = p->has_state ? p->st : nullptr;
+  q_.out = r > 1 ? p->wide : dq; q_.o_ld = r > 1 ? qw : p->ld[3];
+  a.p[0] = v_; a.p[1] = k_; a.p[2] = q_;
+  a.npass = 3;
+  LL_HIP(launch_passes(a, bf16, false, s));
+  if (r > 1) {
+    ll::LinSum m{};
+    m.from[0] = p->wide; m.from[1] = wide_k;
+    m.to[0] = dq; m.to[1] = dk;
+    m.ld[0] = p->ld[3]; m.ld[1] = p->ld[4];
+    m.tokens = (long)d.T_max * d.B;
+    m.Hk = d.Hk; m.r = r; m.D = d.Dk;
+    const dim3 grid((unsigned)((m.tokens * (d.Hk * d.Dk / 4) + 255) / 256), 2);
+    if (bf16) ll::lin_sum_kernel<bf16_t><<<grid, dim3(256), 0, s>>>(m);
+    else ll::lin_sum_kernel<float><<<grid, dim3(256), 0, s>>>(m);
+    LL_HIP(hipGetLastError());
+  }
+  return LL_OK;
+}
+
+ll_status ll_linattn_status_sync(ll_linattn_plan* p, int32_t* device_error) {
+  if (!p) return fail(LL_EINVAL, "plan is NULL");
+  ll::DeviceGuard guard(p->device);
+  return ll::read_error_word(p->a.err, device_error);
+}
+
+ll_status linattn_loop_step(const ll_linattn_desc* desc, void* stream, const void* q, const void* k, const void* v,
+                            const float* g, float* S, const int32_t* slots, int32_t n_slots, void* y,
+                            int32_t* device_error) {
+  LL_STATUS(validate(desc, true));
+  if (!q || !k || !v || !g || !S || !y) return fail(LL_EINVAL, "q, k, v, g, S and y are required");
+  if (n_slots < 1 || (!slots && n_slots < desc->B))
+    return fail(LL_EINVAL, "n_slots = %d is too small for B = %d rows", n_slots, desc->B);
+  LL_ALIGNED(q, 16); LL_ALIGNED(k, 16); LL_ALIGNED(v, 16); LL_ALIGNED(y, 16); LL_ALIGNED(S, 16);
+  LL_ALIGNED(g, 4); LL_ALIGNED(slots, 4); LL_ALIGNED(device_error, 4);
+  ll::LinStepArgs a{};
+  const long qk = (long)desc->Hk * desc->Dk, vw = (long)desc->Hv * desc->Dv;
+  a.B = desc->B; a.Hk = desc->Hk; a.H = desc->Hv; a.Dk = desc->Dk; a.Dv = desc->Dv; a.n_slots = n_slots;
+  a.scale = scale_of(*desc);
+  a.q_ld = desc->q_ld ? desc->q_ld : qk;
+  a.k_ld = desc->k_ld ? desc->k_ld : qk;
+  a.v_ld = desc->v_ld ? desc->v_ld : vw;
+  a.q = q; a.k = k; a.v = v; a.g = g; a.S = S; a.slots = slots; a.y = y; a.err = device_error;
+  const long grid = (long)a.B * a.H * ((a.Dv + ll::kLinStepCols - 1) / ll::kLinStepCols);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (desc->dtype == LL_BF16) ll::lin_step_kernel<bf16_t><<<dim3((unsigned)grid), dim3(256), 0, s>>>(a);
+  else ll::lin_step_kernel<float><<<dim3((unsigned)grid), dim3(256), 0, s>>>(a);
+  LL_HIP(hipGetLastError());
+  return LL_OK;
+}
+
+}  // extern "C"

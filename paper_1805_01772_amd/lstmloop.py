@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_PKG, "liblstmloop.so")
 LL_OK, LL_EINVAL, LL_ENOMEM, LL_EHIP, LL_ESTATE, LL_EUNSUPPORTED = range(6)
 LL_F32, LL_BF16 = 0, 1
 LL_DEVERR_SEQ_LEN, LL_DEVERR_BARRIER, LL_DEVERR_SLOT, LL_DEVERR_TARGET = 1, 2, 4, 8
+LL_DEVERR_TOKEN, LL_DEVERR_BEAM = 16, 32
 LL_LOOPS_GRID, LL_LOOPS_XCD, LL_LOOPS_CHIP = 0, 1, 2
 LL_CELL_LSTM, LL_CELL_RNN, LL_CELL_GRU, LL_CELL_LSTM_SKIP, LL_CELL_LSTM_ACT = 0, 1, 2, 3, 4
 LL_ACT_EPS = 0.01
@@ -36,7 +37,13 @@ EXPORTED = ("ll_plan_create", "ll_plan_destroy", "ll_plan_stack_bytes",
             "delta_loop_fwd", "delta_loop_bwd", "delta_loop_step", "ll_delta_status_sync",
             "ll_logprob_plan_create", "ll_logprob_plan_destroy", "ll_logprob_fwd",
             "ll_logprob_bwd", "ll_logprob_fwd_bwd", "ll_logprob_status_sync",
-            "ll_adamw_plan_create", "ll_adamw_plan_destroy", "ll_adamw_step")
+            "ll_adamw_plan_create", "ll_adamw_plan_destroy", "ll_adamw_step",
+            "ll_linattn_plan_create", "ll_linattn_plan_destroy", "ll_linattn_plan_bytes",
+            "ll_linattn_plan_set_ld", "linattn_loop_fwd", "linattn_loop_bwd", "linattn_loop_step",
+            "ll_linattn_status_sync", "ll_embed_plan_create", "ll_embed_plan_destroy",
+            "ll_embed_plan_bytes", "ll_embed_fwd", "ll_embed_bwd", "ll_embed_status_sync",
+            "ll_beam_plan_create", "ll_beam_plan_destroy", "ll_beam_select", "ll_beam_reorder",
+            "ll_beam_status_sync")
 STAGES = ("prep", "input_proj", "fwd_loop", "bwd_loop", "bwd_operands", "dw", "dx", "loop_setup",
           "recompute")
 
@@ -82,6 +89,29 @@ class ll_adamw_hyper(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
                 ("eps", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint32),
                 ("reserved", ctypes.c_int32)]
+
+
+class ll_linattn_desc(ctypes.Structure):
+    _fields_ = ll_delta_desc._fields_
+
+
+class ll_embed_desc(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("V", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("table_dtype", ctypes.c_int32), ("x_dtype", ctypes.c_int32),
+                ("dx_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
+                ("inference", ctypes.c_int32), ("table_ld", ctypes.c_int64),
+                ("x_ld", ctypes.c_int64), ("dx_ld", ctypes.c_int64), ("grad_ld", ctypes.c_int64),
+                ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class ll_beam_desc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("K", ctypes.c_int32), ("V", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("ld", ctypes.c_int64), ("eos", ctypes.c_int32),
+                ("length_penalty", ctypes.c_float), ("reserved", ctypes.c_int32 * 2)]
+
+
+class ll_beam_tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_bytes", ctypes.c_int64)]
 
 
 class LoopError(RuntimeError):
@@ -160,17 +190,28 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                                          ctypes.POINTER(ll_adamw_tensor), ctypes.c_int, pvp]
     lib.ll_adamw_plan_destroy.argtypes = [vp]
     lib.ll_adamw_step.argtypes = [vp, vp, pvp, ctypes.POINTER(ll_adamw_hyper), vp]
+    lib.ll_linattn_plan_create.argtypes = [ctypes.POINTER(ll_linattn_desc), ctypes.c_int, pvp]
+    lib.ll_linattn_plan_destroy.argtypes = [vp]
+    lib.ll_linattn_plan_bytes.argtypes = [vp, ctypes.POINTER(i64)]
+    lib.ll_linattn_plan_set_ld.argtypes = [vp, ctypes.POINTER(i64)]
+    lib.linattn_loop_fwd.argtypes = [vp] * 10 + [i32]
+    lib.linattn_loop_bwd.argtypes = [vp] * 13
+    lib.linattn_loop_step.argtypes = [ctypes.POINTER(ll_linattn_desc)] + [vp] * 7 + [i32, vp, vp]
+    lib.ll_linattn_status_sync.argtypes = [vp, ctypes.POINTER(i32)]
+    lib.ll_embed_plan_create.argtypes = [ctypes.POINTER(ll_embed_desc), ctypes.c_int, pvp]
+    lib.ll_embed_plan_destroy.argtypes = [vp]
+    lib.ll_embed_plan_bytes.argtypes = [vp, ctypes.POINTER(i64)]
+    lib.ll_embed_fwd.argtypes = [vp, vp, i32, vp, vp, vp]
+    lib.ll_embed_bwd.argtypes = [vp, vp, i32, vp, vp, vp, i32]
+    lib.ll_embed_status_sync.argtypes = [vp, ctypes.POINTER(i32)]
+    lib.ll_beam_plan_create.argtypes = [ctypes.POINTER(ll_beam_desc), ctypes.c_int, pvp]
+    lib.ll_beam_plan_destroy.argtypes = [vp]
+    lib.ll_beam_select.argtypes = [vp, vp, i32] + [vp] * 9
+    lib.ll_beam_reorder.argtypes = [vp, i32, i32, vp, i32, ctypes.POINTER(ll_beam_tensor), vp, i32, vp, vp]
+    lib.ll_beam_status_sync.argtypes = [vp, ctypes.POINTER(i32)]
     lib.ll_last_error.restype = ctypes.c_char_p
     lib.ll_version.restype = ctypes.c_char_p
-    for name in ("ll_plan_create", "ll_plan_destroy", "ll_plan_stack_bytes", "ll_plan_geometry",
-                 "lstm_loop_fwd", "lstm_loop_bwd", "ll_status_sync", "ll_plan_set_timing",
-                 "ll_plan_set_timing_stages", "ll_plan_read_timing", "ll_measure_mfma_peak",
-                 "ll_eval_activations", "lstm_loop_fwd_noalloc", "ll_delta_plan_create",
-                 "ll_delta_plan_destroy", "ll_delta_plan_bytes", "ll_delta_plan_set_ld", "delta_loop_fwd",
-                 "delta_loop_bwd", "delta_loop_step", "ll_delta_status_sync",
-                 "ll_logprob_plan_create", "ll_logprob_plan_destroy", "ll_logprob_fwd",
-                 "ll_logprob_bwd", "ll_logprob_fwd_bwd", "ll_logprob_status_sync",
-                 "ll_adamw_plan_create", "ll_adamw_plan_destroy", "ll_adamw_step"):
+    for name in set(EXPORTED) - {"ll_last_error", "ll_version"}:
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -462,25 +503,18 @@ def make_delta_desc(T_max: int, B: int, Hk: int, Hv: int, Dk: int, Dv: int, dtyp
                          1 if inference else 0, q_ld, k_ld, v_ld, dq_ld, dk_ld, dv_ld, scale, 0)
 
 
-class DeltaPlan(_OpPlan):
-    """The gated delta rule over [T_max, B] tokens (ll_delta_plan)."""
+class _TokenPlan(_OpPlan):
+    """A plan over [T_max, B] tokens whose q, k, v and their gradients may be slices
+    of a projection's rows."""
 
-    _destroy = "ll_delta_plan_destroy"
+    _set_ld = ""
 
-    def __init__(self, T_max: int, B: int, Hk: int, Hv: int, Dk: int, Dv: int, dtype: str = "f32",
-                 inference: bool = False, q_ld: int = 0, k_ld: int = 0, v_ld: int = 0,
-                 dq_ld: int = 0, dk_ld: int = 0, dv_ld: int = 0, scale: float = 0.0,
-                 device: int = 0):
-        self.desc = d = make_delta_desc(T_max, B, Hk, Hv, Dk, Dv, dtype, inference, q_ld, k_ld,
-                                        v_ld, dq_ld, dk_ld, dv_ld, scale)
-        self.dtype = dtype
-        self._t = _dtype(dtype)
-        self._create("ll_delta_plan_create", d, device)
+    def _sizes(self, T_max, B, Hk, Hv, Dk, Dv, q_ld, k_ld, v_ld, dq_ld, dk_ld, dv_ld):
         qk, v = Hk * Dk, Hv * Dv
         self._note(dict(q=q_ld or qk, k=k_ld or qk, v=v_ld or v, dq=dq_ld or qk, dk=dk_ld or qk,
                         dv=dv_ld or v))
         self._qk, self._v = (T_max, B, Hk, Dk), (T_max, B, Hv, Dv)
-        self._gate, self._state = (T_max, B, Hv), (B, Hv, Dk, Dv)
+        self._state = (B, Hv, Dk, Dv)
 
     def _distances(self, **tokens):
         """The plan's distances as these tensors have them.  The tokens of a single
@@ -495,7 +529,8 @@ class DeltaPlan(_OpPlan):
 
     def _set_distances(self, ld):
         names = ("q", "k", "v", "dq", "dk", "dv")
-        _check(self._lib.ll_delta_plan_set_ld(self._h, (ctypes.c_int64 * 6)(*(ld[n] for n in names))))
+        set_ld = getattr(self._lib, self._set_ld)
+        _check(set_ld(self._h, (ctypes.c_int64 * 6)(*(ld[n] for n in names))))
         self._note(ld)
 
     def _note(self, ld):
@@ -514,6 +549,25 @@ class DeltaPlan(_OpPlan):
             if ld is not old:
                 self._set_distances(old)
             raise
+
+
+class DeltaPlan(_TokenPlan):
+    """The gated delta rule over [T_max, B] tokens (ll_delta_plan)."""
+
+    _destroy = "ll_delta_plan_destroy"
+    _set_ld = "ll_delta_plan_set_ld"
+
+    def __init__(self, T_max: int, B: int, Hk: int, Hv: int, Dk: int, Dv: int, dtype: str = "f32",
+                 inference: bool = False, q_ld: int = 0, k_ld: int = 0, v_ld: int = 0,
+                 dq_ld: int = 0, dk_ld: int = 0, dv_ld: int = 0, scale: float = 0.0,
+                 device: int = 0):
+        self.desc = d = make_delta_desc(T_max, B, Hk, Hv, Dk, Dv, dtype, inference, q_ld, k_ld,
+                                        v_ld, dq_ld, dk_ld, dv_ld, scale)
+        self.dtype = dtype
+        self._t = _dtype(dtype)
+        self._create("ll_delta_plan_create", d, device)
+        self._sizes(T_max, B, Hk, Hv, Dk, Dv, q_ld, k_ld, v_ld, dq_ld, dk_ld, dv_ld)
+        self._gate = (T_max, B, Hv)
 
     def _inputs(self, q, k, v, g, beta, seq_len, ld):
         t, f = self._t, _dtype("float32")
@@ -594,6 +648,239 @@ def delta_loop_step(q, k, v, g, beta, S, y, slots=None, scale: float = 0.0, devi
 def _step_desc(B, Hk, Hv, Dk, Dv, dtype, q_ld, k_ld, v_ld, scale):
     return ctypes.byref(make_delta_desc(1, B, Hk, Hv, Dk, Dv, dtype, True, q_ld, k_ld, v_ld,
                                         scale=scale))
+
+
+def make_linattn_desc(*args, **kw) -> ll_linattn_desc:
+    """As make_delta_desc."""
+    d = make_delta_desc(*args, **kw)
+    return ll_linattn_desc(*(getattr(d, n) for n, _ in d._fields_))
+
+
+class LinattnPlan(_TokenPlan):
+    """Linear attention with a decay for each head over [T_max, B] tokens
+    (ll_linattn_plan)."""
+
+    _destroy = "ll_linattn_plan_destroy"
+    _set_ld = "ll_linattn_plan_set_ld"
+
+    def __init__(self, T_max: int, B: int, Hk: int, Hv: int, Dk: int, Dv: int, dtype: str = "f32",
+                 inference: bool = False, q_ld: int = 0, k_ld: int = 0, v_ld: int = 0,
+                 dq_ld: int = 0, dk_ld: int = 0, dv_ld: int = 0, scale: float = 0.0,
+                 device: int = 0):
+        self.desc = d = make_linattn_desc(T_max, B, Hk, Hv, Dk, Dv, dtype, inference, q_ld, k_ld,
+                                          v_ld, dq_ld, dk_ld, dv_ld, scale)
+        self.dtype = dtype
+        self._t = _dtype(dtype)
+        self._create("ll_linattn_plan_create", d, device)
+        self._sizes(T_max, B, Hk, Hv, Dk, Dv, q_ld, k_ld, v_ld, dq_ld, dk_ld, dv_ld)
+
+    def _inputs(self, q, k, v, g, seq_len, ld):
+        t = self._t
+        return (_tokens(q, "q", self._qk, ld["q"], t), _tokens(k, "k", self._qk, ld["k"], t),
+                _tokens(v, "v", self._v, ld["v"], t),
+                _want(g, "g", self._state[1:2], _dtype("float32")),
+                _want(seq_len, "seq_len", self._qk[1:2], _dtype("int32"), optional=True))
+
+    def fwd(self, q, k, v, g, seq_len, S0, y, ST, save_for_backward: bool = True,
+            stream=None) -> None:
+        """linattn_loop_fwd (asynchronous on `stream`, default: torch's current); g [Hv]
+        holds the logarithms of the heads' decays."""
+        f = _dtype("float32")
+        ld = self._distances(q=q, k=k, v=v)
+        self._call(ld, self._lib.linattn_loop_fwd,
+                   _stream(stream), *self._inputs(q, k, v, g, seq_len, ld),
+                   _want(S0, "S0", self._state, f, optional=True), _want(y, "y", self._v, self._t),
+                   _want(ST, "ST", self._state, f, optional=True), 1 if save_for_backward else 0)
+
+    def bwd(self, q, k, v, g, seq_len, dy, dST, dq, dk, dv, dS0=None, stream=None) -> None:
+        """linattn_loop_bwd (asynchronous on `stream`); q .. seq_len are the tensors the
+        saved forward was given."""
+        t, f = self._t, _dtype("float32")
+        ld = self._distances(q=q, k=k, v=v, dq=dq, dk=dk, dv=dv)
+        args = (*self._inputs(q, k, v, g, seq_len, ld),
+                _want(dy, "dy", self._v, t), _want(dST, "dST", self._state, f, optional=True),
+                _tokens(dq, "dq", self._qk, ld["dq"], t), _tokens(dk, "dk", self._qk, ld["dk"], t),
+                _tokens(dv, "dv", self._v, ld["dv"], t),
+                _want(dS0, "dS0", self._state, f, optional=True))
+        self._call(ld, self._lib.linattn_loop_bwd, _stream(stream), *args)
+
+    def bytes(self) -> int:
+        """ll_linattn_plan_bytes: device memory that the plan holds."""
+        n = ctypes.c_int64()
+        _check(self._lib.ll_linattn_plan_bytes(self._h, ctypes.byref(n)))
+        return n.value
+
+    def status_sync(self) -> int:
+        """ll_linattn_status_sync: wait, then return (and clear) the device error word."""
+        return self._status("ll_linattn_status_sync")
+
+
+def linattn_loop_fwd(plan: LinattnPlan, *args, **kw):
+    return plan.fwd(*args, **kw)
+
+
+def linattn_loop_bwd(plan: LinattnPlan, *args, **kw):
+    return plan.bwd(*args, **kw)
+
+
+def linattn_loop_step(q, k, v, g, S, y, slots=None, scale: float = 0.0, device_error=None,
+                      stream=None) -> None:
+    """linattn_loop_step: one token for the B rows of q, k [B, Hk, Dk], v [B, Hv, Dv]
+    (rows may be slices of a projection's), decays g [Hv], states S [n_slots, Hv, Dk,
+    Dv] updated in place (asynchronous on `stream`)."""
+    (B, Hk, Dk), (_, Hv, Dv) = q.shape, v.shape
+    t, f = q.dtype, _dtype("float32")
+    lq, lk, lv = (q.stride(0), k.stride(0), v.stride(0)) if B > 1 else (Hk * Dk, Hk * Dk, Hv * Dv)
+    if t is f:
+        name = "f32"
+    elif t is _dtype("bfloat16"):
+        name = "bf16"
+    else:
+        raise ValueError(f"q: float32 or bfloat16 is wanted, got {t}")
+    _check(load_library().linattn_loop_step(
+        _linattn_step_desc(B, Hk, Hv, Dk, Dv, name, lq, lk, lv, scale), _stream(stream),
+        _tokens(q, "q", (B, Hk, Dk), lq, t), _tokens(k, "k", (B, Hk, Dk), lk, t),
+        _tokens(v, "v", (B, Hv, Dv), lv, t), _want(g, "g", (Hv,), f),
+        _want(S, "S", (S.shape[0], Hv, Dk, Dv), f),
+        _want(slots, "slots", (B,), _dtype("int32"), optional=True), S.shape[0],
+        _want(y, "y", (B, Hv, Dv), t),
+        _want(device_error, "device_error", (1,), _dtype("int32"), optional=True)))
+
+
+@functools.lru_cache(maxsize=256)
+def _linattn_step_desc(B, Hk, Hv, Dk, Dv, dtype, q_ld, k_ld, v_ld, scale):
+    return ctypes.byref(make_linattn_desc(1, B, Hk, Hv, Dk, Dv, dtype, True, q_ld, k_ld, v_ld,
+                                          scale=scale))
+
+
+def _type_code(name: str, what: str) -> int:
+    if name not in ("f32", "bf16"):
+        raise ValueError(f"{what} {name!r} is neither 'f32' nor 'bf16'")
+    return LL_BF16 if name == "bf16" else LL_F32
+
+
+class EmbedPlan(_OpPlan):
+    """Lookups in a table of V rows of D, and the table's gradient (ll_embed_plan), for
+    up to N tokens; rows of the arrays table_ld .. grad_ld elements apart (0: D)."""
+
+    _destroy = "ll_embed_plan_destroy"
+
+    def __init__(self, N: int, V: int, D: int, table_dtype: str = "f32", x_dtype: str = "f32",
+                 dx_dtype: str = "f32", grad_dtype: str = "f32", scale: float = 1.0,
+                 inference: bool = False, table_ld: int = 0, x_ld: int = 0, dx_ld: int = 0,
+                 grad_ld: int = 0, device: int = 0):
+        if scale == 0:
+            raise ValueError("scale must not be 0")
+        names = dict(table_dtype=table_dtype, x_dtype=x_dtype, dx_dtype=dx_dtype, grad_dtype=grad_dtype)
+        codes = [_type_code(t, n) for n, t in names.items()]
+        self.desc = ll_embed_desc(N, V, D, *codes, 1 if inference else 0, table_ld, x_ld, dx_ld,
+                                  grad_ld, scale, 0)
+        self.N, self.V, self.D = N, V, D
+        self._create("ll_embed_plan_create", self.desc, device)
+        self._rows_of = {n: (_dtype(t), ld or D) for n, t, ld in (
+            ("table", table_dtype, table_ld), ("x", x_dtype, x_ld), ("dx", dx_dtype, dx_ld),
+            ("dtable", grad_dtype, grad_ld))}
+
+    def _rows(self, t, name: str, n: int):
+        """Address of n rows of D; any leading dimensions."""
+        dtype, ld = self._rows_of[name]
+        sh, st = t.shape, t.stride()
+        if sh[-1:] != (self.D,) or t.dtype is not dtype or not t.is_cuda or t.numel() != n * self.D:
+            _refuse(t, name, (n, self.D), dtype)
+        bad, want = self.D > 1 and st[-1] != 1, ld
+        for i in range(len(sh) - 2, -1, -1):
+            bad = bad or (sh[i] > 1 and st[i] != want)
+            want *= sh[i]
+        if bad and n:
+            raise ValueError(f"{name}: rows {ld} elements apart are wanted, got strides {tuple(st)}")
+        return t.data_ptr()
+
+    def fwd(self, table, tokens, x, stream=None) -> None:
+        """ll_embed_fwd (asynchronous on `stream`): tokens int32 of any shape, x that
+        shape and D."""
+        n = tokens.numel()
+        _check(self._lib.ll_embed_fwd(
+            self._h, _stream(stream), n, self._rows(table, "table", self.V),
+            _want(tokens, "tokens", tokens.shape, _dtype("int32")), self._rows(x, "x", n)))
+
+    def bwd(self, tokens, dx, dtable, accumulate: bool = False, stream=None) -> None:
+        """ll_embed_bwd (asynchronous on `stream`): dtable is overwritten, or added to."""
+        n = tokens.numel()
+        _check(self._lib.ll_embed_bwd(
+            self._h, _stream(stream), n, _want(tokens, "tokens", tokens.shape, _dtype("int32")),
+            self._rows(dx, "dx", n), self._rows(dtable, "dtable", self.V), 1 if accumulate else 0))
+
+    def bytes(self) -> int:
+        """ll_embed_plan_bytes: device memory that the plan holds."""
+        n = ctypes.c_int64()
+        _check(self._lib.ll_embed_plan_bytes(self._h, ctypes.byref(n)))
+        return n.value
+
+    def status_sync(self) -> int:
+        """ll_embed_status_sync: wait, then return (and clear) the device error word."""
+        return self._status("ll_embed_status_sync")
+
+
+class BeamPlan(_OpPlan):
+    """A step of up to B searches with K beams over V tokens (ll_beam_plan), logits ld
+    elements from row to row (0: V)."""
+
+    _destroy = "ll_beam_plan_destroy"
+
+    def __init__(self, B: int, K: int, V: int, dtype: str = "f32", ld: int = 0, eos: int = -1,
+                 length_penalty: float = 0.0, device: int = 0):
+        self.desc = ll_beam_desc(B, K, V, _type_code(dtype, "dtype"), ld, eos, length_penalty)
+        self.K, self.V, self.ld = K, V, ld or V
+        self._t = _dtype(dtype)
+        self._create("ll_beam_plan_create", self.desc, device)
+
+    def select(self, logits, scores, finished, lengths, parents, tokens, scores_out,
+               finished_out=None, lengths_out=None, stream=None) -> None:
+        """ll_beam_select (asynchronous on `stream`): logits [searches * K, V], the others
+        [searches, K]; finished and lengths may be None."""
+        n, i, f = scores.shape[0], _dtype("int32"), _dtype("float32")
+        rows, shape, st = n * self.K, (n, self.K), logits.stride()
+        if logits.shape != (rows, self.V) or logits.dtype is not self._t or not logits.is_cuda:
+            _refuse(logits, "logits", (rows, self.V), self._t)
+        if (self.V > 1 and st[1] != 1) or (rows > 1 and st[0] != self.ld):
+            raise ValueError(f"logits: rows {self.ld} elements apart are wanted, got strides {tuple(st)}")
+        _check(self._lib.ll_beam_select(
+            self._h, _stream(stream), n, logits.data_ptr(), _want(scores, "scores", shape, f),
+            _want(finished, "finished", shape, i, optional=True),
+            _want(lengths, "lengths", shape, i, optional=True),
+            _want(parents, "parents", shape, i), _want(tokens, "tokens", shape, i),
+            _want(scores_out, "scores_out", shape, f),
+            _want(finished_out, "finished_out", shape, i, optional=True),
+            _want(lengths_out, "lengths_out", shape, i, optional=True)))
+
+    def status_sync(self) -> int:
+        """ll_beam_status_sync: wait, then return (and clear) the device error word."""
+        return self._status("ll_beam_status_sync")
+
+
+def ll_beam_reorder(parents, tensors: Sequence, slots=None, slots_out=None, device_error=None,
+                    stream=None) -> None:
+    """ll_beam_reorder (asynchronous on `stream`): parents [searches, K]; tensors are
+    contiguous with searches * K rows (dimension 0, or [searches, K, ..]), or, with
+    slots [searches, K], with as many rows as their pool has slots."""
+    i = _dtype("int32")
+    shape = tuple(parents.shape)
+    if len(shape) != 2:
+        raise ValueError(f"parents: [searches, K] is wanted, got {shape}")
+    n, K = shape
+    rows = tensors[0].shape[0] if slots is not None and len(tensors) else n * K
+    recs = (ll_beam_tensor * max(1, len(tensors)))()
+    for j, t in enumerate(tensors):
+        if not t.is_cuda or not t.is_contiguous():
+            raise ValueError("tensors passed to the library must live on the GPU and be contiguous")
+        if t.dim() < 1 or (t.shape[0] != rows and (slots is not None or tuple(t.shape[:2]) != shape)):
+            raise ValueError(f"tensors[{j}]: {rows} rows are wanted, got {tuple(t.shape)}")
+        recs[j] = ll_beam_tensor(t.data_ptr(), t.numel() // max(1, rows) * t.element_size())
+    _check(load_library().ll_beam_reorder(
+        _stream(stream), n, K, _want(parents, "parents", shape, i), len(tensors), recs,
+        _want(slots, "slots", shape, i, optional=True), rows if slots is not None else 0,
+        _want(slots_out, "slots_out", shape, i, optional=True),
+        _want(device_error, "device_error", (1,), i, optional=True)))
 
 
 class LogprobPlan(_OpPlan):
