@@ -95,6 +95,23 @@ template <> struct Lin<bf16_t> {
     split8<NP>(f, s.p);
     return s;
   }
+  // A float operand in LDS: `half` 0 or 1 of fragment `at` as its four floats say, and the
+  // whole of it.
+  static constexpr int kHeld = NP * 1024;
+  __device__ static __forceinline__ void put(unsigned char* lds, int at, int half, int l, f32x4 x) {
+    uint32_t a[NP], b[NP];
+    split2<NP>(x[0], x[1], a);
+    split2<NP>(x[2], x[3], b);
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+      *reinterpret_cast<uint2*>(lds + at * kHeld + i * 1024 + l * 16 + half * 8) = make_uint2(a[i], b[i]);
+  }
+  __device__ static __forceinline__ Split get(const unsigned char* lds, int at, int l) {
+    Split s;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) s.p[i] = ld16(lds + at * kHeld + i * 1024 + l * 16);
+    return s;
+  }
   __device__ static __forceinline__ void floats(Raw r, f32x4& x, f32x4& y) {
     const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
@@ -136,6 +153,14 @@ template <> struct Lin<float> {
     return r;
   }
   __device__ static __forceinline__ Split split(f32x4 x, f32x4 y) { return Raw{x, y}; }
+  static constexpr int kHeld = 2048;
+  __device__ static __forceinline__ void put(unsigned char* lds, int at, int half, int l, f32x4 x) {
+    *reinterpret_cast<f32x4*>(lds + at * kHeld + half * 1024 + l * 16) = x;
+  }
+  __device__ static __forceinline__ Split get(const unsigned char* lds, int at, int l) {
+    return Raw{*reinterpret_cast<const f32x4*>(lds + at * kHeld + l * 16),
+               *reinterpret_cast<const f32x4*>(lds + at * kHeld + 1024 + l * 16)};
+  }
   __device__ static __forceinline__ void floats(Raw r, f32x4& x, f32x4& y) {
     x = r.x;
     y = r.y;
@@ -168,13 +193,13 @@ __device__ __forceinline__ void lin_store(void* dst, long at, const float* x, bo
 
 // ---------------------------------------------------------------------------
 // One part of a row, head and pass, 64 NV columns of the state: chunk after chunk.  A
-// wave has 16 NV columns of the state in its accumulators and makes the chunk's products
-// a_i.b_j for itself (a sixth of its matrix instructions), so that nothing but the
-// operands goes through LDS.  LOCAL: only the state of the part's tokens alone.
+// wave has 16 NV columns of the state in its accumulators, and a share of the chunk's
+// products a_i.b_j, which go to the others through LDS as the next product takes them.
+// LOCAL: only the state of the part's tokens alone.
 // KD: rows of the state in steps of 32.
 // ---------------------------------------------------------------------------
 template <typename T, int KD, int NV, bool LOCAL>
-__global__ __launch_bounds__(256) void lin_kernel(LinArgs args) {
+__global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
   typedef Lin<T> L;
   constexpr int CT = LinChunk<T>::n, NI = CT / 16, NM = CT / 32, NC = 64 * NV, Q = 4 * NV;
   constexpr int E = 16 / sizeof(T), PR = 32 * KD + E, PC = NC + E;
@@ -183,6 +208,10 @@ __global__ __launch_bounds__(256) void lin_kernel(LinArgs args) {
   __shared__ __align__(16) T as[LOCAL ? 8 : CT * PR];
   __shared__ __align__(16) T bs[CT * PR];
   __shared__ __align__(16) T cs[CT * PC];
+  // the chunk's products a_i.b_j: pairs of tiles (rows 32 j .., columns 16 i ..)
+  constexpr int NF = NI == 4 ? 6 : 2;
+  auto pair = [](int i, int j) { return i + (i > 2 ? 1 : 0) + j; };   // 0 | 1 | 2 3 | 4 5
+  __shared__ __align__(16) unsigned char ps[LOCAL ? 16 : NF * L::kHeld];
   // items that read the same tokens (columns and passes) lie 8 work-groups apart: on one
   // XCD, one after the other
   const int sub = args.ctiles * args.npass, items = args.B * args.H * args.parts;
@@ -220,7 +249,7 @@ __global__ __launch_bounds__(256) void lin_kernel(LinArgs args) {
   f32x4 S[2 * KD][NV];
   const long stride = (long)args.Dk * args.Dv;
   const float* st = LOCAL || !p.st ? nullptr : p.st + (long)item * stride;
-  auto each_state = [&](auto f) {
+  auto each_state = [&](auto f) __attribute__((always_inline)) {
 #pragma unroll
     for (int d = 0; d < 2 * KD; ++d)
 #pragma unroll
@@ -229,7 +258,7 @@ __global__ __launch_bounds__(256) void lin_kernel(LinArgs args) {
         f(S[d][t], r, (long)r * p.rs + (long)c * p.cs, r < p.Dr && c < p.Dc);
       }
   };
-  each_state([&](f32x4& s, int, long at, bool in) {
+  each_state([&](f32x4& s, int, long at, bool in) __attribute__((always_inline)) {
     s = zero_acc();
     if (!st || !in) return;
     if (p.rs == 1) s = *reinterpret_cast<const f32x4*>(st + at);
@@ -237,8 +266,8 @@ __global__ __launch_bounds__(256) void lin_kernel(LinArgs args) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[e] = st[at + (long)e * p.rs];
   });
-  auto put_state = [&](float* to) {
-    each_state([&](f32x4& s, int, long at, bool in) {
+  auto put_state = [&](float* to) __attribute__((always_inline)) {
+    each_state([&](f32x4& s, int, long at, bool in) __attribute__((always_inline)) {
       if (!in) return;
       if (p.rs == 1) *reinterpret_cast<f32x4*>(to + at) = s;
       else
@@ -248,6 +277,9 @@ __global__ __launch_bounds__(256) void lin_kernel(LinArgs args) {
   };
   if (!LOCAL && p.keep) put_state(p.keep + (long)item * stride);
 
+  // (what lies above the diagonal in a pair's second tile stays zero)
+  if constexpr (!LOCAL)
+    for (int i = tid; i < NF * L::kHeld / 16; i += 256) reinterpret_cast<uint4*>(ps)[i] = zero4();
   const float g = lin_log(args.g, h);
   // weights: of pairs on the diagonal tiles, of pairs one tile apart (more apart: times
   // l^16 each), of a token's place in its tile, and of what a full chunk's tokens leave
@@ -265,7 +297,7 @@ __global__ __launch_bounds__(256) void lin_kernel(LinArgs args) {
   for (int i = 0; i < 4; ++i) l16[i] = expf(g * (16 * i));
 
   uint4 ra[LR], rb[LR], rc[LC];
-  auto load = [&](int t0) {
+  auto load = [&](int t0) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < LR; ++i) {
       const int u = tid + 256 * i, row = u / UR, col = u % UR * E;
@@ -299,53 +331,49 @@ __global__ __launch_bounds__(256) void lin_kernel(LinArgs args) {
     if (t0 + CT < t_end) load(t0 + CT);
     const int m = min(CT, len - t0);
     typename L::Raw cf[NM][NV];
-#pragma unroll
-    for (int j = 0; j < NM; ++j)
-#pragma unroll
-      for (int t = 0; t < NV; ++t) cf[j][t] = L::cols(cs + 32 * j * PC + 16 * NV * w + 4 * t, PC, lo, hi, Q);
     if constexpr (!LOCAL) {
-      f32x4 P[NI][NI], y[NI][NV];
+      // the chunk's products, a tile of 16 x 16 a wave in turn: rows j, columns i >= j
+      for (int at = w; at < NI * (NI + 1) / 2; at += 4) {
+        const int i = at >= 6 ? 3 : at >= 3 ? 2 : at >= 1 ? 1 : 0, j = at - i * (i + 1) / 2;
+        f32x4 x = zero_acc();
 #pragma unroll
-      for (int i = 0; i < NI; ++i) {
+        for (int k = 0; k < KD; ++k)
+          x = L::mm(L::rows(bs + (16 * j + lo) * PR + 32 * k + 4 * hi), L::rows(as + (16 * i + lo) * PR + 32 * k + 4 * hi), x);
+        const float f = i - j > 1 ? l16[i - j - 1] : 1.f;
 #pragma unroll
-        for (int j = 0; j < NI; ++j) P[i][j] = zero_acc();
+        for (int r = 0; r < 4; ++r) x[r] = i == j ? (lo >= 4 * hi + r ? x[r] * near[r] : 0.f) : x[r] * (far[r] * f);
+        L::put(ps, pair(i, j / 2), j & 1, l, x);
+      }
+      f32x4 y[NI][NV];
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int t = 0; t < NV; ++t) y[i][t] = zero_acc();
-      }
 #pragma unroll
       for (int k = 0; k < KD; ++k) {
-        typename L::Raw fa[NI], fb[NI];
+        typename L::Split s[NV];
+#pragma unroll
+        for (int t = 0; t < NV; ++t) s[t] = L::split(S[2 * k][t], S[2 * k + 1][t]);
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-          fa[i] = L::rows(as + (16 * i + lo) * PR + 32 * k + 4 * hi);
-          fb[i] = L::rows(bs + (16 * i + lo) * PR + 32 * k + 4 * hi);
-        }
+          const typename L::Raw fa = L::rows(as + (16 * i + lo) * PR + 32 * k + 4 * hi);
 #pragma unroll
-        for (int i = 0; i < NI; ++i)
-#pragma unroll
-          for (int j = 0; j <= i; ++j) P[i][j] = L::mm(fb[j], fa[i], P[i][j]);
-#pragma unroll
-        for (int t = 0; t < NV; ++t) {
-          const typename L::Split s = L::split(S[2 * k][t], S[2 * k + 1][t]);
-#pragma unroll
-          for (int i = 0; i < NI; ++i) y[i][t] = L::mm(s, fa[i], y[i][t]);
+          for (int t = 0; t < NV; ++t) y[i][t] = L::mm(s[t], fa, y[i][t]);
         }
       }
+      lds_barrier();                                     // the products are there
+#pragma unroll
+      for (int j = 0; j < NM; ++j)
+#pragma unroll
+        for (int t = 0; t < NV; ++t) cf[j][t] = L::cols(cs + 32 * j * PC + 16 * NV * w + 4 * t, PC, lo, hi, Q);
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const float f = place * l16[i];
 #pragma unroll
         for (int t = 0; t < NV; ++t) y[i][t] *= f;
 #pragma unroll
-        for (int j = 0; j <= i; ++j) {
-          const f32x4 x = P[i][j];
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            P[i][j][r] = i == j ? (lo >= 4 * hi + r ? x[r] * near[r] : 0.f) : x[r] * (far[r] * l16[i - j - 1]);
-        }
-#pragma unroll
         for (int j = 0; j <= i / 2; ++j) {
-          const typename L::Split s = L::split(P[i][2 * j], 2 * j + 1 <= i ? P[i][2 * j + 1] : zero_acc());
+          const typename L::Split s = L::get(ps, pair(i, j), l);
 #pragma unroll
           for (int t = 0; t < NV; ++t) y[i][t] = L::mm(cf[j][t], s, y[i][t]);
         }
@@ -359,6 +387,11 @@ __global__ __launch_bounds__(256) void lin_kernel(LinArgs args) {
           lin_store<T, 4 * NV>(p.out, token(tok) * p.o_ld + oh + mine, o, p.wide);
         }
       }
+    } else {
+#pragma unroll
+      for (int j = 0; j < NM; ++j)
+#pragma unroll
+        for (int t = 0; t < NV; ++t) cf[j][t] = L::cols(cs + 32 * j * PC + 16 * NV * w + 4 * t, PC, lo, hi, Q);
     }
     // S' = l^m S + ..; as S + (l^m - 1) S, because a rounded l^m would err the same way in
     // every chunk
