@@ -25,6 +25,8 @@ constexpr int kLinMaxD = 128;
 constexpr int kLinStepCols = 32;
 
 // Tokens of a chunk: 16 KB of 128 columns in either type.
+__device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
+
 template <typename T> struct LinChunk { static constexpr int n = 64; };
 template <> struct LinChunk<float> { static constexpr int n = 32; };
 
@@ -63,6 +65,16 @@ __device__ __forceinline__ float lin_log(const float* g, int h) {
   return x < -200.f ? -200.f : x;
 }
 
+// Rows in LDS have UP units of 16 bytes, a power of two, and hold unit u at u ^ turn(row):
+// 16 lanes that read the same unit of 16 rows, or two units of 8 rows, meet 16 different
+// places of the banks.
+template <int UP>
+__device__ __forceinline__ int lin_turn(int row) {
+  if (UP >= 16) return (row & 7) << 1 | (row >> 3 & 1);
+  if (UP == 8) return (row >> 1 & 3) << 1 | (row >> 3 & 1);
+  return (row >> 2 & 1) << 1 | (row >> 3 & 1);
+}
+
 // Operands over 32 of what a product sums over: a lane holds the four of its group hi
 // in each of two tiles of 16, the four that an accumulator tile gives it.  So states and
 // the chunk's products go from accumulators into the next product as they lie.
@@ -74,18 +86,25 @@ template <> struct Lin<bf16_t> {
   typedef uint4 Raw;
   static constexpr int NP = 3;
   struct Split { uint4 p[NP]; };
-  __device__ static __forceinline__ Raw rows(const bf16_t* p) {
-    const uint2 x = *reinterpret_cast<const uint2*>(p), y = *reinterpret_cast<const uint2*>(p + 16);
+  // Row `row` (16 i + lo), steps k: columns 32 k + 4 hi .. and 16 further on.
+  template <int UP>
+  __device__ static __forceinline__ Raw rows(const bf16_t* m, int row, int k, int hi) {
+    const bf16_t* p = m + row * UP * 8 + 4 * (hi & 1);
+    const int u = (hi >> 1) ^ lin_turn<UP>(row);
+    const uint2 x = *reinterpret_cast<const uint2*>(p + 8 * (u ^ (4 * k)));
+    const uint2 y = *reinterpret_cast<const uint2*>(p + 8 * (u ^ (4 * k + 2)));
     return make_uint4(x.x, x.y, y.x, y.y);
   }
-  // Columns of [32 rows][pitch]: lane lo has the column that element lo % 4 of chunk lo / 4
-  // is (the transposing load takes four rows' chunks from 16 lanes); chunks q apart.
-  __device__ static __forceinline__ Raw cols(const bf16_t* p, int pitch, int lo, int hi, int q) {
+  // Rows row0 .. row0 + 31 down column `col` + Q (lo / 4) + lo % 4 (the transposing load
+  // takes four rows' fours from 16 lanes).
+  template <int UP, int Q>
+  __device__ static __forceinline__ Raw cols(const bf16_t* m, int row0, int col, int lo, int hi) {
     typedef __attribute__((ext_vector_type(4))) short s4;
     typedef __attribute__((address_space(3))) s4* lds4;
-    const bf16_t* at = p + (4 * hi + (lo >> 2)) * pitch + q * (lo & 3);
+    const int row = 4 * hi + (lo >> 2), c = col + Q * (lo & 3);
+    const bf16_t* at = m + (row0 + row) * UP * 8 + 8 * ((c >> 3) ^ lin_turn<UP>(row)) + (c & 7);
     const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at);
-    const s4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 16 * pitch));
+    const s4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 16 * UP * 8));
     const uint2 u = __builtin_bit_cast(uint2, x), v = __builtin_bit_cast(uint2, y);
     return make_uint4(u.x, u.y, v.x, v.y);
   }
@@ -139,16 +158,22 @@ template <> struct Lin<bf16_t> {
 template <> struct Lin<float> {
   struct Raw { f32x4 x, y; };
   typedef Raw Split;
-  __device__ static __forceinline__ Raw rows(const float* p) {
-    return Raw{*reinterpret_cast<const f32x4*>(p), *reinterpret_cast<const f32x4*>(p + 16)};
+  template <int UP>
+  __device__ static __forceinline__ Raw rows(const float* m, int row, int k, int hi) {
+    const float* p = m + row * UP * 4;
+    const int u = hi ^ lin_turn<UP>(row);
+    return Raw{*reinterpret_cast<const f32x4*>(p + 4 * (u ^ (8 * k))), *reinterpret_cast<const f32x4*>(p + 4 * (u ^ (8 * k + 4)))};
   }
-  __device__ static __forceinline__ Raw cols(const float* p, int pitch, int lo, int hi, int q) {
-    const float* at = p + 4 * hi * pitch + q * (lo >> 2) + (lo & 3);
+  template <int UP, int Q>
+  __device__ static __forceinline__ Raw cols(const float* m, int row0, int col, int lo, int hi) {
+    const int c = col + Q * (lo >> 2) + (lo & 3);
     Raw r;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      r.x[i] = at[i * pitch];
-      r.y[i] = at[(16 + i) * pitch];
+      const int row = 4 * hi + i;
+      const float* at = m + (row0 + row) * UP * 4 + 4 * ((c >> 2) ^ lin_turn<UP>(row)) + (c & 3);
+      r.x[i] = at[0];
+      r.y[i] = at[16 * UP * 4];
     }
     return r;
   }
@@ -202,12 +227,13 @@ template <typename T, int KD, int NV, bool LOCAL>
 __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
   typedef Lin<T> L;
   constexpr int CT = LinChunk<T>::n, NI = CT / 16, NM = CT / 32, NC = 64 * NV, Q = 4 * NV;
-  constexpr int E = 16 / sizeof(T), PR = 32 * KD + E, PC = NC + E;
-  constexpr int UR = 32 * KD / E, UC = NC / E;           // 16-byte units of a row
-  constexpr int LR = CT * UR / 256, LC = CT * UC / 256;  // loads of a thread
-  __shared__ __align__(16) T as[LOCAL ? 8 : CT * PR];
-  __shared__ __align__(16) T bs[CT * PR];
-  __shared__ __align__(16) T cs[CT * PC];
+  constexpr int E = 16 / sizeof(T);                      // elements of a 16-byte unit
+  constexpr int UA = 32 * KD / E, UR = UA == 3 * (UA / 3) ? UA / 3 * 4 : UA, UC = NC / E;
+  constexpr int RR = 256 / UR, RC = 256 / UC;            // rows that the work-group loads at once
+  constexpr int LR = CT / RR, LC = CT / RC;              // loads of a thread
+  __shared__ __align__(16) T as[LOCAL ? 8 : CT * UR * E];
+  __shared__ __align__(16) T bs[CT * UR * E];
+  __shared__ __align__(16) T cs[CT * UC * E];
   // the chunk's products a_i.b_j: pairs of tiles (rows 32 j .., columns 16 i ..)
   constexpr int NF = NI == 4 ? 6 : 2;
   auto pair = [](int i, int j) { return i + (i > 2 ? 1 : 0) + j; };   // 0 | 1 | 2 3 | 4 5
@@ -232,20 +258,20 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
   const int part = item % args.parts, bh = item / args.parts, h = bh % args.H, b = bh / args.H;
   const int len = lin_len(args, b), per = args.per * CT;
   const int t_lo = part * per, t_hi = min(args.T, t_lo + per);
-  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, lo = l & 15, hi = l >> 4;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lo_ = tid & 15, hi_ = tid >> 4 & 3;
   if (!LOCAL && h == 0 && part == 0 && which == 0 && tid == 0 && args.seq_len &&
       (args.seq_len[b] < 0 || args.seq_len[b] > args.T))
     atomicOr(args.err, LL_DEVERR_SEQ_LEN_BIT);
   // token number i of the pass is token len - 1 - i where it runs backwards
-  auto token = [&](int i) { return ((long)(p.rev && i < len ? len - 1 - i : i)) * args.B + b; };
-  const int cw = c0 + 16 * NV * w;                       // the wave's columns; a lane's: cw + 4 NV hi + ..
-  const int mine = cw + Q * hi;
+  auto token = [&](int i) { return (long)(p.rev ? len - 1 - i : i) * args.B + b; };
+  const int cw = c0 + 16 * NV * w;                       // the wave's columns; a lane's: cw + 4 NV hi_ + ..
+  const int mine = cw + Q * hi_;
   const T* pa = static_cast<const T*>(p.a) + (long)(h / p.ag) * p.Dr;
   const T* pb = static_cast<const T*>(p.b) + (long)(h / p.bg) * p.Dr;
   const T* pc = static_cast<const T*>(p.c) + (long)(h / p.cg) * p.Dc;
   const long oh = (long)(h / p.og) * p.Dc;
 
-  // the state: rows 16 d + 4 hi + r, column of tile t: cw + 4 NV (lo / 4) + 4 t + lo % 4
+  // the state: rows 16 d + 4 hi_ + r, column of tile t: cw + 4 NV (lo_ / 4) + 4 t + lo_ % 4
   f32x4 S[2 * KD][NV];
   const long stride = (long)args.Dk * args.Dv;
   const float* st = LOCAL || !p.st ? nullptr : p.st + (long)item * stride;
@@ -254,7 +280,7 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
     for (int d = 0; d < 2 * KD; ++d)
 #pragma unroll
       for (int t = 0; t < NV; ++t) {
-        const int r = 16 * d + 4 * hi, c = cw + Q * (lo >> 2) + 4 * t + (lo & 3);
+        const int r = 16 * d + 4 * hi_, c = cw + Q * (lo_ >> 2) + 4 * t + (lo_ & 3);
         f(S[d][t], r, (long)r * p.rs + (long)c * p.cs, r < p.Dr && c < p.Dc);
       }
   };
@@ -286,51 +312,66 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
   f32x4 near, far, leave;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
-    const int d = lo - 4 * hi - r;
+    const int d = lo_ - 4 * hi_ - r;
     near[r] = d < 0 ? 0.f : p.wP * expf(g * d);
     far[r] = p.wP * expf(g * (16 + d));
-    leave[r] = p.wU * expf(g * (16 - 4 * hi - r - p.e));
+    leave[r] = p.wU * expf(g * (16 - 4 * hi_ - r - p.e));
   }
-  const float place = p.wA * expf(g * (lo + p.e));
+  const float place = p.wA * expf(g * (lo_ + p.e));
   float l16[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) l16[i] = expf(g * (16 * i));
+  for (int i = 0; i < 4; ++i) l16[i] = uniform(expf(g * (16 * i)));
 
+  // where this thread loads from: rows ur + RR i of a and b, uc + RC i of c, 16 bytes each
+  const int ur_ = tid / UR, ux_ = tid % UR, uc_ = tid / UC, cx_ = tid % UC;
+  const long dir = p.rev ? -args.B : args.B;
+  const long tok0 = token(0), ahead = tok0 + dir * t_lo;
+  const bool in_r = ux_ * E < p.Dr, in_c = c0 + cx_ * E < p.Dc;
+  const T* la = pa + (ahead + dir * ur_) * p.a_ld + ux_ * E;
+  const T* lb = pb + (ahead + dir * ur_) * p.b_ld + ux_ * E;
+  const T* lc = pc + (ahead + dir * uc_) * p.c_ld + c0 + cx_ * E;
   uint4 ra[LR], rb[LR], rc[LC];
-  auto load = [&](int t0) __attribute__((always_inline)) {
+  auto load = [&](int t0, int ur, int uc) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < LR; ++i) {
-      const int u = tid + 256 * i, row = u / UR, col = u % UR * E;
-      const bool in = t0 + row < len && col < p.Dr;
-      const long tok = token(t0 + row);
-      if (!LOCAL) ra[i] = in ? ld16(pa + tok * p.a_ld + col) : zero4();
-      rb[i] = in ? ld16(pb + tok * p.b_ld + col) : zero4();
+      const bool in = t0 + ur + RR * i < len && in_r;
+      if (!LOCAL) ra[i] = in ? ld16(la + dir * RR * i * p.a_ld) : zero4();
+      rb[i] = in ? ld16(lb + dir * RR * i * p.b_ld) : zero4();
     }
 #pragma unroll
-    for (int i = 0; i < LC; ++i) {
-      const int u = tid + 256 * i, row = u / UC, col = c0 + u % UC * E;
-      rc[i] = t0 + row < len && col < p.Dc ? ld16(pc + token(t0 + row) * p.c_ld + col) : zero4();
-    }
+    for (int i = 0; i < LC; ++i) rc[i] = t0 + uc + RC * i < len && in_c ? ld16(lc + dir * RC * i * p.c_ld) : zero4();
+    la += dir * CT * p.a_ld;
+    lb += dir * CT * p.b_ld;
+    lc += dir * CT * p.c_ld;
   };
+  long out_at = (ahead + dir * lo_) * p.o_ld + oh + mine;
+  // (no instruction moves across: loads from LDS for all of a loop at once would not fit)
+  auto hold = [] { __builtin_amdgcn_sched_barrier(0); };
   const int t_end = min(t_hi, len);
-  if (t_lo < t_end) load(t_lo);
+  if (t_lo < t_end) load(t_lo, ur_, uc_);
   for (int t0 = t_lo; t0 < t_end; t0 += CT) {
+    // the places in LDS are made anew for every chunk: kept, they and the weights' products
+    // would not fit the registers, and a reload from scratch waits for the chunk's loads
+    int me = tid;
+    asm volatile("" : "+v"(me));
+    const int l = me & 63, lo = me & 15, hi = me >> 4 & 3, ur = me / UR, ux = me % UR, uc = me / UC, cx = me % UC;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) asm volatile("" : "+v"(leave[r]));
     lds_barrier();                                       // the chunk before has been read
 #pragma unroll
     for (int i = 0; i < LR; ++i) {
-      const int u = tid + 256 * i, at = u / UR * PR + u % UR * E;
+      const int row = ur + RR * i, at = (row * UR + (ux ^ lin_turn<UR>(row))) * E;
       if (!LOCAL) *reinterpret_cast<uint4*>(as + at) = ra[i];
       *reinterpret_cast<uint4*>(bs + at) = rb[i];
     }
 #pragma unroll
     for (int i = 0; i < LC; ++i) {
-      const int u = tid + 256 * i;
-      *reinterpret_cast<uint4*>(cs + u / UC * PC + u % UC * E) = rc[i];
+      const int row = uc + RC * i;
+      *reinterpret_cast<uint4*>(cs + (row * UC + (cx ^ lin_turn<UC>(row))) * E) = rc[i];
     }
     lds_barrier();
-    if (t0 + CT < t_end) load(t0 + CT);
+    if (LOCAL && t0 + CT < t_end) load(t0 + CT, ur, uc);
     const int m = min(CT, len - t0);
-    typename L::Raw cf[NM][NV];
     if constexpr (!LOCAL) {
       // the chunk's products, a tile of 16 x 16 a wave in turn: rows j, columns i >= j
       for (int at = w; at < NI * (NI + 1) / 2; at += 4) {
@@ -338,7 +379,7 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
         f32x4 x = zero_acc();
 #pragma unroll
         for (int k = 0; k < KD; ++k)
-          x = L::mm(L::rows(bs + (16 * j + lo) * PR + 32 * k + 4 * hi), L::rows(as + (16 * i + lo) * PR + 32 * k + 4 * hi), x);
+          x = L::mm(L::template rows<UR>(bs, 16 * j + lo, k, hi), L::template rows<UR>(as, 16 * i + lo, k, hi), x);
         const float f = i - j > 1 ? l16[i - j - 1] : 1.f;
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[r] = i == j ? (lo >= 4 * hi + r ? x[r] * near[r] : 0.f) : x[r] * (far[r] * f);
@@ -356,16 +397,19 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
         for (int t = 0; t < NV; ++t) s[t] = L::split(S[2 * k][t], S[2 * k + 1][t]);
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-          const typename L::Raw fa = L::rows(as + (16 * i + lo) * PR + 32 * k + 4 * hi);
+          const typename L::Raw fa = L::template rows<UR>(as, 16 * i + lo, k, hi);
 #pragma unroll
           for (int t = 0; t < NV; ++t) y[i][t] = L::mm(s[t], fa, y[i][t]);
         }
+        hold();
       }
       lds_barrier();                                     // the products are there
+      if (t0 + CT < t_end) load(t0 + CT, ur, uc);
+      typename L::Raw cf[NM][NV];
 #pragma unroll
       for (int j = 0; j < NM; ++j)
 #pragma unroll
-        for (int t = 0; t < NV; ++t) cf[j][t] = L::cols(cs + 32 * j * PC + 16 * NV * w + 4 * t, PC, lo, hi, Q);
+        for (int t = 0; t < NV; ++t) cf[j][t] = L::template cols<UC, Q>(cs, 32 * j, 16 * NV * w + 4 * t, lo, hi);
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const float f = place * l16[i];
@@ -377,21 +421,17 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
 #pragma unroll
           for (int t = 0; t < NV; ++t) y[i][t] = L::mm(cf[j][t], s, y[i][t]);
         }
-        const int tok = t0 + 16 * i + lo;
-        if (tok < t_hi && mine < p.Dc) {
+        if (16 * i + lo < m && mine < p.Dc) {
           float o[4 * NV];
 #pragma unroll
           for (int t = 0; t < NV; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[4 * t + r] = tok < len ? y[i][t][r] : 0.f;
-          lin_store<T, 4 * NV>(p.out, token(tok) * p.o_ld + oh + mine, o, p.wide);
+            for (int r = 0; r < 4; ++r) o[4 * t + r] = y[i][t][r];
+          lin_store<T, 4 * NV>(p.out, out_at + dir * 16 * i * p.o_ld, o, p.wide);
         }
+        hold();
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < NM; ++j)
-#pragma unroll
-        for (int t = 0; t < NV; ++t) cf[j][t] = L::cols(cs + 32 * j * PC + 16 * NV * w + 4 * t, PC, lo, hi, Q);
+      out_at += dir * CT * p.o_ld;
     }
     // S' = l^m S + ..; as S + (l^m - 1) S, because a rounded l^m would err the same way in
     // every chunk
@@ -402,7 +442,6 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
       for (int t = 0; t < NV; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) S[d][t][r] = __builtin_fmaf(S[d][t][r], grow, S[d][t][r]);
-    typename L::Split cv[NM][NV];
 #pragma unroll
     for (int j = 0; j < NM; ++j) {
       f32x4 wx, wy;
@@ -417,30 +456,30 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
           wy[r] = p.wU * expf(g * max(0, m - at - 16));
         }
       }
+      typename L::Split cv[NV];
 #pragma unroll
       for (int t = 0; t < NV; ++t) {
         f32x4 x, y;
-        L::floats(cf[j][t], x, y);
-        cv[j][t] = L::split(x * wx, y * wy);
+        L::floats(L::template cols<UC, Q>(cs, 32 * j, 16 * NV * w + 4 * t, lo, hi), x, y);
+        cv[t] = L::split(x * wx, y * wy);
+      }
+#pragma unroll
+      for (int d = 0; d < 2 * KD; ++d) {
+        const typename L::Raw f = L::template cols<UR, 4>(bs, 32 * j, 16 * d, lo, hi);
+#pragma unroll
+        for (int t = 0; t < NV; ++t) S[d][t] = L::mm(f, cv[t], S[d][t]);
+        if (d & 1) hold();
       }
     }
-#pragma unroll
-    for (int d = 0; d < 2 * KD; ++d)
-#pragma unroll
-      for (int j = 0; j < NM; ++j) {
-        const typename L::Raw f = L::cols(bs + 32 * j * PR + 16 * d, PR, lo, hi, 4);
-#pragma unroll
-        for (int t = 0; t < NV; ++t) S[d][t] = L::mm(f, cv[j][t], S[d][t]);
-      }
   }
   if constexpr (LOCAL) {
     put_state(args.local + (long)item * stride);
   } else {
-    // tokens past the row's end, in whole chunks
-    const int first = max(t_lo, (len + CT - 1) / CT * CT);
+    // tokens past the row's end
     if (mine < p.Dc) {
       const float zero[4 * NV] = {};
-      for (int t = first + lo; t < t_hi; t += 16) lin_store<T, 4 * NV>(p.out, token(t) * p.o_ld + oh + mine, zero, p.wide);
+      for (int t = max(t_lo, len) + lo_; t < t_hi; t += 16)
+        lin_store<T, 4 * NV>(p.out, ((long)t * args.B + b) * p.o_ld + oh + mine, zero, p.wide);
     }
     // the part that holds the last token has the last state (the first one of an empty row)
     if (p.last && (part == 0 || t_lo < len) && t_lo + per >= len) put_state(p.last + (long)bh * stride);
