@@ -142,15 +142,13 @@ template <> struct Lin<bf16_t> {
     }
   }
   __device__ static __forceinline__ f32x4 mm(Raw a, Raw b, f32x4 c) { return mfma(as_frag(a), as_frag(b), c); }
-  __device__ static __forceinline__ f32x4 mm(Raw a, const Split& b, f32x4 c) {
-#pragma unroll
-    for (int i = NP - 1; i >= 0; --i) c = mfma(as_frag(a), as_frag(b.p[i]), c);
-    return c;
+  // Term i of a product with a float operand, NP of them, the smallest first: those of
+  // different accumulators in turn, because one waits for the one before.
+  __device__ static __forceinline__ f32x4 mm(Raw a, const Split& b, f32x4 c, int i) {
+    return mfma(as_frag(a), as_frag(b.p[NP - 1 - i]), c);
   }
-  __device__ static __forceinline__ f32x4 mm(const Split& a, Raw b, f32x4 c) {
-#pragma unroll
-    for (int i = NP - 1; i >= 0; --i) c = mfma(as_frag(a.p[i]), as_frag(b), c);
-    return c;
+  __device__ static __forceinline__ f32x4 mm(const Split& a, Raw b, f32x4 c, int i) {
+    return mfma(as_frag(a.p[NP - 1 - i]), as_frag(b), c);
   }
 };
 
@@ -158,6 +156,7 @@ template <> struct Lin<bf16_t> {
 template <> struct Lin<float> {
   struct Raw { f32x4 x, y; };
   typedef Raw Split;
+  static constexpr int NP = 8;
   template <int UP>
   __device__ static __forceinline__ Raw rows(const float* m, int row, int k, int hi) {
     const float* p = m + row * UP * 4;
@@ -189,6 +188,9 @@ template <> struct Lin<float> {
   __device__ static __forceinline__ void floats(Raw r, f32x4& x, f32x4& y) {
     x = r.x;
     y = r.y;
+  }
+  __device__ static __forceinline__ f32x4 mm(const Raw& a, const Raw& b, f32x4 c, int i) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(i < 4 ? a.x[i] : a.y[i - 4], i < 4 ? b.x[i] : b.y[i - 4], c, 0, 0, 0);
   }
   __device__ static __forceinline__ f32x4 mm(const Raw& a, const Raw& b, f32x4 c) {
 #pragma unroll
@@ -330,23 +332,41 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
   const T* la = pa + (ahead + dir * ur_) * p.a_ld + ux_ * E;
   const T* lb = pb + (ahead + dir * ur_) * p.b_ld + ux_ * E;
   const T* lc = pc + (ahead + dir * uc_) * p.c_ld + c0 + cx_ * E;
+  const float grow_all = uniform(expm1f(g * CT));
   uint4 ra[LR], rb[LR], rc[LC];
+#pragma unroll
+  for (int i = 0; i < LR; ++i) ra[i] = rb[i] = zero4();
+#pragma unroll
+  for (int i = 0; i < LC; ++i) rc[i] = zero4();
+  // (columns past the operand's stay the zeros that they are)
   auto load = [&](int t0, int ur, int uc) __attribute__((always_inline)) {
+    if (t0 + CT <= len) {
+      if (in_r) {
 #pragma unroll
-    for (int i = 0; i < LR; ++i) {
-      const bool in = t0 + ur + RR * i < len && in_r;
-      if (!LOCAL) ra[i] = in ? ld16(la + dir * RR * i * p.a_ld) : zero4();
-      rb[i] = in ? ld16(lb + dir * RR * i * p.b_ld) : zero4();
+        for (int i = 0; i < LR; ++i) {
+          if (!LOCAL) ra[i] = ld16(la + dir * RR * i * p.a_ld);
+          rb[i] = ld16(lb + dir * RR * i * p.b_ld);
+        }
+      }
+      if (in_c) {
+#pragma unroll
+        for (int i = 0; i < LC; ++i) rc[i] = ld16(lc + dir * RC * i * p.c_ld);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < LR; ++i) {
+        const bool in = t0 + ur + RR * i < len && in_r;
+        if (!LOCAL) ra[i] = in ? ld16(la + dir * RR * i * p.a_ld) : zero4();
+        rb[i] = in ? ld16(lb + dir * RR * i * p.b_ld) : zero4();
+      }
+#pragma unroll
+      for (int i = 0; i < LC; ++i) rc[i] = t0 + uc + RC * i < len && in_c ? ld16(lc + dir * RC * i * p.c_ld) : zero4();
     }
-#pragma unroll
-    for (int i = 0; i < LC; ++i) rc[i] = t0 + uc + RC * i < len && in_c ? ld16(lc + dir * RC * i * p.c_ld) : zero4();
     la += dir * CT * p.a_ld;
     lb += dir * CT * p.b_ld;
     lc += dir * CT * p.c_ld;
   };
   long out_at = (ahead + dir * lo_) * p.o_ld + oh + mine;
-  // (no instruction moves across: loads from LDS for all of a loop at once would not fit)
-  auto hold = [] { __builtin_amdgcn_sched_barrier(0); };
   const int t_end = min(t_hi, len);
   if (t_lo < t_end) load(t_lo, ur_, uc_);
   for (int t0 = t_lo; t0 < t_end; t0 += CT) {
@@ -373,17 +393,32 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
     if (LOCAL && t0 + CT < t_end) load(t0 + CT, ur, uc);
     const int m = min(CT, len - t0);
     if constexpr (!LOCAL) {
-      // the chunk's products, a tile of 16 x 16 a wave in turn: rows j, columns i >= j
-      for (int at = w; at < NI * (NI + 1) / 2; at += 4) {
-        const int i = at >= 6 ? 3 : at >= 3 ? 2 : at >= 1 ? 1 : 0, j = at - i * (i + 1) / 2;
-        f32x4 x = zero_acc();
+      // the chunk's products, tiles of 16 x 16 (rows j, columns i >= j) a wave in turn
+      constexpr int NT = NI * (NI + 1) / 2, PT = (NT + 3) / 4;
+      int ti[PT], tj[PT];
+      f32x4 x[PT];
 #pragma unroll
-        for (int k = 0; k < KD; ++k)
-          x = L::mm(L::template rows<UR>(bs, 16 * j + lo, k, hi), L::template rows<UR>(as, 16 * i + lo, k, hi), x);
-        const float f = i - j > 1 ? l16[i - j - 1] : 1.f;
+      for (int n = 0; n < PT; ++n) {
+        const int at = min(w + 4 * n, NT - 1);
+        ti[n] = at >= 6 ? 3 : at >= 3 ? 2 : at >= 1 ? 1 : 0;
+        tj[n] = at - ti[n] * (ti[n] + 1) / 2;
+        x[n] = zero_acc();
+      }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = i == j ? (lo >= 4 * hi + r ? x[r] * near[r] : 0.f) : x[r] * (far[r] * f);
-        L::put(ps, pair(i, j / 2), j & 1, l, x);
+      for (int k = 0; k < KD; ++k)
+#pragma unroll
+        for (int n = 0; n < PT; ++n)
+          x[n] = L::mm(L::template rows<UR>(bs, 16 * tj[n] + lo, k, hi), L::template rows<UR>(as, 16 * ti[n] + lo, k, hi), x[n]);
+#pragma unroll
+      for (int n = 0; n < PT; ++n) {
+        const int d = ti[n] - tj[n];
+        const float f = d > 2 ? l16[2] : d > 1 ? l16[1] : 1.f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float on = lo >= 4 * hi + r ? x[n][r] * near[r] : 0.f, off = x[n][r] * (far[r] * f);
+          x[n][r] = d == 0 ? on : off;
+        }
+        if (w + 4 * n < NT) L::put(ps, pair(ti[n], tj[n] / 2), tj[n] & 1, l, x[n]);
       }
       f32x4 y[NI][NV];
 #pragma unroll
@@ -395,13 +430,15 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
         typename L::Split s[NV];
 #pragma unroll
         for (int t = 0; t < NV; ++t) s[t] = L::split(S[2 * k][t], S[2 * k + 1][t]);
+        typename L::Raw fa[NI];
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          const typename L::Raw fa = L::template rows<UR>(as, 16 * i + lo, k, hi);
+        for (int i = 0; i < NI; ++i) fa[i] = L::template rows<UR>(as, 16 * i + lo, k, hi);
 #pragma unroll
-          for (int t = 0; t < NV; ++t) y[i][t] = L::mm(s[t], fa, y[i][t]);
-        }
-        hold();
+        for (int n = 0; n < L::NP; ++n)
+#pragma unroll
+          for (int i = 0; i < NI; ++i)
+#pragma unroll
+            for (int t = 0; t < NV; ++t) y[i][t] = L::mm(s[t], fa[i], y[i][t], n);
       }
       lds_barrier();                                     // the products are there
       if (t0 + CT < t_end) load(t0 + CT, ur, uc);
@@ -419,8 +456,13 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
         for (int j = 0; j <= i / 2; ++j) {
           const typename L::Split s = L::get(ps, pair(i, j), l);
 #pragma unroll
-          for (int t = 0; t < NV; ++t) y[i][t] = L::mm(cf[j][t], s, y[i][t]);
+          for (int n = 0; n < L::NP; ++n)
+#pragma unroll
+            for (int t = 0; t < NV; ++t) y[i][t] = L::mm(cf[j][t], s, y[i][t], n);
         }
+      }
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
         if (16 * i + lo < m && mine < p.Dc) {
           float o[4 * NV];
 #pragma unroll
@@ -429,13 +471,23 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
             for (int r = 0; r < 4; ++r) o[4 * t + r] = y[i][t][r];
           lin_store<T, 4 * NV>(p.out, out_at + dir * 16 * i * p.o_ld, o, p.wide);
         }
-        hold();
       }
       out_at += dir * CT * p.o_ld;
     }
     // S' = l^m S + ..; as S + (l^m - 1) S, because a rounded l^m would err the same way in
     // every chunk
-    const float grow = expm1f(g * m);
+    float grow = grow_all;
+    f32x4 wt[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) wt[i] = leave * l16[NI - 1 - i];
+    if (m != CT) {
+      grow = expm1f(g * m);
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)                      // (tokens past the end are zeros)
+          wt[i][r] = p.wU * expf(g * max(0, m - 16 * i - 4 * hi - r - p.e));
+    }
 #pragma unroll
     for (int d = 0; d < 2 * KD; ++d)
 #pragma unroll
@@ -444,31 +496,24 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
         for (int r = 0; r < 4; ++r) S[d][t][r] = __builtin_fmaf(S[d][t][r], grow, S[d][t][r]);
 #pragma unroll
     for (int j = 0; j < NM; ++j) {
-      f32x4 wx, wy;
-      if (m == CT) {
-        wx = leave * l16[NI - 1 - 2 * j];
-        wy = leave * l16[NI - 2 - 2 * j];
-      } else {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {                    // (tokens past the end are zeros)
-          const int at = 32 * j + 4 * hi + r + p.e;
-          wx[r] = p.wU * expf(g * max(0, m - at));
-          wy[r] = p.wU * expf(g * max(0, m - at - 16));
-        }
-      }
       typename L::Split cv[NV];
 #pragma unroll
       for (int t = 0; t < NV; ++t) {
         f32x4 x, y;
         L::floats(L::template cols<UC, Q>(cs, 32 * j, 16 * NV * w + 4 * t, lo, hi), x, y);
-        cv[t] = L::split(x * wx, y * wy);
+        cv[t] = L::split(x * wt[2 * j], y * wt[2 * j + 1]);
       }
 #pragma unroll
-      for (int d = 0; d < 2 * KD; ++d) {
-        const typename L::Raw f = L::template cols<UR, 4>(bs, 32 * j, 16 * d, lo, hi);
+      for (int d = 0; d < 2 * KD; d += 2) {
+        typename L::Raw f[2];
 #pragma unroll
-        for (int t = 0; t < NV; ++t) S[d][t] = L::mm(f, cv[t], S[d][t]);
-        if (d & 1) hold();
+        for (int e = 0; e < 2; ++e) f[e] = L::template cols<UR, 4>(bs, 32 * j, 16 * (d + e), lo, hi);
+#pragma unroll
+        for (int n = 0; n < L::NP; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int t = 0; t < NV; ++t) S[d + e][t] = L::mm(f[e], cv[t], S[d + e][t], n);
       }
     }
   }
