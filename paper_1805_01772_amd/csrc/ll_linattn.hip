@@ -37,9 +37,11 @@ struct LinPass {
   int ag, bg, cg, og;                  // value heads to a head of the array
   int Dr, Dc;                          // sizes of a and b, of c and out
   const float* st;                     // entering states, part by part; NULL: zeros
-  float* keep;                         // a copy of them is written here, or NULL
+  float* keep;                         // where the parts' states go: LOCAL's, or a copy of st; or NULL
   float* last;                         // the state after the last token, or NULL
-  int rs, cs;                          // distances of a state's rows (Dr) and columns (Dc)
+  int rs, cs;                          // distances of the rows (Dr) and columns (Dc) of st,
+  int krs, kcs;                        // of keep
+  int lrs, lcs;                        // and of last
   float wP, wA, wU;
   int e, rev;
   int wide;                            // out is float whatever the call's type
@@ -51,7 +53,6 @@ struct LinArgs {
   int parts, per, npass, ctiles;       // parts of a row, chunks of a part
   const float* g;
   const int* seq_len;
-  float* local;                        // [row, head, part] states
   int* err;
 };
 
@@ -242,7 +243,8 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
   __shared__ __align__(16) unsigned char ps[LOCAL ? 16 : NF * L::kHeld];
   // items that read the same tokens (columns and passes) lie 8 work-groups apart: on one
   // XCD, one after the other
-  const int sub = args.ctiles * args.npass, items = args.B * args.H * args.parts;
+  const int parts = LOCAL ? args.parts - 1 : args.parts;  // nothing follows the last part's own
+  const int sub = args.ctiles * args.npass, items = args.B * args.H * parts;
   int id = blockIdx.x;
   const int full = items / 8 * 8 * sub;
   int item, which;
@@ -257,7 +259,7 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
   const LinPass& p = args.p[which / args.ctiles];
   const int c0 = which % args.ctiles * NC;
   if (c0 >= p.Dc) return;
-  const int part = item % args.parts, bh = item / args.parts, h = bh % args.H, b = bh / args.H;
+  const int part = item % parts, bh = item / parts, h = bh % args.H, b = bh / args.H;
   const int len = lin_len(args, b), per = args.per * CT;
   const int t_lo = part * per, t_hi = min(args.T, t_lo + per);
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lo_ = tid & 15, hi_ = tid >> 4 & 3;
@@ -275,35 +277,36 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
 
   // the state: rows 16 d + 4 hi_ + r, column of tile t: cw + 4 NV (lo_ / 4) + 4 t + lo_ % 4
   f32x4 S[2 * KD][NV];
-  const long stride = (long)args.Dk * args.Dv;
-  const float* st = LOCAL || !p.st ? nullptr : p.st + (long)item * stride;
-  auto each_state = [&](auto f) __attribute__((always_inline)) {
+  const long stride = (long)args.Dk * args.Dv, slot = ((long)bh * args.parts + part) * stride;
+  auto each_state = [&](int rs, int cs, auto f) __attribute__((always_inline)) {
+    const int c1 = cw + Q * (lo_ >> 2) + (lo_ & 3);
+    const long at = (long)(4 * hi_) * rs + (long)c1 * cs;
 #pragma unroll
     for (int d = 0; d < 2 * KD; ++d)
 #pragma unroll
-      for (int t = 0; t < NV; ++t) {
-        const int r = 16 * d + 4 * hi_, c = cw + Q * (lo_ >> 2) + 4 * t + (lo_ & 3);
-        f(S[d][t], r, (long)r * p.rs + (long)c * p.cs, r < p.Dr && c < p.Dc);
-      }
+      for (int t = 0; t < NV; ++t)
+        f(S[d][t], at + 16l * d * rs + 4l * t * cs, 16 * d + 4 * hi_ < p.Dr && c1 + 4 * t < p.Dc);
   };
-  each_state([&](f32x4& s, int, long at, bool in) __attribute__((always_inline)) {
+  each_state(p.rs, p.cs, [&](f32x4& s, long at, bool in) __attribute__((always_inline)) {
     s = zero_acc();
-    if (!st || !in) return;
-    if (p.rs == 1) s = *reinterpret_cast<const f32x4*>(st + at);
-    else
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] = st[at + (long)e * p.rs];
+    if (LOCAL || !p.st || !in) return;
+    const float* x = p.st + slot + at;
+    if (p.rs == 1) s = *reinterpret_cast<const f32x4*>(x);
+    else s = f32x4{x[0], x[p.rs], x[2l * p.rs], x[3l * p.rs]};
   });
-  auto put_state = [&](float* to) __attribute__((always_inline)) {
-    each_state([&](f32x4& s, int, long at, bool in) __attribute__((always_inline)) {
+  auto put_state = [&](float* to, int rs, int cs) __attribute__((always_inline)) {
+    each_state(rs, cs, [&](f32x4& s, long at, bool in) __attribute__((always_inline)) {
       if (!in) return;
-      if (p.rs == 1) *reinterpret_cast<f32x4*>(to + at) = s;
-      else
+      float* x = to + at;
+      if (rs == 1) {
+        *reinterpret_cast<f32x4*>(x) = s;
+      } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) to[at + (long)e * p.rs] = s[e];
+        for (int e = 0; e < 4; ++e) x[(long)e * rs] = s[e];
+      }
     });
   };
-  if (!LOCAL && p.keep) put_state(p.keep + (long)item * stride);
+  if (!LOCAL && p.keep) put_state(p.keep + slot, p.krs, p.kcs);
 
   // (what lies above the diagonal in a pair's second tile stays zero)
   if constexpr (!LOCAL)
@@ -476,10 +479,12 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
     }
     // S' = l^m S + ..; as S + (l^m - 1) S, because a rounded l^m would err the same way in
     // every chunk
-    float grow = grow_all;
+    // (LOCAL: from zero, so every token's weight is what the part's end leaves of it)
     f32x4 wt[NI];
+    const float after = LOCAL ? uniform(expf(g * max(0, t_end - t0 - CT))) : 1.f;
 #pragma unroll
-    for (int i = 0; i < NI; ++i) wt[i] = leave * l16[NI - 1 - i];
+    for (int i = 0; i < NI; ++i) wt[i] = leave * (l16[NI - 1 - i] * after);
+    float grow = grow_all;
     if (m != CT) {
       grow = expm1f(g * m);
 #pragma unroll
@@ -488,12 +493,14 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
         for (int r = 0; r < 4; ++r)                      // (tokens past the end are zeros)
           wt[i][r] = p.wU * expf(g * max(0, m - 16 * i - 4 * hi - r - p.e));
     }
+    if (!LOCAL) {
 #pragma unroll
-    for (int d = 0; d < 2 * KD; ++d)
+      for (int d = 0; d < 2 * KD; ++d)
 #pragma unroll
-      for (int t = 0; t < NV; ++t)
+        for (int t = 0; t < NV; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[d][t][r] = __builtin_fmaf(S[d][t][r], grow, S[d][t][r]);
+          for (int r = 0; r < 4; ++r) S[d][t][r] = __builtin_fmaf(S[d][t][r], grow, S[d][t][r]);
+    }
 #pragma unroll
     for (int j = 0; j < NM; ++j) {
       typename L::Split cv[NV];
@@ -518,7 +525,7 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
     }
   }
   if constexpr (LOCAL) {
-    put_state(args.local + (long)item * stride);
+    put_state(p.keep + slot, p.krs, p.kcs);
   } else {
     // tokens past the row's end
     if (mine < p.Dc) {
@@ -527,12 +534,13 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
         lin_store<T, 4 * NV>(p.out, ((long)t * args.B + b) * p.o_ld + oh + mine, zero, p.wide);
     }
     // the part that holds the last token has the last state (the first one of an empty row)
-    if (p.last && (part == 0 || t_lo < len) && t_lo + per >= len) put_state(p.last + (long)bh * stride);
+    if (p.last && (part == 0 || t_lo < len) && t_lo + per >= len) put_state(p.last + bh * stride, p.lrs, p.lcs);
   }
 }
 
-// The parts' states from their tokens' own: E_0 as given, E_{p+1} = l^n E_p + local_p.
-__global__ __launch_bounds__(256) void lin_scan_kernel(LinArgs a, const float* S0, int chunk) {
+// The parts' states from their tokens' own: E_0 as given, E_{p+1} = l^n E_p + local_p.  They
+// lie as [Dv][Dk], S0 as [Dk][Dv].
+__global__ __launch_bounds__(256) void lin_scan_kernel(LinArgs a, float* states, const float* S0, int chunk) {
   const long size = (long)a.Dk * a.Dv;
   const int blocks = (int)((size / 4 + 255) / 256);
   const int bh = blockIdx.x / blocks;
@@ -540,14 +548,26 @@ __global__ __launch_bounds__(256) void lin_scan_kernel(LinArgs a, const float* S
   if (at >= size) return;
   const int len = lin_len(a, bh / a.H), per = a.per * chunk;
   const float g = lin_log(a.g, bh % a.H);
-  f32x4 e = S0 ? *reinterpret_cast<const f32x4*>(S0 + bh * size + at) : zero_acc();
-  float* st = a.local + (long)bh * a.parts * size + at;
-  for (int p = 0; p < a.parts; ++p) {
-    const f32x4 own = *reinterpret_cast<const f32x4*>(st + p * size);
-    *reinterpret_cast<f32x4*>(st + p * size) = e;
-    const float grow = expm1f(g * min(per, max(0, len - p * per)));
+  f32x4 e = zero_acc();
+  if (S0) {
+    const float* x = S0 + bh * size + at % a.Dk * a.Dv + at / a.Dk;
+    e = f32x4{x[0], x[a.Dv], x[2l * a.Dv], x[3l * a.Dv]};
+  }
+  float* st = states + (long)bh * a.parts * size + at;
+  constexpr int R = 4;                                   // parts read at once
+  for (int p = 0; p < a.parts; p += R) {
+    f32x4 own[R];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) e[r] = __builtin_fmaf(e[r], grow, e[r]) + own[r];
+    for (int i = 0; i < R; ++i)
+      own[i] = p + i < a.parts - 1 ? *reinterpret_cast<const f32x4*>(st + (p + i) * size) : zero_acc();
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      if (p + i >= a.parts) break;
+      *reinterpret_cast<f32x4*>(st + (p + i) * size) = e;
+      const float grow = expm1f(g * min(per, max(0, len - (p + i) * per)));
+#pragma unroll
+      for (int r = 0; r < 4; ++r) e[r] = __builtin_fmaf(e[r], grow, e[r]) + own[i][r];
+    }
   }
 }
 
@@ -742,7 +762,7 @@ hipError_t launch_passes(ll::LinArgs a, bool bf16, bool local, hipStream_t s) {
   }
   const int nv = dc > 64 ? 2 : 1;
   a.ctiles = 1;
-  const unsigned grid = (unsigned)a.B * a.H * a.parts * a.ctiles * a.npass;
+  const unsigned grid = (unsigned)a.B * a.H * (local ? a.parts - 1 : a.parts) * a.ctiles * a.npass;
   const int kd = (dr + 31) / 32;
   if (bf16) {
     if (kd == 1) launch<bf16_t, 1>(a, nv, local, grid, s);
@@ -760,11 +780,13 @@ hipError_t launch_passes(ll::LinArgs a, bool bf16, bool local, hipStream_t s) {
 
 // The parts' entering states into `to` from the first one; a.p[0] says what makes them.
 hipError_t launch_states(ll::LinArgs a, float* to, const float* first, bool bf16, int chunk, hipStream_t s) {
-  a.local = to;
+  a.p[0].keep = to;
+  a.p[0].krs = 1;
+  a.p[0].kcs = a.Dk;
   a.npass = 1;
   if (hipError_t e = launch_passes(a, bf16, true, s); e != hipSuccess) return e;
   const long blocks = ((long)a.Dk * a.Dv / 4 + 255) / 256;
-  ll::lin_scan_kernel<<<dim3((unsigned)(blocks * a.B * a.H)), dim3(256), 0, s>>>(a, first, chunk);
+  ll::lin_scan_kernel<<<dim3((unsigned)(blocks * a.B * a.H)), dim3(256), 0, s>>>(a, to, first, chunk);
   return hipGetLastError();
 }
 
@@ -868,7 +890,7 @@ ll_status linattn_loop_fwd(ll_linattn_plan* p, void* stream, const void* q, cons
   f.a = q; f.b = k; f.c = v; f.out = y;
   f.a_ld = p->ld[0]; f.b_ld = p->ld[1]; f.c_ld = p->ld[2]; f.o_ld = (long)d.Hv * d.Dv;
   f.ag = f.bg = r; f.cg = f.og = 1;
-  f.Dr = d.Dk; f.Dc = d.Dv; f.rs = d.Dv; f.cs = 1;
+  f.Dr = d.Dk; f.Dc = d.Dv; f.lrs = d.Dv; f.lcs = 1;
   f.wP = f.wA = p->scale; f.wU = 1.f; f.e = 1;
   f.last = ST;
   p->saved = false;
@@ -876,10 +898,11 @@ ll_status linattn_loop_fwd(ll_linattn_plan* p, void* stream, const void* q, cons
   const bool bf16 = d.dtype == LL_BF16;
   if (a.parts > 1) {
     LL_HIP(launch_states(a, p->st, S0, bf16, chunk_of(d), s));
-    f.st = p->st;
+    f.st = p->st; f.rs = 1; f.cs = d.Dk;
   } else {
-    f.st = S0;
+    f.st = S0; f.rs = d.Dv; f.cs = 1;
     f.keep = save_for_backward && S0 ? p->st : nullptr;
+    f.krs = 1; f.kcs = d.Dk;
   }
   LL_HIP(launch_passes(a, bf16, false, s));
   if (save_for_backward) {
@@ -921,27 +944,28 @@ ll_status linattn_loop_bwd(ll_linattn_plan* p, void* stream, const void* q, cons
   v_.a = k; v_.b = q; v_.c = dy; v_.out = dv;
   v_.a_ld = p->ld[1]; v_.b_ld = p->ld[0]; v_.c_ld = y_ld; v_.o_ld = p->ld[5];
   v_.ag = v_.bg = r; v_.cg = v_.og = 1;
-  v_.Dr = d.Dk; v_.Dc = d.Dv; v_.rs = d.Dv; v_.cs = 1;
+  v_.Dr = d.Dk; v_.Dc = d.Dv; v_.lrs = d.Dv; v_.lcs = 1;
   v_.wP = v_.wU = p->scale; v_.wA = 1.f; v_.e = 0; v_.rev = 1;
   v_.last = dS0;
-  v_.st = dST;
+  v_.st = dST; v_.rs = d.Dv; v_.cs = 1;
   if (a.parts > 1) {
     a.p[0] = v_;
     LL_HIP(launch_states(a, p->dst, dST, bf16, chunk_of(d), s));
-    v_.st = p->dst;
+    v_.st = p->dst; v_.rs = 1; v_.cs = d.Dk;
   }
   k_ = v_;
   k_.a = v; k_.b = dy; k_.c = q;
   k_.a_ld = p->ld[2]; k_.b_ld = y_ld; k_.c_ld = p->ld[0];
   k_.ag = k_.bg = 1; k_.cg = r;
-  k_.Dr = d.Dv; k_.Dc = d.Dk; k_.rs = 1; k_.cs = d.Dv;
+  k_.Dr = d.Dv; k_.Dc = d.Dk;
+  std::swap(k_.rs, k_.cs);
   k_.last = nullptr;
   k_.out = r > 1 ? wide_k : dk; k_.o_ld = r > 1 ? qw : p->ld[4]; k_.og = 1; k_.wide = r > 1;
   q_ = k_;
   q_.a = dy; q_.b = v; q_.c = k;
   q_.a_ld = y_ld; q_.b_ld = p->ld[2]; q_.c_ld = p->ld[1];
   q_.wP = q_.wA = p->scale; q_.wU = 1.f; q_.e = 1; q_.rev = 0;
-  q_.st = p->has_state ? p->st : nullptr;
+  q_.st = p->has_state ? p->st : nullptr; q_.rs = d.Dk; q_.cs = 1;
   q_.out = r > 1 ? p->wide : dq; q_.o_ld = r > 1 ? qw : p->ld[3];
   a.p[0] = v_; a.p[1] = k_; a.p[2] = q_;
   a.npass = 3;
