@@ -79,22 +79,36 @@ __device__ __forceinline__ int lin_turn(int row) {
 // Operands over 32 of what a product sums over: a lane holds the four of its group hi
 // in each of two tiles of 16, the four that an accumulator tile gives it.  So states and
 // the chunk's products go from accumulators into the next product as they lie.
-template <typename T> struct Lin;
+//
+// The bfloat16 matrix instructions run at sixteen times the rate of the float ones: a
+// float operand is the sum of three bfloat16 pieces (24 bits, exactly), a bfloat16 one of
+// the call its own piece, and a product takes pieces i and j while i + j <= 2; what is
+// dropped is below 2^-24 of the term.  (float32 calls on the float instructions: 8 rows of
+// 2048 tokens, 16 heads of 128, 972 us instead of F32NEW.)
+// NR: pieces of an operand of the call; CT: rows of it in LDS, a plane for each piece.
+template <int NR, int CT>
+struct Lin {
+  static constexpr int NS = 3;
+  struct Raw { uint4 p[NR]; };
+  struct Split { uint4 p[NS]; };
+  // terms of a product with a float operand, the smallest first
+  static constexpr int NP = NR == 1 ? 3 : 6;
+  __device__ static constexpr int raw_of(int n) { return NR == 1 ? 0 : n == 0 ? 2 : n == 1 || n == 3 ? 1 : 0; }
+  __device__ static constexpr int split_of(int n) { return NR == 1 ? 2 - n : n == 2 ? 2 : n == 1 || n == 4 ? 1 : 0; }
 
-// bfloat16: an operand of the call is its own piece, a float one the sum of three (24
-// bits, exactly), so that a product drops nothing but what a float cannot hold.
-template <> struct Lin<bf16_t> {
-  typedef uint4 Raw;
-  static constexpr int NP = 3;
-  struct Split { uint4 p[NP]; };
   // Row `row` (16 i + lo), steps k: columns 32 k + 4 hi .. and 16 further on.
   template <int UP>
   __device__ static __forceinline__ Raw rows(const bf16_t* m, int row, int k, int hi) {
     const bf16_t* p = m + row * UP * 8 + 4 * (hi & 1);
     const int u = (hi >> 1) ^ lin_turn<UP>(row);
-    const uint2 x = *reinterpret_cast<const uint2*>(p + 8 * (u ^ (4 * k)));
-    const uint2 y = *reinterpret_cast<const uint2*>(p + 8 * (u ^ (4 * k + 2)));
-    return make_uint4(x.x, x.y, y.x, y.y);
+    Raw r;
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const uint2 x = *reinterpret_cast<const uint2*>(p + i * CT * UP * 8 + 8 * (u ^ (4 * k)));
+      const uint2 y = *reinterpret_cast<const uint2*>(p + i * CT * UP * 8 + 8 * (u ^ (4 * k + 2)));
+      r.p[i] = make_uint4(x.x, x.y, y.x, y.y);
+    }
+    return r;
   }
   // Rows row0 .. row0 + 31 down column `col` + Q (lo / 4) + lo % 4 (the transposing load
   // takes four rows' fours from 16 lanes).
@@ -103,102 +117,73 @@ template <> struct Lin<bf16_t> {
     typedef __attribute__((ext_vector_type(4))) short s4;
     typedef __attribute__((address_space(3))) s4* lds4;
     const int row = 4 * hi + (lo >> 2), c = col + Q * (lo & 3);
-    const bf16_t* at = m + (row0 + row) * UP * 8 + 8 * ((c >> 3) ^ lin_turn<UP>(row)) + (c & 7);
-    const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at);
-    const s4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 16 * UP * 8));
-    const uint2 u = __builtin_bit_cast(uint2, x), v = __builtin_bit_cast(uint2, y);
-    return make_uint4(u.x, u.y, v.x, v.y);
+    Raw r;
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const bf16_t* at = m + (i * CT + row0 + row) * UP * 8 + 8 * ((c >> 3) ^ lin_turn<UP>(row)) + (c & 7);
+      const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at);
+      const s4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 16 * UP * 8));
+      const uint2 u = __builtin_bit_cast(uint2, x), v = __builtin_bit_cast(uint2, y);
+      r.p[i] = make_uint4(u.x, u.y, v.x, v.y);
+    }
+    return r;
+  }
+  // 16 bytes of the call's type, number u of row `row`.
+  template <int UP>
+  __device__ static __forceinline__ void put_row(bf16_t* m, int row, int u, uint4 x) {
+    if constexpr (NR == 1) {
+      *reinterpret_cast<uint4*>(m + (row * UP + (u ^ lin_turn<UP>(row))) * 8) = x;
+    } else {
+      const f32x4 f = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w)};
+      split4_store<NR>(f, m + (row * UP + (u >> 1 ^ lin_turn<UP>(row))) * 8 + 4 * (u & 1), CT * UP * 8);
+    }
   }
   __device__ static __forceinline__ Split split(f32x4 x, f32x4 y) {
     const float f[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
     Split s;
-    split8<NP>(f, s.p);
+    split8<NS>(f, s.p);
     return s;
   }
   // A float operand in LDS: `half` 0 or 1 of fragment `at` as its four floats say, and the
   // whole of it.
-  static constexpr int kHeld = NP * 1024;
+  static constexpr int kHeld = NS * 1024;
   __device__ static __forceinline__ void put(unsigned char* lds, int at, int half, int l, f32x4 x) {
-    uint32_t a[NP], b[NP];
-    split2<NP>(x[0], x[1], a);
-    split2<NP>(x[2], x[3], b);
-#pragma unroll
-    for (int i = 0; i < NP; ++i)
-      *reinterpret_cast<uint2*>(lds + at * kHeld + i * 1024 + l * 16 + half * 8) = make_uint2(a[i], b[i]);
+    split4_store<NS>(x, reinterpret_cast<bf16_t*>(lds + at * kHeld + l * 16 + half * 8), 512);
   }
   __device__ static __forceinline__ Split get(const unsigned char* lds, int at, int l) {
     Split s;
 #pragma unroll
-    for (int i = 0; i < NP; ++i) s.p[i] = ld16(lds + at * kHeld + i * 1024 + l * 16);
+    for (int i = 0; i < NS; ++i) s.p[i] = ld16(lds + at * kHeld + i * 1024 + l * 16);
     return s;
   }
-  __device__ static __forceinline__ void floats(Raw r, f32x4& x, f32x4& y) {
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+  __device__ static __forceinline__ void floats(const Raw& r, f32x4& x, f32x4& y) {
+    x = y = zero_acc();
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      y[2 * i] = __uint_as_float(w[2 + i] << 16);
-      y[2 * i + 1] = __uint_as_float(w[2 + i] & 0xffff0000u);
-    }
-  }
-  __device__ static __forceinline__ f32x4 mm(Raw a, Raw b, f32x4 c) { return mfma(as_frag(a), as_frag(b), c); }
-  // Term i of a product with a float operand, NP of them, the smallest first: those of
-  // different accumulators in turn, because one waits for the one before.
-  __device__ static __forceinline__ f32x4 mm(Raw a, const Split& b, f32x4 c, int i) {
-    return mfma(as_frag(a), as_frag(b.p[NP - 1 - i]), c);
-  }
-  __device__ static __forceinline__ f32x4 mm(const Split& a, Raw b, f32x4 c, int i) {
-    return mfma(as_frag(a.p[NP - 1 - i]), as_frag(b), c);
-  }
-};
-
-// float: the float32 matrix instructions take it as it is, a sixteenth of the rate.
-template <> struct Lin<float> {
-  struct Raw { f32x4 x, y; };
-  typedef Raw Split;
-  static constexpr int NP = 8;
-  template <int UP>
-  __device__ static __forceinline__ Raw rows(const float* m, int row, int k, int hi) {
-    const float* p = m + row * UP * 4;
-    const int u = hi ^ lin_turn<UP>(row);
-    return Raw{*reinterpret_cast<const f32x4*>(p + 4 * (u ^ (8 * k))), *reinterpret_cast<const f32x4*>(p + 4 * (u ^ (8 * k + 4)))};
-  }
-  template <int UP, int Q>
-  __device__ static __forceinline__ Raw cols(const float* m, int row0, int col, int lo, int hi) {
-    const int c = col + Q * (lo >> 2) + (lo & 3);
-    Raw r;
+    for (int n = NR - 1; n >= 0; --n) {
+      const uint32_t w[4] = {r.p[n].x, r.p[n].y, r.p[n].z, r.p[n].w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = 4 * hi + i;
-      const float* at = m + (row0 + row) * UP * 4 + 4 * ((c >> 2) ^ lin_turn<UP>(row)) + (c & 3);
-      r.x[i] = at[0];
-      r.y[i] = at[16 * UP * 4];
+      for (int i = 0; i < 2; ++i) {
+        const f32x4 f = {__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u), __uint_as_float(w[2 + i] << 16),
+                         __uint_as_float(w[2 + i] & 0xffff0000u)};
+        x[2 * i] = n == NR - 1 ? f[0] : x[2 * i] + f[0];
+        x[2 * i + 1] = n == NR - 1 ? f[1] : x[2 * i + 1] + f[1];
+        y[2 * i] = n == NR - 1 ? f[2] : y[2 * i] + f[2];
+        y[2 * i + 1] = n == NR - 1 ? f[3] : y[2 * i + 1] + f[3];
+      }
     }
-    return r;
-  }
-  __device__ static __forceinline__ Split split(f32x4 x, f32x4 y) { return Raw{x, y}; }
-  static constexpr int kHeld = 2048;
-  __device__ static __forceinline__ void put(unsigned char* lds, int at, int half, int l, f32x4 x) {
-    *reinterpret_cast<f32x4*>(lds + at * kHeld + half * 1024 + l * 16) = x;
-  }
-  __device__ static __forceinline__ Split get(const unsigned char* lds, int at, int l) {
-    return Raw{*reinterpret_cast<const f32x4*>(lds + at * kHeld + l * 16),
-               *reinterpret_cast<const f32x4*>(lds + at * kHeld + 1024 + l * 16)};
-  }
-  __device__ static __forceinline__ void floats(Raw r, f32x4& x, f32x4& y) {
-    x = r.x;
-    y = r.y;
-  }
-  __device__ static __forceinline__ f32x4 mm(const Raw& a, const Raw& b, f32x4 c, int i) {
-    return __builtin_amdgcn_mfma_f32_16x16x4f32(i < 4 ? a.x[i] : a.y[i - 4], i < 4 ? b.x[i] : b.y[i - 4], c, 0, 0, 0);
   }
   __device__ static __forceinline__ f32x4 mm(const Raw& a, const Raw& b, f32x4 c) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[i], b.x[i], c, 0, 0, 0);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.y[i], b.y[i], c, 0, 0, 0);
+    for (int n = NR == 1 ? 2 : 0; n < NP; ++n) c = mfma(as_frag(a.p[raw_of(n)]), as_frag(b.p[NR == 1 ? 0 : split_of(n)]), c);
     return c;
+  }
+  // Term n of a product with a float operand: those of different accumulators in turn,
+  // because one waits for the one before.
+  __device__ static __forceinline__ f32x4 mm(const Raw& a, const Split& b, f32x4 c, int n) {
+    return mfma(as_frag(a.p[raw_of(n)]), as_frag(b.p[split_of(n)]), c);
+  }
+  __device__ static __forceinline__ f32x4 mm(const Split& a, const Raw& b, f32x4 c, int n) {
+    return mfma(as_frag(a.p[split_of(n)]), as_frag(b.p[raw_of(n)]), c);
   }
 };
 
@@ -228,15 +213,17 @@ __device__ __forceinline__ void lin_store(void* dst, long at, const float* x, bo
 // ---------------------------------------------------------------------------
 template <typename T, int KD, int NV, bool LOCAL>
 __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
-  typedef Lin<T> L;
-  constexpr int CT = LinChunk<T>::n, NI = CT / 16, NM = CT / 32, NC = 64 * NV, Q = 4 * NV;
-  constexpr int E = 16 / sizeof(T);                      // elements of a 16-byte unit
-  constexpr int UA = 32 * KD / E, UR = UA == 3 * (UA / 3) ? UA / 3 * 4 : UA, UC = NC / E;
+  constexpr int NR = sizeof(T) == 2 ? 1 : 3, CT = LinChunk<T>::n;
+  typedef Lin<NR, CT> L;
+  constexpr int NI = CT / 16, NM = CT / 32, NC = 64 * NV, Q = 4 * NV;
+  constexpr int E = 16 / sizeof(T);                      // elements of a load's 16 bytes
+  constexpr int UP = KD == 3 ? 16 : 4 * KD, UQ = NC / 8;  // units of 8 bfloat16 of a row in LDS
+  constexpr int UR = UP * 8 / E, UC = UQ * 8 / E;        // loads of a row
   constexpr int RR = 256 / UR, RC = 256 / UC;            // rows that the work-group loads at once
   constexpr int LR = CT / RR, LC = CT / RC;              // loads of a thread
-  __shared__ __align__(16) T as[LOCAL ? 8 : CT * UR * E];
-  __shared__ __align__(16) T bs[CT * UR * E];
-  __shared__ __align__(16) T cs[CT * UC * E];
+  __shared__ __align__(16) bf16_t as[LOCAL ? 8 : NR * CT * UP * 8];
+  __shared__ __align__(16) bf16_t bs[NR * CT * UP * 8];
+  __shared__ __align__(16) bf16_t cs[NR * CT * UQ * 8];
   // the chunk's products a_i.b_j: pairs of tiles (rows 32 j .., columns 16 i ..)
   constexpr int NF = NI == 4 ? 6 : 2;
   auto pair = [](int i, int j) { return i + (i > 2 ? 1 : 0) + j; };   // 0 | 1 | 2 3 | 4 5
@@ -383,15 +370,11 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
     lds_barrier();                                       // the chunk before has been read
 #pragma unroll
     for (int i = 0; i < LR; ++i) {
-      const int row = ur + RR * i, at = (row * UR + (ux ^ lin_turn<UR>(row))) * E;
-      if (!LOCAL) *reinterpret_cast<uint4*>(as + at) = ra[i];
-      *reinterpret_cast<uint4*>(bs + at) = rb[i];
+      if (!LOCAL) L::template put_row<UP>(as, ur + RR * i, ux, ra[i]);
+      L::template put_row<UP>(bs, ur + RR * i, ux, rb[i]);
     }
 #pragma unroll
-    for (int i = 0; i < LC; ++i) {
-      const int row = uc + RC * i;
-      *reinterpret_cast<uint4*>(cs + (row * UC + (cx ^ lin_turn<UC>(row))) * E) = rc[i];
-    }
+    for (int i = 0; i < LC; ++i) L::template put_row<UQ>(cs, uc + RC * i, cx, rc[i]);
     lds_barrier();
     if (LOCAL && t0 + CT < t_end) load(t0 + CT, ur, uc);
     const int m = min(CT, len - t0);
@@ -411,7 +394,7 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
       for (int k = 0; k < KD; ++k)
 #pragma unroll
         for (int n = 0; n < PT; ++n)
-          x[n] = L::mm(L::template rows<UR>(bs, 16 * tj[n] + lo, k, hi), L::template rows<UR>(as, 16 * ti[n] + lo, k, hi), x[n]);
+          x[n] = L::mm(L::template rows<UP>(bs, 16 * tj[n] + lo, k, hi), L::template rows<UP>(as, 16 * ti[n] + lo, k, hi), x[n]);
 #pragma unroll
       for (int n = 0; n < PT; ++n) {
         const int d = ti[n] - tj[n];
@@ -435,7 +418,7 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
         for (int t = 0; t < NV; ++t) s[t] = L::split(S[2 * k][t], S[2 * k + 1][t]);
         typename L::Raw fa[NI];
 #pragma unroll
-        for (int i = 0; i < NI; ++i) fa[i] = L::template rows<UR>(as, 16 * i + lo, k, hi);
+        for (int i = 0; i < NI; ++i) fa[i] = L::template rows<UP>(as, 16 * i + lo, k, hi);
 #pragma unroll
         for (int n = 0; n < L::NP; ++n)
 #pragma unroll
@@ -449,7 +432,7 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
 #pragma unroll
       for (int j = 0; j < NM; ++j)
 #pragma unroll
-        for (int t = 0; t < NV; ++t) cf[j][t] = L::template cols<UC, Q>(cs, 32 * j, 16 * NV * w + 4 * t, lo, hi);
+        for (int t = 0; t < NV; ++t) cf[j][t] = L::template cols<UQ, Q>(cs, 32 * j, 16 * NV * w + 4 * t, lo, hi);
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const float f = place * l16[i];
@@ -507,14 +490,14 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
 #pragma unroll
       for (int t = 0; t < NV; ++t) {
         f32x4 x, y;
-        L::floats(L::template cols<UC, Q>(cs, 32 * j, 16 * NV * w + 4 * t, lo, hi), x, y);
+        L::floats(L::template cols<UQ, Q>(cs, 32 * j, 16 * NV * w + 4 * t, lo, hi), x, y);
         cv[t] = L::split(x * wt[2 * j], y * wt[2 * j + 1]);
       }
 #pragma unroll
       for (int d = 0; d < 2 * KD; d += 2) {
         typename L::Raw f[2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) f[e] = L::template cols<UR, 4>(bs, 32 * j, 16 * (d + e), lo, hi);
+        for (int e = 0; e < 2; ++e) f[e] = L::template cols<UP, 4>(bs, 32 * j, 16 * (d + e), lo, hi);
 #pragma unroll
         for (int n = 0; n < L::NP; ++n)
 #pragma unroll
