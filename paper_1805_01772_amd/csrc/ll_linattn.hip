@@ -799,8 +799,12 @@ ll_status ll_linattn_plan_create(const ll_linattn_desc* desc, int device, ll_lin
   a.T = desc->T_max; a.B = desc->B; a.H = desc->Hv; a.Dk = desc->Dk; a.Dv = desc->Dv;
   const int chunk = chunk_of(*desc), nch = (desc->T_max + chunk - 1) / chunk;
   const long heads = (long)desc->B * desc->Hv;
-  // parts of a row: two work-groups for a compute unit, each with four chunks at least
-  const int want = (int)std::min<long>((2L * p->cus + heads - 1) / heads, std::max(1, nch / 4));
+  // Parts of a row: two work-groups for a compute unit, as many as it holds, two chunks each
+  // at least;
+  // short rows stay whole, because two launches make the parts' states.  (8 rows of 256 to
+  // 2048 tokens, 16 heads, training: 1 part 444 us, 4 381, 5 353, 8 433; one row of 16384:
+  // 16 parts 447, 32 423, 37 487, 64 494; 64 rows of 100, 8 heads, float32: 1 107, 2 182.)
+  const int want = nch < 8 ? 1 : (int)std::max(1L, std::min(2L * p->cus / heads, nch / 2L));
   a.per = (nch + want - 1) / want;
   a.parts = (nch + a.per - 1) / a.per;
   const size_t st = sizeof(float) * heads * a.parts * desc->Dk * desc->Dv;
