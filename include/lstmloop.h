@@ -721,7 +721,7 @@ ll_status ll_embed_fwd(ll_embed_plan* plan, void* stream, int32_t n, const void*
                        const int32_t* tokens, void* x);
 
 /*
- *   dx       [n, D]; rows without a token are not read.
+ *   dx       [n, D]; rows without a token count for nothing (they may hold NaN).
  *   dtable   [V, D]: overwritten, or, with accumulate, added to (rows that no token
  *            names stay as they are and are not read; grad_dtype bfloat16: the sum with
  *            the old value is rounded once).

@@ -25,8 +25,10 @@ constexpr int kEmbSmall = 4096;        // places that one work-group sorts
 constexpr int kEmbThreads = 512, kEmbWaves = kEmbThreads / 64;
 constexpr int kEmbBits = 10;           // of a digit at most
 constexpr int kEmbTiles = 128;         // work-groups of a sorting pass at most
+constexpr int kEmbHeld = 4;            // keys of a thread that stay in registers
 constexpr int kEmbUnit = 8;            // elements of a thread
-constexpr int kEmbJoin = 1024;         // threads that join a run
+constexpr int kEmbJoin = 256;          // threads that join a run
+constexpr int kEmbSums = 2048;         // waves that sum, where there are places enough
 
 struct EmbedArgs {
   int N, V, D;
@@ -173,7 +175,18 @@ __device__ void embed_pass(const EmbedArgs& a, EmbedSort& sh, int tile, int shif
   const int lo = min(n1, n0 + w * share), hi = min(n1, lo + share);
   for (int d = tid; d < kEmbWaves << a.bits; d += kEmbThreads) sh.cnt[d >> a.bits][d & mask] = 0;
   __syncthreads();
-  for (int n = lo + l; n < hi; n += 64) atomicAdd(&sh.cnt[w][((first ? embed_key(a, n) : key_in[n]) >> shift) & mask], 1);
+  // (the first rounds' keys stay in registers between the two walks over them)
+  int held[kEmbHeld];
+#pragma unroll
+  for (int i = 0; i < kEmbHeld; ++i) {
+    const int n = lo + 64 * i + l;
+    held[i] = n < hi ? (first ? embed_key(a, n) : key_in[n]) : a.V;
+  }
+#pragma unroll
+  for (int i = 0; i < kEmbHeld; ++i)
+    if (lo + 64 * i + l < hi) atomicAdd(&sh.cnt[w][held[i] >> shift & mask], 1);
+  for (int n = lo + 64 * kEmbHeld + l; n < hi; n += 64)
+    atomicAdd(&sh.cnt[w][((first ? embed_key(a, n) : key_in[n]) >> shift) & mask], 1);
   __syncthreads();
   // a thread's two digits: all before them, then in tile and wave order
   constexpr int PER = (1 << kEmbBits) / kEmbThreads;
@@ -218,13 +231,8 @@ __device__ void embed_pass(const EmbedArgs& a, EmbedSort& sh, int tile, int shif
   }
   __syncthreads();
   volatile int* next = sh.cnt[w];
-  for (int n = lo; n < hi; n += 64) {
+  auto place = [&](int n, int key, int pos) {
     const bool in = n + l < hi;
-    int key = a.V, pos = n + l;
-    if (in) {
-      key = first ? embed_key(a, n + l) : key_in[n + l];
-      pos = first ? n + l : pos_in[n + l];
-    }
     const int d = (key >> shift) & mask;
     unsigned long long same = __ballot(in);
     for (int i = 0; i < a.bits; ++i) {
@@ -241,6 +249,23 @@ __device__ void embed_pass(const EmbedArgs& a, EmbedSort& sh, int tile, int shif
       if (rank == 0) next[d] = to + __popcll(same);
     }
     wave_lds_fence();
+  };
+  int from[kEmbHeld];
+#pragma unroll
+  for (int i = 0; i < kEmbHeld; ++i) {
+    const int n = lo + 64 * i + l;
+    from[i] = first || n >= hi ? n : pos_in[n];
+  }
+#pragma unroll
+  for (int i = 0; i < kEmbHeld; ++i)
+    if (lo + 64 * i < hi) place(lo + 64 * i, held[i], from[i]);
+  for (int n = lo + 64 * kEmbHeld; n < hi; n += 64) {
+    int key = a.V, pos = n + l;
+    if (n + l < hi) {
+      key = first ? embed_key(a, n + l) : key_in[n + l];
+      pos = first ? n + l : pos_in[n + l];
+    }
+    place(n, key, pos);
   }
 }
 
@@ -330,16 +355,32 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, int lanes, 
       }
     }
   };
-  const TX* dx = static_cast<const TX*>(a.dx);
+  // eight places at a time (a piece is a multiple of that, and the arrays are padded to
+  // one): their tokens and rows' numbers a step ahead of the rows, the rows without
+  // conditions (what stands behind the last token has a row too, which counts for nothing)
+  const TX* dx = static_cast<const TX*>(a.dx) + (left > 0 ? u : 0);
+  const int cols_left = left > 0 ? left : a.D;
+  auto fetch = [&](int n, int* k, int* at) {
+#pragma unroll
+    for (int j = 0; j < R; j += 4) {
+      const int4 x = *reinterpret_cast<const int4*>(key + n + j), y = *reinterpret_cast<const int4*>(pos + n + j);
+      k[j] = x.x; k[j + 1] = x.y; k[j + 2] = x.z; k[j + 3] = x.w;
+      at[j] = y.x; at[j + 1] = y.y; at[j + 2] = y.z; at[j + 3] = y.w;
+    }
+#pragma unroll
+    for (int j = 0; j < R; ++j)
+      if (n + j >= n1) {
+        k[j] = a.V;
+        at[j] = at[0];
+      }
+  };
+  int k[R], at[R], k2[R], at2[R];
+  fetch(n0, k, at);
   for (int n = n0; n < n1 && cur != a.V; n += R) {
-    int k[R];
     float f[R][kEmbUnit];
 #pragma unroll
-    for (int j = 0; j < R; ++j) {
-      const int at = min(n + j, n1 - 1);
-      k[j] = n + j < n1 ? key[at] : a.V;
-      if (k[j] != a.V && left > 0) load_n(dx + pos[at] * a.dx_ld + u, left, f[j]);
-    }
+    for (int j = 0; j < R; ++j) load_n(dx + at[j] * a.dx_ld, cols_left, f[j]);
+    if (n + R < n1) fetch(n + R, k2, at2);
 #pragma unroll
     for (int j = 0; j < R; ++j) {
       if (cur == a.V) break;
@@ -355,6 +396,11 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, int lanes, 
 #pragma unroll
       for (int e = 0; e < kEmbUnit; ++e) acc[e] += f[j][e];
     }
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      k[j] = k2[j];
+      at[j] = at2[j];
+    }
   }
   if (cur == a.V) return;
   const bool goes_on = after == cur;
@@ -362,10 +408,10 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, int lanes, 
   if (goes_on && !(first && begun) && u == 0) a.heads[atomicAdd(a.count, 1)] = piece;
 }
 
-// Runs that go over pieces: the sixteen waves' shares of the partial sums, joined in order.
+// Runs that go over pieces: the waves' shares of the partial sums, joined in order.
 template <typename TG>
 __global__ __launch_bounds__(kEmbJoin) void embed_join_kernel(EmbedArgs a, const int* key) {
-  constexpr int NW = kEmbJoin / 64, R = 4;
+  constexpr int NW = kEmbJoin / 64, R = 8;
   __shared__ int more;
   __shared__ float sums[NW][64 * kEmbUnit];
   const int tid = threadIdx.x, w = tid >> 6, l = tid & 63;
@@ -434,15 +480,20 @@ void release(ll_embed_plan* p) {
     if (m) (void)hipFree(m);
 }
 
-// Places of a piece for n of them: long ones leave fewer partial sums, short ones fill the
-// chip.
-int piece_of(int n) { return n >= 1 << 16 ? 64 : n >= 1 << 14 ? 32 : n >= 1 << 12 ? 16 : 8; }
-
 // Threads for a row of D: eight elements each, a power of two.
 int lanes_of(int D, int most) {
   int lanes = 1;
   while (lanes < most && lanes * ll::kEmbUnit < D) lanes *= 2;
   return lanes;
+}
+
+// Places of a piece for n of them: long ones leave fewer partial sums, as long as there
+// are waves enough (25600 places of 1024: MEASURE).
+int piece_of(int n, int D) {
+  const int lanes = lanes_of(D, 64), cols = (D + lanes * ll::kEmbUnit - 1) / (lanes * ll::kEmbUnit);
+  int piece = 64;
+  while (piece > 8 && (long)(n / piece) * cols * lanes < 64L * ll::kEmbSums) piece /= 2;
+  return piece;
 }
 
 ll_status validate(const ll_embed_desc* d) {
@@ -501,7 +552,7 @@ void launch_bwd(const ll::EmbedArgs& a, int passes, hipStream_t s) {
   const unsigned grid = (unsigned)((a.pieces + groups - 1) / groups) * cols;
   ll::embed_sum_kernel<TX, TG><<<dim3(grid), dim3(256), 0, s>>>(a, lanes, cols, key, pos);
   if (a.pieces > 1)
-    ll::embed_join_kernel<TG><<<dim3((unsigned)std::min(a.pieces - 1, 256), (unsigned)((a.D + 64 * ll::kEmbUnit - 1) / (64 * ll::kEmbUnit))),
+    ll::embed_join_kernel<TG><<<dim3((unsigned)std::min(a.pieces - 1, 2048), (unsigned)((a.D + 64 * ll::kEmbUnit - 1) / (64 * ll::kEmbUnit))),
                             dim3(ll::kEmbJoin), 0, s>>>(a, key);
 }
 
@@ -536,11 +587,12 @@ ll_status ll_embed_plan_create(const ll_embed_desc* d, int device, ll_embed_plan
   while ((long)1 << key_bits <= d->V) ++key_bits;        // the key V is a place without a token
   p->passes = (key_bits + ll::kEmbBits - 1) / ll::kEmbBits;
   a.bits = (key_bits + p->passes - 1) / p->passes;
-  // partial sums: two a piece, of the most pieces that any number of places up to N has
-  long pieces = 0;
-  for (int n : {d->N, std::min(d->N, (1 << 16) - 1), std::min(d->N, (1 << 14) - 1), std::min(d->N, (1 << 12) - 1)})
-    pieces = std::max(pieces, (long)(n + piece_of(n) - 1) / piece_of(n));
-  const size_t n4 = sizeof(int) * (size_t)d->N;
+  // partial sums: two a piece; the most pieces that any number of places up to N has
+  // (fewer than twice those of the smallest number that takes longer ones)
+  const int lanes = lanes_of(d->D, 64), cols = (d->D + lanes * ll::kEmbUnit - 1) / (lanes * ll::kEmbUnit);
+  const long full = 64L * ll::kEmbSums / ((long)cols * lanes) + 1;
+  const long pieces = std::max((long)(d->N + 63) / 64, std::min((long)(d->N + 7) / 8, 2 * full + 2));
+  const size_t n4 = sizeof(int) * ((size_t)(d->N + 7) / 8 * 8);  // (read eight at a time)
   const bool train = !d->inference;
   struct { void** at; size_t bytes; const char* what; bool want; } bufs[] = {
       {(void**)&a.key[0], n4, "the sorted tokens", train},
@@ -618,7 +670,7 @@ ll_status ll_embed_bwd(ll_embed_plan* p, void* stream, int32_t n, const int32_t*
   ll::DeviceGuard guard(p->device);
   ll::EmbedArgs a = p->a;
   a.N = n; a.tokens = tokens; a.dx = dx; a.dw = dtable; a.accumulate = accumulate != 0;
-  a.piece = piece_of(n);
+  a.piece = piece_of(n, a.D);
   a.pieces = (n + a.piece - 1) / a.piece;
   if (n <= ll::kEmbSmall) {
     a.tiles = 1;
