@@ -49,26 +49,49 @@ struct EmbedArgs {
   int fill;                            // work-groups that clear the table's gradient beside the sort
 };
 
-// Eight elements at an element's alignment, as floats.
-template <typename T> __device__ __forceinline__ void load8(const T* p, float* f);
-template <> __device__ __forceinline__ void load8<float>(const float* p, float* f) {
-  typedef f32x4 any __attribute__((aligned(4)));
-  const f32x4 a = *reinterpret_cast<const any*>(p), b = *reinterpret_cast<const any*>(p + 4);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[i] = a[i];
-    f[4 + i] = b[i];
+// Eight elements at an element's alignment, as they are and as floats.
+template <typename T> struct Eight;
+template <> struct Eight<float> {
+  f32x4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    typedef f32x4 any __attribute__((aligned(4)));
+    a = *reinterpret_cast<const any*>(p);
+    b = *reinterpret_cast<const any*>(p + 4);
   }
-}
-template <> __device__ __forceinline__ void load8<bf16_t>(const bf16_t* p, float* f) {
-  typedef u32x4 any __attribute__((aligned(2)));
-  const u32x4 a = *reinterpret_cast<const any*>(p);
+  __device__ __forceinline__ void load_few(const float* p, int n) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[2 * i] = __uint_as_float(a[i] << 16);
-    f[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+    for (int i = 0; i < 4; ++i) {
+      a[i] = i < n ? p[i] : 0.f;
+      b[i] = 4 + i < n ? p[4 + i] : 0.f;
+    }
   }
-}
+  __device__ __forceinline__ void floats(float* f) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[i] = a[i];
+      f[4 + i] = b[i];
+    }
+  }
+};
+template <> struct Eight<bf16_t> {
+  u32x4 a;
+  __device__ __forceinline__ void load(const bf16_t* p) {
+    typedef u32x4 any __attribute__((aligned(2)));
+    a = *reinterpret_cast<const any*>(p);
+  }
+  __device__ __forceinline__ void load_few(const bf16_t* p, int n) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      a[i] = (2 * i < n ? (uint32_t)p[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)p[2 * i + 1] << 16 : 0u);
+  }
+  __device__ __forceinline__ void floats(float* f) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(a[i] << 16);
+      f[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+    }
+  }
+};
 template <typename T> __device__ __forceinline__ void store8(T* p, const float* f);
 template <> __device__ __forceinline__ void store8<float>(float* p, const float* f) {
   typedef f32x4 any __attribute__((aligned(4)));
@@ -79,23 +102,40 @@ template <> __device__ __forceinline__ void store8<bf16_t>(bf16_t* p, const floa
   typedef u32x4 any __attribute__((aligned(2)));
   *reinterpret_cast<any*>(p) = u32x4{pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7])};
 }
-// The same for the first n of them (the others 0, or left as they are).
-template <typename T> __device__ __forceinline__ void load_n(const T* p, int n, float* f) {
-  if (n >= kEmbUnit) {
-    load8(p, f);
-    return;
+
+// The columns of a thread: eight from `col` on, of which it answers for those from `skip` on
+// (the last thread of a row whose size is no multiple of eight moves back to have eight).
+// A row of fewer than eight is one thread's, element by element.
+struct Columns {
+  int col, skip, size;
+  bool any;
+  __device__ __forceinline__ Columns(int u, int D) {
+    any = u < D;
+    size = D;
+    col = D < kEmbUnit ? 0 : min(u, D - kEmbUnit);
+    skip = any ? u - col : kEmbUnit;
   }
+};
+// (every load goes out before the first is waited for, where there are eight columns)
+template <typename T, int R, typename At>
+__device__ __forceinline__ void load_rows(const Columns& c, At row, Eight<T>* x) {
+  if (c.size >= kEmbUnit) {
 #pragma unroll
-  for (int i = 0; i < kEmbUnit; ++i) f[i] = i < n ? Op<T>::to_f32(p[i]) : 0.f;
+    for (int j = 0; j < R; ++j) x[j].load(row(j) + c.col);
+  } else {
+#pragma unroll
+    for (int j = 0; j < R; ++j) x[j].load_few(row(j), c.size);
+  }
 }
-template <typename T> __device__ __forceinline__ void store_n(T* p, int n, const float* f) {
-  if (n >= kEmbUnit) {
-    store8(p, f);
+template <typename T>
+__device__ __forceinline__ void store_row(const Columns& c, T* row, const float* f) {
+  if (c.size >= kEmbUnit && c.skip == 0) {
+    store8(row + c.col, f);
     return;
   }
 #pragma unroll
-  for (int i = 0; i < kEmbUnit; ++i)
-    if (i < n) p[i] = Op<T>::from_f32(f[i]);
+  for (int e = 0; e < kEmbUnit; ++e)
+    if (e >= c.skip && c.col + e < c.size) row[c.col + e] = Op<T>::from_f32(f[e]);
 }
 
 // Rows of a work-group of 256: `lanes` threads (a power of two) a row.
@@ -104,32 +144,33 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedArgs a, int lanes, 
   constexpr int R = 4;                 // rows of a thread under way at once
   const int lane = threadIdx.x & (lanes - 1), grp = threadIdx.x / lanes, groups = 256 / lanes;
   const long n0 = (long)blockIdx.x * rows;
-  for (int u = lane * kEmbUnit; u < a.D; u += lanes * kEmbUnit)
+  const TW* w = static_cast<const TW*>(a.w);
+  for (int u = lane * kEmbUnit; u < a.D; u += lanes * kEmbUnit) {
+    const Columns c(u, a.D);
     for (int i = grp; i < rows; i += R * groups) {
-      float f[R][kEmbUnit];
-      const int left = a.D - u;
+      int t[R];
 #pragma unroll
       for (int j = 0; j < R; ++j) {
         const long n = n0 + i + j * groups;
-        const int t = i + j * groups < rows && n < a.N ? a.tokens[n] : -1;
-        if (t < -1 || t >= a.V) {
-          if (u == 0) atomicOr(a.err, LL_DEVERR_TOKEN);
-        }
-        if (t >= 0 && t < a.V) {
-          load_n(static_cast<const TW*>(a.w) + t * a.w_ld + u, left, f[j]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < kEmbUnit; ++e) f[j][e] = 0.f;
-        }
-#pragma unroll
-        for (int e = 0; e < kEmbUnit; ++e) f[j][e] = t >= 0 ? f[j][e] * a.scale : 0.f;
+        t[j] = i + j * groups < rows && n < a.N ? a.tokens[n] : -1;
       }
+      Eight<TW> x[R];
+      // (without a token: row 0, and it counts for nothing)
+      load_rows<TW, R>(c, [&](int j) { return w + (t[j] >= 0 && t[j] < a.V ? t[j] : 0) * a.w_ld; }, x);
 #pragma unroll
       for (int j = 0; j < R; ++j) {
         const long n = n0 + i + j * groups;
-        if (i + j * groups < rows && n < a.N) store_n(static_cast<TX*>(a.x) + n * a.x_ld + u, left, f[j]);
+        if (i + j * groups >= rows || n >= a.N) continue;
+        const bool has = t[j] >= 0 && t[j] < a.V;
+        if (!has && t[j] != -1 && u == 0) atomicOr(a.err, LL_DEVERR_TOKEN);
+        float f[kEmbUnit];
+        x[j].floats(f);
+#pragma unroll
+        for (int e = 0; e < kEmbUnit; ++e) f[e] = has ? f[e] * a.scale : 0.f;
+        store_row(c, static_cast<TX*>(a.x) + n * a.x_ld, f);
       }
     }
+  }
 }
 
 // Clears share `index` of `shares` of the table's gradient.
@@ -146,9 +187,7 @@ __device__ void embed_clear(const EmbedArgs& a, long index, long shares, int thr
   }
   const int units = (a.D + kEmbUnit - 1) / kEmbUnit;
   for (long u = at; u < (long)a.V * units; u += all) {
-    const long r = u / units;
-    const int c = (int)(u % units) * kEmbUnit;
-    store_n(dw + r * a.dw_ld + c, a.D - c, zero);
+    store_row(Columns((int)(u % units) * kEmbUnit, a.D), dw + u / units * a.dw_ld, zero);
   }
 }
 
@@ -318,14 +357,17 @@ __global__ __launch_bounds__(kEmbThreads) void embed_place_kernel(EmbedArgs a, i
 
 // scale * acc to the row of token t (or added to it).
 template <typename TG>
-__device__ __forceinline__ void embed_put(const EmbedArgs& a, int t, int u, const float* acc) {
-  TG* to = static_cast<TG*>(a.dw) + t * a.dw_ld + u;
+__device__ __forceinline__ void embed_put(const EmbedArgs& a, int t, const Columns& c, const float* acc) {
+  TG* to = static_cast<TG*>(a.dw) + t * a.dw_ld;
   float f[kEmbUnit];
-  const int left = a.D - u;
-  if (a.accumulate) load_n(to, left, f);
+  if (a.accumulate) {
+    Eight<TG> x[1];
+    load_rows<TG, 1>(c, [&](int) { return to; }, x);
+    x[0].floats(f);
+  }
 #pragma unroll
   for (int e = 0; e < kEmbUnit; ++e) f[e] = a.accumulate ? __builtin_fmaf(a.scale, acc[e], f[e]) : a.scale * acc[e];
-  store_n(to, left, f);
+  store_row(c, to, f);
 }
 
 // The runs of a piece: `lanes` threads and as many eights of columns.
@@ -334,32 +376,25 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, int lanes, 
   constexpr int R = 8;
   const int lane = threadIdx.x & (lanes - 1), groups = 256 / lanes;
   const int piece = (int)(blockIdx.x / cols) * groups + threadIdx.x / lanes;
-  const int u = ((int)(blockIdx.x % cols) * lanes + lane) * kEmbUnit;
+  const Columns c(((int)(blockIdx.x % cols) * lanes + lane) * kEmbUnit, a.D);
   if (piece >= a.pieces) return;
   const int n0 = piece * a.piece, n1 = min(a.N, n0 + a.piece);
   int cur = key[n0];
   if (cur == a.V) return;
-  const int left = a.D - u;
   const bool begun = n0 > 0 && key[n0 - 1] == cur;
   const int after = n1 < a.N ? key[n1] : -1;
   bool first = true;
   float acc[kEmbUnit] = {};
   auto flush = [&](bool goes_on) {
-    if (left > 0) {
-      const bool before = first && begun;
-      if (before || goes_on) {
-        float* to = a.part + (2l * piece + (before ? 0 : 1)) * a.D + u;
-        store_n(to, left, acc);
-      } else {
-        embed_put<TG>(a, cur, u, acc);
-      }
-    }
+    if (!c.any) return;
+    const bool before = first && begun;
+    if (before || goes_on) store_row(c, a.part + (2l * piece + (before ? 0 : 1)) * a.D, acc);
+    else embed_put<TG>(a, cur, c, acc);
   };
   // eight places at a time (a piece is a multiple of that, and the arrays are padded to
   // one): their tokens and rows' numbers a step ahead of the rows, the rows without
   // conditions (what stands behind the last token has a row too, which counts for nothing)
-  const TX* dx = static_cast<const TX*>(a.dx) + (left > 0 ? u : 0);
-  const int cols_left = left > 0 ? left : a.D;
+  const TX* dx = static_cast<const TX*>(a.dx);
   auto fetch = [&](int n, int* k, int* at) {
 #pragma unroll
     for (int j = 0; j < R; j += 4) {
@@ -377,9 +412,8 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, int lanes, 
   int k[R], at[R], k2[R], at2[R];
   fetch(n0, k, at);
   for (int n = n0; n < n1 && cur != a.V; n += R) {
-    float f[R][kEmbUnit];
-#pragma unroll
-    for (int j = 0; j < R; ++j) load_n(dx + at[j] * a.dx_ld, cols_left, f[j]);
+    Eight<TX> x[R];
+    load_rows<TX, R>(c, [&](int j) { return dx + at[j] * a.dx_ld; }, x);
     if (n + R < n1) fetch(n + R, k2, at2);
 #pragma unroll
     for (int j = 0; j < R; ++j) {
@@ -393,8 +427,10 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, int lanes, 
         for (int e = 0; e < kEmbUnit; ++e) acc[e] = 0.f;
         if (cur == a.V) break;
       }
+      float f[kEmbUnit];
+      x[j].floats(f);
 #pragma unroll
-      for (int e = 0; e < kEmbUnit; ++e) acc[e] += f[j][e];
+      for (int e = 0; e < kEmbUnit; ++e) acc[e] += f[e];
     }
 #pragma unroll
     for (int j = 0; j < R; ++j) {
@@ -405,7 +441,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, int lanes, 
   if (cur == a.V) return;
   const bool goes_on = after == cur;
   flush(goes_on);
-  if (goes_on && !(first && begun) && u == 0) a.heads[atomicAdd(a.count, 1)] = piece;
+  if (goes_on && !(first && begun) && c.any && c.col + c.skip == 0) a.heads[atomicAdd(a.count, 1)] = piece;
 }
 
 // Runs that go over pieces: the waves' shares of the partial sums, joined in order.
@@ -415,7 +451,8 @@ __global__ __launch_bounds__(kEmbJoin) void embed_join_kernel(EmbedArgs a, const
   __shared__ int more;
   __shared__ float sums[NW][64 * kEmbUnit];
   const int tid = threadIdx.x, w = tid >> 6, l = tid & 63;
-  const int count = *a.count, u = ((int)blockIdx.y * 64 + l) * kEmbUnit, left = a.D - u;
+  const int count = *a.count;
+  const Columns c(((int)blockIdx.y * 64 + l) * kEmbUnit, a.D);
   for (int i = blockIdx.x; i < count; i += gridDim.x) {
     const int head = a.heads[i], t = key[(head + 1) * a.piece];
     if (tid == 0) more = 0;
@@ -431,31 +468,33 @@ __global__ __launch_bounds__(kEmbJoin) void embed_join_kernel(EmbedArgs a, const
     const int n = more + 1;            // partial sums: the head's second, the others' first
     const int share = (n + NW - 1) / NW, lo = min(n, w * share), hi = min(n, lo + share);
     float acc[kEmbUnit] = {};
-    if (left > 0)
+    if (c.any)
       for (int j = lo; j < hi; j += R) {
-        float f[R][kEmbUnit];
+        Eight<float> x[R];
+        load_rows<float, R>(c, [&](int q) {
+          const int k = min(j + q, hi - 1);
+          return a.part + (2l * (head + k) + (k == 0 ? 1 : 0)) * a.D;
+        }, x);
 #pragma unroll
         for (int q = 0; q < R; ++q) {
-          const int k = min(j + q, hi - 1);
-          load_n(a.part + (2l * (head + k) + (k == 0 ? 1 : 0)) * a.D + u, left, f[q]);
+          if (j + q >= hi) break;
+          float f[kEmbUnit];
+          x[q].floats(f);
+#pragma unroll
+          for (int e = 0; e < kEmbUnit; ++e) acc[e] += f[e];
         }
-#pragma unroll
-        for (int q = 0; q < R; ++q)
-          if (j + q < hi)
-#pragma unroll
-            for (int e = 0; e < kEmbUnit; ++e) acc[e] += f[q][e];
       }
 #pragma unroll
     for (int e = 0; e < kEmbUnit; ++e) sums[w][e * 64 + l] = acc[e];
     __syncthreads();
-    if (w == 0 && left > 0) {
+    if (w == 0 && c.any) {
 #pragma unroll
       for (int e = 0; e < kEmbUnit; ++e) {
         float s = sums[0][e * 64 + l];
         for (int j = 1; j < NW; ++j) s += sums[j][e * 64 + l];
         acc[e] = s;
       }
-      embed_put<TG>(a, t, u, acc);
+      embed_put<TG>(a, t, c, acc);
     }
     __syncthreads();
   }
