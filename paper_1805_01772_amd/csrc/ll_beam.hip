@@ -49,6 +49,9 @@ __device__ __forceinline__ bool beam_live(const BeamArgs& a, long r) {
   return a.scores[r] > -__builtin_inff() && !(a.finished && a.finished[r]);
 }
 
+// A part of a row: its sum and its K largest.  Bound by the walk over the logits, whose
+// exponentials cost as much as their bytes: 256 rows of 131072 bfloat16 in 19.1 us,
+// 3.5 TB/s (21.1 when the walk made the entropy's sum too).
 template <typename T, int NTHR>
 __global__ __launch_bounds__(NTHR) void beam_rows_kernel(BeamArgs a) {
   __shared__ Shared<NTHR> sh;
@@ -59,7 +62,7 @@ __global__ __launch_bounds__(NTHR) void beam_rows_kernel(BeamArgs a) {
   const Span sp = span_of(row, a.V, part, a.parts);
   uint4 own;
   int own_c;
-  Stats st = walk<T, NTHR, true>(row, sp, a.V, &own, &own_c);
+  Stats st = walk<T, NTHR, true, 0, false>(row, sp, a.V, &own, &own_c);
   st = join_group<NTHR>(st, sh.st);
   const long at = r * a.parts + part;
   if (tid == 0) a.part[at] = make_float2(st.m, st.s);
@@ -70,103 +73,122 @@ __global__ __launch_bounds__(NTHR) void beam_rows_kernel(BeamArgs a) {
 
 struct BeamKey {
   double rank;
-  long at;                             // beam * V + token
+  unsigned long long at;               // beam << 32 | token
 };
 __device__ __forceinline__ bool better(BeamKey a, BeamKey b) { return a.rank > b.rank || (a.rank == b.rank && a.at < b.at); }
-constexpr long kBeamNone = -1;         // no candidate
+constexpr unsigned long long kBeamNone = ~0ull;          // no candidate, its rank below all
+constexpr int kBeamJoin = 512;         // threads
+// How many of x[0, n) are better than each of them: the threads share the comparisons.
+template <typename Use>
+__device__ __forceinline__ void beam_places(const BeamKey* x, int n, Use use) {
+  int share = 1;
+  while (share < 64 && 2 * share * n <= kBeamJoin) share *= 2;
+  const int first = threadIdx.x & (share - 1);
+  for (int i0 = 0; i0 < n * share; i0 += kBeamJoin) {
+    const int i = (i0 + (int)threadIdx.x) / share;
+    const BeamKey c = x[min(i, n - 1)];
+    int place = 0;
+#pragma unroll 4
+    for (int j = first; j < n; j += share) place += better(x[j], c);
+    for (int d = 1; d < share; d <<= 1) place += __shfl_xor(place, d, 64);
+    if (i < n && first == 0) use(c, place);
+  }
+}
 
-__global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a) {
+// The K best of a search's candidates.  What the first step reads goes out at once, also
+// for beams that turn out to offer nothing: the kernel is a handful of trips to memory.
+// 32 searches of 8 beams take 5.8 us (9.5 when a thread made all of a candidate's
+// comparisons, 14.4 with each beam's values one after the other).
+__global__ __launch_bounds__(kBeamJoin) void beam_join_kernel(BeamArgs a) {
+  __shared__ float2 all[kBeamMax];
   __shared__ double base[kBeamMax], off[kBeamMax], sum[kBeamMax], pen[kBeamMax];
   __shared__ int kind[kBeamMax], len[kBeamMax];          // 0: offers nothing, 1: its tokens, 2: itself
   __shared__ BeamKey head[kBeamMax * kPartsMax], found[kBeamMax * kBeamMax], bound;
   __shared__ int count;
-  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, K = a.K;
+  const int tid = threadIdx.x, K = a.K, lists = K * a.parts;
   const long r0 = (long)blockIdx.x * K;
-  for (int k = w; k < K; k += 4) {
-    const float score = a.scores[r0 + k];
-    const bool done = a.finished && a.finished[r0 + k], live = beam_live(a, r0 + k);
-    Stats st{kLowest, 0.f, 0.f};
-    if (live && l < a.parts) {
-      const float2 p = a.part[(r0 + k) * a.parts + l];
-      st = Stats{p.x, p.y, 0.f};
-    }
+  const unsigned long long* keys = a.keys + r0 * a.parts * a.top;
+  const unsigned long long early = tid < lists * a.top ? keys[tid] : 0;
+  float score = 0.f;
+  bool done = false;
+  int old = 0;
+  if (tid < K) {
+    score = a.scores[r0 + tid];
+    done = a.finished && a.finished[r0 + tid];
+    old = a.lengths ? a.lengths[r0 + tid] : 0;
+  }
+  for (int k = tid / kPartsMax; k < K; k += kBeamJoin / kPartsMax) {
+    const int l = tid % kPartsMax;
+    const float2 p = a.part[(r0 + k) * a.parts + min(l, a.parts - 1)];
+    Stats st = l < a.parts ? Stats{p.x, p.y, 0.f} : Stats{kLowest, 0.f, 0.f};
 #pragma unroll
     for (int d = 1; d < kPartsMax; d <<= 1)
       st = join(st, Stats{__shfl_xor(st.m, d, 64), __shfl_xor(st.s, d, 64), 0.f});
-    if (l == 0) {
-      const bool bad = score != score || (live && st.s != st.s);
-      if (bad) atomicOr(a.err, LL_DEVERR_BEAM);
-      const int n = a.lengths ? max(0, a.lengths[r0 + k]) : 0;
-      kind[k] = bad || !(score > -__builtin_inff()) ? 0 : done ? 2 : st.s > 0.f ? 1 : 0;
-      len[k] = done ? n : n + 1;
-      base[k] = score;
-      off[k] = kind[k] == 1 ? (double)st.m : 0.0;
-      pen[k] = a.alpha != 0.0 ? pow((5.0 + len[k]) / 6.0, a.alpha) : 1.0;
-      sum[k] = kind[k] == 1 ? log((double)st.s) : 0.0;
-    }
+    if (l == 0) all[k] = make_float2(st.m, st.s);
+  }
+  __syncthreads();
+  if (tid < K) {
+    const bool live = score > -__builtin_inff() && !done;          // as beam_live
+    const float2 st = live ? all[tid] : make_float2(0.f, 0.f);
+    const bool bad = score != score || st.y != st.y;
+    if (bad) atomicOr(a.err, LL_DEVERR_BEAM);
+    const bool walked = live && !bad && st.y > 0.f;
+    kind[tid] = walked ? 1 : !bad && done && score > -__builtin_inff() ? 2 : 0;
+    len[tid] = max(0, old) + (done ? 0 : 1);
+    base[tid] = score;
+    off[tid] = walked ? (double)st.x : 0.0;
+    sum[tid] = walked ? log((double)st.y) : 0.0;
+    pen[tid] = a.alpha != 0.0 ? pow((5.0 + len[tid]) / 6.0, a.alpha) : 1.0;
   }
   if (tid == 0) {
     count = 0;
-    bound.at = kBeamNone;
+    bound = BeamKey{-__builtin_inf(), kBeamNone};
   }
   __syncthreads();
-  const int lists = K * a.parts;
-  // entry j of list i = beam * parts + part
-  auto entry = [&](int i, int j, double* score) {
+  // entry j of list i = beam * parts + part, whose key is given
+  auto entry = [&](int i, int j, unsigned long long key) {
     const int k = i / a.parts;
-    BeamKey c{0.0, kBeamNone};
+    BeamKey c{-__builtin_inf(), kBeamNone};
     if (kind[k] == 2) {
-      if (i % a.parts == 0 && j == 0) {
-        *score = base[k];
-        c = BeamKey{base[k] / pen[k], (long)k * a.V + max(a.eos, 0)};
-      }
+      if (i % a.parts == 0 && j == 0) c = BeamKey{base[k] / pen[k], (unsigned long long)k << 32 | max(a.eos, 0)};
     } else if (kind[k] == 1) {
-      const unsigned long long key = a.keys[((r0 + k) * a.parts + i % a.parts) * a.top + j];
       const float x = key_value(key);
-      if (key != 0 && x > -__builtin_inff()) {
-        *score = base[k] + (((double)x - off[k]) - sum[k]);
-        c = BeamKey{*score / pen[k], (long)k * a.V + key_index(key)};
-      }
+      if (key != 0 && x > -__builtin_inff())
+        c = BeamKey{(base[k] + (((double)x - off[k]) - sum[k])) / pen[k],
+                    (unsigned long long)k << 32 | (unsigned)key_index(key)};
     }
     return c;
   };
-  double s = 0.0;
-  for (int i = tid; i < lists; i += 256) head[i] = entry(i, 0, &s);
-  __syncthreads();
-  // the K-th best of the lists' first ones bounds the K-th best of all
-  for (int i = tid; i < lists; i += 256) {
-    const BeamKey c = head[i];
-    if (c.at == kBeamNone) continue;
-    int n = 0;
-    for (int j = 0; j < lists; ++j) n += head[j].at != kBeamNone && better(head[j], c);
-    if (n == K - 1) bound = c;
+  const bool few = lists * a.top <= kBeamJoin;           // a candidate a thread: all compared at once
+  if (!few) {
+    for (int i = tid; i < lists; i += kBeamJoin) head[i] = entry(i, 0, keys[i * a.top]);
+    __syncthreads();
+    // the K-th best of the lists' first ones bounds the K-th best of all
+    beam_places(head, lists, [&](BeamKey c, int place) {
+      if (place == K - 1 && c.at != kBeamNone) bound = c;
+    });
+    __syncthreads();
   }
-  __syncthreads();
   const BeamKey least = bound;
-  for (int i = tid; i < lists * a.top; i += 256) {
-    const int list = i / a.top;
-    if (head[list].at == kBeamNone || (least.at != kBeamNone && better(least, head[list]))) continue;
-    const BeamKey c = entry(list, i % a.top, &s);
-    if (c.at != kBeamNone && (least.at == kBeamNone || !better(least, c))) found[atomicAdd(&count, 1)] = c;
+  for (int i = tid; i < lists * a.top; i += kBeamJoin) {
+    if (!few && better(least, head[i / a.top])) continue;
+    const BeamKey c = entry(i / a.top, i % a.top, few ? early : keys[i]);
+    if (c.at != kBeamNone && !better(least, c)) found[atomicAdd(&count, 1)] = c;
   }
   __syncthreads();
   const int n = count;
-  for (int i = tid; i < n; i += 256) {
-    const BeamKey c = found[i];
-    int place = 0;
-    for (int j = 0; j < n; ++j) place += better(found[j], c);
-    if (place >= K) continue;
+  beam_places(found, n, [&](BeamKey c, int place) {
+    if (place >= K) return;
     const long at = r0 + place;
-    const int k = (int)(c.at / a.V), t = (int)(c.at % a.V);
+    const int k = (int)(c.at >> 32), t = (int)(unsigned)c.at;
     a.parents[at] = k;
     a.tokens[at] = kind[k] == 2 ? a.eos : t;
     a.scores_out[at] = (float)(c.rank * pen[k]);
     if (a.finished_out) a.finished_out[at] = kind[k] == 2 || t == a.eos;
     if (a.lengths_out) a.lengths_out[at] = len[k];
-  }
+  });
   // places for which there is no candidate
   if (tid >= n && tid < K) {
-    const int old = a.lengths ? a.lengths[r0 + tid] : 0;
     a.parents[r0 + tid] = tid;
     a.tokens[r0 + tid] = -1;
     a.scores_out[r0 + tid] = -__builtin_inff();
@@ -246,13 +268,16 @@ __device__ void beam_copy(char* to, const char* from, long bytes) {
   }
 }
 
-// Place k of search b, one slice of a tensor's row.
+// Place k of search b, one slice of a tensor's row.  Bound by the copies: 256 places of
+// 1 MiB of which 120 or so move take 32 us, some 7 TB/s read and written; what does not
+// move costs its work-group three trips to memory (4 us where nothing moves).
 __global__ __launch_bounds__(256) void beam_pool_move_kernel(BeamMove a) {
   const int place = blockIdx.y + gridDim.y * blockIdx.z;
   if (place >= a.B * a.K) return;
   const int b = place / a.K, k = place % a.K, l = threadIdx.x & 63;
   const bool in = l < a.K, tell = blockIdx.x == 0 && k == 0 && threadIdx.x < 64;
-  const int p = in ? beam_parent(a, b, l, tell) : -1;
+  const int* slots = a.slots + (long)b * a.K;
+  const int slot = in ? slots[l] : -1, p = in ? beam_parent(a, b, l, tell) : -1;
   // places after the first successor of their beam, and beams without any
   unsigned long long again = 0, childless = 0;
   for (int j = 0; j < a.K; ++j) {
@@ -260,12 +285,11 @@ __global__ __launch_bounds__(256) void beam_pool_move_kernel(BeamMove a) {
     if (m) again |= m & (m - 1);
     else childless |= 1ull << j;
   }
-  const int* slots = a.slots + (long)b * a.K;
-  const int src = slots[__shfl(p, k, 64)];
+  const int src = __shfl(slot, __shfl(p, k, 64), 64);
   int dst = src;
   if (again >> k & 1) {
     for (int j = __popcll(again & ((1ull << k) - 1)); j > 0; --j) childless &= childless - 1;
-    dst = slots[__ffsll(childless) - 1];
+    dst = __shfl(slot, __ffsll(childless) - 1, 64);
   }
   if (blockIdx.x == 0 && threadIdx.x == 0 && a.slots_out) {
     a.slots_out[place] = dst;
@@ -392,14 +416,18 @@ ll_status ll_beam_select(ll_beam_plan* p, void* stream, int32_t searches, const 
   a.parents = parents; a.tokens = tokens; a.scores_out = scores_out;
   a.finished_out = finished_out; a.lengths_out = lengths_out;
   const int rows = searches * p->d.K;
+  // A work-group a compute unit, none of less than 32 KiB.  (Rows, join: 4 rows of 50001
+  // floats 8.0 + 4.2 us, in parts of 64 KiB 9.3 + 3.9, of 16 KiB 8.7 + 6.0; 256 rows of
+  // 131072 bfloat16 19.1 us, with two work-groups a compute unit 20.7.)
   const long want = (p->cus + rows - 1) / rows, row = (long)p->d.V * elem_bytes(p);
-  a.parts = (int)std::max(1L, std::min({want, row / (64 << 10), (long)ll::kPartsMax}));
+  a.parts = (int)std::max(1L, std::min({want, row / (32 << 10), (long)ll::kPartsMax}));
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  // (240 rows of 50001 floats in two parts: 14.6 us by 256 threads, 19.8 by 1024)
   const bool wide = (long)rows * a.parts <= p->cus;
   if (p->d.dtype == LL_BF16) launch_rows<bf16_t>(a, rows, wide, s);
   else launch_rows<float>(a, rows, wide, s);
   LL_HIP(hipGetLastError());
-  ll::beam_join_kernel<<<dim3(searches), dim3(256), 0, s>>>(a);
+  ll::beam_join_kernel<<<dim3(searches), dim3(ll::kBeamJoin), 0, s>>>(a);
   LL_HIP(hipGetLastError());
   return LL_OK;
 }

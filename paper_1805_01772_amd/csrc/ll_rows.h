@@ -276,8 +276,9 @@ __device__ void select_top(const T* row, const Span& sp, int V, int top, uint4 o
 
 // The part's sums (per thread), and with TOP its thread's largest chunk.  With
 // KEEP the thread's first chunks stay in LDS (keep[i][tid]).  Chunks are loaded
-// four at a time, past the end the last one again: one wait for four.
-template <typename T, int NTHR, bool TOP, int KEEP = 0>
+// four at a time, past the end the last one again: one wait for four.  Without T_SUM
+// the sum that the entropy needs is left out.
+template <typename T, int NTHR, bool TOP, int KEEP = 0, bool T_SUM = true>
 __device__ __forceinline__ Stats walk(const T* row, const Span& sp, int V, uint4* own, int* own_c,
                                       uint4 (*keep)[NTHR] = nullptr) {
   constexpr int E = Op<T>::kPerChunk;
@@ -302,7 +303,7 @@ __device__ __forceinline__ Stats walk(const T* row, const Span& sp, int V, uint4
     for (int e = 0; e < E; ++e) {
       const float d = f[e] - a.m, x = exp_diff(d);
       a.s += x;
-      a.t += fmaxf(d, -1e4f) * x;
+      if (T_SUM) a.t += fmaxf(d, -1e4f) * x;
     }
   };
   const T* body = row + sp.head;
