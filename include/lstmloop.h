@@ -535,13 +535,15 @@ ll_status delta_loop_step(const ll_delta_desc* desc, void* stream, const void* q
  * Rows keep their state at t >= seq_len[b] and output y = 0 there.  Value head
  * h reads key head h / (Hv / Hk).
  *   T_max, B, Hk, Hv, Dk, Dv >= 1; Hv a multiple of Hk; Dk and Dv multiples of
- *     8, at most 128, T_max <= 2^30, B Hv < 2^21 (one token: B Hv ceil(Dv / 32) <
- *     2^24; else LL_EUNSUPPORTED); dtype an ll_dtype, the type of q, k, v, y and
+ *     8, at most 128, T_max <= 2^30, B Hv < 2^21, T_max B Hk Dk <= 2^34 (one token:
+ *     B Hv ceil(Dv / 32) < 2^24; else LL_EUNSUPPORTED); dtype an ll_dtype, the type of q, k, v, y and
  *     their gradients (decays, states and their gradients are float).  Inside, sums
  *     and states are float, products keep float's 24 bits.
  *   inference, q_ld .. dv_ld, scale  as for ll_delta_desc.
- * The decays are constants of the layer: they get no gradient.  A token that holds
- * NaN or infinity may reach y from up to 63 tokens before it on (what it leaves in
+ * The decays are constants of the layer: they get no gradient.  Infinity in an
+ * operand or a state, and a float above bfloat16's largest (3.39e38), give NaN in a
+ * loop (the step computes with them as float does).  A token that holds such a
+ * value or NaN may reach y from up to 63 tokens before it on (what it leaves in
  * the state stays there).  Outputs overlap no input, but for ST, which may be S0.
  * g, seq_len, slots and device_error need 4 bytes' alignment, every other array 16.
  */

@@ -269,7 +269,7 @@ __device__ void beam_copy(char* to, const char* from, long bytes) {
 }
 
 // Place k of search b, one slice of a tensor's row.  Bound by the copies: 256 places of
-// 1 MiB of which 120 or so move take 32 us, some 7 TB/s read and written; what does not
+// 1 MiB of which 110 or so move take 33 us, some 7 TB/s read and written; what does not
 // move costs its work-group three trips to memory (4 us where nothing moves).
 __global__ __launch_bounds__(256) void beam_pool_move_kernel(BeamMove a) {
   const int place = blockIdx.y + gridDim.y * blockIdx.z;
@@ -416,7 +416,7 @@ ll_status ll_beam_select(ll_beam_plan* p, void* stream, int32_t searches, const 
   a.parents = parents; a.tokens = tokens; a.scores_out = scores_out;
   a.finished_out = finished_out; a.lengths_out = lengths_out;
   const int rows = searches * p->d.K;
-  // A work-group a compute unit, none of less than 32 KiB.  (Rows, join: 4 rows of 50001
+  // A work-group a compute unit, none of less than 32 KiB.  (Rows, join: 4 rows of 32000
   // floats 8.0 + 4.2 us, in parts of 64 KiB 9.3 + 3.9, of 16 KiB 8.7 + 6.0; 256 rows of
   // 131072 bfloat16 19.1 us, with two work-groups a compute unit 20.7.)
   const long want = (p->cus + rows - 1) / rows, row = (long)p->d.V * elem_bytes(p);

@@ -299,6 +299,27 @@ def test_state_in_place_and_repeatable(T):
     assert torch.equal(S, a["ST"]) and torch.equal(y, a["y"])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", ["q", "k", "v", "S0"])
+@pytest.mark.parametrize("T", [40, 1100])
+def test_infinity_stays_in_its_row_and_head(T, name, dtype):
+    """NaN or infinity comes out of the head that held it, and nothing in the others."""
+    c = make(T, 3, 2, 2, 24, 16, dtype, lens=[T, T - 5, T // 2])
+    clean, _ = run(c, dtype)
+    if name == "S0":
+        c[name][1, 1, 3, 5] = math.inf
+    else:
+        c[name][T // 3, 1, 1, 4] = math.inf
+    r, err = run(c, dtype)
+    assert err == 0
+    assert not torch.isfinite(r["y"][:, 1, 1]).all()
+    for n, want in clean.items():
+        got = r[n].clone()
+        got.select(1 if n in ("y", "dq", "dk", "dv") else 0, 1).select(-3 if n in ("ST", "dS0") else -2, 1).zero_()
+        want.select(1 if n in ("y", "dq", "dk", "dv") else 0, 1).select(-3 if n in ("ST", "dS0") else -2, 1).zero_()
+        assert torch.equal(got, want), n
+
+
 def test_bad_length_counts_as_zero_and_is_reported():
     c = make(20, 3, 1, 1, 16, 16, "f32", [20, 21, -1], seed=12)
     got, err = run(c, "f32")
