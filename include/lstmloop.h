@@ -773,7 +773,7 @@ ll_status ll_beam_plan_destroy(ll_beam_plan* plan);
  *   scores   [searches,K] float; minus infinity: a beam that does not count (all but
  *            one at a search's first step).
  *   finished [searches,K] int32, nonzero: this beam is finished; NULL: none is.
- *   lengths  [searches,K] int32, or NULL (length_penalty 0 only).
+ *   lengths  [searches,K] int32 (negative: 0), or NULL (length_penalty 0 only).
  *   parents  [searches,K] int32: the beam that each next one continues, 0 .. K - 1.
  *   tokens   [searches,K] int32: its token (eos for a beam that was finished, also
  *            where that is -1).

@@ -134,7 +134,7 @@ __global__ __launch_bounds__(kBeamJoin) void beam_join_kernel(BeamArgs a) {
     if (bad) atomicOr(a.err, LL_DEVERR_BEAM);
     const bool walked = live && !bad && st.y > 0.f;
     kind[tid] = walked ? 1 : !bad && done && score > -__builtin_inff() ? 2 : 0;
-    len[tid] = max(0, old) + (done ? 0 : 1);
+    len[tid] = done ? max(0, old) : min(max(0, old), 0x7ffffffe) + 1;
     base[tid] = score;
     off[tid] = walked ? (double)st.x : 0.0;
     sum[tid] = walked ? log((double)st.y) : 0.0;

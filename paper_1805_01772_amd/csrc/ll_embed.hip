@@ -204,7 +204,7 @@ struct EmbedSort {
   int wave[kEmbWaves];
 };
 
-// A pass waits for memory and LDS more than it moves: 131072 places in 128 tiles take 4.8
+// A pass waits for memory and LDS more than it moves: 131072 places in 64 tiles take 4.8
 // us to count and 14 to place, 1 MB each way; places a wave puts down together find their
 // rank by a ballot for each bit of the digit, without atomics.
 //
@@ -360,26 +360,29 @@ __global__ __launch_bounds__(kEmbThreads) void embed_place_kernel(EmbedArgs a, i
              a.key[pass & 1], a.pos[pass & 1]);
 }
 
-// scale * acc to the row of token t (or added to it).
-template <typename TG>
-__device__ __forceinline__ void embed_put(const EmbedArgs& a, int t, const Columns& c, const float* acc) {
+// scale * acc to the row of token t, or added to it: to `old`, where that has been read.
+template <typename TG, bool ADD>
+__device__ __forceinline__ void embed_put(const EmbedArgs& a, int t, const Columns& c, const float* acc,
+                                          const Eight<TG>* old = nullptr) {
   TG* to = static_cast<TG*>(a.dw) + t * a.dw_ld;
   float f[kEmbUnit];
-  if (a.accumulate) {
+  if (ADD) {
     Eight<TG> x[1];
-    load_rows<TG, 1>(c, [&](int) { return to; }, x);
+    if (old) x[0] = *old;
+    else load_rows<TG, 1>(c, [&](int) { return to; }, x);
     x[0].floats(f);
   }
 #pragma unroll
-  for (int e = 0; e < kEmbUnit; ++e) f[e] = a.accumulate ? __builtin_fmaf(a.scale, acc[e], f[e]) : a.scale * acc[e];
+  for (int e = 0; e < kEmbUnit; ++e) f[e] = ADD ? __builtin_fmaf(a.scale, acc[e], f[e]) : a.scale * acc[e];
   store_row(c, to, f);
 }
 
 // The runs of a piece: `lanes` threads and as many eights of columns.  Bound by the rows of
 // dx that it gathers and the rows it writes: 131072 places of 1024 bfloat16, onto old
-// floats, in 152 us; 25600 places of float in 26.9 us, 3.9 TB/s of dx alone (47 when the
+// floats (ADD), in 142 us, 3.7 TB/s (152 when a run's old row was read at its end, one
+// after the other); 25600 places of float in 27 us, 3.9 TB/s of dx alone (47 when the
 // places were fetched with their rows).
-template <typename TX, typename TG>
+template <typename TX, typename TG, bool ADD>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, int lanes, int cols, const int* key, const int* pos) {
   constexpr int R = 8;
   const int lane = threadIdx.x & (lanes - 1), groups = 256 / lanes;
@@ -393,11 +396,11 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, int lanes, 
   const int after = n1 < a.N ? key[n1] : -1;
   bool first = true;
   float acc[kEmbUnit] = {};
-  auto flush = [&](bool goes_on) {
+  auto flush = [&](bool goes_on, const Eight<TG>* old) __attribute__((always_inline)) {
     if (!c.any) return;
     const bool before = first && begun;
     if (before || goes_on) store_row(c, a.part + (2l * piece + (before ? 0 : 1)) * a.D, acc);
-    else embed_put<TG>(a, cur, c, acc);
+    else embed_put<TG, ADD>(a, cur, c, acc, old);
   };
   // eight places at a time (a piece is a multiple of that, and the arrays are padded to
   // one): their tokens and rows' numbers a step ahead of the rows, the rows without
@@ -422,13 +425,23 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, int lanes, 
   for (int n = n0; n < n1 && cur != a.V; n += R) {
     Eight<TX> x[R];
     load_rows<TX, R>(c, [&](int j) { return dx + at[j] * a.dx_ld; }, x);
+    // the old rows of the runs that end here, beside them
+    Eight<TG> old[ADD ? R : 1];
+    if (ADD) {
+#pragma unroll
+      for (int j = 0; j < R; ++j) {
+        const int t = j ? k[j - 1] : cur;
+        if (t != k[j] && t != a.V && n + j < n1)
+          load_rows<TG, 1>(c, [&](int) { return static_cast<const TG*>(a.dw) + t * a.dw_ld; }, old + j);
+      }
+    }
     if (n + R < n1) fetch(n + R, k2, at2);
 #pragma unroll
     for (int j = 0; j < R; ++j) {
       if (cur == a.V) break;
       if (k[j] != cur) {
         if (n + j >= n1) break;        // the piece's end: below
-        flush(false);
+        flush(false, ADD ? old + j : nullptr);
         first = false;
         cur = k[j];
 #pragma unroll
@@ -448,13 +461,13 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, int lanes, 
   }
   if (cur == a.V) return;
   const bool goes_on = after == cur;
-  flush(goes_on);
+  flush(goes_on, nullptr);
   if (goes_on && !(first && begun) && c.any && c.col + c.skip == 0) a.heads[atomicAdd(a.count, 1)] = piece;
 }
 
 // Runs that go over pieces: the waves' shares of the partial sums, joined in order (7 us
 // for 25600 places in pieces of 16, 13 for 131072 in pieces of 64: a few long runs).
-template <typename TG>
+template <typename TG, bool ADD>
 __global__ __launch_bounds__(kEmbJoin) void embed_join_kernel(EmbedArgs a, const int* key) {
   constexpr int NW = kEmbJoin / 64, R = 8;
   __shared__ int more;
@@ -503,7 +516,7 @@ __global__ __launch_bounds__(kEmbJoin) void embed_join_kernel(EmbedArgs a, const
         for (int j = 1; j < NW; ++j) s += sums[j][e * 64 + l];
         acc[e] = s;
       }
-      embed_put<TG>(a, t, c, acc);
+      embed_put<TG, ADD>(a, t, c, acc);
     }
     __syncthreads();
   }
@@ -529,18 +542,18 @@ void release(ll_embed_plan* p) {
 }
 
 // Threads for a row of D: eight elements each, a power of two.
-int lanes_of(int D, int most) {
+int lanes_of(int D) {
   int lanes = 1;
-  while (lanes < most && lanes * ll::kEmbUnit < D) lanes *= 2;
+  while (lanes < 256 && lanes * ll::kEmbUnit < D) lanes *= 2;
   return lanes;
 }
 
 // Places of a piece for n of them: long ones leave fewer partial sums, as long as there
-// are waves enough.  (Sums and joins of 25600 places of 1024 floats: pieces of 64 places
+// are waves enough.  (Sums and joins, before old rows were read ahead, of 25600 places of 1024 floats: pieces of 64 places
 // 40.4 + 4.9 us, 32 33.0 + 6.2, 16 26.9 + 7.4, 8 26.5 + 13.1; 131072 places of bfloat16:
 // 64 152 + 12.7, 32 145 + 22.7.)
 int piece_of(int n, int D) {
-  const int lanes = lanes_of(D, 64), cols = (D + lanes * ll::kEmbUnit - 1) / (lanes * ll::kEmbUnit);
+  const int lanes = lanes_of(D), cols = (D + lanes * ll::kEmbUnit - 1) / (lanes * ll::kEmbUnit);
   int piece = 64;
   while (piece > 8 && (long)(n / piece) * cols * lanes < 64L * ll::kEmbSums) piece /= 2;
   return piece;
@@ -583,11 +596,13 @@ void launch_bwd(const ll::EmbedArgs& a, int passes, hipStream_t s) {
   if (a.N <= ll::kEmbSmall) {
     ll::embed_sort_small_kernel<TG><<<dim3(1 + a.fill), dim3(threads), 0, s>>>(a, passes);
   } else {
-    // the clearing work-groups go out with the sort's launches, as many with each
+    // the clearing work-groups go out with the sort's launches, three quarters of them beside
+    // the longer one of a pass (131 MB with 25600 places: 44 us of sort, 47 in equal shares,
+    // 37 without any clearing)
     const int launches = 2 * passes;
     long done = 0;
     for (int i = 0; i < launches; ++i) {
-      const long upto = (long)a.fill * (i + 1) / launches;
+      const long upto = (long)a.fill * (i & 1 ? 4 * (i / 2 + 1) : 4 * (i / 2) + 1) / (4 * passes);
       const dim3 grid((unsigned)(a.tiles + upto - done));
       if (i & 1) ll::embed_place_kernel<TG><<<grid, dim3(threads), 0, s>>>(a, i / 2, done, a.fill);
       else ll::embed_count_kernel<TG><<<grid, dim3(threads), 0, s>>>(a, i / 2, done, a.fill);
@@ -597,13 +612,18 @@ void launch_bwd(const ll::EmbedArgs& a, int passes, hipStream_t s) {
   if (a.pieces == 0) return;
   const int* key = a.key[(passes - 1) & 1];
   const int* pos = a.pos[(passes - 1) & 1];
-  const int lanes = lanes_of(a.D, 64), cols = (a.D + lanes * ll::kEmbUnit - 1) / (lanes * ll::kEmbUnit);
+  const int lanes = lanes_of(a.D), cols = (a.D + lanes * ll::kEmbUnit - 1) / (lanes * ll::kEmbUnit);
   const int groups = 256 / lanes;
   const unsigned grid = (unsigned)((a.pieces + groups - 1) / groups) * cols;
-  ll::embed_sum_kernel<TX, TG><<<dim3(grid), dim3(256), 0, s>>>(a, lanes, cols, key, pos);
-  if (a.pieces > 1)
-    ll::embed_join_kernel<TG><<<dim3((unsigned)std::min(a.pieces - 1, 2048), (unsigned)((a.D + 64 * ll::kEmbUnit - 1) / (64 * ll::kEmbUnit))),
-                            dim3(ll::kEmbJoin), 0, s>>>(a, key);
+  const dim3 joins((unsigned)std::min(a.pieces - 1, 2048),
+                   (unsigned)((a.D + 64 * ll::kEmbUnit - 1) / (64 * ll::kEmbUnit)));
+  if (a.accumulate) {
+    ll::embed_sum_kernel<TX, TG, true><<<dim3(grid), dim3(256), 0, s>>>(a, lanes, cols, key, pos);
+    if (a.pieces > 1) ll::embed_join_kernel<TG, true><<<joins, dim3(ll::kEmbJoin), 0, s>>>(a, key);
+  } else {
+    ll::embed_sum_kernel<TX, TG, false><<<dim3(grid), dim3(256), 0, s>>>(a, lanes, cols, key, pos);
+    if (a.pieces > 1) ll::embed_join_kernel<TG, false><<<joins, dim3(ll::kEmbJoin), 0, s>>>(a, key);
+  }
 }
 
 }  // namespace
@@ -639,7 +659,7 @@ ll_status ll_embed_plan_create(const ll_embed_desc* d, int device, ll_embed_plan
   a.bits = (key_bits + p->passes - 1) / p->passes;
   // partial sums: two a piece; the most pieces that any number of places up to N has
   // (fewer than twice those of the smallest number that takes longer ones)
-  const int lanes = lanes_of(d->D, 64), cols = (d->D + lanes * ll::kEmbUnit - 1) / (lanes * ll::kEmbUnit);
+  const int lanes = lanes_of(d->D), cols = (d->D + lanes * ll::kEmbUnit - 1) / (lanes * ll::kEmbUnit);
   const long full = 64L * ll::kEmbSums / ((long)cols * lanes) + 1;
   const long pieces = std::max((long)(d->N + 63) / 64, std::min((long)(d->N + 7) / 8, 2 * full + 2));
   const size_t n4 = sizeof(int) * ((size_t)(d->N + 7) / 8 * 8);  // (read eight at a time)
@@ -696,7 +716,7 @@ ll_status ll_embed_fwd(ll_embed_plan* p, void* stream, int32_t n, const void* ta
   ll::DeviceGuard guard(p->device);
   ll::EmbedArgs a = p->a;
   a.N = n; a.w = table; a.tokens = tokens; a.x = x;
-  const int lanes = lanes_of(a.D, 256);
+  const int lanes = lanes_of(a.D);
   // four rows a thread where there are rows enough for all compute units
   const int groups = 256 / lanes;
   const int rows = (long)n >= 8L * p->cus * groups ? 4 * groups : groups;
@@ -726,6 +746,7 @@ ll_status ll_embed_bwd(ll_embed_plan* p, void* stream, int32_t n, const int32_t*
     a.tiles = 1;
     a.tile = n;
   } else {
+    // (131072 places in 64 tiles: 14.0 us to place, in 128 17.3: each reads all counts)
     a.tiles = std::min(ll::kEmbTiles, (n + 2047) / 2048);
     a.tile = (n + a.tiles - 1) / a.tiles;
   }
