@@ -268,8 +268,9 @@ def _ptr_array(ts):
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
+        # torch.cuda.current_stream() makes an object of it: 2.9 us, this 0.3
         import torch
-        stream = torch.cuda.current_stream()
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream
 
 
