@@ -869,7 +869,10 @@ def ll_beam_reorder(parents, tensors: Sequence, slots=None, slots_out=None, devi
     if len(shape) != 2:
         raise ValueError(f"parents: [searches, K] is wanted, got {shape}")
     n, K = shape
-    rows = tensors[0].shape[0] if slots is not None and len(tensors) else n * K
+    if slots is None:
+        rows = n * K
+    else:                                    # without a pool its slots have no bound
+        rows = tensors[0].shape[0] if len(tensors) else 2 ** 31 - 1
     recs = (ll_beam_tensor * max(1, len(tensors)))()
     for j, t in enumerate(tensors):
         if not t.is_cuda or not t.is_contiguous():
@@ -877,6 +880,8 @@ def ll_beam_reorder(parents, tensors: Sequence, slots=None, slots_out=None, devi
         if t.dim() < 1 or (t.shape[0] != rows and (slots is not None or tuple(t.shape[:2]) != shape)):
             raise ValueError(f"tensors[{j}]: {rows} rows are wanted, got {tuple(t.shape)}")
         recs[j] = ll_beam_tensor(t.data_ptr(), t.numel() // max(1, rows) * t.element_size())
+    if n == 0:
+        return
     _check(load_library().ll_beam_reorder(
         _stream(stream), n, K, _want(parents, "parents", shape, i), len(tensors), recs,
         _want(slots, "slots", shape, i, optional=True), rows if slots is not None else 0,

@@ -312,3 +312,31 @@ def test_reorder_refusals():
         ll.ll_beam_reorder(p.flatten(), [x])
     with pytest.raises(ValueError):
         ll.ll_beam_reorder(p.long(), [x])
+
+
+def test_slots_alone_and_no_searches():
+    """Slots without tensors may have any numbers; a call for no searches does nothing."""
+    parents = torch.tensor([[1, 1, 0]], dtype=torch.int32, device=DEV)
+    slots = torch.tensor([[70, 9, 500]], dtype=torch.int32, device=DEV)
+    out, err = torch.zeros_like(slots), torch.zeros(1, dtype=torch.int32, device=DEV)
+    ll.ll_beam_reorder(parents, [], slots=slots, slots_out=out, device_error=err)
+    assert out.tolist() == [[9, 500, 70]] and err.item() == 0
+    none = torch.zeros(0, 3, dtype=torch.int32, device=DEV)
+    ll.ll_beam_reorder(none, [torch.zeros(0, 5, device=DEV)])
+    pool = torch.ones(4, 5, device=DEV)
+    ll.ll_beam_reorder(none, [pool], slots=none, slots_out=none.clone())
+    c = {n: t[:0] for n, t in make(2, 3, 50, "f32").items()}
+    with ll.BeamPlan(2, 3, 50) as p:
+        assert run(c, plan=p)[1] == 0
+    assert (pool == 1).all()
+
+
+def test_lengths_at_the_types_ends():
+    c = make(2, 3, 50, "f32", first=False, done=0)
+    c["lengths"][:] = torch.tensor([2 ** 31 - 1, -5, 3], dtype=torch.int32, device=DEV)
+    out, err = run(c, penalty=0.5)
+    assert err == 0
+    grown = torch.tensor([2 ** 31 - 1, 1, 4], dtype=torch.int32, device=DEV)
+    for b in range(2):
+        assert torch.equal(out["lengths"][b], grown[out["parents"][b].long()])
+        assert torch.isfinite(out["scores"][b]).all()
