@@ -549,9 +549,9 @@ int lanes_of(int D) {
 }
 
 // Places of a piece for n of them: long ones leave fewer partial sums, as long as there
-// are waves enough.  (Sums and joins, before old rows were read ahead, of 25600 places of 1024 floats: pieces of 64 places
-// 40.4 + 4.9 us, 32 33.0 + 6.2, 16 26.9 + 7.4, 8 26.5 + 13.1; 131072 places of bfloat16:
-// 64 152 + 12.7, 32 145 + 22.7.)
+// are waves enough.  (Sums and joins of 25600 places of 1024 floats: pieces of 64 places
+// 40.4 + 4.9 us, 32 33.0 + 6.2, 16 26.9 + 7.4, 8 26.5 + 13.1; of 131072 places of bfloat16,
+// before old rows were read ahead: 64 152 + 12.7, 32 145 + 22.7.)
 int piece_of(int n, int D) {
   const int lanes = lanes_of(D), cols = (D + lanes * ll::kEmbUnit - 1) / (lanes * ll::kEmbUnit);
   int piece = 64;
@@ -570,7 +570,7 @@ ll_status validate(const ll_embed_desc* d) {
       return fail(LL_EINVAL, "a distance of rows is %lld: it must be 0, or D = %d .. 2^31", (long long)ld, d->D);
   if (!std::isfinite(d->scale)) return fail(LL_EINVAL, "scale is not finite");
   if (d->reserved) return fail(LL_EINVAL, "reserved must be 0");
-  // work-groups of the sums: a piece of 64 places and 512 columns each
+  // work-groups of the sums (a piece of 64 places and 512 columns each) at most
   const int64_t groups = ((int64_t)(d->N + 63) / 64) * ((d->D + 511) / 512);
   if (groups > ll::max_groups(256))
     return fail(LL_EUNSUPPORTED, "N = %d with D = %d: %lld work-groups, a launch holds %lld", d->N, d->D,
