@@ -181,9 +181,12 @@ __device__ void embed_clear(const EmbedArgs& a, long index, long shares, int thr
   const long at = index * threads + threadIdx.x, all = shares * threads;
   const float zero[kEmbUnit] = {};
   if (a.dw_ld == a.D) {
-    const long n = (long)a.V * a.D, units = n / kEmbUnit;
-    for (long u = at; u < units; u += all) store8(dw + u * kEmbUnit, zero);
-    if (at < n - units * kEmbUnit) dw[units * kEmbUnit + at] = 0;
+    // (16 bytes a lane, neighbours side by side)
+    constexpr int E = 16 / sizeof(TG);
+    typedef u32x4 any __attribute__((aligned(2)));
+    const long n = (long)a.V * a.D, units = n / E;
+    for (long u = at; u < units; u += all) *reinterpret_cast<any*>(dw + u * E) = u32x4{0, 0, 0, 0};
+    if (at < n - units * E) dw[units * E + at] = 0;
     return;
   }
   const int units = (a.D + kEmbUnit - 1) / kEmbUnit;
@@ -205,7 +208,7 @@ struct EmbedSort {
 };
 
 // A pass waits for memory and LDS more than it moves: 131072 places in 64 tiles take 4.8
-// us to count and 14 to place, 1 MB each way; places a wave puts down together find their
+// us to count and 11.7 to place, 1 MB each way; places a wave puts down together find their
 // rank by a ballot for each bit of the digit, without atomics.
 //
 // One pass over the digit at `shift` for tile `tile`: places [n0, n1) of the source go to
@@ -234,23 +237,26 @@ __device__ void embed_pass(const EmbedArgs& a, EmbedSort& sh, int tile, int shif
   __syncthreads();
   // a thread's two digits: all before them, then in tile and wave order
   constexpr int PER = (1 << kEmbBits) / kEmbThreads;
+  static_assert(PER == 2, "two digits a thread, read at once");
   int total[PER], before[PER], sum = 0;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int d = tid * PER + i;
-    total[i] = before[i] = 0;
-    if (d >= digits) continue;
+  for (int i = 0; i < PER; ++i) total[i] = before[i] = 0;
+  if (tid * PER < digits) {            // (digits is a multiple of PER)
     if (alone) {
-      for (int j = 0; j < kEmbWaves; ++j) total[i] += sh.cnt[j][d];
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        for (int j = 0; j < kEmbWaves; ++j) total[i] += sh.cnt[j][tid * PER + i];
     } else {
-#pragma unroll 8
+#pragma unroll 16
       for (int t = 0; t < a.tiles; ++t) {
-        const int c = a.hist[(long)t * digits + d];
-        total[i] += c;
-        before[i] += t < tile ? c : 0;
+        const int2 c = *reinterpret_cast<const int2*>(a.hist + (long)t * digits + tid * PER);
+        total[0] += c.x;
+        total[1] += c.y;
+        before[0] += t < tile ? c.x : 0;
+        before[1] += t < tile ? c.y : 0;
       }
     }
-    sum += total[i];
+    sum = total[0] + total[1];
   }
   int scan = sum;
   for (int d = 1; d < 64; d <<= 1) {
@@ -274,7 +280,10 @@ __device__ void embed_pass(const EmbedArgs& a, EmbedSort& sh, int tile, int shif
     at += total[i];
   }
   __syncthreads();
-  volatile int* next = sh.cnt[w];
+  // (an address in LDS: accesses through a general one wait for the stores to memory too,
+  // 14 us instead of 11.7 for 131072 places)
+  typedef __attribute__((address_space(3))) volatile int* lds_int;
+  lds_int next = (lds_int)sh.cnt[w];
   auto place = [&](int n, int key, int pos) {
     const bool in = n + l < hi;
     const int d = (key >> shift) & mask;
@@ -597,8 +606,8 @@ void launch_bwd(const ll::EmbedArgs& a, int passes, hipStream_t s) {
     ll::embed_sort_small_kernel<TG><<<dim3(1 + a.fill), dim3(threads), 0, s>>>(a, passes);
   } else {
     // the clearing work-groups go out with the sort's launches, three quarters of them beside
-    // the longer one of a pass (131 MB with 25600 places: 44 us of sort, 47 in equal shares,
-    // 37 without any clearing)
+    // the longer one of a pass (131 MB with 25600 places: 41 us of sort, 3 more in equal
+    // shares)
     const int launches = 2 * passes;
     long done = 0;
     for (int i = 0; i < launches; ++i) {
@@ -746,7 +755,7 @@ ll_status ll_embed_bwd(ll_embed_plan* p, void* stream, int32_t n, const int32_t*
     a.tiles = 1;
     a.tile = n;
   } else {
-    // (131072 places in 64 tiles: 14.0 us to place, in 128 17.3: each reads all counts)
+    // (131072 places: 128 tiles take 3 us longer to place than 64, each reads all counts)
     a.tiles = std::min(ll::kEmbTiles, (n + 2047) / 2048);
     a.tile = (n + a.tiles - 1) / a.tiles;
   }
