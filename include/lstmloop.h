@@ -416,7 +416,8 @@ ll_status ll_eval_activations(int32_t device, const float* in, float* out, int64
  */
 
 /* More device error word bits. */
-#define LL_DEVERR_SLOT 4     /* a state slot >= n_slots                       */
+#define LL_DEVERR_SLOT 4     /* a state slot < -1 or >= n_slots; a state for  */
+                             /* which ll_beam_reorder has no slot             */
 #define LL_DEVERR_TARGET 8   /* a target < -1 or >= V                         */
 #define LL_DEVERR_TOKEN 16   /* a token < -1 or >= V                          */
 #define LL_DEVERR_BEAM 32    /* a parent outside [0, K); NaN among a beam's   */
@@ -805,9 +806,12 @@ typedef struct {
  *            Else [searches,K] int32 into tensors of n_slots rows, and slots_out
  *            [searches,K], another array, required: the slot of each next beam.  A
  *            beam's first successor keeps its slot; the state is copied for the further
- *            ones only, into the slots of beams without a successor.  Slots are
- *            distinct; -1: no state (nothing is copied from or to it); < -1 or >=
- *            n_slots: the same, and sets LL_DEVERR_SLOT.
+ *            ones only, into the slots of beams without a successor, in order.  Slots
+ *            are distinct.  -1: no state; all successors of such a beam have -1, and
+ *            no state is put there.  A state that finds no slot is lost: its successor
+ *            has -1, and LL_DEVERR_SLOT is set.  (So slots that nobody needs are in no
+ *            place of slots_out.)  A slot < -1 or >= n_slots sets LL_DEVERR_SLOT and
+ *            counts as no state; handed on, it keeps its number.
  *   device_error  device int32 whose bits are set (never cleared), or NULL.
  */
 ll_status ll_beam_reorder(void* stream, int32_t searches, int32_t K, const int32_t* parents,

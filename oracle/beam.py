@@ -48,16 +48,18 @@ def beam_select(logits, scores, finished=None, lengths=None, eos=-1, length_pena
 
 def beam_slots(parents, slots):
     """The slots of the next beams and the copies (from, to) that they need: a beam's
-    first successor keeps its slot, further ones get those of beams without any."""
+    first successor keeps its slot, further ones get those of beams without any.  -1: no
+    state, which all its successors have, and no place for one."""
     parents, slots = np.asarray(parents), np.asarray(slots)
-    out, copies = np.empty_like(slots), []
+    out, copies = np.full_like(slots, -1), []
     for b in range(len(parents)):
         seen = set()
-        free = [k for k in range(parents.shape[1]) if k not in parents[b]]
+        free = [k for k in range(parents.shape[1]) if k not in parents[b] and slots[b, k] != -1]
         for k, p in enumerate(parents[b]):
-            at = int(p) if p not in seen else free.pop(0)
-            if p in seen:
-                copies.append((int(slots[b, p]), int(slots[b, at])))
+            if p not in seen:
+                out[b, k] = slots[b, p]
+            elif slots[b, p] >= 0 and free:
+                out[b, k] = slots[b, free.pop(0)]
+                copies.append((int(slots[b, p]), int(out[b, k])))
             seen.add(p)
-            out[b, k] = slots[b, at]
     return out, copies

@@ -12,7 +12,7 @@
 // Reordering in place: a thread has the same few bytes of all K rows, so it reads what it
 // needs before it writes.  In a pool (rows by slots) no row moves that need not: a beam's
 // first successor takes its slot over, the further ones copy the state into the slots of
-// beams without a successor.
+// beams without a successor.  A beam without a state (slot -1) has successors without one.
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -276,8 +276,10 @@ __global__ __launch_bounds__(256) void beam_pool_move_kernel(BeamMove a) {
   if (place >= a.B * a.K) return;
   const int b = place / a.K, k = place % a.K, l = threadIdx.x & 63;
   const bool in = l < a.K, tell = blockIdx.x == 0 && k == 0 && threadIdx.x < 64;
+  const bool tell_place = blockIdx.x == 0 && threadIdx.x == 0;
   const int* slots = a.slots + (long)b * a.K;
   const int slot = in ? slots[l] : -1, p = in ? beam_parent(a, b, l, tell) : -1;
+  if (tell && in && (slot < -1 || slot >= a.n_slots) && a.err) atomicOr(a.err, LL_DEVERR_SLOT);
   // places after the first successor of their beam, and beams without any
   unsigned long long again = 0, childless = 0;
   for (int j = 0; j < a.K; ++j) {
@@ -285,16 +287,20 @@ __global__ __launch_bounds__(256) void beam_pool_move_kernel(BeamMove a) {
     if (m) again |= m & (m - 1);
     else childless |= 1ull << j;
   }
-  const int src = __shfl(slot, __shfl(p, k, 64), 64);
+  // the former need a slot where their beam has a state, the latter offer theirs, in order
+  const int old = __shfl(slot, p, 64);
+  const unsigned long long needs = again & __ballot(in && old >= 0 && old < a.n_slots);
+  childless &= ~__ballot(slot == -1);
+  const int src = __shfl(old, k, 64);
   int dst = src;
   if (again >> k & 1) {
-    for (int j = __popcll(again & ((1ull << k) - 1)); j > 0; --j) childless &= childless - 1;
-    dst = __shfl(slot, __ffsll(childless) - 1, 64);
+    for (int j = __popcll(needs & ((1ull << k) - 1)); j > 0; --j) childless &= childless - 1;
+    const bool some = needs >> k & 1 && childless != 0;
+    const int free = __shfl(slot, some ? __ffsll(childless) - 1 : 0, 64);
+    dst = some ? free : -1;
+    if (tell_place && needs >> k & 1 && !some && a.err) atomicOr(a.err, LL_DEVERR_SLOT);
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0 && a.slots_out) {
-    a.slots_out[place] = dst;
-    if ((dst < -1 || dst >= a.n_slots) && a.err) atomicOr(a.err, LL_DEVERR_SLOT);
-  }
+  if (tell_place && a.slots_out) a.slots_out[place] = dst;
   if (dst == src || a.n == 0 || src < 0 || dst < 0 || src >= a.n_slots || dst >= a.n_slots) return;
   int i = 0;
   while (i + 1 < a.n && (int)blockIdx.x >= a.t[i + 1].first) ++i;

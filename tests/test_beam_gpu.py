@@ -340,3 +340,65 @@ def test_lengths_at_the_types_ends():
     for b in range(2):
         assert torch.equal(out["lengths"][b], grown[out["parents"][b].long()])
         assert torch.isfinite(out["scores"][b]).all()
+
+
+# ------------------------------------------------------------ places without a state
+def in_pool(parents, slots, n_slots):
+    """ll_beam_reorder of a pool whose slot s holds s: new slots, the pool, the error word."""
+    parents = torch.tensor(parents, dtype=torch.int32, device=DEV)
+    slots = torch.tensor(slots, dtype=torch.int32, device=DEV)
+    out, err = torch.full_like(slots, -5), torch.zeros(1, dtype=torch.int32, device=DEV)
+    pool = torch.arange(n_slots, device=DEV, dtype=torch.float32)[:, None].repeat(1, 5)
+    ll.ll_beam_reorder(parents, [pool], slots=slots, slots_out=out, device_error=err)
+    return out.tolist(), pool[:, 0].tolist(), err.item()
+
+
+def test_successors_of_a_beam_without_a_state_have_none():
+    """Not the slot, and the old state, of a beam that ended."""
+    out, pool, err = in_pool([[0, 0, 2, 2]], [[-1, 4, 1, 0]], 6)
+    assert out == [[-1, -1, 1, 4]] and err == 0
+    assert pool == [0, 1, 2, 3, 1, 5]
+    # 4 is nobody's where no beam with a state needs it
+    out, pool, err = in_pool([[0, 0, 2]], [[-1, 4, 1]], 6)
+    assert out == [[-1, -1, 1]] and err == 0 and pool == [0, 1, 2, 3, 4, 5]
+
+
+def test_a_state_takes_a_free_slot_behind_places_without_one():
+    out, pool, err = in_pool([[3, 3, 3, 0]], [[2, -1, 5, 0]], 6)
+    assert out == [[0, 5, -1, 2]] and err == ll.LL_DEVERR_SLOT      # two successors, one free slot
+    assert pool == [0, 1, 2, 3, 4, 0]
+
+
+def test_a_state_that_finds_no_slot_is_reported():
+    """A search's first step whose single beam alone has a slot."""
+    out, pool, err = in_pool([[0, 0, 0], [2, 1, 0]], [[3, -1, -1], [0, -1, 1]], 4)
+    assert out == [[3, -1, -1], [1, -1, 0]] and err == ll.LL_DEVERR_SLOT
+    assert pool == [0, 1, 2, 3]
+    out, pool, err = in_pool([[2, 1, 0]], [[0, -1, 1]], 4)
+    assert out == [[1, -1, 0]] and err == 0
+
+
+@pytest.mark.parametrize("K", [2, 3, 5, 8, 32])
+def test_pool_with_places_without_a_state(K):
+    """Every place's state is its parent's, or there is none; nothing else is written."""
+    B, n_slots = 40, 40 * K + 7
+    gen = torch.Generator(device=DEV).manual_seed(K)
+    parents = torch.randint(0, K, (B, K), device=DEV, generator=gen).int()
+    slots = torch.randperm(n_slots, device=DEV, generator=gen)[:B * K].view(B, K).int()
+    slots[torch.rand(B, K, device=DEV, generator=gen) < 0.3] = -1
+    pool = torch.arange(n_slots, device=DEV).float()[:, None].repeat(1, 33)
+    out, err = torch.full_like(slots, -5), torch.zeros(1, dtype=torch.int32, device=DEV)
+    ll.ll_beam_reorder(parents, [pool], slots=slots, slots_out=out, device_error=err)
+    want, copies = ob.beam_slots(parents.cpu().numpy(), slots.cpu().numpy())
+    assert out.cpu().numpy().tolist() == want.tolist()
+    old = slots.gather(1, parents.long())
+    assert ((out >= 0) <= (old >= 0)).all()
+    lost = ((old >= 0) & (out < 0)).any().item()
+    assert err.item() == (ll.LL_DEVERR_SLOT if lost else 0)
+    rows = torch.arange(n_slots, device=DEV).float()
+    for src, dst in copies:
+        rows[dst] = src
+    assert torch.equal(pool, rows[:, None].expand_as(pool))
+    held = out >= 0
+    assert torch.equal(pool[out[held].long(), 0], old[held].float())
+    assert out[held].unique().numel() == int(held.sum())
