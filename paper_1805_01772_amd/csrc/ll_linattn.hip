@@ -67,6 +67,16 @@ __device__ __forceinline__ float lin_log(const float* g, int h) {
   return x < -200.f ? -200.f : x;
 }
 
+// What a decay l = e^x leaves of a state.  Near 1 as S + (l - 1) S, because a rounded l would
+// err the same way in every chunk; else as l S, because S + (l - 1) S would leave roundings
+// of S itself, and l S may be less than those.
+struct LinLeft {
+  float f;                             // l - 1 or l
+  bool near;
+  __device__ __forceinline__ explicit LinLeft(float x) : f(x > -0.69f ? expm1f(x) : expf(x)), near(x > -0.69f) {}
+  __device__ __forceinline__ float of(float s) const { return near ? __builtin_fmaf(s, f, s) : s * f; }
+};
+
 // Rows in LDS have UP units of 16 bytes, a power of two, and hold unit u at u ^ turn(row):
 // 16 lanes that read the same unit of 16 rows, or two units of 8 rows, meet 16 different
 // places of the banks.
@@ -330,7 +340,8 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
   const T* la = pa + (ahead + dir * ur_) * p.a_ld + ux_ * E;
   const T* lb = pb + (ahead + dir * ur_) * p.b_ld + ux_ * E;
   const T* lc = pc + (ahead + dir * uc_) * p.c_ld + c0 + cx_ * E;
-  const float grow_all = uniform(expm1f(g * CT));
+  LinLeft left_all(g * CT);
+  left_all.f = uniform(left_all.f);
   uint4 ra[LR], rb[LR], rc[LC];
 #pragma unroll
   for (int i = 0; i < LR; ++i) ra[i] = rb[i] = zero4();
@@ -468,16 +479,15 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
       }
       out_at += dir * CT * p.o_ld;
     }
-    // S' = l^m S + ..; as S + (l^m - 1) S, because a rounded l^m would err the same way in
-    // every chunk
+    // S' = l^m S + ..
     // (LOCAL: from zero, so every token's weight is what the part's end leaves of it)
     f32x4 wt[NI];
     const float after = LOCAL ? uniform(expf(g * max(0, t_end - t0 - CT))) : 1.f;
 #pragma unroll
     for (int i = 0; i < NI; ++i) wt[i] = leave * (l16[NI - 1 - i] * after);
-    float grow = grow_all;
+    LinLeft left = left_all;
     if (m != CT) {
-      grow = expm1f(g * m);
+      left = LinLeft(g * m);
 #pragma unroll
       for (int i = 0; i < NI; ++i)
 #pragma unroll
@@ -485,12 +495,16 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
           wt[i][r] = p.wU * expf(g * max(0, m - 16 * i - 4 * hi - r - p.e));
     }
     if (!LOCAL) {
+      auto each = [&](auto f) __attribute__((always_inline)) {
 #pragma unroll
-      for (int d = 0; d < 2 * KD; ++d)
+        for (int d = 0; d < 2 * KD; ++d)
 #pragma unroll
-        for (int t = 0; t < NV; ++t)
+          for (int t = 0; t < NV; ++t)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) S[d][t][r] = __builtin_fmaf(S[d][t][r], grow, S[d][t][r]);
+            for (int r = 0; r < 4; ++r) S[d][t][r] = f(S[d][t][r]);
+      };
+      if (left.near) each([&](float x) { return __builtin_fmaf(x, left.f, x); });
+      else each([&](float x) { return x * left.f; });
     }
 #pragma unroll
     for (int j = 0; j < NM; ++j) {
@@ -556,9 +570,9 @@ __global__ __launch_bounds__(256) void lin_scan_kernel(LinArgs a, float* states,
     for (int i = 0; i < R; ++i) {
       if (p + i >= a.parts) break;
       *reinterpret_cast<f32x4*>(st + (p + i) * size) = e;
-      const float grow = expm1f(g * min(per, max(0, len - (p + i) * per)));
+      const LinLeft left(g * min(per, max(0, len - (p + i) * per)));
 #pragma unroll
-      for (int r = 0; r < 4; ++r) e[r] = __builtin_fmaf(e[r], grow, e[r]) + own[i][r];
+      for (int r = 0; r < 4; ++r) e[r] = left.of(e[r]) + own[i][r];
     }
   }
 }
@@ -624,7 +638,7 @@ __global__ __launch_bounds__(256) void lin_step_kernel(LinStepArgs a) {
   const T* q = static_cast<const T*>(a.q) + b * a.q_ld + (long)hk * a.Dk;
   const T* v = static_cast<const T*>(a.v) + b * a.v_ld + (long)h * a.Dv + c;
   float* S = a.S + ((long)slot * a.H + h) * a.Dk * a.Dv + c;
-  const float grow = expm1f(lin_log(a.g, h));
+  const LinLeft left(lin_log(a.g, h));
   f32x4 s[4];
   float kd[4], qd[4], vc[4];
 #pragma unroll
@@ -642,8 +656,7 @@ __global__ __launch_bounds__(256) void lin_step_kernel(LinStepArgs a) {
     const int d = r0 + 32 * i;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      // (l S as S + (l - 1) S: a rounded l would err the same way at every token)
-      s[i][e] = __builtin_fmaf(kd[i], vc[e], __builtin_fmaf(s[i][e], grow, s[i][e]));
+      s[i][e] = __builtin_fmaf(kd[i], vc[e], left.of(s[i][e]));
       o[e] = __builtin_fmaf(qd[i], s[i][e], o[e]);
     }
     if (in && d < a.Dk) *reinterpret_cast<f32x4*>(S + (long)d * a.Dv) = s[i];

@@ -482,3 +482,44 @@ def test_step_refuses_rows_that_overlap():
     S, y = c["S0"].clone(), torch.empty_like(c["v"][0])
     with pytest.raises(ValueError, match="overlap"):
         ll.linattn_loop_step(c["q"][0][:1].expand(4, 1, 16), c["k"][0], c["v"][0], c["g"], S, y)
+
+
+# ------------------------------------------------------------ what a decay leaves of a state
+def units(g, T, times):
+    """Roundings (2^-24 each) of a state that e^g has been applied to for T tokens, by `times`
+    products: the exponent's (|g| T in all), and for each product its exponential's last
+    place (two), another of the exponent's product and its own."""
+    return (abs(g) * T + 4 * times) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("g,T", [(-0.25, 64), (-0.25, 100), (-1.0, 33), (-0.05, 64), (-0.011, 128), (-0.02, 70), (-5.0, 5),
+                                 (-0.05, 1100), (-0.01, 2111)])
+def test_what_is_left_of_a_state_keeps_its_bits(g, T, dtype):
+    """Tokens that add nothing: each element of the last state is e^{g T} of the first one's,
+    whatever that factor is, and so is the state's gradient (l S as S + (l - 1) S would leave
+    roundings of S itself, which are anything of a small l S)."""
+    c = make(T, 2, 1, 2, 24, 40, dtype, [T, T - 3], seed=T)
+    c["g"].copy_(torch.tensor([g, g / 2]))
+    c["k"].zero_()
+    c["dy"].zero_()
+    r, err = run(c, dtype)
+    assert err == 0
+    for b, L in enumerate((T, T - 3)):
+        for h, x in enumerate(c["g"].double().tolist()):
+            for got, first in (("ST", "S0"), ("dS0", "dST")):
+                want = math.exp(x * L) * c[first][b, h].double()
+                off = ((r[got][b, h].double() - want).abs() / want.abs()).max().item()
+                assert off <= units(x, L, -(-L // 32) + 1), (got, b, h, off)
+
+
+def test_step_keeps_what_is_left_of_a_state():
+    c = make(1, 2, 1, 6, 16, 24, "f32", seed=20)
+    c["g"].copy_(torch.tensor([-0.1, -0.69, -0.7, -3.0, -9.0, -17.0]))
+    c["k"].zero_()
+    S, y = c["S0"].clone(), torch.empty_like(c["v"][0])
+    for _ in range(3):
+        ll.linattn_loop_step(c["q"][0], c["k"][0], c["v"][0], c["g"], S, y)
+    for h, x in enumerate(c["g"].double().tolist()):
+        want = math.exp(3 * x) * c["S0"][:, h].double()
+        assert ((S[:, h].double() - want).abs() / want.abs()).max() <= units(x, 3, 3), x
