@@ -341,6 +341,16 @@ void launch_rows(const ll::BeamArgs& a, int rows, bool wide, hipStream_t s) {
   else ll::beam_rows_kernel<T, 256><<<grid, dim3(256), 0, s>>>(a);
 }
 
+// Bytes moved at once, and the work-groups that move a row.
+int unit_of(const ll_beam_tensor& t) {
+  const uintptr_t both = reinterpret_cast<uintptr_t>(t.data) | (uintptr_t)t.row_bytes;
+  return both % 16 == 0 ? 16 : both % 4 == 0 ? 4 : both % 2 == 0 ? 2 : 1;
+}
+int64_t slices_of(const ll_beam_tensor& t, bool pool) {
+  const int64_t each = pool ? ll::kBeamSlice : 256 * unit_of(t);
+  return (t.row_bytes + each - 1) / each;
+}
+
 template <int KM>
 void launch_in_place(const ll::BeamMove& m, dim3 grid, hipStream_t s) {
   ll::beam_rows_move_kernel<KM><<<grid, dim3(256), 0, s>>>(m);
@@ -463,32 +473,41 @@ ll_status ll_beam_reorder(void* stream, int32_t searches, int32_t K, const int32
     }
   }
   if (searches == 0) return LL_OK;
+  // blocks times searches (places) in 2^32 work-items; tensors go to as many launches as
+  // hold them, all of them counted before the first
+  const int64_t outer = slots ? (int64_t)searches * K : searches;
+  const int64_t z = (outer + 32767) / 32768, y = (outer + z - 1) / z;
+  const int64_t most = ll::max_groups(256) / (y * z);
+  int first[LL_BEAM_TENSORS + 1] = {0}, launches = 0;
+  int64_t blocks = 0;
+  for (int i = 0; i < n_tensors; ++i) {
+    const int64_t n = slices_of(tensors[i], slots != nullptr);
+    if (n > most)
+      return fail(LL_EUNSUPPORTED, "tensors[%d]: %lld slices of %lld rows are more than a launch holds (%lld)", i,
+                  (long long)n, (long long)(y * z), (long long)ll::max_groups(256));
+    if (i - first[launches] == ll::kBeamTensors || blocks + n > most) {
+      first[++launches] = i;
+      blocks = 0;
+    }
+    blocks += n;
+  }
+  if (n_tensors || slots) first[++launches] = n_tensors;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  for (int i0 = 0; i0 < n_tensors || (i0 == 0 && slots); i0 += ll::kBeamTensors) {
+  for (int j = 0; j < launches; ++j) {
     ll::BeamMove m{};
     m.B = searches; m.K = K; m.n_slots = n_slots;
-    m.parents = parents; m.slots = slots; m.slots_out = i0 == 0 ? slots_out : nullptr; m.err = device_error;
-    m.n = std::min(n_tensors - i0, ll::kBeamTensors);
-    int64_t blocks = 0;
+    m.parents = parents; m.slots = slots; m.slots_out = j == 0 ? slots_out : nullptr; m.err = device_error;
+    m.n = first[j + 1] - first[j];
+    blocks = 0;
     for (int i = 0; i < m.n; ++i) {
-      const ll_beam_tensor& t = tensors[i0 + i];
-      const uintptr_t both = reinterpret_cast<uintptr_t>(t.data) | (uintptr_t)t.row_bytes;
-      const int unit = both % 16 == 0 ? 16 : both % 4 == 0 ? 4 : both % 2 == 0 ? 2 : 1;
+      const ll_beam_tensor& t = tensors[first[j] + i];
       m.t[i].data = static_cast<char*>(t.data);
       m.t[i].row = t.row_bytes;
-      m.t[i].unit = unit;
+      m.t[i].unit = unit_of(t);
       m.t[i].first = (int)blocks;
-      const int64_t each = slots ? ll::kBeamSlice : 256 * unit;
-      blocks += (t.row_bytes + each - 1) / each;
+      blocks += slices_of(t, slots != nullptr);
     }
-    blocks = std::max<int64_t>(blocks, 1);
-    // blocks times searches (places) in 2^32 work-items
-    const int64_t outer = slots ? (int64_t)searches * K : searches;
-    if (blocks * outer > ll::max_groups(256))
-      return fail(LL_EUNSUPPORTED, "%lld slices of %lld rows are more than a launch holds (%lld)", (long long)blocks,
-                  (long long)outer, (long long)ll::max_groups(256));
-    const unsigned y = (unsigned)std::min<int64_t>(outer, 32768), z = (unsigned)((outer + y - 1) / y);
-    const dim3 grid((unsigned)blocks, y, z);
+    const dim3 grid((unsigned)std::max<int64_t>(blocks, 1), (unsigned)y, (unsigned)z);
     if (slots) ll::beam_pool_move_kernel<<<grid, dim3(256), 0, s>>>(m);
     else if (K <= 4) launch_in_place<4>(m, grid, s);
     else if (K <= 8) launch_in_place<8>(m, grid, s);

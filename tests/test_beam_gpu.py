@@ -402,3 +402,20 @@ def test_pool_with_places_without_a_state(K):
     held = out >= 0
     assert torch.equal(pool[out[held].long(), 0], old[held].float())
     assert out[held].unique().numel() == int(held.sum())
+
+
+def test_tensors_of_more_than_one_launch():
+    """Two tensors that a launch holds one of: 4.3 million work-groups each move bytes here,
+    twice (K = 2 rows, 2 searches, of an odd number of bytes)."""
+    row = 1_100_000_003
+    parents = torch.tensor([[1, 1], [1, 0]], dtype=torch.int32, device=DEV)
+    ts = [torch.zeros(4, row, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    small = torch.arange(4, device=DEV)
+    for i, t in enumerate(ts):
+        t[:, :100] = t[:, -100:] = torch.arange(4, device=DEV, dtype=torch.uint8)[:, None] + 10 * i
+    ll.ll_beam_reorder(parents, [ts[0], ts[1], small])
+    for i, t in enumerate(ts):
+        for part in (t[:, :100], t[:, -100:]):
+            assert (part == torch.tensor([1, 1, 3, 2], device=DEV, dtype=torch.uint8)[:, None] + 10 * i).all()
+        assert not t[:, 100:-100].any()
+    assert small.tolist() == [1, 1, 3, 2]

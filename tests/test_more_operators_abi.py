@@ -153,3 +153,15 @@ def test_beam_reorder_arguments(change, status):
 @pytest.mark.parametrize("name", ["ll_linattn_desc", "ll_embed_desc", "ll_beam_desc", "ll_beam_tensor"])
 def test_structures(name):
     structure_follows_the_header(name)
+
+
+@pytest.mark.parametrize("pool", [False, True])
+@pytest.mark.parametrize("n", [33, 64, 65, 256])
+def test_beam_reorder_refuses_before_it_moves(n, pool):
+    """The last tensor of many is too large for a launch: nothing of the others moves (the
+    first launch of them would fail here, where there is no device)."""
+    lib = _lib()
+    t = (ll.ll_beam_tensor * n)(*[ll.ll_beam_tensor((i + 1) << 20, 64) for i in range(n)])
+    t[n - 1] = ll.ll_beam_tensor(1 << 40, 1 << 36)
+    st = lib.ll_beam_reorder(None, 64, 4, 4096, n, t, *((4096, 256, 8192) if pool else (None, 0, None)), None)
+    assert st == ll.LL_EUNSUPPORTED and f"tensors[{n - 1}]" in ll.ll_last_error()
