@@ -863,7 +863,8 @@ def ll_beam_reorder(parents, tensors: Sequence, slots=None, slots_out=None, devi
                     stream=None) -> None:
     """ll_beam_reorder (asynchronous on `stream`): parents [searches, K]; tensors are
     contiguous with searches * K rows (dimension 0, or [searches, K, ..]), or, with
-    slots [searches, K], with as many rows as their pool has slots."""
+    slots [searches, K], with as many rows as their pool has slots.  (Rows may hold
+    nothing.)"""
     i = _dtype("int32")
     shape = tuple(parents.shape)
     if len(shape) != 2:
@@ -873,17 +874,19 @@ def ll_beam_reorder(parents, tensors: Sequence, slots=None, slots_out=None, devi
         rows = n * K
     else:                                    # without a pool its slots have no bound
         rows = tensors[0].shape[0] if len(tensors) else 2 ** 31 - 1
-    recs = (ll_beam_tensor * max(1, len(tensors)))()
+    recs = []
     for j, t in enumerate(tensors):
         if not t.is_cuda or not t.is_contiguous():
             raise ValueError("tensors passed to the library must live on the GPU and be contiguous")
         if t.dim() < 1 or (t.shape[0] != rows and (slots is not None or tuple(t.shape[:2]) != shape)):
             raise ValueError(f"tensors[{j}]: {rows} rows are wanted, got {tuple(t.shape)}")
-        recs[j] = ll_beam_tensor(t.data_ptr(), t.numel() // max(1, rows) * t.element_size())
+        if t.numel():
+            recs.append((t.data_ptr(), t.numel() // rows * t.element_size()))
     if n == 0:
         return
     _check(load_library().ll_beam_reorder(
-        _stream(stream), n, K, _want(parents, "parents", shape, i), len(tensors), recs,
+        _stream(stream), n, K, _want(parents, "parents", shape, i), len(recs),
+        (ll_beam_tensor * max(1, len(recs)))(*recs),
         _want(slots, "slots", shape, i, optional=True), rows if slots is not None else 0,
         _want(slots_out, "slots_out", shape, i, optional=True),
         _want(device_error, "device_error", (1,), i, optional=True)))

@@ -1,0 +1,45 @@
+"""The binding of beam search (no GPU: a stub in the library's place, tensors of host
+memory that call themselves the device's)."""
+import types
+
+import pytest
+import torch
+
+from paper_1805_01772_amd import lstmloop as ll
+
+
+class OnDevice(torch.Tensor):
+    is_cuda = True
+
+
+STREAM = types.SimpleNamespace(cuda_stream=0)
+
+
+def new(*shape, dtype=torch.float32):
+    return torch.zeros(*shape, dtype=dtype).as_subclass(OnDevice)
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    got = []
+
+    class Stub:
+        def ll_beam_reorder(self, stream, searches, K, parents, n, tensors, slots, n_slots, slots_out, err):
+            got.append(([(t.data, t.row_bytes) for t in tensors[:n]], n_slots))
+            return ll.LL_OK
+    monkeypatch.setattr(ll, "load_library", lambda *a: Stub())
+    return got
+
+
+def test_rows_that_hold_no_bytes_need_no_move(calls):
+    """A history of width 0, as a search's first step has it, beside a tensor that has rows."""
+    parents, x = new(2, 3, dtype=torch.int32), new(6, 5)
+    ll.ll_beam_reorder(parents, [new(2, 3, 0), x, new(6, 0, 7, dtype=torch.int32)], stream=STREAM)
+    ll.ll_beam_reorder(parents, [new(6, 0)], stream=STREAM)
+    slots, pool = new(2, 3, dtype=torch.int32), new(9, 4)
+    ll.ll_beam_reorder(parents, [new(9, 0), pool], slots=slots, slots_out=slots.clone(), stream=STREAM)
+    ll.ll_beam_reorder(parents, [new(9, 0)], slots=slots, slots_out=slots.clone(), stream=STREAM)
+    assert calls == [([(x.data_ptr(), 20)], 0), ([], 0), ([(pool.data_ptr(), 16)], 9), ([], 9)]
+    for bad in (new(5, 0), new(2, 4, 0)):
+        with pytest.raises(ValueError, match="rows are wanted"):
+            ll.ll_beam_reorder(parents, [bad], stream=STREAM)
