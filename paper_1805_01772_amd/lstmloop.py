@@ -268,9 +268,13 @@ def _ptr_array(ts):
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        # torch.cuda.current_stream() makes an object of it: 2.9 us, this 0.3
+        # torch.cuda.current_stream() makes an object of it: 2.9 us, the handle alone 0.3
+        # (it is no part of torch's public interface)
         import torch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            return raw(torch.cuda.current_device())
+        stream = torch.cuda.current_stream()
     return stream.cuda_stream
 
 

@@ -43,3 +43,15 @@ def test_rows_that_hold_no_bytes_need_no_move(calls):
     for bad in (new(5, 0), new(2, 4, 0)):
         with pytest.raises(ValueError, match="rows are wanted"):
             ll.ll_beam_reorder(parents, [bad], stream=STREAM)
+
+
+def test_current_stream_with_and_without_torchs_short_way(monkeypatch):
+    """The stream's handle alone is not in torch's public interface: where torch does not
+    have it, the stream's object says the same."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: types.SimpleNamespace(cuda_stream=77))
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 40 + device, raising=False)
+    assert ll._stream(None) == 43
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
+    assert ll._stream(None) == 77
+    assert ll._stream(STREAM) == 0
