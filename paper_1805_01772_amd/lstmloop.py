@@ -774,8 +774,8 @@ class EmbedPlan(_OpPlan):
                  dx_dtype: str = "f32", grad_dtype: str = "f32", scale: float = 1.0,
                  inference: bool = False, table_ld: int = 0, x_ld: int = 0, dx_ld: int = 0,
                  grad_ld: int = 0, device: int = 0):
-        if scale == 0:
-            raise ValueError("scale must not be 0")
+        if ctypes.c_float(scale).value == 0:
+            raise ValueError("scale must not be 0 (as a float)")
         names = dict(table_dtype=table_dtype, x_dtype=x_dtype, dx_dtype=dx_dtype, grad_dtype=grad_dtype)
         codes = [_type_code(t, n) for n, t in names.items()]
         self.desc = ll_embed_desc(N, V, D, *codes, 1 if inference else 0, table_ld, x_ld, dx_ld,

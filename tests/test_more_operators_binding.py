@@ -55,3 +55,10 @@ def test_current_stream_with_and_without_torchs_short_way(monkeypatch):
     monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
     assert ll._stream(None) == 77
     assert ll._stream(STREAM) == 0
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-60, -1e-46])
+def test_embed_scale_that_is_zero_in_float(scale):
+    """The descriptor's 0 means 1: a factor of 0 is refused, also one that a float holds as 0."""
+    with pytest.raises(ValueError, match="scale"):
+        ll.EmbedPlan(4, 10, 16, scale=scale)
