@@ -536,7 +536,7 @@ ll_status delta_loop_step(const ll_delta_desc* desc, void* stream, const void* q
  * Rows keep their state at t >= seq_len[b] and output y = 0 there.  Value head
  * h reads key head h / (Hv / Hk).
  *   T_max, B, Hk, Hv, Dk, Dv >= 1; Hv a multiple of Hk; Dk and Dv multiples of
- *     8, at most 128, T_max <= 2^30, B Hv < 2^21, T_max B Hk Dk <= 2^34 (one token:
+ *     8, at most 128, T_max <= 2^30, B Hv < 2^22, T_max B Hk Dk <= 2^34 (one token:
  *     B Hv ceil(Dv / 32) < 2^24; else LL_EUNSUPPORTED); dtype an ll_dtype, the type of q, k, v, y and
  *     their gradients (decays, states and their gradients are float).  Inside, sums
  *     and states are float, products keep float's 24 bits.

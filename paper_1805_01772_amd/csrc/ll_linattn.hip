@@ -51,7 +51,7 @@ struct LinPass {
 struct LinArgs {
   LinPass p[3];
   int T, B, H, Dk, Dv;                 // H: value heads
-  int parts, per, npass, ctiles;       // parts of a row, chunks of a part
+  int parts, per, npass;               // parts of a row, chunks of a part
   const float* g;
   const int* seq_len;
   int* err;
@@ -216,7 +216,7 @@ __device__ __forceinline__ void lin_store(void* dst, long at, const float* x, bo
 }
 
 // ---------------------------------------------------------------------------
-// One part of a row, head and pass, 64 NV columns of the state: chunk after chunk.  A
+// One part of a row, head and pass, up to 64 NV columns of the state: chunk after chunk.  A
 // wave has 16 NV columns of the state in its accumulators, and a share of the chunk's
 // products a_i.b_j, which go to the others through LDS as the next product takes them.
 // LOCAL: only the state of the part's tokens alone.
@@ -246,24 +246,21 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
   constexpr int NF = NI == 4 ? 6 : 2;
   auto pair = [](int i, int j) { return i + (i > 2 ? 1 : 0) + j; };   // 0 | 1 | 2 3 | 4 5
   __shared__ __align__(16) unsigned char ps[LOCAL ? 16 : NF * L::kHeld];
-  // items that read the same tokens (columns and passes) lie 8 work-groups apart: on one
-  // XCD, one after the other
+  // passes that read the same tokens lie 8 work-groups apart: on one XCD, one after the other
   const int parts = LOCAL ? args.parts - 1 : args.parts;  // nothing follows the last part's own
-  const int sub = args.ctiles * args.npass, items = args.B * args.H * parts;
+  const int items = args.B * args.H * parts;
   int id = blockIdx.x;
-  const int full = items / 8 * 8 * sub;
+  const int full = items / 8 * 8 * args.npass;
   int item, which;
   if (id < full) {
-    item = id / (8 * sub) * 8 + id % 8;
-    which = id / 8 % sub;
+    item = id / (8 * args.npass) * 8 + id % 8;
+    which = id / 8 % args.npass;
   } else {
     id -= full;
     item = items / 8 * 8 + id % (items % 8);
     which = id / (items % 8);
   }
-  const LinPass& p = args.p[which / args.ctiles];
-  const int c0 = which % args.ctiles * NC;
-  if (c0 >= p.Dc) return;
+  const LinPass& p = args.p[which];
   const int part = item % parts, bh = item / parts, h = bh % args.H, b = bh / args.H;
   const int len = lin_len(args, b), per = args.per * CT;
   const int t_lo = part * per, t_hi = min(args.T, t_lo + per);
@@ -273,7 +270,7 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
     atomicOr(args.err, LL_DEVERR_SEQ_LEN_BIT);
   // token number i of the pass is token len - 1 - i where it runs backwards
   auto token = [&](int i) { return (long)(p.rev ? len - 1 - i : i) * args.B + b; };
-  const int cw = c0 + 16 * NV * w;                       // the wave's columns; a lane's: cw + 4 NV hi_ + ..
+  const int cw = 16 * NV * w;                            // the wave's columns; a lane's: cw + 4 NV hi_ + ..
   const int mine = cw + Q * hi_;
   const T* pa = static_cast<const T*>(p.a) + (long)(h / p.ag) * p.Dr;
   const T* pb = static_cast<const T*>(p.b) + (long)(h / p.bg) * p.Dr;
@@ -336,10 +333,10 @@ __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
   const int ur_ = tid / UR, ux_ = tid % UR, uc_ = tid / UC, cx_ = tid % UC;
   const long dir = p.rev ? -args.B : args.B;
   const long tok0 = token(0), ahead = tok0 + dir * t_lo;
-  const bool in_r = ux_ * E < p.Dr, in_c = c0 + cx_ * E < p.Dc;
+  const bool in_r = ux_ * E < p.Dr, in_c = cx_ * E < p.Dc;
   const T* la = pa + (ahead + dir * ur_) * p.a_ld + ux_ * E;
   const T* lb = pb + (ahead + dir * ur_) * p.b_ld + ux_ * E;
-  const T* lc = pc + (ahead + dir * uc_) * p.c_ld + c0 + cx_ * E;
+  const T* lc = pc + (ahead + dir * uc_) * p.c_ld + cx_ * E;
   LinLeft left_all(g * CT);
   left_all.f = uniform(left_all.f);
   uint4 ra[LR], rb[LR], rc[LC];
@@ -716,12 +713,12 @@ ll_status validate(const ll_linattn_desc* d, bool step) {
       return fail(LL_EINVAL, "%s = %lld must be 0, or at least %lld, at most 2^31 and a multiple of 16 bytes",
                   names[i], (long long)ld[i], (long long)need[i]);
   if (d->T_max > 1 << 30) return fail(LL_EUNSUPPORTED, "T_max = %d is more than 2^30", d->T_max);
-  // work-groups: at most six a head and part (three passes of two column tiles), and the
-  // sums of shared heads' gradients; the step's column tiles
+  // work-groups: three passes of each head and part (rows have parts only where heads are
+  // few); the step's column tiles
   const int64_t heads = (int64_t)d->B * d->Hv;
-  const int64_t groups = step ? heads * ((d->Dv + ll::kLinStepCols - 1) / ll::kLinStepCols) : 6 * heads + (1 << 14);
+  const int64_t groups = heads * (step ? (d->Dv + ll::kLinStepCols - 1) / ll::kLinStepCols : 3);
   const int64_t most = ll::max_groups(256);
-  if (heads > 1 << 24 || groups > most)
+  if (heads >= 1 << (step ? 24 : 22) || groups > most)
     return fail(LL_EUNSUPPORTED, "B * Hv = %lld: %lld work-groups, a launch holds %lld", (long long)heads,
                 (long long)groups, (long long)most);
   if (!step && (int64_t)d->T_max * d->B * qk / 4 > most * 256)
@@ -769,8 +766,7 @@ hipError_t launch_passes(ll::LinArgs a, bool bf16, bool local, hipStream_t s) {
     dc = std::max(dc, a.p[i].Dc);
   }
   const int nv = dc > 64 ? 2 : 1;
-  a.ctiles = 1;
-  const unsigned grid = (unsigned)a.B * a.H * (local ? a.parts - 1 : a.parts) * a.ctiles * a.npass;
+  const unsigned grid = (unsigned)a.B * a.H * (local ? a.parts - 1 : a.parts) * a.npass;
   const int kd = (dr + 31) / 32;
   if (bf16) {
     if (kd == 1) launch<bf16_t, 1>(a, nv, local, grid, s);

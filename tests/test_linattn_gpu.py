@@ -523,3 +523,26 @@ def test_step_keeps_what_is_left_of_a_state():
     for h, x in enumerate(c["g"].double().tolist()):
         want = math.exp(3 * x) * c["S0"][:, h].double()
         assert ((S[:, h].double() - want).abs() / want.abs()).max() <= units(x, 3, 3), x
+
+
+def test_many_heads():
+    """3.5 million rows of one head: more work-groups than 2^23 in the gradient."""
+    B, D = 3_500_000, 8
+    gen = torch.Generator(device=DEV).manual_seed(21)
+    n = lambda *s: torch.randn(*s, device=DEV, generator=gen)
+    c = dict(q=n(1, B, 1, D), k=n(1, B, 1, D), v=n(1, B, 1, D), g=torch.tensor([-0.3], device=DEV), seq_len=None,
+             S0=n(B, 1, D, D), dy=n(1, B, 1, D), dST=n(B, 1, D, D))
+    r, err = run(c, "f32", scale=1.0)
+    assert err == 0
+    q, k, v, dy = (c[x][0, :, 0].double() for x in ("q", "k", "v", "dy"))
+    left = math.exp(c["g"].double().item())
+    S = left * c["S0"][:, 0].double() + k[:, :, None] * v[:, None, :]
+    dS = c["dST"][:, 0].double() + q[:, :, None] * dy[:, None, :]
+    want = dict(y=(q[:, :, None] * S).sum(1), ST=S, dq=(S * dy[:, None, :]).sum(2), dk=(dS * v[:, None, :]).sum(2),
+                dv=(dS * k[:, :, None]).sum(1), dS0=left * dS)
+    for x, w in want.items():
+        a = r[x].double().view_as(w)
+        off = (a - w).flatten(1).norm(dim=1) / w.flatten(1).norm(dim=1)
+        for rows in (off[:1000], off[-1000:]):
+            assert rows.max() < 1e-4, x          # (a row's own norm may be small next to its terms')
+        assert ((a - w).norm() / w.norm()).item() <= 5e-6, x

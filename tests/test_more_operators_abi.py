@@ -165,3 +165,13 @@ def test_beam_reorder_refuses_before_it_moves(n, pool):
     t[n - 1] = ll.ll_beam_tensor(1 << 40, 1 << 36)
     st = lib.ll_beam_reorder(None, 64, 4, 4096, n, t, *((4096, 256, 8192) if pool else (None, 0, None)), None)
     assert st == ll.LL_EUNSUPPORTED and f"tensors[{n - 1}]" in ll.ll_last_error()
+
+
+@pytest.mark.parametrize("B,Hv,fits", [(1 << 22, 1, False), ((1 << 22) - 1, 1, True), (1 << 20, 4, False), (1 << 20, 3, True)])
+def test_linattn_heads_of_a_plan(B, Hv, fits):
+    """Three passes of each head in one launch: 3 * 2^22 work-groups."""
+    lib, h = _lib(), ctypes.c_void_p()
+    d = ll.make_linattn_desc(1, B, 1, Hv, 8, 8, "bf16")
+    st = lib.ll_linattn_plan_create(ctypes.byref(d), NOWHERE, ctypes.byref(h))
+    assert (st == ll.LL_EUNSUPPORTED and "work-groups" in ll.ll_last_error()) is not fits
+    assert st != ll.LL_OK and h.value is None
