@@ -240,3 +240,29 @@ def test_refusals():
             p.fwd(table, t, x[:7])
         with pytest.raises(ValueError):
             p.bwd(t, x, d.double())
+
+
+@pytest.mark.parametrize("types", [("f32", "f32"), ("bf16", "bf16")], ids=" ".join)
+@pytest.mark.parametrize("case", [
+    (300001, 3000, 9, "text"),               # tiles of more than 2048 places, 128 of them
+    (262145, 70, 4, "even"),
+    (20000, (1 << 20) + 5, 8, "even"),       # three digits, counted and placed by many work-groups
+    (300001, (1 << 20) + 5, 3, "text"),
+], ids=lambda c: "x".join(map(str, c)))
+def test_long_batches_and_large_vocabularies(case, types):
+    N, V, D, kind = case
+    t = tokens(N, V, seed=N + D, kind=kind)
+    t[:2], t[-2:] = V - 1, 0
+    dx = rows(N, D, types[0], seed=2)
+    with ll.EmbedPlan(N, V, D, dx_dtype=types[0], grad_dtype=types[1], scale=0.75) as p:
+        d = torch.full((V, D), math.nan, dtype=OP[types[1]], device=DEV)
+        p.bwd(t, dx, d)
+        check_grad(d, t, dx, V, 0.75, types[1])
+        again = torch.full_like(d, math.nan)
+        p.bwd(t, dx, again)
+        assert torch.equal(d, again)
+        old = rows(V, D, types[1], seed=3).clone()
+        d = old.clone()
+        p.bwd(t, dx, d, accumulate=True)
+        check_grad(d, t, dx, V, 0.75, types[1], old)
+        assert p.status_sync() == 0

@@ -546,3 +546,37 @@ def test_many_heads():
         for rows in (off[:1000], off[-1000:]):
             assert rows.max() < 1e-4, x          # (a row's own norm may be small next to its terms')
         assert ((a - w).norm() / w.norm()).item() <= 5e-6, x
+
+
+# ------------------------------------------------------------ bfloat16 results, element by element
+def check_rounded_once(got, want, name):
+    """Each element is the float result, rounded once: half a step of bfloat16 at that value
+    (2^-8 of the power of two below it), and what the float result may be off by itself: 5e-6 of
+    a row's norm as above, times four for the largest of its elements.  (A product that kept
+    one bfloat16 piece of a state or of another product would be off by about a step more.)"""
+    a = got.double().cpu().numpy()
+    step = np.where(want == 0, 0.0, 2.0 ** (np.floor(np.log2(np.abs(want) + (want == 0))) - 8))
+    rms = np.sqrt((want ** 2).mean(-1, keepdims=True))
+    over = np.abs(a - want) - step - 2e-5 * rms
+    print(f"    {name}: {over.max():.2e}", flush=True)
+    assert (over <= 0).all(), (name, over.max(), (over > 0).mean())
+
+
+@pytest.mark.parametrize("case", [c for c in CASES if c[0] in (31, 64, 65, 129, 200)] +
+                         [(1500, 2, 1, 2, 40, 64, [1500, 777]), (1100, 2, 1, 1, 128, 128, [65, 1100])],
+                         ids=lambda c: "x".join(map(str, c[:6])))
+def test_bfloat16_results_are_rounded_once(case):
+    *sizes, lens = case
+    c = make(*sizes, "bf16", lens, seed=sum(sizes) + 1)
+    got, err = run(c, "bf16")
+    assert err == 0
+    want = by_pairs(c)
+    for n in ("y", "dq", "dk", "dv"):
+        check_rounded_once(got[n], want[n], n)
+
+
+def test_bfloat16_step_is_rounded_once():
+    c = make(1, 40, 2, 4, 128, 104, "bf16", seed=23)
+    S, y = c["S0"].clone(), torch.empty_like(c["v"][0])
+    ll.linattn_loop_step(c["q"][0], c["k"][0], c["v"][0], c["g"], S, y)
+    check_rounded_once(y, reference(c, backward=False)["y"][0], "y")
