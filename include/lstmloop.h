@@ -800,18 +800,19 @@ typedef struct {
  * the next beams, in place, no plan.  Launches on the calling thread's current device.
  *   parents  [searches,K] as above; one outside [0, K) counts as its own place and
  *            sets LL_DEVERR_BEAM.
- *   tensors  host array of n_tensors (0 .. LL_BEAM_TENSORS) that do not overlap.
+ *   tensors  host array of n_tensors (0 .. LL_BEAM_TENSORS) that overlap neither each
+ *            other nor parents, slots or slots_out.
  *   slots    NULL: a tensor has searches K rows, and row (b, k) gets what row (b,
  *            parents[b,k]) held.
  *            Else [searches,K] int32 into tensors of n_slots rows, and slots_out
- *            [searches,K], another array, required: the slot of each next beam.  A
- *            beam's first successor keeps its slot; the state is copied for the further
- *            ones only, into the slots of beams without a successor, in order.  Slots
- *            are distinct.  -1: no state; all successors of such a beam have -1, and
- *            no state is put there.  A state that finds no slot is lost: its successor
- *            has -1, and LL_DEVERR_SLOT is set.  (So slots that nobody needs are in no
- *            place of slots_out.)  A slot < -1 or >= n_slots sets LL_DEVERR_SLOT and
- *            counts as no state; handed on, it keeps its number.
+ *            [searches,K], another array than slots and parents, required: the slot of
+ *            each next beam.  A beam's first successor keeps its slot; the state is
+ *            copied for the further ones only, into the slots of beams without a
+ *            successor, in order.  Slots are distinct.  -1: no state; all successors of
+ *            such a beam have -1, and no state is put there.  A state that finds no slot
+ *            is lost: its successor has -1, and LL_DEVERR_SLOT is set.  (So slots that
+ *            nobody needs are in no place of slots_out.)  A slot < -1 or >= n_slots sets
+ *            LL_DEVERR_SLOT and counts as no state; handed on, it keeps its number.
  *   device_error  device int32 whose bits are set (never cleared), or NULL.
  */
 ll_status ll_beam_reorder(void* stream, int32_t searches, int32_t K, const int32_t* parents,

@@ -341,6 +341,16 @@ void launch_rows(const ll::BeamArgs& a, int rows, bool wide, hipStream_t s) {
   else ll::beam_rows_kernel<T, 256><<<grid, dim3(256), 0, s>>>(a);
 }
 
+// Bytes of a tensor of `rows` rows (more than there are addresses: all of them).
+uint64_t bytes_of(const ll_beam_tensor& t, uint64_t rows) {
+  uint64_t n;
+  return __builtin_mul_overflow(rows, (uint64_t)t.row_bytes, &n) ? ~0ull : n;
+}
+bool overlap(const void* x, uint64_t nx, const void* y, uint64_t ny) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
+  return a <= b ? b - a < nx : a - b < ny;
+}
+
 // Bytes moved at once, and the work-groups that move a row.
 int unit_of(const ll_beam_tensor& t) {
   const uintptr_t both = reinterpret_cast<uintptr_t>(t.data) | (uintptr_t)t.row_bytes;
@@ -458,19 +468,22 @@ ll_status ll_beam_reorder(void* stream, int32_t searches, int32_t K, const int32
     return fail(LL_EINVAL, "n_tensors = %d must be 0 .. %d", n_tensors, LL_BEAM_TENSORS);
   if (!parents || (n_tensors && !tensors)) return fail(LL_EINVAL, "parents and tensors are required");
   if (!slots != !slots_out) return fail(LL_EINVAL, "slots and slots_out go together");
-  if (slots && slots == slots_out) return fail(LL_EINVAL, "slots_out must be another array than slots");
   if (slots && n_slots < 1) return fail(LL_EINVAL, "n_slots = %d must be at least 1", n_slots);
   LL_ALIGNED(parents, 4); LL_ALIGNED(slots, 4); LL_ALIGNED(slots_out, 4); LL_ALIGNED(device_error, 4);
-  const int64_t rows = slots ? n_slots : (int64_t)searches * K;
+  const uint64_t rows = slots ? n_slots : (int64_t)searches * K, list = 4ull * searches * K;
+  if (slots && (overlap(slots_out, list, slots, list) || overlap(slots_out, list, parents, list)))
+    return fail(LL_EINVAL, "slots_out overlaps slots or parents: it must be another array");
   for (int i = 0; i < n_tensors; ++i) {
     const ll_beam_tensor& t = tensors[i];
     if (!t.data || t.row_bytes < 1 || t.row_bytes > (int64_t)1 << 36)
       return fail(LL_EINVAL, "tensors[%d]: data is NULL or row_bytes = %lld is not 1 .. 2^36", i, (long long)t.row_bytes);
-    for (int j = 0; j < i; ++j) {
-      const char *x = (const char*)t.data, *y = (const char*)tensors[j].data;
-      if (x < y + rows * tensors[j].row_bytes && y < x + rows * t.row_bytes)
+    const uint64_t bytes = bytes_of(t, rows);
+    for (const int32_t* x : {parents, slots, (const int32_t*)slots_out})
+      if (x && overlap(t.data, bytes, x, list))
+        return fail(LL_EINVAL, "tensors[%d] overlaps %s", i, x == parents ? "parents" : x == slots ? "slots" : "slots_out");
+    for (int j = 0; j < i; ++j)
+      if (overlap(t.data, bytes, tensors[j].data, bytes_of(tensors[j], rows)))
         return fail(LL_EINVAL, "tensors[%d] and tensors[%d] overlap", j, i);
-    }
   }
   if (searches == 0) return LL_OK;
   // blocks times searches (places) in 2^32 work-items; tensors go to as many launches as

@@ -175,3 +175,27 @@ def test_linattn_heads_of_a_plan(B, Hv, fits):
     st = lib.ll_linattn_plan_create(ctypes.byref(d), NOWHERE, ctypes.byref(h))
     assert (st == ll.LL_EUNSUPPORTED and "work-groups" in ll.ll_last_error()) is not fits
     assert st != ll.LL_OK and h.value is None
+
+
+@pytest.mark.parametrize("change,what", [
+    (dict(slots_out=4096), "slots_out"), (dict(slots_out=4096 + 28), "slots_out"), (dict(slots_out=8192 - 28), "slots_out"),
+    (dict(slots_out=8192 + 4), "slots_out"), (dict(data=4096), "parents"), (dict(data=4096 - 600), "parents"),
+    (dict(data=8192), "slots"), (dict(data=12288 + 16), "slots_out"), (dict(data=12288 - 640 + 16), "slots_out"),
+    (dict(slots=None, slots_out=None, data=4096 + 16), "parents"),
+])
+def test_beam_reorder_arrays_that_are_read_and_written(change, what):
+    """Work-groups read parents and slots while others write: no array of theirs is a result."""
+    lib = _lib()
+    a = dict(slots=8192, slots_out=12288, data=1 << 20)
+    a.update(change)
+    t = (ll.ll_beam_tensor * 1)(ll.ll_beam_tensor(a["data"], 64))
+    st = lib.ll_beam_reorder(None, 2, 4, 4096, 1, t, a["slots"], 10 if a["slots"] else 0, a["slots_out"], None)
+    assert st == ll.LL_EINVAL and "overlap" in ll.ll_last_error() and what in ll.ll_last_error()
+
+
+def test_beam_reorder_pools_that_overlap_far_apart():
+    """Sizes whose product passes 63 bits."""
+    lib = _lib()
+    t = (ll.ll_beam_tensor * 2)(ll.ll_beam_tensor(1 << 20, 1 << 36), ll.ll_beam_tensor(1 << 40, 16))
+    st = lib.ll_beam_reorder(None, 2, 4, 4096, 2, t, 8192, 2 ** 31 - 1, 12288, None)
+    assert st == ll.LL_EINVAL and "overlap" in ll.ll_last_error()
