@@ -419,3 +419,21 @@ def test_tensors_of_more_than_one_launch():
             assert (part == torch.tensor([1, 1, 3, 2], device=DEV, dtype=torch.uint8)[:, None] + 10 * i).all()
         assert not t[:, 100:-100].any()
     assert small.tolist() == [1, 1, 3, 2]
+
+
+@pytest.mark.parametrize("B,K", [(33001, 2), (65535, 16), (1 << 15, 32)])
+def test_many_searches(B, K):
+    """More searches, or places, than a launch's second dimension is given."""
+    gen = torch.Generator(device=DEV).manual_seed(K)
+    parents = torch.randint(0, K, (B, K), device=DEV, generator=gen).int()
+    x = torch.arange(B * K, device=DEV).view(B, K)
+    y = x.int().clone()
+    pool = torch.arange(B * K, device=DEV).float()[:, None].repeat(1, 3)
+    ll.ll_beam_reorder(parents, [moved := x.clone(), y])
+    want = x.gather(1, parents.long())
+    assert torch.equal(moved, want) and torch.equal(y, want.int())
+    slots = torch.randperm(B * K, device=DEV, generator=gen).view(B, K).int()
+    out, err = torch.empty_like(slots), torch.zeros(1, dtype=torch.int32, device=DEV)
+    ll.ll_beam_reorder(parents, [pool], slots=slots, slots_out=out, device_error=err)
+    assert err.item() == 0
+    assert torch.equal(pool[out.long(), 0], slots.gather(1, parents.long()).float())
