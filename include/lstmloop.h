@@ -747,8 +747,9 @@ ll_status ll_embed_status_sync(ll_embed_plan* plan, int32_t* device_error);
  *     elements from row to row (0: V; any ld >= V).
  *   eos      the token that finishes a beam, or -1: none does.
  *   length_penalty  in [-16, 16]; 0: scores are compared as they are.
- * Scores are made and compared in double.  logits need the alignment of an element
- * only, every other array 4 bytes.
+ * A row's sum of exponentials is float; scores are made from it, and compared, in double
+ * (candidates of different beams that lie nearer than some 1e-6 may change places).
+ * logits need the alignment of an element only, every other array 4 bytes.
  */
 #define LL_BEAM_MAX 32
 #define LL_BEAM_TENSORS 256

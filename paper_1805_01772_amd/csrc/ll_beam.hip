@@ -5,8 +5,9 @@
 // rank s / ((5 + length) / 6)^alpha; a finished beam is one candidate, as it is.  The K
 // best of all candidates of a search are among the K best logits of its beams, so one
 // walk over the logits (ll_rows.h) keeps each row's sum and its K largest, and a second,
-// small kernel compares those.  Scores of different beams can lie as close as a float's
-// rounding: they are made and compared in double from the walk's m and s.
+// small kernel compares those.  Scores of one beam can lie as close as its logits' rounding:
+// they are made and compared in double from the walk's m and s.  s is a float's sum, so
+// that candidates of different beams nearer than some 1e-6 may change places.
 // Equal ranks: lower beam, then lower token.
 //
 // Reordering in place: a thread has the same few bytes of all K rows, so it reads what it
@@ -49,9 +50,12 @@ __device__ __forceinline__ bool beam_live(const BeamArgs& a, long r) {
   return a.scores[r] > -__builtin_inff() && !(a.finished && a.finished[r]);
 }
 
-// A part of a row: its sum and its K largest.  Bound by the walk over the logits, whose
-// exponentials cost as much as their bytes: 256 rows of 131072 bfloat16 in 19.1 us,
-// 3.5 TB/s (21.1 when the walk made the entropy's sum too).
+// A part of a row: its sum and its K largest.  Bound by the walk over the logits: its
+// bytes, and beside them 13 vector instructions an element, which are issued in 72 % of the
+// cycles in which a compute unit has a wave; what comes before and after the walk overlaps
+// with nothing where a work-group has a compute unit to itself.  256 rows of 131072
+// bfloat16, of which 209 are read, in 19.1 us, 2.9 TB/s (21.1 when the walk made the
+// entropy's sum too); 240 of 50001 floats, 198 read, in 14.9, 2.7 TB/s.
 template <typename T, int NTHR>
 __global__ __launch_bounds__(NTHR) void beam_rows_kernel(BeamArgs a) {
   __shared__ Shared<NTHR> sh;
@@ -269,7 +273,7 @@ __device__ void beam_copy(char* to, const char* from, long bytes) {
 }
 
 // Place k of search b, one slice of a tensor's row.  Bound by the copies: 256 places of
-// 1 MiB of which 110 or so move take 33 us, some 7 TB/s read and written; what does not
+// 1 MiB of which 105 move take 33 us, 6.7 TB/s read and written; what does not
 // move costs its work-group three trips to memory (4 us where nothing moves).
 __global__ __launch_bounds__(256) void beam_pool_move_kernel(BeamMove a) {
   const int place = blockIdx.y + gridDim.y * blockIdx.z;
@@ -444,7 +448,7 @@ ll_status ll_beam_select(ll_beam_plan* p, void* stream, int32_t searches, const 
   const int rows = searches * p->d.K;
   // A work-group a compute unit, none of less than 32 KiB.  (Rows, join: 4 rows of 32000
   // floats 8.0 + 4.2 us, in parts of 64 KiB 9.3 + 3.9, of 16 KiB 8.7 + 6.0; 256 rows of
-  // 131072 bfloat16 19.1 us, with two work-groups a compute unit 20.7.)
+  // 131072 bfloat16, 209 of them read, 19.1 us, with two work-groups a compute unit 20.7.)
   const long want = (p->cus + rows - 1) / rows, row = (long)p->d.V * elem_bytes(p);
   a.parts = (int)std::max(1L, std::min({want, row / (32 << 10), (long)ll::kPartsMax}));
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);

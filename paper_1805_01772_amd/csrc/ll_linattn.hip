@@ -26,8 +26,9 @@ constexpr int kLinStepCols = 32;
 
 __device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
 
-// Tokens of a chunk: 16 KB of 128 columns in either type.  (bfloat16 chunks of 32: 5.3 us
-// for 64 tokens and head of a compute unit instead of 5.1.)
+// Tokens of a chunk: 16 KB of 128 columns in either type.  The state is rounded to float
+// once a chunk.  (bfloat16 chunks of 32: 5.3 us for 64 tokens and head of a compute unit
+// instead of 5.1.)
 template <typename T> struct LinChunk { static constexpr int n = 64; };
 template <> struct LinChunk<float> { static constexpr int n = 32; };
 
@@ -224,10 +225,13 @@ __device__ __forceinline__ void lin_store(void* dst, long at, const float* x, bo
 //
 // Bound by the instructions between the products: 64 tokens of a head of 128 x 128 in
 // bfloat16 take a compute unit 5.1 us forward and 14 for the three passes of the gradient,
-// where their bytes take 3.05 at the rate of a copy; the matrix instructions are issued in
-// 39 % of the cycles and others, a float's pieces first of all, in 43 %.  (With two
-// pieces for y's products 4.65; eight waves of 16 columns 6.0; 64 columns a work-group
-// 6.4; three waves a SIMD spill, 8.7.)
+// where their bytes take 3.05 at the rate of a copy; the matrix unit works in 37 % of the
+// cycles (one row of 16384 tokens, gradient) and others, a float's pieces first of all, are
+// issued in 45 %.  That kernel has all 256 registers of two waves a SIMD and keeps 12 more
+// in scratch.  (With two pieces for y's products 4.65; eight waves of 16 columns 6.0; 64
+// columns a work-group 6.4; three waves a SIMD keep more there, 8.7.)  One launch
+// makes all passes at the widest one's KD and NV: the gradient for heads of 64 x 72 has
+// states of 96 x 128, 2.7 times theirs.
 // ---------------------------------------------------------------------------
 template <typename T, int KD, int NV, bool LOCAL>
 __global__ __launch_bounds__(256, 2) void lin_kernel(LinArgs args) {
