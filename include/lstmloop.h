@@ -811,9 +811,10 @@ typedef struct {
  *            copied for the further ones only, into the slots of beams without a
  *            successor, in order.  Slots are distinct.  -1: no state; all successors of
  *            such a beam have -1, and no state is put there.  A state that finds no slot
- *            is lost: its successor has -1, and LL_DEVERR_SLOT is set.  (So slots that
- *            nobody needs are in no place of slots_out.)  A slot < -1 or >= n_slots sets
- *            LL_DEVERR_SLOT and counts as no state; handed on, it keeps its number.
+ *            is lost: its successor (also a place that ll_beam_select had no candidate
+ *            for) has -1, and LL_DEVERR_SLOT is set.  (So slots that nobody needs are in
+ *            no place of slots_out.)  A slot < -1 or >= n_slots sets LL_DEVERR_SLOT and
+ *            counts as no state; handed on, it keeps its number.
  *   device_error  device int32 whose bits are set (never cleared), or NULL.
  */
 ll_status ll_beam_reorder(void* stream, int32_t searches, int32_t K, const int32_t* parents,
