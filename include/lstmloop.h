@@ -541,7 +541,8 @@ ll_status delta_loop_step(const ll_delta_desc* desc, void* stream, const void* q
  *     their gradients (decays, states and their gradients are float).  Inside, sums
  *     and states are float, products keep float's 24 bits.
  *   inference, q_ld .. dv_ld, scale  as for ll_delta_desc.
- * The decays are constants of the layer: they get no gradient.  Infinity in an
+ * The decays are constants of the layer: they get no gradient.  Numbers below 2^-109
+ * (1.5e-33) are operands of a loop's products as multiples of 2^-133.  Infinity in an
  * operand or a state, and a float above bfloat16's largest (3.39e38), give NaN in a
  * loop (the step computes with them as float does).  A token that holds such a
  * value or NaN may reach y from up to 63 tokens before it on (what it leaves in

@@ -580,3 +580,19 @@ def test_bfloat16_step_is_rounded_once():
     S, y = c["S0"].clone(), torch.empty_like(c["v"][0])
     ll.linattn_loop_step(c["q"][0], c["k"][0], c["v"][0], c["g"], S, y)
     check_rounded_once(y, reference(c, backward=False)["y"][0], "y")
+
+
+@pytest.mark.parametrize("power,tol", [(-105, 5e-6), (-118, 5e-6 + 2.0 ** -12)])
+@pytest.mark.parametrize("name", ["k", "v"])
+def test_small_numbers(name, power, tol):
+    """Operands near 1 times 2^power: all their bits down to 2^-109; below, a bfloat16 piece is
+    a multiple of 2^-133, so an operand is off by at most 2^-134, here 2^-16 of one near 1; the
+    sums' norm by sixteen times that at most."""
+    c = make(70, 1, 1, 2, 32, 40, "f32", seed=22)
+    c[name] *= 2.0 ** power
+    c["S0"] *= 2.0 ** power
+    got, err = run(c, "f32")
+    assert err == 0
+    for n, want in by_pairs(c).items():
+        off = np.linalg.norm(got[n].double().cpu().numpy() - want) / np.linalg.norm(want)
+        assert off <= tol, (n, off)
